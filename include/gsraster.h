@@ -430,7 +430,125 @@ gs_status gs_render_bwd_adam(const gs_camera* cam, const gs_gaussians* g, const 
                              const gs_grads* grads, const gs_adam_tensor* adam, float beta1, float eps, int64_t step,
                              void* workspace, size_t workspace_bytes, void* stream);
 
-/* Workspace bytes needed by any call for these sizes (host only). */
+/* ---- Row operators: a decoder wider than the fused ones, and its clipped step -------
+ * The fused decoders (LATENT_MLP, NEURAL) have up to 32 neurons per layer. A wider
+ * decoder runs over a row per Gaussian with the calls below, forward and backward;
+ * its weight gradients are fp32 arrays that gs_grad_norm and gs_adam_step take.
+ * Matrices are row-major with a row stride in elements (ld >= columns), at any
+ * alignment of the element type; element (r, c) is at r * ld + c. `type` is the
+ * matrices' element type. Statistics, sums and biases are fp32. Outputs must not
+ * overlap inputs or each other. rows = 0 is allowed: nothing is written but sums over
+ * the rows, which are zero. */
+enum { GS_F32 = 0, GS_F16 = 1, GS_BF16 = 2 };   /* element types: fp32, binary16, bfloat16 */
+#define GS_MAX_DIM (1 << 20)                    /* columns of a row operator's matrices, at most */
+
+/*
+ * gs_layer_norm_fwd -- layer norm of each row: mu = mean of the row, var = mean of
+ * (x - mu)^2, rstd = 1 / sqrt(var + eps), y = (x - mu) rstd w + b.
+ * x: [rows][dim]; w, b: [dim] fp32, or NULL for 1 and 0; y: [rows][dim]; mean,
+ * rstd: [rows] fp32, what gs_layer_norm_bwd needs, or NULL.
+ * Limits: 0 <= rows < 2^31, 1 <= dim <= GS_MAX_DIM, eps >= 0.
+ */
+gs_status gs_layer_norm_fwd(int32_t type, int64_t rows, int64_t dim, const void* x, int64_t ldx, const float* w,
+                            const float* b, float eps, void* y, int64_t ldy, float* mean, float* rstd, void* stream);
+
+/*
+ * gs_layer_norm_bwd -- with xh = (x - mean) rstd and g = dy w, per row:
+ *   dx = rstd (g - mean(g) - xh mean(g xh)) [+ add],
+ * and over the rows dw = sum of dy xh, db = sum of dy.
+ * mean, rstd: as gs_layer_norm_fwd wrote them. add: [rows][dim] or NULL, a gradient
+ * that joins dx (that of a skip connection around the norm). dw, db: [dim] fp32,
+ * overwritten; either may be NULL. The sums are taken in a fixed order: the same call
+ * gives the same bits.
+ * workspace: gs_layer_norm_workspace_size bytes, 256-byte aligned.
+ */
+gs_status gs_layer_norm_bwd(int32_t type, int64_t rows, int64_t dim, const void* dy, int64_t lddy, const void* x,
+                            int64_t ldx, const float* w, const float* mean, const float* rstd, const void* add,
+                            int64_t ldadd, void* dx, int64_t lddx, float* dw, float* db, void* workspace,
+                            size_t workspace_bytes, void* stream);
+gs_status gs_layer_norm_workspace_size(int32_t type, int64_t rows, int64_t dim, size_t* bytes);
+
+enum {
+    GS_ACT_NONE = 0,
+    GS_ACT_RELU = 1,
+    GS_ACT_GELU = 2,          /* z Phi(z), Phi the normal distribution function */
+    GS_ACT_SILU = 3,          /* z / (1 + exp(-z)) */
+    GS_ACT_TANH = 4,
+    GS_ACT_SIGMOID = 5,
+};
+
+/* A layer's shape and operands. */
+typedef struct gs_linear {
+    int32_t type;             /* of x, w, residual, y, z, dy and dx */
+    int32_t act;              /* GS_ACT_* */
+    int64_t rows, n_in, n_out;
+    const void* x;            /* [rows][n_in], row stride ldx */
+    const void* w;            /* [n_out][n_in], row stride ldw */
+    const float* bias;        /* [n_out] fp32, or NULL */
+    int64_t ldx, ldw;
+} gs_linear;
+
+/*
+ * gs_linear_fwd -- z = x w^T + bias, y = act(z) + residual: one pass, the products in
+ * fp32 sums on the matrix cores, one rounding of z and of y.
+ * residual: [rows][n_out] or NULL; y: [rows][n_out]; z: [rows][n_out] or NULL, what
+ * gs_linear_bwd needs of an activation.
+ * Limits: 0 <= rows < 2^31, 1 <= n_in, n_out <= GS_MAX_DIM (GS_ERR_UNSUPPORTED if rows
+ * times n_out or n_in exceed the grid: about 2^38 values).
+ * workspace: gs_linear_workspace_size bytes, 256-byte aligned; NULL where that is 0.
+ */
+gs_status gs_linear_fwd(const gs_linear* p, const void* residual, int64_t ldr, void* y, int64_t ldy, void* z,
+                        int64_t ldz, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * gs_linear_bwd -- dz = dy act'(z), dx = dz w, dw = dz^T x, db = sum over rows of dz
+ * (the residual's gradient is dy itself). p->bias is not read.
+ * z: as gs_linear_fwd wrote it (not read for GS_ACT_NONE). dx: [rows][n_in]; dw:
+ * [n_out][n_in] of dw_type, GS_F32 or p->type; db: [n_out] fp32. dx, dw and db are
+ * overwritten and may each be NULL. For dx, and for dw in a 16-bit type, dz is
+ * rounded to p->type; for dw in fp32 it is kept to 22 bits or more (a dz beyond the
+ * type's range counts as infinite). The same call gives the same bits.
+ * workspace: gs_linear_workspace_size bytes, 256-byte aligned.
+ */
+gs_status gs_linear_bwd(const gs_linear* p, const void* dy, int64_t lddy, const void* z, int64_t ldz, void* dx,
+                        int64_t lddx, void* dw, int64_t lddw, int32_t dw_type, float* db, void* workspace,
+                        size_t workspace_bytes, void* stream);
+/* Bytes for the forward and the backward of a layer; dw_type -1: for the forward alone. */
+gs_status gs_linear_workspace_size(int32_t type, int32_t act, int64_t rows, int64_t n_in, int64_t n_out, int32_t dw_type,
+                                   size_t* bytes);
+
+/* One gradient of the global norm. Host struct. */
+typedef struct gs_grad_tensor {
+    void* grad;               /* [n] of `type` */
+    float* out;               /* NULL: clipped in place; else [n] fp32 that receives the clipped values */
+    int64_t n;                /* 0 <= n < 2^40 */
+    int32_t type;
+} gs_grad_tensor;
+
+/*
+ * gs_grad_norm -- the global norm of several gradients and the coefficient that clips
+ * it: norm = sqrt(sum over all tensors of g^2), squares added up in fp64 in a fixed
+ * order, c = min(1, max_norm / (norm + 1e-6)) (not a number if the norm is not).
+ * result: [2] fp32 device array, norm and c. The coefficient stays on the device, for
+ * gs_adam_step_scaled. tensors: host array of `count` >= 0.
+ * workspace: gs_grad_workspace_size bytes, 256-byte aligned.
+ */
+gs_status gs_grad_norm(const gs_grad_tensor* tensors, int32_t count, float max_norm, float* result, void* workspace,
+                       size_t workspace_bytes, void* stream);
+/* gs_grad_clip -- gs_grad_norm, and each gradient times c, in place or into its `out`. */
+gs_status gs_grad_clip(const gs_grad_tensor* tensors, int32_t count, float max_norm, float* result, void* workspace,
+                       size_t workspace_bytes, void* stream);
+gs_status gs_grad_workspace_size(const gs_grad_tensor* tensors, int32_t count, size_t* bytes);
+
+/*
+ * gs_adam_step_scaled -- gs_adam_step with every gradient multiplied by *grad_scale (a
+ * device value: the clipping coefficient of gs_grad_norm) as it is read; the arrays in
+ * `grad` keep their values. NULL: gs_adam_step itself.
+ */
+gs_status gs_adam_step_scaled(const gs_adam_tensor* tensors, int32_t count, float beta1, float eps, int64_t step,
+                              const float* grad_scale, void* stream);
+
+/* Workspace bytes needed by any rasterizer call for these sizes (host only). */
 gs_status gs_workspace_size(int64_t n, int32_t width, int32_t height, uint64_t capacity, int32_t kind,
                             size_t* bytes);
 
@@ -448,7 +566,8 @@ enum {
     GS_KERNEL_PREPROCESS = 0, GS_KERNEL_PAIR_COUNT, GS_KERNEL_DEPTH_SORT, GS_KERNEL_ENTRY_OFFSETS,
     GS_KERNEL_BLOCK_ENTRIES, GS_KERNEL_BLOCK_SORT, GS_KERNEL_TILE_LISTS, GS_KERNEL_BLEND_FWD,
     GS_KERNEL_BWD_PREP, GS_KERNEL_BLEND_BWD, GS_KERNEL_PREPROCESS_BWD, GS_KERNEL_MLP_REDUCE,
-    GS_KERNEL_ADAM, GS_KERNEL_NEURAL_FOLD, GS_KERNEL_COUNT
+    GS_KERNEL_ADAM, GS_KERNEL_NEURAL_FOLD, GS_KERNEL_LAYER_NORM_FWD, GS_KERNEL_LAYER_NORM_BWD, GS_KERNEL_LINEAR_FWD,
+    GS_KERNEL_LINEAR_BWD, GS_KERNEL_GRAD_NORM, GS_KERNEL_COUNT
 };   /* GS_KERNEL_BWD_PREP: the backward's accumulator clear and its tile order.
       * gs_bin_sort of few Gaussians (its method's second form) has no block
       * entries: GS_KERNEL_ENTRY_OFFSETS, _BLOCK_ENTRIES and _BLOCK_SORT count

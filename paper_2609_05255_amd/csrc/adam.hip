@@ -38,10 +38,13 @@ struct AdamArgs {
     int32_t count;
     AdamTensorArgs t[GS_ADAM_MAX_TENSORS];
     AdamStep c;
+    const float* grad_scale;   // the clipping coefficient, SCALED only
 };
 
+template <bool SCALED>
 __global__ __launch_bounds__(kBlock) void k_adam(AdamArgs a)
 {
+    const float scale = SCALED ? *a.grad_scale : 1.f;
     const int64_t b = blockIdx.x;
     int k = 0;
     while (k + 1 < a.count && b >= a.t[k + 1].chunk0) ++k;
@@ -71,6 +74,7 @@ __global__ __launch_bounds__(kBlock) void k_adam(AdamArgs a)
         const int64_t e = e0 + (int64_t)j * kBlock;
         if (e >= T.n) continue;
         const int64_t i = rbase + e;
+        if (SCALED) g[j] *= scale;
         adam_update(p[j], m[j], v[j], g[j], a.c.b1, a.c.omb1, b2, omb2, isbc2, a.c.eps, step);
         __builtin_nontemporal_store(m[j], T.m + i);
         __builtin_nontemporal_store(v[j], T.v + i);
@@ -101,7 +105,8 @@ void adam_step_constants(const gs_adam_tensor* ts, int count, float beta1, float
     }
 }
 
-hipError_t launch_adam(const gs_adam_tensor* ts, int count, float beta1, float eps, int64_t step, hipStream_t s)
+hipError_t launch_adam(const gs_adam_tensor* ts, int count, float beta1, float eps, int64_t step,
+                       const float* grad_scale, hipStream_t s)
 {
     AdamArgs a;
     memset(&a, 0, sizeof(a));
@@ -122,7 +127,11 @@ hipError_t launch_adam(const gs_adam_tensor* ts, int count, float beta1, float e
         chunks += (int64_t)t.rows * T.chunks_per_row;
     }
     if (chunks == 0) return hipSuccess;
-    hipLaunchKernelGGL(k_adam, dim3((unsigned)chunks), dim3(kBlock), 0, s, a);
+    a.grad_scale = grad_scale;
+    if (grad_scale)
+        hipLaunchKernelGGL(k_adam<true>, dim3((unsigned)chunks), dim3(kBlock), 0, s, a);
+    else
+        hipLaunchKernelGGL(k_adam<false>, dim3((unsigned)chunks), dim3(kBlock), 0, s, a);
     return hipGetLastError();
 }
 

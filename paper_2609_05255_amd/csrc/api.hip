@@ -166,7 +166,8 @@ void resolve_pending(gs_timer* t)
 
 const char* const kKernelNames[GS_KERNEL_COUNT] = {
     "preprocess", "pair_count", "depth_sort", "entry_offsets", "block_entries", "block_sort", "tile_lists",
-    "blend_fwd", "bwd_prep", "blend_bwd", "preprocess_bwd", "mlp_reduce", "adam", "neural_fold"};
+    "blend_fwd", "bwd_prep", "blend_bwd", "preprocess_bwd", "mlp_reduce", "adam", "neural_fold",
+    "layer_norm_fwd", "layer_norm_bwd", "linear_fwd", "linear_bwd", "grad_norm"};
 
 }  // namespace
 
@@ -261,6 +262,12 @@ const char* gs_version(void) { return "gsraster 0.1.0 (gfx950)"; }
 gs_status gs_adam_step(const gs_adam_tensor* tensors, int32_t count, float beta1, float eps, int64_t step,
                        void* stream)
 {
+    return gs_adam_step_scaled(tensors, count, beta1, eps, step, nullptr, stream);
+}
+
+gs_status gs_adam_step_scaled(const gs_adam_tensor* tensors, int32_t count, float beta1, float eps, int64_t step,
+                              const float* grad_scale, void* stream)
+{
     GS_CHECK(tensors != nullptr, "tensors is NULL");
     GS_CHECK(count >= 1 && count <= GS_ADAM_MAX_TENSORS, "count %d outside [1, %d]", count, GS_ADAM_MAX_TENSORS);
     GS_CHECK(step >= 1, "step %lld must be at least 1", (long long)step);
@@ -279,7 +286,7 @@ gs_status gs_adam_step(const gs_adam_tensor* tensors, int32_t count, float beta1
     GS_CHECK(rows <= GS_ADAM_MAX_ROWS, "%lld rows in total exceed %d", (long long)rows, GS_ADAM_MAX_ROWS);
     hipStream_t s = static_cast<hipStream_t>(stream);
     timing_begin(GS_KERNEL_ADAM, s);
-    GS_HIP(launch_adam(tensors, count, beta1, eps, step, s));
+    GS_HIP(launch_adam(tensors, count, beta1, eps, step, grad_scale, s));
     timing_end(GS_KERNEL_ADAM, s);
     return ok();
 }
@@ -624,6 +631,215 @@ gs_status gs_neural_fold(const uint16_t* features, const uint16_t* mlp_w, int64_
     GS_HIP(launch_neural_fold(features, mlp_w, n, preact, s));
     timing_end(GS_KERNEL_NEURAL_FOLD, s);
     return ok();
+}
+
+}  // extern "C"
+
+namespace {
+
+bool type_ok(int32_t type) { return type == GS_F32 || type == GS_F16 || type == GS_BF16; }
+
+// A matrix of a row operator: an array where there are rows, at its type's alignment, and a row stride.
+gs_status check_matrix(const char* name, const void* p, int64_t rows, int64_t cols, int64_t ld, int32_t type)
+{
+    GS_CHECK(rows == 0 || p != nullptr, "%s is NULL", name);
+    GS_CHECK(ld >= cols && ld < ((int64_t)1 << 31), "%s: row stride %lld outside [%lld, 2^31)", name, (long long)ld,
+             (long long)cols);
+    GS_CHECK(((uintptr_t)p & (type == GS_F32 ? 3 : 1)) == 0, "%s is not aligned to its element type", name);
+    return GS_OK;
+}
+
+gs_status check_rows(int32_t type, int64_t rows)
+{
+    GS_CHECK(type_ok(type), "unknown element type %d", type);
+    GS_CHECK(rows >= 0 && rows < ((int64_t)1 << 31), "rows = %lld out of range [0, 2^31)", (long long)rows);
+    return GS_OK;
+}
+
+gs_status check_dim(const char* name, int64_t dim)
+{
+    GS_CHECK(dim >= 1 && dim <= GS_MAX_DIM, "%s = %lld outside [1, %d]", name, (long long)dim, GS_MAX_DIM);
+    return GS_OK;
+}
+
+gs_status check_linear(const gs_linear* p)
+{
+    gs_status st;
+    GS_CHECK(p != nullptr, "the layer is NULL");
+    if ((st = check_rows(p->type, p->rows)) != GS_OK) return st;
+    GS_CHECK(p->act >= GS_ACT_NONE && p->act <= GS_ACT_SIGMOID, "unknown activation %d", p->act);
+    if ((st = check_dim("n_in", p->n_in)) != GS_OK) return st;
+    if ((st = check_dim("n_out", p->n_out)) != GS_OK) return st;
+    if ((st = check_matrix("x", p->x, p->rows, p->n_in, p->ldx, p->type)) != GS_OK) return st;
+    if ((st = check_matrix("w", p->w, p->n_out, p->n_in, p->ldw, p->type)) != GS_OK) return st;
+    if (!linear_grid_fits(p->rows, p->n_out) || !linear_grid_fits(p->rows, p->n_in))
+        return fail(GS_ERR_UNSUPPORTED, "%lld rows of %lld and %lld values exceed the grid", (long long)p->rows,
+                    (long long)p->n_in, (long long)p->n_out);
+    return GS_OK;
+}
+
+gs_status check_workspace(const void* workspace, size_t have, size_t need)
+{
+    if (have < need) return fail(GS_ERR_CAPACITY, "workspace of %zu bytes: %zu needed", have, need);
+    GS_CHECK(need == 0 || workspace != nullptr, "workspace is NULL");
+    GS_CHECK(need == 0 || ((uintptr_t)workspace & 255) == 0, "workspace must be 256-byte aligned");
+    return GS_OK;
+}
+
+gs_status check_grads(const gs_grad_tensor* tensors, int32_t count)
+{
+    GS_CHECK(count >= 0, "count %d is negative", count);
+    GS_CHECK(count == 0 || tensors != nullptr, "tensors is NULL");
+    for (int k = 0; k < count; ++k) {
+        const gs_grad_tensor& t = tensors[k];
+        GS_CHECK(type_ok(t.type), "tensor %d: unknown element type %d", k, t.type);
+        GS_CHECK(t.n >= 0 && t.n < ((int64_t)1 << 40), "tensor %d: n out of range", k);
+        GS_CHECK(t.n == 0 || t.grad != nullptr, "tensor %d: grad is NULL", k);
+        GS_CHECK(((uintptr_t)t.grad & (t.type == GS_F32 ? 3 : 1)) == 0 && ((uintptr_t)t.out & 3) == 0,
+                 "tensor %d: an array is not aligned to its element type", k);
+    }
+    return GS_OK;
+}
+
+gs_status grad_clip(const gs_grad_tensor* tensors, int32_t count, float max_norm, float* result, void* workspace,
+                    size_t workspace_bytes, void* stream, bool scale)
+{
+    gs_status st;
+    if ((st = check_grads(tensors, count)) != GS_OK) return st;
+    GS_CHECK(max_norm >= 0.f, "max_norm must not be negative or undefined");
+    GS_CHECK(result != nullptr && ((uintptr_t)result & 3) == 0, "result is NULL or unaligned");
+    if ((st = check_workspace(workspace, workspace_bytes, sizeof(double) * (size_t)grad_parts(tensors, count))) != GS_OK)
+        return st;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    timing_begin(GS_KERNEL_GRAD_NORM, s);
+    GS_HIP(launch_grad_clip(tensors, count, max_norm, result, (double*)workspace, scale, s));
+    timing_end(GS_KERNEL_GRAD_NORM, s);
+    return ok();
+}
+
+}  // namespace
+
+extern "C" {
+
+gs_status gs_layer_norm_fwd(int32_t type, int64_t rows, int64_t dim, const void* x, int64_t ldx, const float* w,
+                            const float* b, float eps, void* y, int64_t ldy, float* mean, float* rstd, void* stream)
+{
+    gs_status st;
+    if ((st = check_rows(type, rows)) != GS_OK) return st;
+    if ((st = check_dim("dim", dim)) != GS_OK) return st;
+    if ((st = check_matrix("x", x, rows, dim, ldx, type)) != GS_OK) return st;
+    if ((st = check_matrix("y", y, rows, dim, ldy, type)) != GS_OK) return st;
+    GS_CHECK(eps >= 0.f, "eps must not be negative or undefined");
+    if (rows == 0) return ok();
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    timing_begin(GS_KERNEL_LAYER_NORM_FWD, s);
+    GS_HIP(launch_layer_norm_fwd(type, x, ldx, w, b, rows, (int)dim, eps, y, ldy, mean, rstd, s));
+    timing_end(GS_KERNEL_LAYER_NORM_FWD, s);
+    return ok();
+}
+
+gs_status gs_layer_norm_workspace_size(int32_t type, int64_t rows, int64_t dim, size_t* bytes)
+{
+    gs_status st;
+    GS_CHECK(bytes != nullptr, "bytes is NULL");
+    if ((st = check_rows(type, rows)) != GS_OK) return st;
+    if ((st = check_dim("dim", dim)) != GS_OK) return st;
+    *bytes = layer_norm_workspace(type, rows, dim);
+    return ok();
+}
+
+gs_status gs_layer_norm_bwd(int32_t type, int64_t rows, int64_t dim, const void* dy, int64_t lddy, const void* x,
+                            int64_t ldx, const float* w, const float* mean, const float* rstd, const void* add,
+                            int64_t ldadd, void* dx, int64_t lddx, float* dw, float* db, void* workspace,
+                            size_t workspace_bytes, void* stream)
+{
+    gs_status st;
+    if ((st = check_rows(type, rows)) != GS_OK) return st;
+    if ((st = check_dim("dim", dim)) != GS_OK) return st;
+    if ((st = check_matrix("dy", dy, rows, dim, lddy, type)) != GS_OK) return st;
+    if ((st = check_matrix("x", x, rows, dim, ldx, type)) != GS_OK) return st;
+    if ((st = check_matrix("dx", dx, rows, dim, lddx, type)) != GS_OK) return st;
+    if (add && (st = check_matrix("add", add, rows, dim, ldadd, type)) != GS_OK) return st;
+    GS_CHECK(rows == 0 || (mean && rstd), "mean or rstd is NULL");
+    if ((st = check_workspace(workspace, workspace_bytes, layer_norm_workspace(type, rows, dim))) != GS_OK) return st;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    timing_begin(GS_KERNEL_LAYER_NORM_BWD, s);
+    GS_HIP(launch_layer_norm_bwd(type, dy, lddy, x, ldx, w, mean, rstd, add, ldadd, rows, (int)dim, dx, lddx, dw, db,
+                                 (float*)workspace, s));
+    timing_end(GS_KERNEL_LAYER_NORM_BWD, s);
+    return ok();
+}
+
+gs_status gs_linear_workspace_size(int32_t type, int32_t act, int64_t rows, int64_t n_in, int64_t n_out, int32_t dw_type,
+                                   size_t* bytes)
+{
+    gs_status st;
+    GS_CHECK(bytes != nullptr, "bytes is NULL");
+    if ((st = check_rows(type, rows)) != GS_OK) return st;
+    GS_CHECK(act >= GS_ACT_NONE && act <= GS_ACT_SIGMOID, "unknown activation %d", act);
+    if ((st = check_dim("n_in", n_in)) != GS_OK) return st;
+    if ((st = check_dim("n_out", n_out)) != GS_OK) return st;
+    GS_CHECK(dw_type == -1 || dw_type == GS_F32 || dw_type == type, "dw_type %d: fp32, the layer's type or -1", dw_type);
+    *bytes = linear_workspace(type, act, rows, n_in, n_out, dw_type);
+    return ok();
+}
+
+gs_status gs_linear_fwd(const gs_linear* p, const void* residual, int64_t ldr, void* y, int64_t ldy, void* z,
+                        int64_t ldz, void* workspace, size_t workspace_bytes, void* stream)
+{
+    gs_status st;
+    if ((st = check_linear(p)) != GS_OK) return st;
+    if ((st = check_matrix("y", y, p->rows, p->n_out, ldy, p->type)) != GS_OK) return st;
+    if (residual && (st = check_matrix("residual", residual, p->rows, p->n_out, ldr, p->type)) != GS_OK) return st;
+    if (z && (st = check_matrix("z", z, p->rows, p->n_out, ldz, p->type)) != GS_OK) return st;
+    if (p->rows == 0) return ok();
+    if ((st = check_workspace(workspace, workspace_bytes, linear_fwd_workspace(*p))) != GS_OK) return st;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    timing_begin(GS_KERNEL_LINEAR_FWD, s);
+    GS_HIP(launch_linear_fwd(*p, residual, ldr, y, ldy, z, ldz, workspace, s));
+    timing_end(GS_KERNEL_LINEAR_FWD, s);
+    return ok();
+}
+
+gs_status gs_linear_bwd(const gs_linear* p, const void* dy, int64_t lddy, const void* z, int64_t ldz, void* dx,
+                        int64_t lddx, void* dw, int64_t lddw, int32_t dw_type, float* db, void* workspace,
+                        size_t workspace_bytes, void* stream)
+{
+    gs_status st;
+    if ((st = check_linear(p)) != GS_OK) return st;
+    if ((st = check_matrix("dy", dy, p->rows, p->n_out, lddy, p->type)) != GS_OK) return st;
+    if (p->act != GS_ACT_NONE && (st = check_matrix("z", z, p->rows, p->n_out, ldz, p->type)) != GS_OK) return st;
+    if (dx && (st = check_matrix("dx", dx, p->rows, p->n_in, lddx, p->type)) != GS_OK) return st;
+    GS_CHECK(dw_type == GS_F32 || dw_type == p->type, "dw_type %d: fp32 or the layer's type", dw_type);
+    if (dw && (st = check_matrix("dw", dw, p->n_out, p->n_in, lddw, dw_type)) != GS_OK) return st;
+    if ((st = check_workspace(workspace, workspace_bytes, linear_bwd_workspace(*p, dy, lddy, dw_type))) != GS_OK)
+        return st;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    timing_begin(GS_KERNEL_LINEAR_BWD, s);
+    GS_HIP(launch_linear_bwd(*p, dy, lddy, z, ldz, dx, lddx, dw, lddw, dw_type, db, workspace, s));
+    timing_end(GS_KERNEL_LINEAR_BWD, s);
+    return ok();
+}
+
+gs_status gs_grad_workspace_size(const gs_grad_tensor* tensors, int32_t count, size_t* bytes)
+{
+    gs_status st;
+    GS_CHECK(bytes != nullptr, "bytes is NULL");
+    if ((st = check_grads(tensors, count)) != GS_OK) return st;
+    *bytes = sizeof(double) * (size_t)grad_parts(tensors, count);
+    return ok();
+}
+
+gs_status gs_grad_norm(const gs_grad_tensor* tensors, int32_t count, float max_norm, float* result, void* workspace,
+                       size_t workspace_bytes, void* stream)
+{
+    return grad_clip(tensors, count, max_norm, result, workspace, workspace_bytes, stream, false);
+}
+
+gs_status gs_grad_clip(const gs_grad_tensor* tensors, int32_t count, float max_norm, float* result, void* workspace,
+                       size_t workspace_bytes, void* stream)
+{
+    return grad_clip(tensors, count, max_norm, result, workspace, workspace_bytes, stream, true);
 }
 
 gs_status gs_timer_create(gs_timer** out)

@@ -1,0 +1,273 @@
+// Global norm of many gradient tensors and clipping by it.
+//
+//   norm = sqrt(sum over all tensors of g^2), c = min(1, max_norm / (norm + 1e-6)), g <- c g
+//
+// Bound by HBM: one read of the gradients for the norm, and where they are
+// clipped one more read and a write. The tensors are cut into chunks of
+// kGradChunk elements that the workgroups take in turn; a tensor table of up to
+// kGradTable entries travels in the kernel arguments, so that many tensors take
+// one launch. Squares are added up in fp64 (one conversion and one fused
+// multiply-add per element, a sixth of what HBM leaves time for), so that
+// neither large nor tiny gradients leave the range. Each workgroup writes one
+// partial sum; every workgroup of the next kernel adds all of them up in the
+// same fixed order, so no atomics and no third launch are needed and the same
+// gradients give the same bits. Where c is 1 and the gradients stay in place
+// nothing is read again.
+#include "gs_internal.h"
+#include "vec.h"
+
+namespace gsr {
+
+namespace {
+
+constexpr int kGradChunk = 8192;
+constexpr int kGradTable = 100;
+constexpr int kGradBlocks = 2048;        // workgroups of all launches of a norm together, about
+constexpr int kGradSmall = 16;           // chunks that one workgroup takes alone, in one launch
+constexpr int kSmallThreads = 1024;
+
+struct GradEntry {
+    void* g;
+    float* out;
+    int64_t n;
+    uint32_t chunk0;      // first chunk of this tensor within the table
+    int32_t type;
+};
+
+struct GradTable {
+    int32_t count;
+    uint32_t chunks;
+    GradEntry t[kGradTable];
+};
+
+// Clipping coefficient; a norm that is not a number makes it one.
+__device__ __forceinline__ float clip_scale(double sum, float max_norm, float* norm)
+{
+    *norm = (float)sqrt(sum);
+    const float c = max_norm / (*norm + 1e-6f);
+    return c > 1.f ? 1.f : c;
+}
+
+__device__ __forceinline__ int tensor_of(const GradTable& a, uint32_t chunk)
+{
+    int lo = 0, hi = a.count - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (a.t[mid].chunk0 <= chunk)
+            lo = mid;
+        else
+            hi = mid - 1;
+    }
+    return lo;
+}
+
+template <typename T, int THREADS>
+__device__ __forceinline__ double chunk_squares(const T* g, int64_t left)
+{
+    constexpr int N = Vec<T>::N;
+    double s = 0.0;
+#pragma unroll 4
+    for (int c = threadIdx.x * N; c < kGradChunk; c += THREADS * N) {
+        float v[N];
+        load_vec(g + c, left - c, v);
+#pragma unroll
+        for (int j = 0; j < N; ++j) s = fma((double)v[j], (double)v[j], s);
+    }
+    return s;
+}
+
+template <int THREADS>
+__device__ __forceinline__ double squares_of(const GradEntry& e, uint32_t chunk)
+{
+    const int64_t at = (int64_t)(chunk - e.chunk0) * kGradChunk;
+    if (e.type == GS_F16) return chunk_squares<f16, THREADS>((const f16*)e.g + at, e.n - at);
+    if (e.type == GS_BF16) return chunk_squares<bf16, THREADS>((const bf16*)e.g + at, e.n - at);
+    return chunk_squares<float, THREADS>((const float*)e.g + at, e.n - at);
+}
+
+template <typename T, int THREADS>
+__device__ __forceinline__ void chunk_scale(T* g, float* out, int64_t left, float c)
+{
+    constexpr int N = Vec<T>::N;
+#pragma unroll 4
+    for (int i = threadIdx.x * N; i < kGradChunk; i += THREADS * N) {
+        float v[N];
+        load_vec(g + i, left - i, v);
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] *= c;
+        if (out) {
+            if constexpr (N == 8) {
+                store_vec(out + i, left - i, v);
+                store_vec(out + i + 4, left - i - 4, v + 4);
+            } else {
+                store_vec(out + i, left - i, v);
+            }
+        } else {
+            store_vec(g + i, left - i, v);
+        }
+    }
+}
+
+template <int THREADS>
+__device__ __forceinline__ void scale_chunk(const GradEntry& e, uint32_t chunk, float c)
+{
+    const int64_t at = (int64_t)(chunk - e.chunk0) * kGradChunk;
+    float* out = e.out ? e.out + at : nullptr;
+    if (e.type == GS_F16)
+        chunk_scale<f16, THREADS>((f16*)e.g + at, out, e.n - at, c);
+    else if (e.type == GS_BF16)
+        chunk_scale<bf16, THREADS>((bf16*)e.g + at, out, e.n - at, c);
+    else
+        chunk_scale<float, THREADS>((float*)e.g + at, out, e.n - at, c);
+}
+
+// Sum over the workgroup, in a fixed order, left in every thread.
+template <int THREADS>
+__device__ __forceinline__ double block_sum(double v)
+{
+    __shared__ double s[THREADS / 64];
+    v = lane_sum64(v);
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0.0;
+#pragma unroll
+    for (int k = 0; k < THREADS / 64; ++k) v += s[k];
+    return v;
+}
+
+__global__ __launch_bounds__(kBlock) void k_grad_squares(GradTable a, double* __restrict__ part)
+{
+    double s = 0.0;
+    for (uint32_t c = blockIdx.x; c < a.chunks; c += gridDim.x)
+        s += squares_of<kBlock>(a.t[tensor_of(a, c)], c);
+    s = block_sum<kBlock>(s);
+    if (threadIdx.x == 0) part[blockIdx.x] = s;
+}
+
+__device__ __forceinline__ float coefficient(const double* __restrict__ part, int parts, float max_norm, float* norm)
+{
+    double s = 0.0;
+    for (int k = threadIdx.x; k < parts; k += kBlock) s += part[k];
+    return clip_scale(block_sum<kBlock>(s), max_norm, norm);
+}
+
+// result: [2] norm and coefficient
+__global__ __launch_bounds__(kBlock) void k_grad_result(const double* __restrict__ part, int parts, float max_norm,
+                                                        float* __restrict__ result)
+{
+    float norm;
+    const float c = coefficient(part, parts, max_norm, &norm);
+    if (threadIdx.x == 0) {
+        result[0] = norm;
+        result[1] = c;
+    }
+}
+
+__global__ __launch_bounds__(kBlock) void k_grad_scale(GradTable a, const double* __restrict__ part, int parts,
+                                                       float max_norm, float* __restrict__ result)
+{
+    float norm;
+    const float c = coefficient(part, parts, max_norm, &norm);
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        result[0] = norm;
+        result[1] = c;
+    }
+    for (uint32_t k = blockIdx.x; k < a.chunks; k += gridDim.x) {
+        const GradEntry& e = a.t[tensor_of(a, k)];
+        if (c != 1.f || e.out) scale_chunk<kBlock>(e, k, c);
+    }
+}
+
+// Norm, and clipping unless `scale` is 0, of a few chunks by one workgroup.
+__global__ __launch_bounds__(kSmallThreads) void k_grad_small(GradTable a, float max_norm, float* __restrict__ result,
+                                                              int scale)
+{
+    double s = 0.0;
+    for (uint32_t c = 0; c < a.chunks; ++c) s += squares_of<kSmallThreads>(a.t[tensor_of(a, c)], c);
+    float norm;
+    const float c = clip_scale(block_sum<kSmallThreads>(s), max_norm, &norm);
+    if (threadIdx.x == 0) {
+        result[0] = norm;
+        result[1] = c;
+    }
+    if (!scale) return;
+    for (uint32_t k = 0; k < a.chunks; ++k) {
+        const GradEntry& e = a.t[tensor_of(a, k)];
+        if (c != 1.f || e.out) scale_chunk<kSmallThreads>(e, k, c);
+    }
+}
+
+// Fills the table with tensors from `at` on (empty ones are left out); returns the first that it leaves.
+int fill_table(const gs_grad_tensor* ts, int count, int at, GradTable& a)
+{
+    a.count = 0;
+    a.chunks = 0;
+    for (; at < count && a.count < kGradTable; ++at) {
+        if (ts[at].n == 0) continue;
+        const int64_t chunks = div_up(ts[at].n, kGradChunk);
+        if (a.chunks + chunks > 0x7FFFFFFF) break;
+        a.t[a.count++] = {ts[at].grad, ts[at].out, ts[at].n, a.chunks, ts[at].type};
+        a.chunks += (uint32_t)chunks;
+    }
+    return at;
+}
+
+int table_blocks(const GradTable& a, int tables)
+{
+    return (int)std::min<int64_t>(a.chunks, std::max(kGradBlocks / tables, 64));
+}
+
+int table_count(const gs_grad_tensor* ts, int count)
+{
+    int tables = 0;
+    GradTable a;
+    for (int at = 0; at < count; ++tables) at = fill_table(ts, count, at, a);
+    return tables;
+}
+
+}  // namespace
+
+int64_t grad_parts(const gs_grad_tensor* ts, int count)
+{
+    const int tables = table_count(ts, count);
+    int64_t parts = 0;
+    GradTable a;
+    for (int at = 0; at < count;) {
+        at = fill_table(ts, count, at, a);
+        parts += table_blocks(a, tables);
+    }
+    return parts;
+}
+
+hipError_t launch_grad_clip(const gs_grad_tensor* ts, int count, float max_norm, float* result, double* part,
+                            bool scale, hipStream_t s)
+{
+    GradTable a;
+    int at = fill_table(ts, count, 0, a);
+    if (at == count && a.chunks <= kGradSmall) {
+        hipLaunchKernelGGL(k_grad_small, dim3(1), dim3(kSmallThreads), 0, s, a, max_norm, result, scale ? 1 : 0);
+        return hipGetLastError();
+    }
+    const int tables = table_count(ts, count);
+    int parts = 0;
+    for (at = 0; at < count;) {
+        at = fill_table(ts, count, at, a);
+        const int blocks = table_blocks(a, tables);
+        if (blocks == 0) continue;   // only empty tensors
+        hipLaunchKernelGGL(k_grad_squares, dim3(blocks), dim3(kBlock), 0, s, a, part + parts);
+        parts += blocks;
+    }
+    if (!scale) {
+        hipLaunchKernelGGL(k_grad_result, dim3(1), dim3(kBlock), 0, s, part, parts, max_norm, result);
+        return hipGetLastError();
+    }
+    for (at = 0; at < count;) {
+        at = fill_table(ts, count, at, a);
+        const int blocks = table_blocks(a, tables);
+        if (blocks == 0) continue;
+        hipLaunchKernelGGL(k_grad_scale, dim3(blocks), dim3(kBlock), 0, s, a, part, parts, max_norm, result);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace gsr

@@ -196,7 +196,30 @@ hipError_t launch_preprocess_bwd(const Cam& cam, const gs_gaussians& g, const gs
                                  hipStream_t s, const gs_adam_tensor* adam = nullptr, float beta1 = 0.f,
                                  float eps = 0.f, int64_t step = 0);
 hipError_t launch_mlp_reduce(int64_t n, const gs_appearance& app, const Workspace& ws, float* dmlp_w, hipStream_t s);
-hipError_t launch_adam(const gs_adam_tensor* tensors, int count, float beta1, float eps, int64_t step, hipStream_t s);
+// grad_scale: NULL, or a device value that every gradient is multiplied by
+hipError_t launch_adam(const gs_adam_tensor* tensors, int count, float beta1, float eps, int64_t step,
+                       const float* grad_scale, hipStream_t s);
+// Row operators (layer_norm.hip, linear.hip, grad_norm.hip). out[c] = sum over k of part[k][c], columns below
+// `split` to out0, the others to out1.
+hipError_t launch_column_sum(const float* part, int count, int64_t cols, int64_t split, float* out0, float* out1,
+                             hipStream_t s);
+size_t layer_norm_workspace(int type, int64_t rows, int64_t dim);
+hipError_t launch_layer_norm_fwd(int type, const void* x, int64_t ldx, const float* w, const float* b, int64_t rows,
+                                 int dim, float eps, void* y, int64_t ldy, float* mean, float* rstd, hipStream_t s);
+hipError_t launch_layer_norm_bwd(int type, const void* dy, int64_t lddy, const void* x, int64_t ldx, const float* w,
+                                 const float* mean, const float* rstd, const void* add, int64_t ldadd, int64_t rows,
+                                 int dim, void* dx, int64_t lddx, float* dw, float* db, float* part, hipStream_t s);
+size_t linear_workspace(int type, int act, int64_t rows, int64_t in, int64_t out, int dw_type);   // -1: forward only
+size_t linear_fwd_workspace(const gs_linear& p);
+size_t linear_bwd_workspace(const gs_linear& p, const void* dy, int64_t lddy, int dw_type);
+bool linear_grid_fits(int64_t rows, int64_t cols);
+hipError_t launch_linear_fwd(const gs_linear& p, const void* residual, int64_t ldr, void* y, int64_t ldy, void* z,
+                             int64_t ldz, void* ws, hipStream_t s);
+hipError_t launch_linear_bwd(const gs_linear& p, const void* dy, int64_t lddy, const void* z, int64_t ldz, void* dx,
+                             int64_t lddx, void* dw, int64_t lddw, int dw_type, float* db, void* ws, hipStream_t s);
+int64_t grad_parts(const gs_grad_tensor* tensors, int count);   // fp64 partial sums of a norm
+hipError_t launch_grad_clip(const gs_grad_tensor* tensors, int count, float max_norm, float* result, double* part,
+                            bool scale, hipStream_t s);
 hipError_t launch_mlp_eval(const uint16_t* x, int64_t rows, const uint16_t* w, float* out, hipStream_t s);
 hipError_t launch_neural_fold(const uint16_t* features, const uint16_t* w, int64_t n, uint16_t* preact,
                               hipStream_t s);

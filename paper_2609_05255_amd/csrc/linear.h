@@ -1,0 +1,78 @@
+// Shared between the per-type instances of the linear operators (linear_f16.hip,
+// linear_bf16.hip, linear_f32.hip) and their dispatch (linear.hip).
+#pragma once
+
+#include "gs_internal.h"
+#include "vec.h"
+
+namespace gsr {
+
+// One product C[i][j] = sum over c of A(i, c) B(j, c), i < rows, j < cols, c < len.
+// NT: A(i, c) = a[i lda + c], B(j, c) = b[j ldb + c] (both contiguous along the sum).
+// TT: A(i, c) = a[c lda + i], B(j, c) = b[c ldb + j] (both contiguous across it).
+// The sum may be split: part z = plane * splits + split covers c in [split * split_len, ...) of A plane
+// `plane` (a + plane * plane_stride).
+struct GemmArgs {
+    const void* a;
+    const void* b;
+    int64_t lda, ldb;
+    int64_t rows, cols, len;
+    int64_t a_rows, b_rows;        // stored rows of a and b (NT: rows, cols; TT: len)
+    int64_t split_len;
+    int32_t splits, planes;
+    int64_t plane_stride;
+    // epilogue: out = act(C + bias) + residual, z = C + bias
+    const float* bias;
+    const void* residual;
+    void* out;
+    void* z;
+    int64_t ldr, ldo, ldz;
+    int32_t act;
+    int32_t out_f32;               // out is fp32 whatever the type (residual, z: unused)
+    float* part;                   // [planes * splits][rows][cols] fp32 instead of the epilogue, or NULL
+};
+
+// dz = dy act'(z) of [rows][cols], as `planes` planes of the element type whose sum it is (plane k scaled by
+// plane_scale^k), [rows][ldo] each, zero in the padding columns; and partial column sums of dz.
+struct SlopeArgs {
+    const void* dy;
+    const void* z;
+    int64_t lddy, ldz, ldo;
+    int64_t rows, cols;
+    int32_t act, planes;
+    void* out;                     // NULL: column sums only
+    int64_t plane_stride;
+    float* sums;                   // [workgroups along the rows][cols], or NULL
+    int32_t row_blocks;
+};
+
+enum { kTile256 = 0, kTile128, kTile64, kTile128x32, kTileCount };
+
+struct TileShape {
+    int bi, bj, threads;
+};
+inline TileShape tile_shape(int tile)
+{
+    switch (tile) {
+    case kTile256: return {256, 256, 512};
+    case kTile128: return {128, 128, 256};
+    case kTile64: return {64, 64, 256};
+    default: return {128, 32, 256};
+    }
+}
+
+// per type T (the files linear_*.hip)
+template <typename T>
+struct LinearOps {
+    // fast_a (NT), fast_b (TT): the operand's rows are 16-byte aligned and whole 16-byte vectors
+    static hipError_t gemm_nt(int tile, bool fast_a, const GemmArgs& g, hipStream_t s);
+    static hipError_t gemm_tt(int tile, bool fast_b, const GemmArgs& g, hipStream_t s);
+    static hipError_t skinny(const GemmArgs& g, hipStream_t s);
+    static hipError_t slope(const SlopeArgs& p, hipStream_t s);
+    static hipError_t join(const GemmArgs& g, float plane_scale, hipStream_t s);   // adds the parts up, with the epilogue
+    // dst[c][r] (ldd) = src[r][c], or dst[r][c]; zero in the padding columns
+    static hipError_t layout(const void* src, int64_t lds, int64_t rows, int64_t cols, bool transpose, void* dst,
+                             int64_t ldd, hipStream_t s);
+};
+
+}  // namespace gsr

@@ -1,0 +1,309 @@
+// The linear operators' plans: which kernel takes a product, how its sum is
+// split and what is laid out in the workspace.
+//
+//   fwd: z = x W^T + b, y = act(z) + residual
+//   bwd: dz = dy act'(z), dx = dz W, dW = dz^T x, db = column sums of dz
+//
+// Products are tiled on the matrix cores (gemm.h). The forward and dx sum along
+// rows of both operands (NT; dx against a transposed copy of W in the workspace,
+// in * out values once per call), dW sums over the rows (TT). dz is written once
+// in the element type, with its column sums; without an activation dy is dz.
+#include "linear.h"
+
+namespace gsr {
+
+namespace {
+
+constexpr int64_t kSkinnyRows = 64;      // rows up to which the weights' bytes bound the product
+constexpr int kFillTiles = 256;          // compute units
+constexpr int kSlopeBlocks = 2048;
+constexpr int64_t kJoinSplitLen = 256;   // values of the sum in a split of a product of few tiles, at least
+constexpr int64_t kRowSplitLen = 512;    // rows in a split of dW's sum, at least
+
+int elem(int type) { return type == GS_F32 ? 4 : 2; }
+int64_t vec(int type) { return 16 / elem(type); }
+int64_t padded(int type, int64_t n) { return div_up(n, vec(type)) * vec(type); }
+
+// Rows that can be read as whole aligned 16-byte vectors, a tile's at 31-bit offsets.
+bool fast(const void* p, int64_t ld, int64_t cols, int type)
+{
+    return ((uintptr_t)p & 15) == 0 && ld % vec(type) == 0 && cols % vec(type) == 0 && ld <= GS_MAX_DIM;
+}
+
+struct Plan {
+    int tile;
+    int splits;
+    int64_t split_len;
+};
+
+// NT: the largest tile that still fills the compute units; the sum is split where even the smallest does not.
+Plan plan_nt(int type, int64_t rows, int64_t cols, int64_t len)
+{
+    Plan p = {kTile64, 1, len};
+    if (cols <= 32) {
+        p.tile = kTile128x32;
+        return p;
+    }
+    if (div_up(rows, 128) * div_up(cols, 128) >= kFillTiles) {
+        p.tile = kTile128;
+        return p;
+    }
+    const int64_t tiles = div_up(rows, 64) * div_up(cols, 64);
+    if (tiles < kFillTiles && len >= 2 * kJoinSplitLen) {
+        const int64_t want = std::min(div_up(2 * kFillTiles, tiles), len / kJoinSplitLen);
+        p.split_len = div_up(div_up(len, want), 64) * 64;
+        p.splits = (int)div_up(len, p.split_len);
+    }
+    return p;
+}
+
+// TT: the sum runs over the rows; its splits fill the compute units.
+Plan plan_tt(int64_t out, int64_t in, int64_t rows, int planes)
+{
+    Plan p;
+    p.tile = out >= 96 && in >= 96 ? kTile128 : kTile64;
+    const TileShape t = tile_shape(p.tile);
+    const int64_t tiles = div_up(out, t.bi) * div_up(in, t.bj) * planes;
+    const int64_t want = std::max<int64_t>(1, std::min(div_up(2 * kFillTiles, tiles), rows / kRowSplitLen));
+    p.split_len = std::max<int64_t>(64, div_up(div_up(rows, want), 64) * 64);
+    p.splits = (int)std::max<int64_t>(1, div_up(rows, p.split_len));
+    return p;
+}
+
+// Planes of dz: an fp32 weight gradient keeps what rounding dz to 16 bits would drop, as further planes of the
+// type; without an activation, or with relu, dz is dy or 0 and needs none.
+int planes_of(int type, int act, int dw_type)
+{
+    if (type == GS_F32 || dw_type != GS_F32 || act == GS_ACT_NONE || act == GS_ACT_RELU) return 1;
+    return type == GS_F16 ? 2 : 3;
+}
+
+float plane_scale(int type) { return type == GS_F16 ? 1.f / 2048.f : 1.f / 256.f; }
+
+int slope_row_blocks(int type, int64_t rows, int64_t cols)
+{
+    const int64_t blocks_x = div_up(div_up(cols, vec(type)), 64);
+    return (int)std::max<int64_t>(1, std::min(div_up(kSlopeBlocks, blocks_x), div_up(rows, 32)));
+}
+
+// Workspace: regions taken in order, 256-byte aligned.
+struct Regions {
+    char* base;
+    size_t at = 0;
+    void* take(int64_t bytes)
+    {
+        void* p = base ? base + at : nullptr;
+        at += align_up((size_t)bytes, 256);
+        return p;
+    }
+};
+
+struct FwdSpace {
+    void* w;       // W with padded rows, where its own cannot be read in vectors
+    float* part;
+    size_t bytes;
+};
+
+FwdSpace fwd_space(void* base, int type, int64_t rows, int64_t in, int64_t out, bool copy_w)
+{
+    Regions r{(char*)base};
+    FwdSpace f = {};
+    if (rows > kSkinnyRows) {
+        if (copy_w) f.w = r.take(out * padded(type, in) * elem(type));
+        const Plan p = plan_nt(type, rows, out, in);
+        if (p.splits > 1) f.part = (float*)r.take((int64_t)p.splits * rows * out * 4);
+    }
+    f.bytes = r.at;
+    return f;
+}
+
+struct BwdSpace {
+    void* dz;
+    void* wt;      // W transposed, [in][padded out]
+    float* sums;
+    float* part;   // of dx and of dW, one after the other
+    size_t bytes;
+};
+
+BwdSpace bwd_space(void* base, int type, int act, int64_t rows, int64_t in, int64_t out, int dw_type, bool need_dz)
+{
+    Regions r{(char*)base};
+    BwdSpace b = {};
+    const int planes = planes_of(type, act, dw_type);
+    if (need_dz) b.dz = r.take(planes * rows * padded(type, out) * elem(type));
+    b.wt = r.take(in * padded(type, out) * elem(type));
+    b.sums = (float*)r.take((int64_t)slope_row_blocks(type, rows, out) * out * 4);
+    int64_t part = 0;
+    if (rows > kSkinnyRows) {
+        const Plan x = plan_nt(type, rows, in, out);
+        if (x.splits > 1) part = (int64_t)x.splits * rows * in * 4;
+    }
+    const Plan w = plan_tt(out, in, rows, planes);
+    if (w.splits * planes > 1) part = std::max(part, (int64_t)w.splits * planes * out * in * 4);
+    b.part = (float*)r.take(part);
+    b.bytes = r.at;
+    return b;
+}
+
+// A product along rows with its epilogue: few rows, one launch of tiles, or splits and their join.
+template <typename T>
+hipError_t run_nt(int type, GemmArgs g, bool fast_a, float* part, hipStream_t s)
+{
+    g.splits = g.planes = 1;
+    g.split_len = g.len;
+    g.a_rows = g.rows;
+    g.b_rows = g.cols;
+    if (g.rows <= kSkinnyRows) return LinearOps<T>::skinny(g, s);
+    const Plan p = plan_nt(type, g.rows, g.cols, g.len);
+    g.splits = p.splits;
+    g.split_len = p.split_len;
+    g.part = p.splits > 1 ? part : nullptr;
+    const hipError_t e = LinearOps<T>::gemm_nt(p.tile, fast_a, g, s);
+    if (e != hipSuccess || p.splits == 1) return e;
+    return LinearOps<T>::join(g, 1.f, s);
+}
+
+template <typename T>
+hipError_t linear_fwd(const gs_linear& p, const void* residual, int64_t ldr, void* y, int64_t ldy, void* z,
+                      int64_t ldz, void* ws, hipStream_t s)
+{
+    const bool copy_w = !fast(p.w, p.ldw, p.n_in, p.type);
+    const FwdSpace f = fwd_space(ws, p.type, p.rows, p.n_in, p.n_out, copy_w);
+    GemmArgs g = {};
+    g.a = p.x;
+    g.lda = p.ldx;
+    g.b = p.w;
+    g.ldb = p.ldw;
+    if (f.w) {
+        g.b = f.w;
+        g.ldb = padded(p.type, p.n_in);
+        const hipError_t e = LinearOps<T>::layout(p.w, p.ldw, p.n_out, p.n_in, false, f.w, g.ldb, s);
+        if (e != hipSuccess) return e;
+    }
+    g.rows = p.rows;
+    g.cols = p.n_out;
+    g.len = p.n_in;
+    g.bias = p.bias;
+    g.act = p.act;
+    g.residual = residual;
+    g.ldr = ldr;
+    g.out = y;
+    g.ldo = ldy;
+    g.z = z;
+    g.ldz = ldz;
+    return run_nt<T>(p.type, g, fast(p.x, p.ldx, p.n_in, p.type), f.part, s);
+}
+
+template <typename T>
+hipError_t linear_bwd(const gs_linear& p, const void* dy, int64_t lddy, const void* z, int64_t ldz, void* dx,
+                      int64_t lddx, void* dw, int64_t lddw, int dw_type, float* db, void* ws, hipStream_t s)
+{
+    const bool need_dz = p.act != GS_ACT_NONE || !fast(dy, lddy, p.n_out, p.type);
+    const BwdSpace b = bwd_space(ws, p.type, p.act, p.rows, p.n_in, p.n_out, dw_type, need_dz);
+    const int planes = dw ? planes_of(p.type, p.act, dw_type) : 1;
+    const int64_t ldo = need_dz ? padded(p.type, p.n_out) : lddy;
+    const void* dz = need_dz ? b.dz : dy;
+    hipError_t e = hipSuccess;
+    if (need_dz || db) {
+        SlopeArgs a = {};
+        a.dy = dy;
+        a.lddy = lddy;
+        a.z = z;
+        a.ldz = ldz;
+        a.rows = p.rows;
+        a.cols = p.n_out;
+        a.act = p.act;
+        a.planes = planes;
+        a.out = need_dz ? b.dz : nullptr;
+        a.ldo = need_dz ? ldo : 0;
+        a.plane_stride = p.rows * ldo;
+        a.row_blocks = slope_row_blocks(p.type, p.rows, p.n_out);
+        a.sums = db ? (a.row_blocks == 1 ? db : b.sums) : nullptr;
+        e = LinearOps<T>::slope(a, s);
+        if (e == hipSuccess && db && a.row_blocks > 1)
+            e = launch_column_sum(b.sums, a.row_blocks, p.n_out, p.n_out, db, nullptr, s);
+        if (e != hipSuccess) return e;
+    }
+    if (dx && p.rows > 0) {
+        GemmArgs g = {};
+        const int64_t ldt = padded(p.type, p.n_out);
+        e = LinearOps<T>::layout(p.w, p.ldw, p.n_out, p.n_in, true, b.wt, ldt, s);
+        if (e != hipSuccess) return e;
+        g.a = dz;
+        g.lda = ldo;
+        g.b = b.wt;
+        g.ldb = ldt;
+        g.rows = p.rows;
+        g.cols = p.n_in;
+        g.len = p.n_out;
+        g.out = dx;
+        g.ldo = lddx;
+        e = run_nt<T>(p.type, g, true, b.part, s);
+        if (e != hipSuccess) return e;
+    }
+    if (dw) {
+        GemmArgs g = {};
+        const Plan plan = plan_tt(p.n_out, p.n_in, p.rows, planes);
+        g.a = dz;
+        g.lda = ldo;
+        g.b = p.x;
+        g.ldb = p.ldx;
+        g.rows = p.n_out;
+        g.cols = p.n_in;
+        g.len = g.a_rows = g.b_rows = p.rows;
+        g.splits = plan.splits;
+        g.split_len = plan.split_len;
+        g.planes = planes;
+        g.plane_stride = p.rows * ldo;
+        g.out = dw;
+        g.ldo = lddw;
+        g.out_f32 = dw_type == GS_F32;
+        g.part = plan.splits * planes > 1 ? b.part : nullptr;
+        e = LinearOps<T>::gemm_tt(plan.tile, fast(p.x, p.ldx, p.n_in, p.type), g, s);
+        if (e == hipSuccess && g.part) e = LinearOps<T>::join(g, plane_scale(p.type), s);
+    }
+    return e;
+}
+
+}  // namespace
+
+size_t linear_fwd_workspace(const gs_linear& p)
+{
+    return fwd_space(nullptr, p.type, p.rows, p.n_in, p.n_out, !fast(p.w, p.ldw, p.n_in, p.type)).bytes;
+}
+
+size_t linear_bwd_workspace(const gs_linear& p, const void* dy, int64_t lddy, int dw_type)
+{
+    return bwd_space(nullptr, p.type, p.act, p.rows, p.n_in, p.n_out, dw_type,
+                     p.act != GS_ACT_NONE || !fast(dy, lddy, p.n_out, p.type)).bytes;
+}
+
+size_t linear_workspace(int type, int act, int64_t rows, int64_t in, int64_t out, int dw_type)
+{
+    const size_t fwd = fwd_space(nullptr, type, rows, in, out, true).bytes;
+    return dw_type < 0 ? fwd : std::max(fwd, bwd_space(nullptr, type, act, rows, in, out, dw_type, true).bytes);
+}
+
+// Work items of a launch are counted in 32 bits.
+bool linear_grid_fits(int64_t rows, int64_t cols)
+{
+    return div_up(rows, 128) * div_up(cols, cols <= 32 ? 32 : 128) * 256 < ((int64_t)1 << 32);
+}
+
+hipError_t launch_linear_fwd(const gs_linear& p, const void* residual, int64_t ldr, void* y, int64_t ldy, void* z,
+                             int64_t ldz, void* ws, hipStream_t s)
+{
+    if (p.type == GS_F16) return linear_fwd<f16>(p, residual, ldr, y, ldy, z, ldz, ws, s);
+    if (p.type == GS_BF16) return linear_fwd<bf16>(p, residual, ldr, y, ldy, z, ldz, ws, s);
+    return linear_fwd<float>(p, residual, ldr, y, ldy, z, ldz, ws, s);
+}
+
+hipError_t launch_linear_bwd(const gs_linear& p, const void* dy, int64_t lddy, const void* z, int64_t ldz, void* dx,
+                             int64_t lddx, void* dw, int64_t lddw, int dw_type, float* db, void* ws, hipStream_t s)
+{
+    if (p.type == GS_F16) return linear_bwd<f16>(p, dy, lddy, z, ldz, dx, lddx, dw, lddw, dw_type, db, ws, s);
+    if (p.type == GS_BF16) return linear_bwd<bf16>(p, dy, lddy, z, ldz, dx, lddx, dw, lddw, dw_type, db, ws, s);
+    return linear_bwd<float>(p, dy, lddy, z, ldz, dx, lddx, dw, lddw, dw_type, db, ws, s);
+}
+
+}  // namespace gsr

@@ -32,7 +32,10 @@ def neural_weight_count(arch=None) -> int:
     layers, width = (2, 16) if arch is None else (int(arch[0]), int(arch[1]))
     return 32 * width + (layers - 1) * width * width + 3 * width
 KERNEL_NAMES = ["preprocess", "pair_count", "depth_sort", "entry_offsets", "block_entries", "block_sort", "tile_lists",
-                "blend_fwd", "bwd_prep", "blend_bwd", "preprocess_bwd", "mlp_reduce", "adam", "neural_fold"]
+                "blend_fwd", "bwd_prep", "blend_bwd", "preprocess_bwd", "mlp_reduce", "adam", "neural_fold",
+                "layer_norm_fwd", "layer_norm_bwd", "linear_fwd", "linear_bwd", "grad_norm"]
+TYPE_IDS = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}   # GS_F32, GS_F16, GS_BF16
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3, "tanh": 4, "sigmoid": 5}   # GS_ACT_*
 ADAM_MAX_TENSORS = 8
 ADAM_MAX_ROWS = 128
 SPLAT_BYTES = 64
@@ -87,6 +90,16 @@ class AdamTensor(C.Structure):
                 ("lr", C.POINTER(C.c_float))]
 
 
+class Linear(C.Structure):
+    _fields_ = [("type", C.c_int32), ("act", C.c_int32), ("rows", C.c_int64), ("n_in", C.c_int64),
+                ("n_out", C.c_int64), ("x", C.c_void_p), ("w", C.c_void_p), ("bias", C.c_void_p), ("ldx", C.c_int64),
+                ("ldw", C.c_int64)]
+
+
+class GradTensor(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("type", C.c_int32)]
+
+
 _lib = None
 
 
@@ -109,6 +122,17 @@ def lib() -> C.CDLL:
         L.gs_mlp_eval.argtypes = [vp, i64, vp, vp, vp]
         L.gs_neural_fold.argtypes = [vp, vp, i64, vp, vp]
         L.gs_adam_step.argtypes = [P(AdamTensor), i32, C.c_float, C.c_float, i64, vp]
+        L.gs_adam_step_scaled.argtypes = [P(AdamTensor), i32, C.c_float, C.c_float, i64, vp, vp]
+        L.gs_layer_norm_fwd.argtypes = [i32, i64, i64, vp, i64, vp, vp, C.c_float, vp, i64, vp, vp, vp]
+        L.gs_layer_norm_bwd.argtypes = [i32, i64, i64, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp, sz,
+                                        vp]
+        L.gs_layer_norm_workspace_size.argtypes = [i32, i64, i64, P(sz)]
+        L.gs_linear_fwd.argtypes = [P(Linear), vp, i64, vp, i64, vp, i64, vp, sz, vp]
+        L.gs_linear_bwd.argtypes = [P(Linear), vp, i64, vp, i64, vp, i64, vp, i64, i32, vp, vp, sz, vp]
+        L.gs_linear_workspace_size.argtypes = [i32, i32, i64, i64, i64, i32, P(sz)]
+        L.gs_grad_norm.argtypes = [P(GradTensor), i32, C.c_float, vp, vp, sz, vp]
+        L.gs_grad_clip.argtypes = [P(GradTensor), i32, C.c_float, vp, vp, sz, vp]
+        L.gs_grad_workspace_size.argtypes = [P(GradTensor), i32, P(sz)]
         L.gs_render_bwd_adam.argtypes = [P(Camera), P(Gaussians), P(Appearance), P(Preprocessed), vp, vp, vp, vp,
                                          vp, P(Grads), P(AdamTensor), C.c_float, C.c_float, i64, vp, sz, vp]
         L.gs_timer_create.argtypes = [P(vp)]
@@ -118,7 +142,9 @@ def lib() -> C.CDLL:
         L.gs_timer_read.argtypes = [vp, P(C.c_double), P(i64), i32]
         for f in ("gs_preprocess", "gs_preprocess_noalloc", "gs_bin_sort", "gs_render_fwd", "gs_render_work",
                   "gs_render_bwd", "gs_render_bwd_adam", "gs_workspace_size", "gs_mlp_eval", "gs_neural_fold",
-                  "gs_adam_step", "gs_timer_create", "gs_timer_destroy", "gs_timer_attach", "gs_timer_reset",
+                  "gs_adam_step", "gs_adam_step_scaled", "gs_layer_norm_fwd", "gs_layer_norm_bwd",
+                  "gs_layer_norm_workspace_size", "gs_linear_fwd", "gs_linear_bwd", "gs_linear_workspace_size",
+                  "gs_grad_norm", "gs_grad_clip", "gs_grad_workspace_size", "gs_timer_create", "gs_timer_destroy", "gs_timer_attach", "gs_timer_reset",
                   "gs_timer_read"):
             getattr(L, f).restype = C.c_int
         L.gs_last_error.restype = C.c_char_p
@@ -288,11 +314,18 @@ def _adam_tensors(tensors):
     return arr, keep
 
 
-def gs_adam_step(tensors, beta1: float, eps: float, step: int, stream=None):
+def gs_adam_step(tensors, beta1: float, eps: float, step: int, stream=None, grad_scale=None):
     """tensors: list of dicts with param, grad, exp_avg, exp_avg_sq (device fp32 [rows][n]), optional
-    param_half (device int16/uint16 [rows][n]), rows, n, beta2 and lr (a sequence of `rows` floats)."""
+    param_half (device int16/uint16 [rows][n]), rows, n, beta2 and lr (a sequence of `rows` floats).
+    grad_scale: optional device fp32 value (gs_grad_norm's coefficient) that multiplies every gradient."""
     arr, keep = _adam_tensors(tensors)
-    _check(lib().gs_adam_step(arr, len(tensors), float(beta1), float(eps), int(step), _stream(stream)))
+    if grad_scale is None:
+        _check(lib().gs_adam_step(arr, len(tensors), float(beta1), float(eps), int(step), _stream(stream)))
+    else:
+        if grad_scale.dtype != torch.float32 or grad_scale.numel() < 1 or not grad_scale.is_cuda:
+            raise ValueError("grad_scale: a float32 value on the GPU expected")
+        _check(lib().gs_adam_step_scaled(arr, len(tensors), float(beta1), float(eps), int(step), _ptr(grad_scale),
+                                         _stream(stream)))
 
 
 GS_RENDER_ADAM_TENSORS = 5
@@ -310,6 +343,175 @@ def gs_render_bwd_adam(cam: Camera, g: Gaussians, app: Appearance, pre: Preproce
                                     _ptr(tile_ranges), _ptr(final_T), _ptr(n_contrib), _ptr(dL_dimage),
                                     C.byref(grads), arr, float(beta1), float(eps), int(step), _ptr(workspace),
                                     ws_bytes, _stream(stream)))
+
+
+# ---- row operators: layer norm, linear, gradient clipping ----------------------
+
+
+def _type_id(t) -> int:
+    k = TYPE_IDS.get(t.dtype)
+    if k is None:
+        raise ValueError("element type %s: float32, float16 or bfloat16 expected" % t.dtype)
+    return k
+
+
+def _matrix(name, t, rows, cols, dtype):
+    """Address and row stride of a [rows][cols] matrix on the GPU, its columns next to each other."""
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or t.dtype != dtype:
+        raise ValueError("%s: %s of %s, a [%d][%d] matrix of %s expected" % (name, tuple(t.shape), t.dtype, rows, cols,
+                                                                            dtype))
+    if not t.is_cuda:
+        raise ValueError("%s is not on the GPU" % name)
+    ld, step = t.stride()
+    if cols > 1 and step != 1:
+        raise ValueError("%s: columns %d elements apart, neighbours expected" % (name, step))
+    return t.data_ptr(), (ld if rows > 1 else cols)
+
+
+def _vector(name, t, n):
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError("%s: a contiguous float32 array of %d values on the GPU expected" % (name, n))
+    return t.data_ptr()
+
+
+def _space(workspace):
+    if workspace is None:
+        return None, 0
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _shape(name, t):
+    if t.dim() != 2:
+        raise ValueError("%s: a matrix expected, not %s" % (name, tuple(t.shape)))
+    return t.shape
+
+
+def gs_layer_norm_workspace_size(x) -> int:
+    """Workspace bytes of gs_layer_norm_bwd for x's shape and type."""
+    rows, dim = _shape("x", x)
+    out = C.c_size_t(0)
+    _check(lib().gs_layer_norm_workspace_size(_type_id(x), rows, dim, C.byref(out)))
+    return out.value
+
+
+def gs_layer_norm_fwd(x, w, b, eps: float, y, mean=None, rstd=None, stream=None):
+    """Layer norm of each row of x into y (matrices of one type); w and b: float32 [dim] or None; mean and rstd:
+    float32 [rows], kept for the backward."""
+    rows, dim = _shape("x", x)
+    px, ldx = _matrix("x", x, rows, dim, x.dtype)
+    py, ldy = _matrix("y", y, rows, dim, x.dtype)
+    _check(lib().gs_layer_norm_fwd(_type_id(x), rows, dim, px, ldx, _vector("w", w, dim), _vector("b", b, dim), eps, py,
+                                   ldy, _vector("mean", mean, rows), _vector("rstd", rstd, rows), _stream(stream)))
+
+
+def gs_layer_norm_bwd(dy, x, w, mean, rstd, dx, dw, db, workspace, add=None, stream=None):
+    """Backward of gs_layer_norm_fwd: dx (plus `add`, a gradient of x's shape), and float32 dw, db (or None)."""
+    rows, dim = _shape("x", x)
+    t = x.dtype
+    px, ldx = _matrix("x", x, rows, dim, t)
+    pdy, lddy = _matrix("dy", dy, rows, dim, t)
+    pdx, lddx = _matrix("dx", dx, rows, dim, t)
+    padd, ldadd = (None, 0) if add is None else _matrix("add", add, rows, dim, t)
+    ws, ws_bytes = _space(workspace)
+    _check(lib().gs_layer_norm_bwd(_type_id(x), rows, dim, pdy, lddy, px, ldx, _vector("w", w, dim),
+                                   _vector("mean", mean, rows), _vector("rstd", rstd, rows), padd, ldadd, pdx, lddx,
+                                   _vector("dw", dw, dim), _vector("db", db, dim), ws, ws_bytes, _stream(stream)))
+
+
+def _activation(act) -> int:
+    k = ACTIVATIONS.get(act)
+    if k is None:
+        raise ValueError("activation %r: one of %s expected" % (act, ", ".join(ACTIVATIONS)))
+    return k
+
+
+def gs_linear_workspace_size(x, w, act: str = "none", dw_type=torch.float32) -> int:
+    """Workspace bytes of gs_linear_fwd and gs_linear_bwd for these shapes; dw_type: the weight gradient's type
+    (None: for the forward alone)."""
+    rows, n_in = _shape("x", x)
+    n_out = _shape("w", w)[0]
+    out = C.c_size_t(0)
+    _check(lib().gs_linear_workspace_size(_type_id(x), _activation(act), rows, n_in, n_out,
+                                          -1 if dw_type is None else TYPE_IDS[dw_type], C.byref(out)))
+    return out.value
+
+
+def _layer(x, w, bias, act):
+    rows, n_in = _shape("x", x)
+    n_out = _shape("w", w)[0]
+    px, ldx = _matrix("x", x, rows, n_in, x.dtype)
+    pw, ldw = _matrix("w", w, n_out, n_in, x.dtype)
+    return Linear(_type_id(x), _activation(act), rows, n_in, n_out, px, pw, _vector("bias", bias, n_out), ldx, ldw)
+
+
+def gs_linear_fwd(x, w, bias, y, workspace=None, act: str = "none", residual=None, z=None, stream=None):
+    """y = act(x w^T + bias) + residual; w: [out][in] of x's type, bias: float32 [out] or None; z, if given, receives
+    x w^T + bias for the backward."""
+    p = _layer(x, w, bias, act)
+    rows, n_out, t = p.rows, p.n_out, x.dtype
+    py, ldy = _matrix("y", y, rows, n_out, t)
+    pr, ldr = (None, 0) if residual is None else _matrix("residual", residual, rows, n_out, t)
+    pz, ldz = (None, 0) if z is None else _matrix("z", z, rows, n_out, t)
+    ws, ws_bytes = _space(workspace)
+    _check(lib().gs_linear_fwd(C.byref(p), pr, ldr, py, ldy, pz, ldz, ws, ws_bytes, _stream(stream)))
+
+
+def gs_linear_bwd(dy, x, w, z, dx, dw, db, workspace, act: str = "none", stream=None):
+    """Backward of gs_linear_fwd: dx of x's type, dw float32 or of x's type, db float32 (each may be None); z as the
+    forward wrote it (None without an activation)."""
+    p = _layer(x, w, None, act)
+    rows, n_in, n_out, t = p.rows, p.n_in, p.n_out, x.dtype
+    pdy, lddy = _matrix("dy", dy, rows, n_out, t)
+    pz, ldz = (None, 0) if z is None else _matrix("z", z, rows, n_out, t)
+    pdx, lddx = (None, 0) if dx is None else _matrix("dx", dx, rows, n_in, t)
+    pdw, lddw, dw_type = None, 0, 0
+    if dw is not None:
+        pdw, lddw = _matrix("dw", dw, n_out, n_in, torch.float32 if dw.dtype == torch.float32 else t)
+        dw_type = TYPE_IDS[dw.dtype]
+    ws, ws_bytes = _space(workspace)
+    _check(lib().gs_linear_bwd(C.byref(p), pdy, lddy, pz, ldz, pdx, lddx, pdw, lddw, dw_type, _vector("db", db, n_out),
+                               ws, ws_bytes, _stream(stream)))
+
+
+class GradSet:
+    """The gradients of one global norm, as gs_grad_norm and gs_grad_clip take them: contiguous tensors of any element
+    type, clipped in place or, where `out` has a float32 tensor for them, into that. Keeps the tensors alive; the
+    values may change between calls, the storage may not."""
+
+    def __init__(self, grads, out=None):
+        self.grads = list(grads)
+        self.out = [None] * len(self.grads) if out is None else list(out)
+        if len(self.out) != len(self.grads):
+            raise ValueError("out needs an entry for each gradient")
+        self.array = (GradTensor * max(1, len(self.grads)))()
+        for k, (g, o) in enumerate(zip(self.grads, self.out)):
+            if not g.is_contiguous() or not g.is_cuda:
+                raise ValueError("gradient %d: a contiguous tensor on the GPU expected" % k)
+            if o is not None:
+                _vector("out %d" % k, o, g.numel())
+            self.array[k] = GradTensor(g.data_ptr(), None if o is None else o.data_ptr(), g.numel(), _type_id(g))
+
+
+def gs_grad_workspace_size(grads: GradSet) -> int:
+    out = C.c_size_t(0)
+    _check(lib().gs_grad_workspace_size(grads.array, len(grads.grads), C.byref(out)))
+    return out.value
+
+
+def gs_grad_norm(grads: GradSet, max_norm: float, result, workspace, stream=None):
+    """result (float32 [2] on the GPU) = the global norm and the coefficient min(1, max_norm / (norm + 1e-6))."""
+    ws, ws_bytes = _space(workspace)
+    _check(lib().gs_grad_norm(grads.array, len(grads.grads), max_norm, _vector("result", result, 2), ws, ws_bytes,
+                              _stream(stream)))
+
+
+def gs_grad_clip(grads: GradSet, max_norm: float, result, workspace, stream=None):
+    """gs_grad_norm, and every gradient times the coefficient, in place or into the set's `out`."""
+    ws, ws_bytes = _space(workspace)
+    _check(lib().gs_grad_clip(grads.array, len(grads.grads), max_norm, _vector("result", result, 2), ws, ws_bytes,
+                              _stream(stream)))
 
 
 class Timer:
