@@ -367,20 +367,6 @@ __global__ __launch_bounds__(WI* WJ * 64) void k_gemm(GemmArgs g)
 // weights.
 constexpr int kSkinnyWaves = 8;
 
-template <typename T>
-__device__ __forceinline__ typename Vec<T>::Packed load_any(const T* p, int64_t left)
-{
-    typename Vec<T>::Packed t = {};
-    if (left >= Vec<T>::N) {
-        t = *reinterpret_cast<const typename Vec<T>::Any*>(p);
-    } else {
-#pragma unroll
-        for (int j = 0; j < Vec<T>::N; ++j)
-            if (j < left) t[j] = p[j];
-    }
-    return t;
-}
-
 template <typename T, int MF>
 __global__ __launch_bounds__(kSkinnyWaves * 64) void k_skinny(GemmArgs g)
 {
@@ -437,37 +423,49 @@ __global__ __launch_bounds__(kSkinnyWaves * 64) void k_skinny(GemmArgs g)
     }
 }
 
-// Adds up the parts of a split product in a fixed order and applies the epilogue: a thread per 4 values of a row.
+// Adds up the parts of a split product in a fixed order and applies the epilogue. A workgroup takes 4 values each of
+// kBlock / slices places; `slices` threads share a place's parts and meet in LDS.
 template <typename T>
-__global__ __launch_bounds__(kBlock) void k_join(GemmArgs g, float plane_scale)
+__global__ __launch_bounds__(kBlock) void k_join(GemmArgs g, float plane_scale, int slices)
 {
+    __shared__ f32x4 sums[kBlock];
     const int64_t quads = (g.cols + 3) / 4, total = g.rows * quads;
     const int64_t size = g.rows * g.cols;
-    for (int64_t k = (int64_t)blockIdx.x * kBlock + threadIdx.x; k < total; k += (int64_t)gridDim.x * kBlock) {
-        const int64_t i = k / quads, j = (k - i * quads) * 4, left = g.cols - j;
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
+    const int places = kBlock / slices, place = threadIdx.x % places, slice = threadIdx.x / places;
+    const int64_t k = (int64_t)blockIdx.x * places + place;
+    const int64_t i = k / quads, j = (k - i * quads) * 4, left = g.cols - j;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (k < total)
         for (int p = g.planes - 1; p >= 0; --p) {
-            float t[4] = {0.f, 0.f, 0.f, 0.f}, u[4];
-            for (int s = 0; s < g.splits; ++s) {
-                load_vec(g.part + (int64_t)(p * g.splits + s) * size + i * g.cols + j, left, u);
+            const float* part = g.part + (int64_t)p * g.splits * size + i * g.cols + j;
+            f32x4 t = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+            for (int s = slice; s < g.splits; s += slices) {
+                float u[4];
+                load_vec(part + (int64_t)s * size, left, u);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) t[e] += u[e];
             }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = v[e] * plane_scale + t[e];
+            v = v * plane_scale + t;
         }
+    if (slices > 1) {
+        sums[threadIdx.x] = v;
+        __syncthreads();
+        if (slice == 0)
+            for (int q = 1; q < slices; ++q) v += sums[q * places + place];
+    }
+    if (slice != 0 || k >= total) return;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if (e >= left) break;
-            float t = v[e] + (g.bias ? g.bias[j + e] : 0.f);
-            if (g.z) ((T*)g.z)[i * g.ldz + j + e] = (T)t;
-            activate<1>(g.act, &t);
-            if (g.residual) t += (float)((const T*)g.residual)[i * g.ldr + j + e];
-            if (g.out_f32)
-                ((float*)g.out)[i * g.ldo + j + e] = t;
-            else
-                ((T*)g.out)[i * g.ldo + j + e] = (T)t;
-        }
+    for (int e = 0; e < 4; ++e) {
+        if (e >= left) break;
+        float t = v[e] + (g.bias ? g.bias[j + e] : 0.f);
+        if (g.z) ((T*)g.z)[i * g.ldz + j + e] = (T)t;
+        activate<1>(g.act, &t);
+        if (g.residual) t += (float)((const T*)g.residual)[i * g.ldr + j + e];
+        if (g.out_f32)
+            ((float*)g.out)[i * g.ldo + j + e] = t;
+        else
+            ((T*)g.out)[i * g.ldo + j + e] = (T)t;
     }
 }
 
@@ -524,29 +522,40 @@ __global__ __launch_bounds__(kBlock) void k_slope(SlopeArgs p, int lanes)
     }
 }
 
-// 32 x 32 tiles through LDS. dst has `drows` rows of ldd values, all written (padding: zero).
+// 64 x 64 tiles through LDS, whole 16-byte vectors in and out. dst: aligned rows of ldd values, a multiple of a
+// vector, all written (padding: zero).
+constexpr int kLayoutTile = 64;
+
 template <typename T>
 __global__ __launch_bounds__(kBlock) void k_layout(const T* __restrict__ src, int64_t lds, int64_t rows, int64_t cols,
                                                    int transpose, T* __restrict__ dst, int64_t ldd)
 {
-    __shared__ T t[32][33];
-    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
-    const int64_t r0 = (int64_t)blockIdx.y * 32, c0 = (int64_t)blockIdx.x * 32;
+    constexpr int N = Vec<T>::N, kRowVecs = kLayoutTile / N;
+    __shared__ T t[kLayoutTile][kLayoutTile + 4 / sizeof(T)];
+    const int64_t r0 = (int64_t)blockIdx.y * kLayoutTile, c0 = (int64_t)blockIdx.x * kLayoutTile;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int64_t r = r0 + y + 8 * k, c = c0 + x;
-        t[y + 8 * k][x] = r < rows && c < cols ? src[r * lds + c] : (T)0.f;
+    for (int q = threadIdx.x; q < kLayoutTile * kRowVecs; q += kBlock) {
+        const int r = q / kRowVecs, c = q % kRowVecs * N;
+        const typename Vec<T>::Packed v = load_any(src + (r0 + r) * lds + c0 + c, r0 + r < rows ? cols - c0 - c : 0);
+        if (!transpose) {
+            if (r0 + r < rows && c0 + c < ldd)
+                *reinterpret_cast<typename Vec<T>::Packed*>(dst + (r0 + r) * ldd + c0 + c) = v;
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e) t[r][c + e] = v[e];
+        }
     }
+    if (!transpose) return;
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        if (transpose) {
-            const int64_t r = c0 + y + 8 * k, c = r0 + x;
-            if (r < cols && c < ldd) dst[r * ldd + c] = t[x][y + 8 * k];
-        } else {
-            const int64_t r = r0 + y + 8 * k, c = c0 + x;
-            if (r < rows && c < ldd) dst[r * ldd + c] = t[y + 8 * k][x];
-        }
+    for (int q = threadIdx.x; q < kLayoutTile * kRowVecs; q += kBlock) {
+        // neighbouring lanes take neighbouring columns of the tile: LDS reads without conflicts
+        const int r = q % kLayoutTile, c = q / kLayoutTile * N;
+        if (c0 + r >= cols || r0 + c >= ldd) continue;
+        typename Vec<T>::Packed v;
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = t[c + e][r];
+        *reinterpret_cast<typename Vec<T>::Packed*>(dst + (c0 + r) * ldd + r0 + c) = v;
     }
 }
 
@@ -564,6 +573,7 @@ hipError_t run_gemm(const GemmArgs& g, hipStream_t s)
 template <typename T>
 hipError_t LinearOps<T>::gemm_nt(int tile, bool fast_a, const GemmArgs& g, hipStream_t s)
 {
+    if (tile == kTile256) return run_gemm<T, false, 256, 256, 2, 4, true>(g, s);   // fast_a only
     if (tile == kTile128)
         return fast_a ? run_gemm<T, false, 128, 128, 2, 2, true>(g, s) : run_gemm<T, false, 128, 128, 2, 2, false>(g, s);
     if (tile == kTile128x32)
@@ -574,6 +584,7 @@ hipError_t LinearOps<T>::gemm_nt(int tile, bool fast_a, const GemmArgs& g, hipSt
 template <typename T>
 hipError_t LinearOps<T>::gemm_tt(int tile, bool fast_b, const GemmArgs& g, hipStream_t s)
 {
+    if (tile == kTile256) return run_gemm<T, true, 256, 256, 2, 4, true>(g, s);   // fast_b only
     if (tile == kTile128)
         return fast_b ? run_gemm<T, true, 128, 128, 2, 2, true>(g, s) : run_gemm<T, true, 128, 128, 2, 2, false>(g, s);
     return fast_b ? run_gemm<T, true, 64, 64, 2, 2, true>(g, s) : run_gemm<T, true, 64, 64, 2, 2, false>(g, s);
@@ -606,8 +617,12 @@ hipError_t LinearOps<T>::slope(const SlopeArgs& p, hipStream_t s)
 template <typename T>
 hipError_t LinearOps<T>::join(const GemmArgs& g, float plane_scale, hipStream_t s)
 {
-    const int64_t blocks = std::min<int64_t>(div_up(g.rows * div_up(g.cols, 4), kBlock), 4096);
-    hipLaunchKernelGGL((k_join<T>), dim3((unsigned)blocks), dim3(kBlock), 0, s, g, plane_scale);
+    // enough workgroups to fill the compute units, at least 4 parts a thread
+    const int64_t places = g.rows * div_up(g.cols, 4);
+    int slices = 1;
+    while (slices < 32 && places * slices < 1024 * kBlock && g.splits >= 8 * slices) slices *= 2;
+    hipLaunchKernelGGL((k_join<T>), dim3((unsigned)div_up(places, kBlock / slices)), dim3(kBlock), 0, s, g, plane_scale,
+                       slices);
     return hipGetLastError();
 }
 
@@ -616,8 +631,8 @@ hipError_t LinearOps<T>::layout(const void* src, int64_t lds, int64_t rows, int6
                                 int64_t ldd, hipStream_t s)
 {
     const int64_t w = transpose ? cols : std::max(cols, ldd), h = transpose ? std::max(rows, ldd) : rows;
-    hipLaunchKernelGGL((k_layout<T>), dim3((unsigned)div_up(w, 32), (unsigned)div_up(h, 32)), dim3(kBlock), 0, s,
-                       (const T*)src, lds, rows, cols, transpose ? 1 : 0, (T*)dst, ldd);
+    hipLaunchKernelGGL((k_layout<T>), dim3((unsigned)div_up(w, kLayoutTile), (unsigned)div_up(h, kLayoutTile)),
+                       dim3(kBlock), 0, s, (const T*)src, lds, rows, cols, transpose ? 1 : 0, (T*)dst, ldd);
     return hipGetLastError();
 }
 

@@ -23,7 +23,9 @@ namespace {
 constexpr int kGradChunk = 8192;
 constexpr int kGradTable = 100;
 constexpr int kGradBlocks = 2048;        // workgroups of all launches of a norm together, about
-constexpr int kGradSmall = 16;           // chunks that one workgroup takes alone, in one launch
+// One workgroup takes a few gradients alone, in one launch, a chunk of kSmallChunk elements per wave.
+constexpr int kSmallChunk = 1024;
+constexpr int kSmallChunks = 128;
 constexpr int kSmallThreads = 1024;
 
 struct GradEntry {
@@ -61,13 +63,14 @@ __device__ __forceinline__ int tensor_of(const GradTable& a, uint32_t chunk)
     return lo;
 }
 
-template <typename T, int THREADS>
-__device__ __forceinline__ double chunk_squares(const T* g, int64_t left)
+// LANES threads, of which this is number `lane`, take a chunk of CHUNK elements
+template <typename T, int LANES, int CHUNK>
+__device__ __forceinline__ double chunk_squares(const T* g, int64_t left, int lane)
 {
     constexpr int N = Vec<T>::N;
     double s = 0.0;
 #pragma unroll 4
-    for (int c = threadIdx.x * N; c < kGradChunk; c += THREADS * N) {
+    for (int c = lane * N; c < CHUNK; c += LANES * N) {
         float v[N];
         load_vec(g + c, left - c, v);
 #pragma unroll
@@ -76,21 +79,21 @@ __device__ __forceinline__ double chunk_squares(const T* g, int64_t left)
     return s;
 }
 
-template <int THREADS>
-__device__ __forceinline__ double squares_of(const GradEntry& e, uint32_t chunk)
+template <int LANES, int CHUNK>
+__device__ __forceinline__ double squares_of(const GradEntry& e, uint32_t chunk, int lane)
 {
-    const int64_t at = (int64_t)(chunk - e.chunk0) * kGradChunk;
-    if (e.type == GS_F16) return chunk_squares<f16, THREADS>((const f16*)e.g + at, e.n - at);
-    if (e.type == GS_BF16) return chunk_squares<bf16, THREADS>((const bf16*)e.g + at, e.n - at);
-    return chunk_squares<float, THREADS>((const float*)e.g + at, e.n - at);
+    const int64_t at = (int64_t)(chunk - e.chunk0) * CHUNK;
+    if (e.type == GS_F16) return chunk_squares<f16, LANES, CHUNK>((const f16*)e.g + at, e.n - at, lane);
+    if (e.type == GS_BF16) return chunk_squares<bf16, LANES, CHUNK>((const bf16*)e.g + at, e.n - at, lane);
+    return chunk_squares<float, LANES, CHUNK>((const float*)e.g + at, e.n - at, lane);
 }
 
-template <typename T, int THREADS>
-__device__ __forceinline__ void chunk_scale(T* g, float* out, int64_t left, float c)
+template <typename T, int LANES, int CHUNK>
+__device__ __forceinline__ void chunk_scale(T* g, float* out, int64_t left, float c, int lane)
 {
     constexpr int N = Vec<T>::N;
 #pragma unroll 4
-    for (int i = threadIdx.x * N; i < kGradChunk; i += THREADS * N) {
+    for (int i = lane * N; i < CHUNK; i += LANES * N) {
         float v[N];
         load_vec(g + i, left - i, v);
 #pragma unroll
@@ -108,17 +111,17 @@ __device__ __forceinline__ void chunk_scale(T* g, float* out, int64_t left, floa
     }
 }
 
-template <int THREADS>
-__device__ __forceinline__ void scale_chunk(const GradEntry& e, uint32_t chunk, float c)
+template <int LANES, int CHUNK>
+__device__ __forceinline__ void scale_chunk(const GradEntry& e, uint32_t chunk, float c, int lane)
 {
-    const int64_t at = (int64_t)(chunk - e.chunk0) * kGradChunk;
+    const int64_t at = (int64_t)(chunk - e.chunk0) * CHUNK;
     float* out = e.out ? e.out + at : nullptr;
     if (e.type == GS_F16)
-        chunk_scale<f16, THREADS>((f16*)e.g + at, out, e.n - at, c);
+        chunk_scale<f16, LANES, CHUNK>((f16*)e.g + at, out, e.n - at, c, lane);
     else if (e.type == GS_BF16)
-        chunk_scale<bf16, THREADS>((bf16*)e.g + at, out, e.n - at, c);
+        chunk_scale<bf16, LANES, CHUNK>((bf16*)e.g + at, out, e.n - at, c, lane);
     else
-        chunk_scale<float, THREADS>((float*)e.g + at, out, e.n - at, c);
+        chunk_scale<float, LANES, CHUNK>((float*)e.g + at, out, e.n - at, c, lane);
 }
 
 // Sum over the workgroup, in a fixed order, left in every thread.
@@ -139,7 +142,7 @@ __global__ __launch_bounds__(kBlock) void k_grad_squares(GradTable a, double* __
 {
     double s = 0.0;
     for (uint32_t c = blockIdx.x; c < a.chunks; c += gridDim.x)
-        s += squares_of<kBlock>(a.t[tensor_of(a, c)], c);
+        s += squares_of<kBlock, kGradChunk>(a.t[tensor_of(a, c)], c, threadIdx.x);
     s = block_sum<kBlock>(s);
     if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
@@ -174,7 +177,7 @@ __global__ __launch_bounds__(kBlock) void k_grad_scale(GradTable a, const double
     }
     for (uint32_t k = blockIdx.x; k < a.chunks; k += gridDim.x) {
         const GradEntry& e = a.t[tensor_of(a, k)];
-        if (c != 1.f || e.out) scale_chunk<kBlock>(e, k, c);
+        if (c != 1.f || e.out) scale_chunk<kBlock, kGradChunk>(e, k, c, threadIdx.x);
     }
 }
 
@@ -182,8 +185,12 @@ __global__ __launch_bounds__(kBlock) void k_grad_scale(GradTable a, const double
 __global__ __launch_bounds__(kSmallThreads) void k_grad_small(GradTable a, float max_norm, float* __restrict__ result,
                                                               int scale)
 {
+    // the wave's number through a scalar register: the tensor table is then read by scalar loads
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
     double s = 0.0;
-    for (uint32_t c = 0; c < a.chunks; ++c) s += squares_of<kSmallThreads>(a.t[tensor_of(a, c)], c);
+    for (uint32_t c = wave; c < a.chunks; c += kSmallThreads / 64)
+        s += squares_of<64, kSmallChunk>(a.t[tensor_of(a, c)], c, lane);
     float norm;
     const float c = clip_scale(block_sum<kSmallThreads>(s), max_norm, &norm);
     if (threadIdx.x == 0) {
@@ -191,20 +198,20 @@ __global__ __launch_bounds__(kSmallThreads) void k_grad_small(GradTable a, float
         result[1] = c;
     }
     if (!scale) return;
-    for (uint32_t k = 0; k < a.chunks; ++k) {
+    for (uint32_t k = wave; k < a.chunks; k += kSmallThreads / 64) {
         const GradEntry& e = a.t[tensor_of(a, k)];
-        if (c != 1.f || e.out) scale_chunk<kSmallThreads>(e, k, c);
+        if (c != 1.f || e.out) scale_chunk<64, kSmallChunk>(e, k, c, lane);
     }
 }
 
 // Fills the table with tensors from `at` on (empty ones are left out); returns the first that it leaves.
-int fill_table(const gs_grad_tensor* ts, int count, int at, GradTable& a)
+int fill_table(const gs_grad_tensor* ts, int count, int at, GradTable& a, int chunk = kGradChunk)
 {
     a.count = 0;
     a.chunks = 0;
     for (; at < count && a.count < kGradTable; ++at) {
         if (ts[at].n == 0) continue;
-        const int64_t chunks = div_up(ts[at].n, kGradChunk);
+        const int64_t chunks = div_up(ts[at].n, chunk);
         if (a.chunks + chunks > 0x7FFFFFFF) break;
         a.t[a.count++] = {ts[at].grad, ts[at].out, ts[at].n, a.chunks, ts[at].type};
         a.chunks += (uint32_t)chunks;
@@ -243,8 +250,8 @@ hipError_t launch_grad_clip(const gs_grad_tensor* ts, int count, float max_norm,
                             bool scale, hipStream_t s)
 {
     GradTable a;
-    int at = fill_table(ts, count, 0, a);
-    if (at == count && a.chunks <= kGradSmall) {
+    int at = fill_table(ts, count, 0, a, kSmallChunk);
+    if (at == count && a.chunks <= kSmallChunks) {
         hipLaunchKernelGGL(k_grad_small, dim3(1), dim3(kSmallThreads), 0, s, a, max_norm, result, scale ? 1 : 0);
         return hipGetLastError();
     }

@@ -21,8 +21,8 @@ namespace gsr {
 namespace {
 
 constexpr int kNormWaves = 4;            // waves of a workgroup whose rows lie within one wave
-constexpr int kSumCols = 32;             // columns per workgroup of k_column_sum
-constexpr int kSumSlices = 16;           // row slices of k_column_sum
+constexpr int kSumCols = 16;             // columns per workgroup of k_column_sum
+constexpr int kSumSlices = 64;           // row slices of k_column_sum
 
 // Sum of v over the G lanes of a row, left in all of them. G > 64: the row is the workgroup's; `slot` is LDS
 // of G / 64 floats that the previous call did not use.
@@ -59,17 +59,29 @@ __global__ __launch_bounds__(G > 64 ? G : kNormWaves * 64) void k_norm_fwd(
             wv[k][j] = w && c < dim ? w[c] : 1.f;
             bv[k][j] = b && c < dim ? b[c] : 0.f;
         }
-    for (int64_t r = (int64_t)blockIdx.x * (kThreads / G) + threadIdx.x / G; r < rows;
-         r += (int64_t)gridDim.x * (kThreads / G)) {
-        float v[NV][N];
-        float s = 0.f;
+    // a row's vectors are fetched while the row before it is worked on
+    const int64_t step = (int64_t)gridDim.x * (kThreads / G);
+    typename Vec<T>::Packed next[NV];
+    auto fetch = [&](int64_t r) {
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = (k * G + lane) * N;
-            load_vec(x + r * ldx + c, dim - c, v[k]);
-#pragma unroll
-            for (int j = 0; j < N; ++j) s += v[k][j];
+            next[k] = load_any(x + r * ldx + c, dim - c);
         }
+    };
+    const int64_t first = (int64_t)blockIdx.x * (kThreads / G) + threadIdx.x / G;
+    if (first < rows) fetch(first);
+    for (int64_t r = first; r < rows; r += step) {
+        float v[NV][N];
+        float s = 0.f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                v[k][j] = (float)next[k][j];   // 0 beyond the row
+                s += v[k][j];
+            }
+        if (r + step < rows) fetch(r + step);
         const float mu = row_sum<G>(s, slots[0]) * inv;
         float q = 0.f;
 #pragma unroll
@@ -167,17 +179,38 @@ __global__ __launch_bounds__(G > 64 ? G : kNormWaves * 64) void k_norm_bwd(
             wv[k][j] = w && c < dim ? w[c] : 1.f;
             sw[k][j] = sb[k][j] = 0.f;
         }
-    for (int64_t r = (int64_t)blockIdx.x * (kThreads / G) + threadIdx.x / G; r < rows;
-         r += (int64_t)gridDim.x * (kThreads / G)) {
-        const float mu = mean[r], rs = rstd[r];
-        float xh[NV][N], g[NV][N];
-        float s1 = 0.f, s2 = 0.f;
+    // a row's vectors are fetched while the row before it is worked on
+    const int64_t step = (int64_t)gridDim.x * (kThreads / G);
+    typename Vec<T>::Packed nx[NV], ng[NV], na[NV];
+    float nmu = 0.f, nrs = 0.f;
+    auto fetch = [&](int64_t r) {
+        nmu = mean[r];
+        nrs = rstd[r];
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = (k * G + lane) * N;
-            load_vec(x + r * ldx + c, dim - c, xh[k], mu);
-            load_vec(dy + r * lddy + c, dim - c, g[k]);
+            nx[k] = load_any(x + r * ldx + c, dim - c);
+            ng[k] = load_any(dy + r * lddy + c, dim - c);
+            if (add) na[k] = load_any(add + r * ldadd + c, dim - c);
         }
+    };
+    const int64_t first = (int64_t)blockIdx.x * (kThreads / G) + threadIdx.x / G;
+    if (first < rows) fetch(first);
+    for (int64_t r = first; r < rows; r += step) {
+        const float mu = nmu, rs = nrs;
+        float xh[NV][N], g[NV][N];
+        typename Vec<T>::Packed ar[NV];
+        float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            ar[k] = na[k];
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                xh[k][j] = (float)nx[k][j];
+                g[k][j] = (float)ng[k][j];   // 0 beyond the row, and with it all that such a place adds
+            }
+        }
+        if (r + step < rows) fetch(r + step);
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
@@ -215,11 +248,10 @@ __global__ __launch_bounds__(G > 64 ? G : kNormWaves * 64) void k_norm_bwd(
         for (int k = 0; k < NV; ++k) {
             const int c = (k * G + lane) * N;
             float o[N];
-            if (add) load_vec(add + r * ldadd + c, dim - c, o);
 #pragma unroll
             for (int j = 0; j < N; ++j) {
                 const float t = rs * (g[k][j] - s1 - xh[k][j] * s2);
-                o[j] = add ? t + o[j] : t;
+                o[j] = add ? t + (float)ar[k][j] : t;
             }
             store_vec(dx + r * lddx + c, dim - c, o);
         }
@@ -342,6 +374,7 @@ __global__ __launch_bounds__(kSumCols* kSumSlices) void k_column_sum(const float
     const int64_t c = (int64_t)blockIdx.x * kSumCols + col;
     float t = 0.f;
     if (c < cols)
+#pragma unroll 8
         for (int k = slice; k < count; k += kSumSlices) t += part[(int64_t)k * cols + c];
     s[slice][col] = t;
     __syncthreads();
@@ -367,11 +400,15 @@ RowShape row_shape(int type, int64_t dim, bool backward)
     for (int g = 1; g <= 64; g <<= 1)
         if (vecs <= g) return {g, 1};
     if (vecs <= 128) return {64, 2};
+    if (backward) {
+        for (int g = 256; g <= 1024; g <<= 1)
+            if (vecs <= g) return {g, 1};
+        return {0, 0};
+    }
     if (vecs <= 256) return {64, 4};
     if (vecs <= 512) return {256, 2};
-    if (vecs <= 1024) return {backward ? 1024 : 256, backward ? 1 : 4};
-    // (the backward of 16-bit rows that long would need more than a 1,024-thread workgroup's 128 registers)
-    if (vecs <= 2048 && !(backward && n == 8)) return {1024, 2};
+    if (vecs <= 1024) return {256, 4};
+    if (vecs <= 2048) return {1024, 2};
     return {0, 0};
 }
 
@@ -384,7 +421,7 @@ int norm_bwd_blocks(int type, int64_t rows, int64_t dim)
     const RowShape sh = row_shape(type, dim, true);
     if (sh.g == 0) return (int)std::min<int64_t>(std::max<int64_t>(rows / 64, 1), 64);
     const int64_t per = sh.g > 64 ? 1 : kNormWaves * 64 / sh.g;
-    int64_t most = sh.g == 1024 ? 256 : kNormParts;
+    int64_t most = sh.g > 256 ? 256 * 1024 / sh.g : kNormParts;
     most = std::min(most, std::max<int64_t>(rows / 32, 1));
     return (int)std::max<int64_t>(1, std::min(most, div_up(rows, per * 2)));
 }
@@ -418,10 +455,7 @@ void norm_bwd(const void* dy, int64_t lddy, const void* x, int64_t ldx, const fl
     case 16 * 8 + 1: call(16, 1); break;            \
     case 32 * 8 + 1: call(32, 1); break;            \
     case 64 * 8 + 1: call(64, 1); break;            \
-    case 64 * 8 + 2: call(64, 2); break;            \
-    case 64 * 8 + 4: call(64, 4); break;            \
-    case 256 * 8 + 2: call(256, 2); break;          \
-    case 1024 * 8 + 2: call(1024, 2); break;
+    case 64 * 8 + 2: call(64, 2); break;
 
 template <typename T>
 hipError_t norm_fwd_type(int type, const void* x, int64_t ldx, const float* w, const float* b, int64_t rows, int dim,
@@ -430,7 +464,10 @@ hipError_t norm_fwd_type(int type, const void* x, int64_t ldx, const float* w, c
     const RowShape sh = row_shape(type, dim, false);
 #define CALL(G, NV) norm_fwd<T, G, NV>(x, ldx, w, b, rows, dim, eps, y, ldy, mean, rstd, s)
     GS_NORM_SHAPES(CALL)
+    case 64 * 8 + 4: CALL(64, 4); break;
+    case 256 * 8 + 2: CALL(256, 2); break;
     case 256 * 8 + 4: CALL(256, 4); break;
+    case 1024 * 8 + 2: CALL(1024, 2); break;
     default:
         hipLaunchKernelGGL((k_norm_fwd_long<T>), dim3((unsigned)std::min<int64_t>(rows, 512)), dim3(1024), 0, s,
                            (const T*)x, ldx, w, b, rows, dim, eps, (T*)y, ldy, mean, rstd);
@@ -450,6 +487,8 @@ hipError_t norm_bwd_type(int type, const void* dy, int64_t lddy, const void* x, 
 #define CALL(G, NV) \
     norm_bwd<T, G, NV>(dy, lddy, x, ldx, w, mean, rstd, add, ldadd, rows, dim, dx, lddx, dw, db, p, blocks, s)
     GS_NORM_SHAPES(CALL)
+    case 256 * 8 + 1: CALL(256, 1); break;
+    case 512 * 8 + 1: CALL(512, 1); break;
     case 1024 * 8 + 1: CALL(1024, 1); break;
     default:
         if (rows > 0)

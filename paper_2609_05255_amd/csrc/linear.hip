@@ -37,11 +37,15 @@ struct Plan {
 };
 
 // NT: the largest tile that still fills the compute units; the sum is split where even the smallest does not.
-Plan plan_nt(int type, int64_t rows, int64_t cols, int64_t len)
+Plan plan_nt(int type, int64_t rows, int64_t cols, int64_t len, bool fast_a)
 {
     Plan p = {kTile64, 1, len};
     if (cols <= 32) {
         p.tile = kTile128x32;
+        return p;
+    }
+    if (fast_a && type != GS_F32 && div_up(rows, 256) * div_up(cols, 256) >= kFillTiles && cols >= 192 && len >= 512) {
+        p.tile = kTile256;
         return p;
     }
     if (div_up(rows, 128) * div_up(cols, 128) >= kFillTiles) {
@@ -58,10 +62,11 @@ Plan plan_nt(int type, int64_t rows, int64_t cols, int64_t len)
 }
 
 // TT: the sum runs over the rows; its splits fill the compute units.
-Plan plan_tt(int64_t out, int64_t in, int64_t rows, int planes)
+Plan plan_tt(int type, int64_t out, int64_t in, int64_t rows, int planes, bool fast_b)
 {
     Plan p;
     p.tile = out >= 96 && in >= 96 ? kTile128 : kTile64;
+    if (fast_b && type != GS_F32 && div_up(out, 256) * div_up(in, 256) * planes >= kFillTiles) p.tile = kTile256;
     const TileShape t = tile_shape(p.tile);
     const int64_t tiles = div_up(out, t.bi) * div_up(in, t.bj) * planes;
     const int64_t want = std::max<int64_t>(1, std::min(div_up(2 * kFillTiles, tiles), rows / kRowSplitLen));
@@ -110,7 +115,7 @@ FwdSpace fwd_space(void* base, int type, int64_t rows, int64_t in, int64_t out, 
     FwdSpace f = {};
     if (rows > kSkinnyRows) {
         if (copy_w) f.w = r.take(out * padded(type, in) * elem(type));
-        const Plan p = plan_nt(type, rows, out, in);
+        const Plan p = plan_nt(type, rows, out, in, false);
         if (p.splits > 1) f.part = (float*)r.take((int64_t)p.splits * rows * out * 4);
     }
     f.bytes = r.at;
@@ -135,11 +140,14 @@ BwdSpace bwd_space(void* base, int type, int act, int64_t rows, int64_t in, int6
     b.sums = (float*)r.take((int64_t)slope_row_blocks(type, rows, out) * out * 4);
     int64_t part = 0;
     if (rows > kSkinnyRows) {
-        const Plan x = plan_nt(type, rows, in, out);
+        const Plan x = plan_nt(type, rows, in, out, true);
         if (x.splits > 1) part = (int64_t)x.splits * rows * in * 4;
     }
-    const Plan w = plan_tt(out, in, rows, planes);
-    if (w.splits * planes > 1) part = std::max(part, (int64_t)w.splits * planes * out * in * 4);
+    // (a workspace is sized for either operand's alignment)
+    for (int fast_x = 0; fast_x < 2; ++fast_x) {
+        const Plan w = plan_tt(type, out, in, rows, planes, fast_x != 0);
+        if (w.splits * planes > 1) part = std::max(part, (int64_t)w.splits * planes * out * in * 4);
+    }
     b.part = (float*)r.take(part);
     b.bytes = r.at;
     return b;
@@ -154,7 +162,7 @@ hipError_t run_nt(int type, GemmArgs g, bool fast_a, float* part, hipStream_t s)
     g.a_rows = g.rows;
     g.b_rows = g.cols;
     if (g.rows <= kSkinnyRows) return LinearOps<T>::skinny(g, s);
-    const Plan p = plan_nt(type, g.rows, g.cols, g.len);
+    const Plan p = plan_nt(type, g.rows, g.cols, g.len, fast_a);
     g.splits = p.splits;
     g.split_len = p.split_len;
     g.part = p.splits > 1 ? part : nullptr;
@@ -243,7 +251,8 @@ hipError_t linear_bwd(const gs_linear& p, const void* dy, int64_t lddy, const vo
     }
     if (dw) {
         GemmArgs g = {};
-        const Plan plan = plan_tt(p.n_out, p.n_in, p.rows, planes);
+        const bool fast_x = fast(p.x, p.ldx, p.n_in, p.type);
+        const Plan plan = plan_tt(p.type, p.n_out, p.n_in, p.rows, planes, fast_x);
         g.a = dz;
         g.lda = ldo;
         g.b = p.x;
@@ -259,7 +268,7 @@ hipError_t linear_bwd(const gs_linear& p, const void* dy, int64_t lddy, const vo
         g.ldo = lddw;
         g.out_f32 = dw_type == GS_F32;
         g.part = plan.splits * planes > 1 ? b.part : nullptr;
-        e = LinearOps<T>::gemm_tt(plan.tile, fast(p.x, p.ldx, p.n_in, p.type), g, s);
+        e = LinearOps<T>::gemm_tt(plan.tile, fast_x, g, s);
         if (e == hipSuccess && g.part) e = LinearOps<T>::join(g, plane_scale(p.type), s);
     }
     return e;

@@ -34,6 +34,21 @@ __device__ __forceinline__ void load_vec(const T* p, int64_t left, float* out, f
     }
 }
 
+// The same as stored: elements beyond `left` read as 0.
+template <typename T>
+__device__ __forceinline__ typename Vec<T>::Packed load_any(const T* p, int64_t left)
+{
+    typename Vec<T>::Packed t = {};
+    if (left >= Vec<T>::N) {
+        t = *reinterpret_cast<const typename Vec<T>::Any*>(p);
+    } else {
+#pragma unroll
+        for (int j = 0; j < Vec<T>::N; ++j)
+            if (j < left) t[j] = p[j];
+    }
+    return t;
+}
+
 template <typename T>
 __device__ __forceinline__ void store_vec(T* p, int64_t left, const float* in)
 {
