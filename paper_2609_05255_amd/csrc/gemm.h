@@ -1,11 +1,15 @@
 // Matrix product on the matrix cores with the linear operators' epilogue, one
 // template for binary16, bfloat16 (16x16x32 MFMA) and fp32 (16x16x4 MFMA).
 //
-// A workgroup computes a BI x BJ tile of C with WI x WJ waves; the operands'
-// tiles (128 bytes along the sum: 64 16-bit or 32 fp32 values) go from memory to
-// LDS with buffer loads that write LDS directly, double-buffered, one barrier
-// per step: the next tile's loads run under the current one's MFMAs. Out of
-// range rows come out of the buffer descriptor's range check as zeros.
+// A workgroup computes a BI x BJ tile of C with WI x WJ waves. The operands'
+// tiles (64 bytes along the sum: 32 16-bit or 16 fp32 values) go from memory to
+// LDS with buffer loads that write LDS directly, through a ring of STAGES tiles:
+// STAGES - 1 of them are on their way while one is worked on, and a wait for the
+// oldest alone (vmcnt) replaces a wait for all. Every step issues its loads, past
+// the end too (the descriptor's range check turns those, like rows beyond the
+// matrix, into zeros without reading), so that the counts stay the same.
+// With AHEAD, a wave's fragments of the next tile are read under the MFMAs of
+// this one.
 //
 // LDS slots are 16 bytes. Reading a fragment takes one slot from each of 16
 // rows (NT), or four 4-value pieces of rows through the transposing LDS read
@@ -35,7 +39,7 @@ constexpr uint32_t kOutOfRange = 0x80000000u;   // beyond any descriptor's range
 template <typename T>
 struct Mma {
     typedef T Frag __attribute__((ext_vector_type(8)));   // 16-bit: 8 values along the sum
-    static constexpr int kBK = 64;                        // values along the sum per tile
+    static constexpr int kStep = 32;                      // values along the sum per fragment
     static __device__ __forceinline__ f32x4 mma(const Frag& a, const Frag& b, f32x4 c)
     {
         if constexpr (__is_same(T, f16))
@@ -48,7 +52,7 @@ struct Mma {
 template <>
 struct Mma<float> {
     typedef float Frag __attribute__((ext_vector_type(4)));
-    static constexpr int kBK = 32;
+    static constexpr int kStep = 16;
     static __device__ __forceinline__ f32x4 mma(const Frag& a, const Frag& b, f32x4 c)
     {
 #pragma unroll
@@ -59,11 +63,33 @@ struct Mma<float> {
 
 // ---- operand tiles ----------------------------------------------------------
 
-// NT: X rows of 8 slots along the sum. Fragment rows are base + l%16 (A) or the interleaved columns (B).
-__device__ __forceinline__ int nt_hash_a(int row) { return row & 7; }
-__device__ __forceinline__ int nt_hash_b(int row) { return (row & 3) | ((row >> 1) & 4); }
+// s_waitcnt until at most n vector memory operations are under way (the other counters: any number).
+template <int n>
+__device__ __forceinline__ void wait_loads()
+{
+    __builtin_amdgcn_s_waitcnt((n & 15) | (7 << 4) | (15 << 8) | ((n >> 4) << 14));
+    asm volatile("" ::: "memory");
+}
 
-// TT: kBK rows c of X * sizeof(T) / 16 slots.
+__device__ __forceinline__ void barrier()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// NT: X rows of 4 KS slots along the sum; fragment rows are base + i (A) or the interleaved columns
+// base + (i & 3) + 8 (i >> 2) (B), i = lane % 16. A 16-byte LDS read of half a wave takes two turns of 16 lanes, {0..3,
+// 12..15, 20..23, 24..27} and the others (found from the conflict counter); the hash gives each turn's lanes different
+// slots of the 256 bytes that the banks hold.
+template <int KS, bool IS_B>
+__device__ __forceinline__ int nt_hash(int row)
+{
+    if constexpr (KS == 1) return -(IS_B ? row >> 3 : row >> 2) & 3;
+    return IS_B ? ((row >> 2) & 6) | ((row >> 1) & 1) : (row >> 1) & 7;
+}
+
+// TT: rows c of X * sizeof(T) / 16 slots.
 template <typename T, int X>
 __device__ __forceinline__ int tt_hash(int c)
 {
@@ -78,21 +104,20 @@ __device__ __forceinline__ int tt_hash(int c)
 }
 
 // Geometry of one operand's tile: which slot of which row a thread fills, and from which vector of that row.
-template <typename T, int X, bool TT, bool IS_B, int THREADS>
+template <typename T, int X, int KS, bool TT, bool IS_B, int THREADS>
 struct Tile {
-    static constexpr int kBK = Mma<T>::kBK;
     static constexpr int kVec = 16 / (int)sizeof(T);
-    static constexpr int kRowSlots = TT ? X / kVec : 8;
-    static constexpr int kSlotsTotal = X * 8;             // X * 128 bytes
+    static constexpr int kRowSlots = TT ? X / kVec : 4 * KS;
+    static constexpr int kSlotsTotal = X * 4 * KS;
     static constexpr int kPasses = kSlotsTotal / THREADS;
-    static constexpr int kBytes = X * 128;
+    static constexpr int kBytes = X * 64 * KS;
     static_assert(kSlotsTotal % THREADS == 0, "whole passes");
 
     static __device__ __forceinline__ int row(int q) { return q / kRowSlots; }
     static __device__ __forceinline__ int vec(int q)
     {
         const int r = row(q), s = q % kRowSlots;
-        return TT ? s ^ tt_hash<T, X>(r) : s ^ (IS_B ? nt_hash_b(r) : nt_hash_a(r));
+        return s ^ (TT ? tt_hash<T, X>(r) : nt_hash<KS, IS_B>(r));
     }
 
     // LDS <- memory. p: the operand, stored rows of ld values; x0: first row (NT) or column (TT) of the tile;
@@ -105,7 +130,7 @@ struct Tile {
         const int64_t first = r0 * ld;
         // bytes from the tile's first row to the end of its last valid one
         const int64_t bytes = ((rows_end < stored ? rows_end : stored) - r0) * ld * (int64_t)sizeof(T);
-        const int range = bytes > 0x7FFFFFF0 ? 0x7FFFFFF0 : (int)bytes;
+        const int range = bytes > 0x7FFFFFF0 ? 0x7FFFFFF0 : bytes < 0 ? 0 : (int)bytes;
         __amdgpu_buffer_rsrc_t rsrc =
             __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(p + first), 0, range, 0x00027000);
         const int64_t v0 = TT ? x0 : c0, v_end = TT ? x_end : c_end;
@@ -152,15 +177,14 @@ struct Tile {
         for (int k = 0; k < kPasses; ++k) *reinterpret_cast<Packed*>(lds + (k * THREADS + threadIdx.x) * 16) = r[k];
     }
 
-    // Fragment for values [32 s, 32 s + 32) (16-bit) or [16 s, ...) (fp32) of the sum. f: fragment of the wave's
-    // `wx` first row or column.
+    // Fragment f of step s of a wave whose first row or column of the tile is wx.
     static __device__ __forceinline__ typename Mma<T>::Frag frag(const char* lds, int wx, int f, int s)
     {
         const int lane = threadIdx.x & 63, g = lane >> 4, i = lane & 15;
         if constexpr (!TT) {
             const int r = IS_B ? wx + 32 * (f >> 1) + 4 * (f & 1) + 8 * (i >> 2) + (i & 3) : wx + 16 * f + i;
-            const int slot = (4 * s + g) ^ (IS_B ? nt_hash_b(r) : nt_hash_a(r));
-            return *reinterpret_cast<const typename Mma<T>::Frag*>(lds + r * 128 + slot * 16);
+            const int slot = (4 * s + g) ^ nt_hash<KS, IS_B>(r);
+            return *reinterpret_cast<const typename Mma<T>::Frag*>(lds + r * (64 * KS) + slot * 16);
         } else if constexpr (sizeof(T) == 2) {
             typename Mma<T>::Frag out;
             s16x4 h[2];
@@ -202,52 +226,56 @@ __device__ __forceinline__ void tile_of(int64_t b, int64_t tiles_i, int64_t tile
     *tj = in / h;
 }
 
-// 8 neighbouring values of row i, columns [j, j + 8) of which `left` exist.
-template <typename T>
-__device__ __forceinline__ void epilogue8(const GemmArgs& g, int64_t i, int64_t j, int64_t left, float* v,
-                                          const float* bias)
+// BI, BJ: the workgroup's tile; WI, WJ: its waves; KS: steps of the sum per tile in LDS; STAGES: tiles in the ring;
+// AHEAD: fragments are read a tile ahead of their MFMAs. FAST: the operand that may be the caller's (A in NT, B in TT)
+// is loaded asynchronously as well, as the other always is; otherwise it goes through registers, at any alignment.
+template <bool TT_, int BI_, int BJ_, int WI_, int WJ_, int KS_, int STAGES_, bool AHEAD_, bool FAST_>
+struct Shape {
+    static constexpr bool TT = TT_, AHEAD = AHEAD_, FAST = FAST_;
+    static constexpr int BI = BI_, BJ = BJ_, WI = WI_, WJ = WJ_, KS = KS_, STAGES = STAGES_;
+    static constexpr int THREADS = WI * WJ * 64;
+};
+
+// Stores a wave's WR x WC block of results whose 8-value groups are in LDS, whole rows of it at a time: row r's
+// vector v is at slot v ^ (r & 7) of its row.
+template <typename T, int WR, int WC>
+__device__ __forceinline__ void store_block(const char* lds, T* out, int64_t ld, int64_t i, int64_t rows, int64_t j,
+                                            int64_t cols)
 {
-    constexpr int N = Vec<T>::N;
+    constexpr int N = Vec<T>::N, kVecs = WC / N, kRowBytes = WC * (int)sizeof(T);
+    const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] += bias[e];
-    if (g.z) {
-        T* z = (T*)g.z + i * g.ldz + j;
+    for (int k = 0; k < WR * kVecs / 64; ++k) {
+        const int q = k * 64 + lane, r = q / kVecs, v = q % kVecs;
+        const int64_t left = cols - (j + v * N);
+        if (i + r >= rows || left <= 0) continue;
+        const typename Vec<T>::Packed t =
+            *reinterpret_cast<const typename Vec<T>::Packed*>(lds + r * kRowBytes + (v ^ (r & 7 & (kVecs - 1))) * 16);
+        T* o = out + (i + r) * ld + j + v * N;
+        if (left >= N) {
+            *reinterpret_cast<typename Vec<T>::Any*>(o) = t;
+        } else {
 #pragma unroll
-        for (int e = 0; e < 8; e += N) store_vec(z + e, left - e, v + e);
-    }
-    activate<8>(g.act, v);
-    if (g.residual) {
-        const T* r = (const T*)g.residual + i * g.ldr + j;
-        float t[8];
-#pragma unroll
-        for (int e = 0; e < 8; e += N) load_vec(r + e, left - e, t + e);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += t[e];
-    }
-    if (g.out_f32) {
-        float* o = (float*)g.out + i * g.ldo + j;
-        store_vec(o, left, v);
-        store_vec(o + 4, left - 4, v + 4);
-    } else {
-        T* o = (T*)g.out + i * g.ldo + j;
-#pragma unroll
-        for (int e = 0; e < 8; e += N) store_vec(o + e, left - e, v + e);
+            for (int e = 0; e < N; ++e)
+                if (e < left) o[e] = t[e];
+        }
     }
 }
 
-// FAST: the operand that may be the caller's (A in NT, B in TT) is loaded asynchronously as well; the other
-// always is.
-template <typename T, bool TT, int BI, int BJ, int WI, int WJ, bool FAST>
-__global__ __launch_bounds__(WI* WJ * 64) void k_gemm(GemmArgs g)
+template <typename T, class S>
+__global__ __launch_bounds__(S::THREADS) void k_gemm(GemmArgs g)
 {
-    constexpr int THREADS = WI * WJ * 64;
-    constexpr int FI = BI / WI / 16, FJ = BJ / WJ / 16;
-    constexpr int kBK = Mma<T>::kBK;
-    using TA = Tile<T, BI, TT, false, THREADS>;
-    using TB = Tile<T, BJ, TT, true, THREADS>;
-    constexpr bool kAsyncA = FAST || TT, kAsyncB = FAST || !TT;
+    constexpr bool TT = S::TT;
+    constexpr int BI = S::BI, BJ = S::BJ, WI = S::WI, WJ = S::WJ, KS = S::KS, kStages = S::STAGES;
+    constexpr int WR = BI / WI, WC = BJ / WJ, FI = WR / 16, FJ = WC / 16;
+    constexpr int kBK = Mma<T>::kStep * KS;
+    using TA = Tile<T, BI, KS, TT, false, S::THREADS>;
+    using TB = Tile<T, BJ, KS, TT, true, S::THREADS>;
+    constexpr int kTileBytes = TA::kBytes + TB::kBytes;
+    constexpr bool kAsyncA = S::FAST || TT, kAsyncB = S::FAST || !TT;
     static_assert(TT || FJ % 2 == 0, "columns interleave between pairs of fragments");
-    __shared__ __attribute__((aligned(1024))) char lds[2][TA::kBytes + TB::kBytes];
+    static_assert(TT || WI * WJ * WR * WC * (int)sizeof(T) <= kStages * kTileBytes, "the results pass through LDS");
+    __shared__ __attribute__((aligned(1024))) char lds[kStages * kTileBytes];
 
     const int64_t tiles_i = (g.rows + BI - 1) / BI, tiles_j = (g.cols + BJ - 1) / BJ;
     int64_t ti, tj;
@@ -258,49 +286,125 @@ __global__ __launch_bounds__(WI* WJ * 64) void k_gemm(GemmArgs g)
     const int64_t c_end = c_begin + g.split_len < g.len ? c_begin + g.split_len : g.len;
     const T* a = (const T*)g.a + plane * g.plane_stride;
     const T* b = (const T*)g.b;
-    const int wave = threadIdx.x >> 6, wi = (wave / WJ) * (BI / WI), wj = (wave % WJ) * (BJ / WJ);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wi = (wave / WJ) * WR, wj = (wave % WJ) * WC;
     const int lane = threadIdx.x & 63, lg = lane >> 4, li = lane & 15;
 
+    typedef typename Mma<T>::Frag Frag;
     f32x4 acc[FI][FJ] = {};
-    typename TA::Packed ra[kAsyncA ? 1 : TA::kPasses];
-    typename TB::Packed rb[kAsyncB ? 1 : TB::kPasses];
-    auto fetch = [&](char* to, int64_t c0) {
-        if constexpr (kAsyncA)
-            TA::load_async(to, a, g.lda, g.a_rows, i0, g.rows, c0, c_end);
-        else
-            TA::load_regs(ra, a, g.lda, i0, g.rows, c0, c_end);
-        if constexpr (kAsyncB)
-            TB::load_async(to + TA::kBytes, b, g.ldb, g.b_rows, j0, g.cols, c0, c_end);
-        else
-            TB::load_regs(rb, b, g.ldb, j0, g.cols, c0, c_end);
+    auto read = [&](const char* from, Frag(&fa)[KS][FI], Frag(&fb)[KS][FJ]) {
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+#pragma unroll
+            for (int f = 0; f < FJ; ++f) fb[s][f] = TB::frag(from + TA::kBytes, wj, f, s);
+#pragma unroll
+            for (int f = 0; f < FI; ++f) fa[s][f] = TA::frag(from, wi, f, s);
+        }
     };
-    auto settle = [&](char* to) {
-        if constexpr (!kAsyncA) TA::store_regs(to, ra);
-        if constexpr (!kAsyncB) TB::store_regs(to + TA::kBytes, rb);
-    };
-    const int steps = c_end > c_begin ? (int)((c_end - c_begin + kBK - 1) / kBK) : 0;
-    if (steps > 0) {
-        fetch(lds[0], c_begin);
-        settle(lds[0]);
-    }
-    for (int t = 0; t < steps; ++t) {
-        char* cur = lds[t & 1];
-        char* nxt = lds[(t + 1) & 1];
-        __syncthreads();   // cur has arrived, and nxt is no longer read
-        if (t + 1 < steps) fetch(nxt, c_begin + (int64_t)(t + 1) * kBK);
+    auto multiply = [&](const Frag(&fa)[KS][FI], const Frag(&fb)[KS][FJ]) {
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            typename Mma<T>::Frag fa[FI], fb[FJ];
-#pragma unroll
-            for (int f = 0; f < FI; ++f) fa[f] = TA::frag(cur, wi, f, s);
-#pragma unroll
-            for (int f = 0; f < FJ; ++f) fb[f] = TB::frag(cur + TA::kBytes, wj, f, s);
+        for (int s = 0; s < KS; ++s)
 #pragma unroll
             for (int p = 0; p < FI; ++p)
 #pragma unroll
-                for (int q = 0; q < FJ; ++q) acc[p][q] = Mma<T>::mma(fb[q], fa[p], acc[p][q]);
+                for (int q = 0; q < FJ; ++q) acc[p][q] = Mma<T>::mma(fb[s][q], fa[s][p], acc[p][q]);
+    };
+    const int steps = c_end > c_begin ? (int)((c_end - c_begin + kBK - 1) / kBK) : 0;
+    if constexpr (S::FAST) {
+        constexpr int kLoads = TA::kPasses + TB::kPasses;   // of a thread per tile
+        int64_t c0 = c_begin;
+        auto fetch = [&](char* to) {
+            TA::load_async(to, a, g.lda, g.a_rows, i0, g.rows, c0, c_end);
+            TB::load_async(to + TA::kBytes, b, g.ldb, g.b_rows, j0, g.cols, c0, c_end);
+            c0 += kBK;
+        };
+        char* cur = lds;
+        char* to = lds;
+        auto next = [&](char* p) { return p + kTileBytes == lds + kStages * kTileBytes ? lds : p + kTileBytes; };
+        for (int k = 0; k < kStages - 1; ++k, to = next(to)) fetch(to);   // (AHEAD: all of them)
+        if constexpr (S::AHEAD) {
+            static_assert(KS == 2 && kStages == 2, "two halves of two tiles");
+            Frag fa[2][FI], fb[2][FJ];
+            auto half = [&](const char* from, int s, Frag(&ra)[FI], Frag(&rb)[FJ]) {
+#pragma unroll
+                for (int f = 0; f < FJ; ++f) rb[f] = TB::frag(from + TA::kBytes, wj, f, s);
+#pragma unroll
+                for (int f = 0; f < FI; ++f) ra[f] = TA::frag(from, wi, f, s);
+            };
+            auto product = [&](const Frag(&ma)[FI], const Frag(&mb)[FJ]) {
+#pragma unroll
+                for (int p = 0; p < FI; ++p)
+#pragma unroll
+                    for (int q = 0; q < FJ; ++q) acc[p][q] = Mma<T>::mma(mb[q], ma[p], acc[p][q]);
+                // the reads spread over the MFMAs
+                constexpr int kReads = (FI + FJ) * (TT ? 2 : 1);
+#pragma unroll
+                for (int k = 0; k < kReads; ++k) {
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x008, FI * FJ / kReads, 0);
+                }
+            };
+            fetch(to);
+            wait_loads<kLoads>();
+            barrier();
+            half(cur, 0, fa[0], fb[0]);
+            for (int t = 0; t < steps; ++t) {
+                half(cur, 1, fa[1], fb[1]);
+                product(fa[0], fb[0]);
+                __builtin_amdgcn_sched_barrier(0);
+                wait_loads<0>();
+                __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): this wave is done with tile t
+                barrier();                            // as all are, and tile t + 1 is here
+                fetch(cur);                           // tile t + 2
+                cur = next(cur);
+                half(cur, 0, fa[0], fb[0]);
+                product(fa[1], fb[1]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        } else {
+            Frag fa[KS][FI], fb[KS][FJ];
+            for (int t = 0; t < steps; ++t) {
+                wait_loads<(kStages - 2) * kLoads>();
+                barrier();   // tile t is here, and all waves are done with tile t - 1
+                fetch(to);
+                read(cur, fa, fb);
+                multiply(fa, fb);
+                cur = next(cur);
+                to = next(to);
+            }
         }
-        if (t + 1 < steps) settle(nxt);
+        wait_loads<0>();   // nothing may still write to LDS
+    } else {
+        static_assert(kStages == 2, "two stages");
+        Frag fa[KS][FI], fb[KS][FJ];
+        typename TA::Packed ra[kAsyncA ? 1 : TA::kPasses];
+        typename TB::Packed rb[kAsyncB ? 1 : TB::kPasses];
+        auto fetch = [&](char* to, int64_t c0) {
+            if constexpr (kAsyncA)
+                TA::load_async(to, a, g.lda, g.a_rows, i0, g.rows, c0, c_end);
+            else
+                TA::load_regs(ra, a, g.lda, i0, g.rows, c0, c_end);
+            if constexpr (kAsyncB)
+                TB::load_async(to + TA::kBytes, b, g.ldb, g.b_rows, j0, g.cols, c0, c_end);
+            else
+                TB::load_regs(rb, b, g.ldb, j0, g.cols, c0, c_end);
+        };
+        auto settle = [&](char* to) {
+            if constexpr (!kAsyncA) TA::store_regs(to, ra);
+            if constexpr (!kAsyncB) TB::store_regs(to + TA::kBytes, rb);
+        };
+        if (steps > 0) {
+            fetch(lds, c_begin);
+            settle(lds);
+        }
+        for (int t = 0; t < steps; ++t) {
+            char* nxt = lds + ((t + 1) & 1) * kTileBytes;
+            __syncthreads();   // tile t has arrived, and the other is no longer read
+            if (t + 1 < steps) fetch(nxt, c_begin + (int64_t)(t + 1) * kBK);
+            read(lds + (t & 1) * kTileBytes, fa, fb);
+            multiply(fa, fb);
+            if (t + 1 < steps) settle(nxt);
+        }
     }
 
     // acc[p][q][r] is row i0 + wi + 16 p + li, column (TT) wj + 16 q + 4 lg + r or (NT) the interleaved one
@@ -332,34 +436,88 @@ __global__ __launch_bounds__(WI* WJ * 64) void k_gemm(GemmArgs g)
                     }
                 }
             }
-    } else {
+        return;
+    }
+    const int64_t i1 = i0 + wi, j1 = j0 + wj;
+    if (g.part) {
 #pragma unroll
         for (int q = 0; q < FJ; q += 2) {
-            const int64_t j = j0 + wj + 16 * q + 8 * lg;
-            if (j >= g.cols) continue;
-            float bias[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) bias[e] = g.bias && !g.part && j + e < g.cols ? g.bias[j + e] : 0.f;
+            const int64_t j = j1 + 16 * q + 8 * lg;
 #pragma unroll
             for (int p = 0; p < FI; ++p) {
-                const int64_t i = i0 + wi + 16 * p + li;
-                if (i >= g.rows) continue;
-                float v[8];
+                const int64_t i = i1 + 16 * p + li;
+                if (i >= g.rows || j >= g.cols) continue;
+                float* o = g.part + ((int64_t)part * g.rows + i) * g.cols + j;
+                float lo[4], hi[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    v[e] = acc[p][q][e];
-                    v[4 + e] = acc[p][q + 1][e];
+                    lo[e] = acc[p][q][e];
+                    hi[e] = acc[p][q + 1][e];
                 }
-                if (g.part) {
-                    float* o = g.part + ((int64_t)part * g.rows + i) * g.cols + j;
-                    store_vec(o, g.cols - j, v);
-                    store_vec(o + 4, g.cols - j - 4, v + 4);
-                } else {
-                    epilogue8<T>(g, i, j, g.cols - j, v, bias);
-                }
+                store_vec(o, g.cols - j, lo);
+                store_vec(o + 4, g.cols - j - 4, hi);
             }
         }
+        return;
     }
+    // A wave's results go through its own part of LDS, so that they are stored as whole rows of its block: z, then y.
+    constexpr int N = Vec<T>::N, kVecs = WC / N;
+    char* block = lds + wave * (WR * WC * (int)sizeof(T));
+    auto put = [&](int p, int q, const float* v) {
+        const int r = 16 * p + li;
+#pragma unroll
+        for (int e = 0; e < 8; e += N) {
+            typename Vec<T>::Packed t;
+#pragma unroll
+            for (int k = 0; k < N; ++k) t[k] = (T)v[e + k];
+            const int vec = (16 * q + 8 * lg + e) / N;
+            *reinterpret_cast<typename Vec<T>::Packed*>(block + r * (WC * (int)sizeof(T)) +
+                                                        (vec ^ (r & 7 & (kVecs - 1))) * 16) = t;
+        }
+    };
+    barrier();   // all waves are done with the tiles
+#pragma unroll
+    for (int q = 0; q < FJ; ++q) {
+        const int64_t j = j1 + 16 * (q & ~1) + 8 * lg + 4 * (q & 1);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float bias = g.bias && j + e < g.cols ? g.bias[j + e] : 0.f;
+#pragma unroll
+            for (int p = 0; p < FI; ++p) acc[p][q][e] += bias;
+        }
+    }
+    if (g.z) {
+#pragma unroll
+        for (int p = 0; p < FI; ++p)
+#pragma unroll
+            for (int q = 0; q < FJ; q += 2) {
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = acc[p][q + (e >> 2)][e & 3];
+                put(p, q, v);
+            }
+        store_block<T, WR, WC>(block, (T*)g.z, g.ldz, i1, g.rows, j1, g.cols);
+    }
+#pragma unroll
+    for (int p = 0; p < FI; ++p)
+#pragma unroll
+        for (int q = 0; q < FJ; q += 2) {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = acc[p][q + (e >> 2)][e & 3];
+            activate<8>(g.act, v);
+            const int64_t i = i1 + 16 * p + li, j = j1 + 16 * q + 8 * lg;
+            if (g.residual && i < g.rows && j < g.cols) {
+                const T* r = (const T*)g.residual + i * g.ldr + j;
+                float t[8];
+#pragma unroll
+                for (int e = 0; e < 8; e += N) load_vec(r + e, g.cols - j - e, t + e);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] += t[e];
+            }
+            put(p, q, v);
+        }
+    store_block<T, WR, WC>(block, (T*)g.out, g.ldo, i1, g.rows, j1, g.cols);
 }
 
 // Few rows (NT, rows <= 16 MF): a workgroup takes 16 columns j and its waves share the sum; the weights go from
@@ -559,13 +717,20 @@ __global__ __launch_bounds__(kBlock) void k_layout(const T* __restrict__ src, in
     }
 }
 
-template <typename T, bool TT, int BI, int BJ, int WI, int WJ, bool FAST>
+template <typename T, class S>
 hipError_t run_gemm(const GemmArgs& g, hipStream_t s)
 {
-    const int64_t tiles = div_up(g.rows, BI) * div_up(g.cols, BJ);
-    hipLaunchKernelGGL((k_gemm<T, TT, BI, BJ, WI, WJ, FAST>), dim3((unsigned)tiles, (unsigned)(g.planes * g.splits)),
-                       dim3(WI * WJ * 64), 0, s, g);
+    const int64_t tiles = div_up(g.rows, S::BI) * div_up(g.cols, S::BJ);
+    hipLaunchKernelGGL((k_gemm<T, S>), dim3((unsigned)tiles, (unsigned)(g.planes * g.splits)), dim3(S::THREADS), 0, s,
+                       g);
     return hipGetLastError();
+}
+
+template <typename T, bool TT, int BI, int BJ, int WI, int WJ>
+hipError_t run_any(bool fast, const GemmArgs& g, hipStream_t s)
+{
+    return fast ? run_gemm<T, Shape<TT, BI, BJ, WI, WJ, 2, 2, false, true>>(g, s)
+                : run_gemm<T, Shape<TT, BI, BJ, WI, WJ, 2, 2, false, false>>(g, s);
 }
 
 }  // namespace
@@ -573,21 +738,22 @@ hipError_t run_gemm(const GemmArgs& g, hipStream_t s)
 template <typename T>
 hipError_t LinearOps<T>::gemm_nt(int tile, bool fast_a, const GemmArgs& g, hipStream_t s)
 {
-    if (tile == kTile256) return run_gemm<T, false, 256, 256, 2, 4, true>(g, s);   // fast_a only
-    if (tile == kTile128)
-        return fast_a ? run_gemm<T, false, 128, 128, 2, 2, true>(g, s) : run_gemm<T, false, 128, 128, 2, 2, false>(g, s);
-    if (tile == kTile128x32)
-        return fast_a ? run_gemm<T, false, 128, 32, 4, 1, true>(g, s) : run_gemm<T, false, 128, 32, 4, 1, false>(g, s);
-    return fast_a ? run_gemm<T, false, 64, 64, 2, 2, true>(g, s) : run_gemm<T, false, 64, 64, 2, 2, false>(g, s);
+    if (tile == kTile256) {   // fast_a, 16-bit
+        if constexpr (sizeof(T) == 2) return run_gemm<T, Shape<false, 256, 256, 2, 4, 2, 2, true, true>>(g, s);
+    }
+    if (tile == kTile128) return run_any<T, false, 128, 128, 2, 2>(fast_a, g, s);
+    if (tile == kTile128x64) return run_any<T, false, 128, 64, 4, 1>(fast_a, g, s);
+    return run_any<T, false, 64, 64, 2, 2>(fast_a, g, s);
 }
 
 template <typename T>
 hipError_t LinearOps<T>::gemm_tt(int tile, bool fast_b, const GemmArgs& g, hipStream_t s)
 {
-    if (tile == kTile256) return run_gemm<T, true, 256, 256, 2, 4, true>(g, s);   // fast_b only
-    if (tile == kTile128)
-        return fast_b ? run_gemm<T, true, 128, 128, 2, 2, true>(g, s) : run_gemm<T, true, 128, 128, 2, 2, false>(g, s);
-    return fast_b ? run_gemm<T, true, 64, 64, 2, 2, true>(g, s) : run_gemm<T, true, 64, 64, 2, 2, false>(g, s);
+    if (tile == kTile256) {   // fast_b, 16-bit
+        if constexpr (sizeof(T) == 2) return run_gemm<T, Shape<true, 256, 256, 2, 4, 2, 2, true, true>>(g, s);
+    }
+    if (tile == kTile128) return run_any<T, true, 128, 128, 2, 2>(fast_b, g, s);
+    return run_any<T, true, 64, 64, 2, 2>(fast_b, g, s);
 }
 
 template <typename T>

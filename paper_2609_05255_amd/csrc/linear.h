@@ -46,7 +46,7 @@ struct SlopeArgs {
     int32_t row_blocks;
 };
 
-enum { kTile256 = 0, kTile128, kTile64, kTile128x32, kTileCount };
+enum { kTile256 = 0, kTile128, kTile64, kTile128x64 };
 
 struct TileShape {
     int bi, bj, threads;
@@ -57,7 +57,7 @@ inline TileShape tile_shape(int tile)
     case kTile256: return {256, 256, 512};
     case kTile128: return {128, 128, 256};
     case kTile64: return {64, 64, 256};
-    default: return {128, 32, 256};
+    default: return {128, 64, 256};
     }
 }
 

@@ -40,8 +40,8 @@ struct Plan {
 Plan plan_nt(int type, int64_t rows, int64_t cols, int64_t len, bool fast_a)
 {
     Plan p = {kTile64, 1, len};
-    if (cols <= 32) {
-        p.tile = kTile128x32;
+    if (cols <= 64 && div_up(rows, 128) >= kFillTiles) {
+        p.tile = kTile128x64;
         return p;
     }
     if (fast_a && type != GS_F32 && div_up(rows, 256) * div_up(cols, 256) >= kFillTiles && cols >= 192 && len >= 512) {
@@ -69,7 +69,9 @@ Plan plan_tt(int type, int64_t out, int64_t in, int64_t rows, int planes, bool f
     if (fast_b && type != GS_F32 && div_up(out, 256) * div_up(in, 256) * planes >= kFillTiles) p.tile = kTile256;
     const TileShape t = tile_shape(p.tile);
     const int64_t tiles = div_up(out, t.bi) * div_up(in, t.bj) * planes;
-    const int64_t want = std::max<int64_t>(1, std::min(div_up(2 * kFillTiles, tiles), rows / kRowSplitLen));
+    // two workgroups per compute unit, one of the largest tile
+    const int64_t fill = p.tile == kTile256 ? kFillTiles : 2 * kFillTiles;
+    const int64_t want = std::max<int64_t>(1, std::min(div_up(fill, tiles), rows / kRowSplitLen));
     p.split_len = std::max<int64_t>(64, div_up(div_up(rows, want), 64) * 64);
     p.splits = (int)std::max<int64_t>(1, div_up(rows, p.split_len));
     return p;
@@ -296,7 +298,7 @@ size_t linear_workspace(int type, int act, int64_t rows, int64_t in, int64_t out
 // Work items of a launch are counted in 32 bits.
 bool linear_grid_fits(int64_t rows, int64_t cols)
 {
-    return div_up(rows, 128) * div_up(cols, cols <= 32 ? 32 : 128) * 256 < ((int64_t)1 << 32);
+    return div_up(rows, 128) * div_up(cols, cols <= 64 ? 64 : 128) * 256 < ((int64_t)1 << 32);
 }
 
 hipError_t launch_linear_fwd(const gs_linear& p, const void* residual, int64_t ldr, void* y, int64_t ldy, void* z,
