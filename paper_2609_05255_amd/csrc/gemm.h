@@ -30,16 +30,19 @@ namespace gsr {
 namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 constexpr uint32_t kOutOfRange = 0x80000000u;   // beyond any descriptor's range (at most 2^31 - 1 bytes)
 
+// D[j][i] += sum over kStep values of B[j] A[i], 16 x 16. A lane holds one row (lane % 16) of an operand, 16 bytes of
+// it, and of D the column i = lane % 16, rows j = 4 (lane / 16) + r.
 template <typename T>
 struct Mma {
-    typedef T Frag __attribute__((ext_vector_type(8)));   // 16-bit: 8 values along the sum
-    static constexpr int kStep = 32;                      // values along the sum per fragment
+    typedef T Frag __attribute__((ext_vector_type(8)));
+    static constexpr int kStep = 32;
     static __device__ __forceinline__ f32x4 mma(const Frag& a, const Frag& b, f32x4 c)
     {
         if constexpr (__is_same(T, f16))
@@ -78,74 +81,105 @@ __device__ __forceinline__ void barrier()
     asm volatile("" ::: "memory");
 }
 
-// NT: X rows of 4 KS slots along the sum; fragment rows are base + i (A) or the interleaved columns
-// base + (i & 3) + 8 (i >> 2) (B), i = lane % 16. A 16-byte LDS read of half a wave takes two turns of 16 lanes, {0..3,
-// 12..15, 20..23, 24..27} and the others (found from the conflict counter); the hash gives each turn's lanes different
-// slots of the 256 bytes that the banks hold.
-template <int KS, bool IS_B>
-__device__ __forceinline__ int nt_hash(int row)
-{
-    if constexpr (KS == 1) return -(IS_B ? row >> 3 : row >> 2) & 3;
-    return IS_B ? ((row >> 2) & 6) | ((row >> 1) & 1) : (row >> 1) & 7;
-}
-
-// TT: rows c of X * sizeof(T) / 16 slots.
-template <typename T, int X>
-__device__ __forceinline__ int tt_hash(int c)
-{
-    constexpr int kSlots = X * (int)sizeof(T) / 16;
-    if constexpr (sizeof(T) == 2) {
-        // the 32 lanes of half a wave read 32 bytes of each of 8 rows
-        const int h = (c & 3) | ((c >> 1) & 4);
-        return (h << 1) & (kSlots - 1);
-    } else {
-        return ((c & 3) << 2) & (kSlots - 1);   // 64 bytes of each of 4 rows
-    }
-}
-
-// Geometry of one operand's tile: which slot of which row a thread fills, and from which vector of that row.
-template <typename T, int X, int KS, bool TT, bool IS_B, int THREADS>
+// Geometry of one operand's tile in LDS: X rows or columns, 128 bytes of the sum, slots of 16 bytes.
+//
+// NT: X rows of 8 slots along the sum. A fragment's lane i reads row base + i (A) or base + interleaved(i) (B). A
+// 16-byte LDS read of half a wave takes two turns of 16 lanes, {0..3, 12..15, 20..23, 24..27} and the others (found
+// from the conflict counter); the hash gives the lanes of a turn different slots of the 256 bytes that the banks hold.
+//
+// TT: blocks of 128 bytes across (64 16-bit or 32 fp32 columns), each kBK rows of 8 slots. 16-bit fragments come
+// through the transposing read, which gives 16 lanes the columns of 4 rows of 32 bytes; the sum's order within a
+// fragment is free as long as A and B agree: value 4 t + e of lane group g is row 16 t + 4 g + e, so that the hash, and with it the address but for a constant, does not depend on t or on the step.
+template <typename T, int X, bool TT, bool IS_B, int THREADS>
 struct Tile {
     static constexpr int kVec = 16 / (int)sizeof(T);
-    static constexpr int kRowSlots = TT ? X / kVec : 4 * KS;
-    static constexpr int kSlotsTotal = X * 4 * KS;
+    static constexpr int kBK = 128 / (int)sizeof(T);       // values along the sum
+    static constexpr int kSlotsTotal = X * 8;
     static constexpr int kPasses = kSlotsTotal / THREADS;
-    static constexpr int kBytes = X * 64 * KS;
+    static constexpr int kBytes = X * 128;
+    static constexpr int kBlockBytes = kBK * 128;          // TT
     static_assert(kSlotsTotal % THREADS == 0, "whole passes");
+    typedef typename Mma<T>::Frag Frag;
 
-    static __device__ __forceinline__ int row(int q) { return q / kRowSlots; }
+    static __device__ __forceinline__ int hash(int row)
+    {
+        if constexpr (TT) return sizeof(T) == 2 ? row & 6 : (row & 2) << 1;
+        return IS_B ? ((row >> 2) & 6) | ((row >> 1) & 1) : (row >> 1) & 7;
+    }
+    // The row of LDS, and the vector of the operand's row, that slot q holds.
+    static __device__ __forceinline__ int row(int q) { return TT ? q / 8 % kBK : q / 8; }
     static __device__ __forceinline__ int vec(int q)
     {
-        const int r = row(q), s = q % kRowSlots;
-        return s ^ (TT ? tt_hash<T, X>(r) : nt_hash<KS, IS_B>(r));
+        const int v = (q & 7) ^ hash(row(q));
+        return TT ? q / (8 * kBK) * 8 + v : v;
     }
 
-    // LDS <- memory. p: the operand, stored rows of ld values; x0: first row (NT) or column (TT) of the tile;
-    // c0: position along the sum; c_end, x_end: where both end.
-    static __device__ __forceinline__ void load_async(char* lds, const T* p, int64_t ld, int64_t stored, int64_t x0,
-                                                      int64_t x_end, int64_t c0, int64_t c_end)
-    {
-        const int64_t r0 = TT ? c0 : x0;
-        const int64_t rows_end = TT ? c_end : x_end;
-        const int64_t first = r0 * ld;
-        // bytes from the tile's first row to the end of its last valid one
-        const int64_t bytes = ((rows_end < stored ? rows_end : stored) - r0) * ld * (int64_t)sizeof(T);
-        const int range = bytes > 0x7FFFFFF0 ? 0x7FFFFFF0 : bytes < 0 ? 0 : (int)bytes;
-        __amdgpu_buffer_rsrc_t rsrc =
-            __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(p + first), 0, range, 0x00027000);
-        const int64_t v0 = TT ? x0 : c0, v_end = TT ? x_end : c_end;
-        const int wave = threadIdx.x >> 6;
+    // LDS <- memory, 16 bytes per lane and pass. Issued by hand, and waited for by hand (wait_loads): the compiler would
+    // wait for all of them before each transposing read, as it takes the two for accesses to the same memory. The
+    // instruction has no destination register. Every pass of every tile is issued: what lies beyond the operand, or
+    // beyond the part of the sum that ends at c_end, is turned into zeros by the descriptor's range check.
+    struct Source {
+        const T* p;             // the tile's first row (NT) or column (TT), at its position along the sum
+        int64_t step;           // values per tile along the sum, in p
+        int row_bytes, x_bytes;
+        int x_left, c_left;     // rows (NT) or columns (TT), and values of the sum from here on
+        int wave_bytes;         // this wave's part of a pass
+        uint32_t off[kPasses];  // of each pass, from p
+        __device__ __forceinline__ Source(const T* base, int64_t ld, int64_t x0, int64_t x_end, int64_t c0, int64_t c_end)
+        {
+            p = TT ? base + c0 * ld + x0 : base + x0 * ld + c0;
+            step = (int64_t)kBK * (TT ? ld : 1);
+            row_bytes = (int)(ld * (int64_t)sizeof(T));
+            x_bytes = TT ? (int)(x0 * (int64_t)sizeof(T)) : 0;
+            x_left = (int)(x_end - x0);
+            c_left = (int)(c_end - c0);
+            wave_bytes = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 1024;
 #pragma unroll
-        for (int k = 0; k < kPasses; ++k) {
-            const int q = k * THREADS + threadIdx.x;
-            const int64_t v = v0 + (int64_t)vec(q) * kVec;
-            // (vectors are whole in this form: v < v_end covers all of one)
-            uint32_t off = (uint32_t)row(q) * (uint32_t)(ld * (int64_t)sizeof(T)) + (uint32_t)(v * (int64_t)sizeof(T));
-            if (v >= v_end) off = kOutOfRange;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(lds + (k * (THREADS / 64) + wave) * 1024), 16,
-                                                     off, 0, 0, 0);
+            for (int k = 0; k < kPasses; ++k) {
+                const int q = k * THREADS + threadIdx.x;
+                off[k] = (uint32_t)(row(q) * row_bytes) + vec(q) * 16;
+                if (TT && vec(q) * kVec >= x_left) off[k] = kOutOfRange;
+            }
+            cut();
         }
-    }
+        // (vectors are whole in this form: the sum ends between them)
+        __device__ __forceinline__ void cut()
+        {
+            if (!TT && c_left < kBK)
+#pragma unroll
+                for (int k = 0; k < kPasses; ++k)
+                    if (vec(k * THREADS + threadIdx.x) * kVec >= c_left) off[k] = kOutOfRange;
+        }
+        __device__ __forceinline__ void pass(char* lds, int k) const
+        {
+            // bytes from p to the end of the tile's last row: of X rows, or of the tile's part of the sum. At most 2^30.
+            const int rows = TT ? min(max(c_left, 0), kBK) : min(x_left, X);
+            const uint64_t at = reinterpret_cast<uint64_t>(p);
+            u32x4 rsrc;   // base, no stride, range, untyped
+            rsrc[0] = __builtin_amdgcn_readfirstlane((uint32_t)at);
+            rsrc[1] = __builtin_amdgcn_readfirstlane((uint32_t)(at >> 32) & 0xFFFF);
+            rsrc[2] = __builtin_amdgcn_readfirstlane(max(rows * row_bytes - x_bytes, 0));
+            rsrc[3] = 0x00027000;
+            const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void*)lds) + k * (THREADS * 16) +
+                                wave_bytes;
+            asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
+                         :
+                         : "v"(off[k]), "s"(rsrc), "s"(to)
+                         : "memory", "m0");
+        }
+        __device__ __forceinline__ void advance()
+        {
+            p += step;
+            c_left -= kBK;
+            cut();
+        }
+        __device__ __forceinline__ void load(char* lds)
+        {
+#pragma unroll
+            for (int k = 0; k < kPasses; ++k) pass(lds, k);
+            advance();
+        }
+    };
 
     // registers <- memory at any alignment, masked value by value at the ends
     typedef typename Vec<T>::Packed Packed;
@@ -178,35 +212,30 @@ struct Tile {
     }
 
     // Fragment f of step s of a wave whose first row or column of the tile is wx.
-    static __device__ __forceinline__ typename Mma<T>::Frag frag(const char* lds, int wx, int f, int s)
+    static __device__ __forceinline__ Frag frag(const char* lds, int wx, int f, int s)
     {
-        const int lane = threadIdx.x & 63, g = lane >> 4, i = lane & 15;
+        const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
         if constexpr (!TT) {
             const int r = IS_B ? wx + 32 * (f >> 1) + 4 * (f & 1) + 8 * (i >> 2) + (i & 3) : wx + 16 * f + i;
-            const int slot = (4 * s + g) ^ nt_hash<KS, IS_B>(r);
-            return *reinterpret_cast<const typename Mma<T>::Frag*>(lds + r * (64 * KS) + slot * 16);
+            const int slot = (4 * s + g) ^ hash(r);
+            return *reinterpret_cast<const Frag*>(lds + r * 128 + slot * 16);
         } else if constexpr (sizeof(T) == 2) {
-            typename Mma<T>::Frag out;
-            s16x4 h[2];
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const int c = 32 * s + 8 * g + 4 * t + (i >> 2);
-                const int col = wx + 16 * f + 4 * (i & 3);
-                const int slot = (col / 8) ^ tt_hash<T, X>(c);
-                h[t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (lds_s16x4*)(lds + c * (X * 2) + slot * 16 + (col & 7) * 2));
-            }
-            __builtin_memcpy(&out, h, 16);
+            // 16 lanes: 4 rows of one group of 16 columns
+            const int n = wx / 16 + f, r = 4 * g + (i >> 2);
+            const char* at = lds + (n >> 2) * kBlockBytes + r * 128 + ((((n & 3) * 2) ^ hash(r)) + ((i >> 1) & 1)) * 16 +
+                             (i & 1) * 8 + s * (32 * 128);
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 16 * 128));
+            s16x4 both[2] = {lo, hi};
+            Frag out;
+            __builtin_memcpy(&out, both, 16);
             return out;
         } else {
-            typename Mma<T>::Frag out;
+            const int col = wx + 16 * f + i;
+            const char* at = lds + (col >> 5) * kBlockBytes + g * 128 + ((((col & 31) >> 2) ^ hash(g)) * 4 + (col & 3)) * 4;
+            Frag out;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int c = 16 * s + 4 * e + g;
-                const int col = wx + 16 * f + i;
-                const int slot = (col / 4) ^ tt_hash<T, X>(c);
-                out[e] = *reinterpret_cast<const float*>(lds + c * (X * 4) + slot * 16 + (col & 3) * 4);
-            }
+            for (int e = 0; e < 4; ++e) out[e] = *reinterpret_cast<const float*>(at + (16 * s + 4 * e) * 128);
             return out;
         }
     }
@@ -226,13 +255,13 @@ __device__ __forceinline__ void tile_of(int64_t b, int64_t tiles_i, int64_t tile
     *tj = in / h;
 }
 
-// BI, BJ: the workgroup's tile; WI, WJ: its waves; KS: steps of the sum per tile in LDS; STAGES: tiles in the ring;
-// AHEAD: fragments are read a tile ahead of their MFMAs. FAST: the operand that may be the caller's (A in NT, B in TT)
-// is loaded asynchronously as well, as the other always is; otherwise it goes through registers, at any alignment.
-template <bool TT_, int BI_, int BJ_, int WI_, int WJ_, int KS_, int STAGES_, bool AHEAD_, bool FAST_>
+// BI, BJ: the workgroup's tile; WI, WJ: its waves; AHEAD: fragments are read half a tile ahead of their MFMAs. FAST: the
+// operand that may be the caller's (A in NT, B in TT) is loaded asynchronously as well, as the other always is;
+// otherwise it goes through registers, at any alignment.
+template <bool TT_, int BI_, int BJ_, int WI_, int WJ_, bool AHEAD_, bool FAST_>
 struct Shape {
     static constexpr bool TT = TT_, AHEAD = AHEAD_, FAST = FAST_;
-    static constexpr int BI = BI_, BJ = BJ_, WI = WI_, WJ = WJ_, KS = KS_, STAGES = STAGES_;
+    static constexpr int BI = BI_, BJ = BJ_, WI = WI_, WJ = WJ_;
     static constexpr int THREADS = WI * WJ * 64;
 };
 
@@ -266,16 +295,17 @@ template <typename T, class S>
 __global__ __launch_bounds__(S::THREADS) void k_gemm(GemmArgs g)
 {
     constexpr bool TT = S::TT;
-    constexpr int BI = S::BI, BJ = S::BJ, WI = S::WI, WJ = S::WJ, KS = S::KS, kStages = S::STAGES;
+    constexpr int BI = S::BI, BJ = S::BJ, WI = S::WI, WJ = S::WJ;
     constexpr int WR = BI / WI, WC = BJ / WJ, FI = WR / 16, FJ = WC / 16;
-    constexpr int kBK = Mma<T>::kStep * KS;
-    using TA = Tile<T, BI, KS, TT, false, S::THREADS>;
-    using TB = Tile<T, BJ, KS, TT, true, S::THREADS>;
+    using Mm = Mma<T>;
+    using TA = Tile<T, BI, TT, false, S::THREADS>;
+    using TB = Tile<T, BJ, TT, true, S::THREADS>;
+    constexpr int kBK = TA::kBK, kSteps = kBK / Mm::kStep;   // of the sum, and of MFMAs, per tile
     constexpr int kTileBytes = TA::kBytes + TB::kBytes;
     constexpr bool kAsyncA = S::FAST || TT, kAsyncB = S::FAST || !TT;
     static_assert(TT || FJ % 2 == 0, "columns interleave between pairs of fragments");
-    static_assert(TT || WI * WJ * WR * WC * (int)sizeof(T) <= kStages * kTileBytes, "the results pass through LDS");
-    __shared__ __attribute__((aligned(1024))) char lds[kStages * kTileBytes];
+    static_assert(TT || WI * WJ * WR * WC * (int)sizeof(T) <= 2 * kTileBytes, "the results pass through LDS");
+    __shared__ __attribute__((aligned(1024))) char lds[2 * kTileBytes + (S::AHEAD ? TA::kBytes : 0)];
 
     const int64_t tiles_i = (g.rows + BI - 1) / BI, tiles_j = (g.cols + BJ - 1) / BJ;
     int64_t ti, tj;
@@ -288,104 +318,119 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(GemmArgs g)
     const T* b = (const T*)g.b;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wi = (wave / WJ) * WR, wj = (wave % WJ) * WC;
-    const int lane = threadIdx.x & 63, lg = lane >> 4, li = lane & 15;
+    const int lane = threadIdx.x & 63;
 
-    typedef typename Mma<T>::Frag Frag;
+    typedef typename Mm::Frag Frag;
     f32x4 acc[FI][FJ] = {};
-    auto read = [&](const char* from, Frag(&fa)[KS][FI], Frag(&fb)[KS][FJ]) {
+    auto read = [&](const char* from, Frag(&fa)[kSteps][FI], Frag(&fb)[kSteps][FJ]) {
 #pragma unroll
-        for (int s = 0; s < KS; ++s) {
+        for (int s = 0; s < kSteps; ++s) {
 #pragma unroll
             for (int f = 0; f < FJ; ++f) fb[s][f] = TB::frag(from + TA::kBytes, wj, f, s);
 #pragma unroll
             for (int f = 0; f < FI; ++f) fa[s][f] = TA::frag(from, wi, f, s);
         }
     };
-    auto multiply = [&](const Frag(&fa)[KS][FI], const Frag(&fb)[KS][FJ]) {
+    auto multiply = [&](const Frag(&fa)[kSteps][FI], const Frag(&fb)[kSteps][FJ]) {
 #pragma unroll
-        for (int s = 0; s < KS; ++s)
+        for (int s = 0; s < kSteps; ++s)
 #pragma unroll
             for (int p = 0; p < FI; ++p)
 #pragma unroll
-                for (int q = 0; q < FJ; ++q) acc[p][q] = Mma<T>::mma(fb[s][q], fa[s][p], acc[p][q]);
+                for (int q = 0; q < FJ; ++q) acc[p][q] = Mm::mma(fb[s][q], fa[s][p], acc[p][q]);
     };
     const int steps = c_end > c_begin ? (int)((c_end - c_begin + kBK - 1) / kBK) : 0;
     if constexpr (S::FAST) {
         constexpr int kLoads = TA::kPasses + TB::kPasses;   // of a thread per tile
-        int64_t c0 = c_begin;
-        auto fetch = [&](char* to) {
-            TA::load_async(to, a, g.lda, g.a_rows, i0, g.rows, c0, c_end);
-            TB::load_async(to + TA::kBytes, b, g.ldb, g.b_rows, j0, g.cols, c0, c_end);
-            c0 += kBK;
-        };
-        char* cur = lds;
-        char* to = lds;
-        auto next = [&](char* p) { return p + kTileBytes == lds + kStages * kTileBytes ? lds : p + kTileBytes; };
-        for (int k = 0; k < kStages - 1; ++k, to = next(to)) fetch(to);   // (AHEAD: all of them)
+        typename TA::Source sa(a, g.lda, i0, g.rows, c_begin, c_end);
+        typename TB::Source sb(b, g.ldb, j0, g.cols, c_begin, c_end);
         if constexpr (S::AHEAD) {
-            static_assert(KS == 2 && kStages == 2, "two halves of two tiles");
-            Frag fa[2][FI], fb[2][FJ];
-            auto half = [&](const char* from, int s, Frag(&ra)[FI], Frag(&rb)[FJ]) {
-#pragma unroll
-                for (int f = 0; f < FJ; ++f) rb[f] = TB::frag(from + TA::kBytes, wj, f, s);
-#pragma unroll
-                for (int f = 0; f < FI; ++f) ra[f] = TA::frag(from, wi, f, s);
-            };
-            auto product = [&](const Frag(&ma)[FI], const Frag(&mb)[FJ]) {
-#pragma unroll
-                for (int p = 0; p < FI; ++p)
-#pragma unroll
-                    for (int q = 0; q < FJ; ++q) acc[p][q] = Mma<T>::mma(mb[q], ma[p], acc[p][q]);
-                // the reads spread over the MFMAs
-                constexpr int kReads = (FI + FJ) * (TT ? 2 : 1);
-#pragma unroll
-                for (int k = 0; k < kReads; ++k) {
-                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                    __builtin_amdgcn_sched_group_barrier(0x008, FI * FJ / kReads, 0);
-                }
-            };
-            fetch(to);
+            // Three tiles of A and two of B in LDS, each of two halves along the sum. While a half's MFMAs run, the next
+            // half's fragments are read; A's tile t + 2 is loaded under the first half of tile t, B's under the second,
+            // where tile t's own fragments have all been read. Behind each row of MFMAs stand a few reads and loads:
+            // issued together they would hold the wave, and the MFMAs behind them, until the memory pipe takes them.
+            constexpr int kHalf = kSteps / 2, kRows = kHalf * FI;   // rows of MFMAs in a half
+            static_assert(kRows == 2 * TA::kPasses && kRows == 2 * TB::kPasses &&
+                              kHalf * (FI + FJ) <= 2 * (kRows - 1), "the loads and reads of a half fit its rows");
+            char* a_lds[3] = {lds, lds + TA::kBytes, lds + 2 * TA::kBytes};
+            char* b_lds[2] = {lds + 3 * TA::kBytes, lds + 3 * TA::kBytes + TB::kBytes};
+            Frag fa[2][kHalf][FI], fb[2][kHalf][FJ];
+            for (int k = 0; k < 2; ++k) {
+                sa.load(a_lds[k]);
+                sb.load(b_lds[k]);
+            }
             wait_loads<kLoads>();
             barrier();
-            half(cur, 0, fa[0], fb[0]);
+            auto fetch = [&](const char* from_a, const char* from_b, int half, int k, Frag(&na)[kHalf][FI],
+                             Frag(&nb)[kHalf][FJ]) {
+                const int s = k / (FI + FJ), f = k % (FI + FJ);
+                if (s >= kHalf) return;
+                if (f < FJ)
+                    nb[s][f] = TB::frag(from_b, wj, f, half * kHalf + s);
+                else
+                    na[s][f - FJ] = TA::frag(from_a, wi, f - FJ, half * kHalf + s);
+            };
+#pragma unroll
+            for (int k = 0; k < 2 * kRows; ++k) fetch(a_lds[0], b_lds[0], 0, k, fa[0], fb[0]);
+            auto half = [&](const Frag(&ma)[kHalf][FI], const Frag(&mb)[kHalf][FJ], const char* from_a,
+                            const char* from_b, int h, Frag(&na)[kHalf][FI], Frag(&nb)[kHalf][FJ], auto load) {
+#pragma unroll
+                for (int u = 0; u < kRows; ++u) {
+                    const int s = u / FI, p = u % FI;
+#pragma unroll
+                    for (int q = 0; q < FJ; ++q) acc[p][q] = Mm::mma(mb[s][q], ma[s][p], acc[p][q]);
+                    __builtin_amdgcn_sched_barrier(0);
+                    fetch(from_a, from_b, h, 2 * u, na, nb);
+                    fetch(from_a, from_b, h, 2 * u + 1, na, nb);
+                    if (u % 2 == 0) load(u / 2);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            };
             for (int t = 0; t < steps; ++t) {
-                half(cur, 1, fa[1], fb[1]);
-                product(fa[0], fb[0]);
-                __builtin_amdgcn_sched_barrier(0);
-                wait_loads<0>();
-                __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): this wave is done with tile t
-                barrier();                            // as all are, and tile t + 1 is here
-                fetch(cur);                           // tile t + 2
-                cur = next(cur);
-                half(cur, 0, fa[0], fb[0]);
-                product(fa[1], fb[1]);
-                __builtin_amdgcn_sched_barrier(0);
+                half(fa[0], fb[0], a_lds[0], b_lds[0], 1, fa[1], fb[1], [&](int k) { sa.pass(a_lds[2], k); });
+                sa.advance();
+                __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): this wave has tile t's fragments
+                wait_loads<TA::kPasses>();
+                barrier();                            // as all have, and tile t + 1 is here
+                half(fa[1], fb[1], a_lds[1], b_lds[1], 0, fa[0], fb[0], [&](int k) { sb.pass(b_lds[0], k); });
+                sb.advance();
+                char* x = a_lds[0];
+                a_lds[0] = a_lds[1];
+                a_lds[1] = a_lds[2];
+                a_lds[2] = x;
+                x = b_lds[0];
+                b_lds[0] = b_lds[1];
+                b_lds[1] = x;
             }
         } else {
-            Frag fa[KS][FI], fb[KS][FJ];
+            Frag fa[kSteps][FI], fb[kSteps][FJ];
+            sa.load(lds);
+            sb.load(lds + TA::kBytes);
             for (int t = 0; t < steps; ++t) {
-                wait_loads<(kStages - 2) * kLoads>();
+                char* cur = lds + (t & 1) * kTileBytes;
+                char* nxt = lds + ((t + 1) & 1) * kTileBytes;
+                wait_loads<0>();
                 barrier();   // tile t is here, and all waves are done with tile t - 1
-                fetch(to);
+                sa.load(nxt);
+                sb.load(nxt + TA::kBytes);
                 read(cur, fa, fb);
                 multiply(fa, fb);
-                cur = next(cur);
-                to = next(to);
             }
         }
         wait_loads<0>();   // nothing may still write to LDS
     } else {
-        static_assert(kStages == 2, "two stages");
-        Frag fa[KS][FI], fb[KS][FJ];
+        Frag fa[kSteps][FI], fb[kSteps][FJ];
         typename TA::Packed ra[kAsyncA ? 1 : TA::kPasses];
         typename TB::Packed rb[kAsyncB ? 1 : TB::kPasses];
+        typename TA::Source sa(a, g.lda, i0, g.rows, c_begin, c_end);
+        typename TB::Source sb(b, g.ldb, j0, g.cols, c_begin, c_end);
         auto fetch = [&](char* to, int64_t c0) {
             if constexpr (kAsyncA)
-                TA::load_async(to, a, g.lda, g.a_rows, i0, g.rows, c0, c_end);
+                sa.load(to);
             else
                 TA::load_regs(ra, a, g.lda, i0, g.rows, c0, c_end);
             if constexpr (kAsyncB)
-                TB::load_async(to + TA::kBytes, b, g.ldb, g.b_rows, j0, g.cols, c0, c_end);
+                sb.load(to + TA::kBytes);
             else
                 TB::load_regs(rb, b, g.ldb, j0, g.cols, c0, c_end);
         };
@@ -399,6 +444,7 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(GemmArgs g)
         }
         for (int t = 0; t < steps; ++t) {
             char* nxt = lds + ((t + 1) & 1) * kTileBytes;
+            wait_loads<0>();
             __syncthreads();   // tile t has arrived, and the other is no longer read
             if (t + 1 < steps) fetch(nxt, c_begin + (int64_t)(t + 1) * kBK);
             read(lds + (t & 1) * kTileBytes, fa, fb);
@@ -407,117 +453,107 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(GemmArgs g)
         }
     }
 
-    // acc[p][q][r] is row i0 + wi + 16 p + li, column (TT) wj + 16 q + 4 lg + r or (NT) the interleaved one
-    if constexpr (TT) {
-        float* out = g.part ? g.part + (int64_t)part * g.rows * g.cols : nullptr;
+    // A lane's values of row i0 + wi + 16 p + li, in groups of 4 (TT) or 8 (NT) neighbouring columns: group k is
+    // acc[p][k], or acc[p][2 k] and acc[p][2 k + 1].
+    const int li = lane & 15, lg = lane >> 4;
+    constexpr int kGroup = TT ? 4 : 8, kGroups = FJ * 4 / kGroup;
+    auto column = [&](int k) { return TT ? 16 * k + 4 * lg : 32 * k + 8 * lg; };
+    auto value = [&](int p, int k, int e) -> float { return acc[p][(k * kGroup + e) / 4][e & 3]; };
+    const int64_t i1 = i0 + wi, j1 = j0 + wj;
+    if (TT || g.part) {
+        float* out = g.part ? g.part + (int64_t)part * g.rows * g.cols : (float*)g.out;
+        const int64_t ldo = g.part ? g.cols : g.ldo;
 #pragma unroll
         for (int p = 0; p < FI; ++p)
 #pragma unroll
-            for (int q = 0; q < FJ; ++q) {
-                const int64_t i = i0 + wi + 16 * p + li, j = j0 + wj + 16 * q + 4 * lg;
+            for (int k = 0; k < kGroups; ++k) {
+                const int64_t i = i1 + 16 * p + li, j = j1 + column(k);
                 if (i >= g.rows || j >= g.cols) continue;
-                float v[4] = {acc[p][q][0], acc[p][q][1], acc[p][q][2], acc[p][q][3]};
-                if (out || g.out_f32) {
-                    float* o = out ? out + i * g.cols + j : (float*)g.out + i * g.ldo + j;
-                    store_vec(o, g.cols - j, v);
+                if (g.part || g.out_f32) {
+                    float v[kGroup];
+#pragma unroll
+                    for (int e = 0; e < kGroup; ++e) v[e] = value(p, k, e);
+#pragma unroll
+                    for (int e = 0; e < kGroup; e += 4) store_vec(out + i * ldo + j + e, g.cols - j - e, v + e);
                 } else {
-                    T* o = (T*)g.out + i * g.ldo + j;
-                    if (sizeof(T) == 2 && j + 4 <= g.cols) {
-                        typedef T V4 __attribute__((ext_vector_type(4)));
-                        typedef V4 V4any __attribute__((aligned(sizeof(T))));
+                    T* o = (T*)g.out + i * ldo + j;
+                    typedef T V4 __attribute__((ext_vector_type(4)));
+                    typedef V4 V4any __attribute__((aligned(sizeof(T))));
+                    if (j + 4 <= g.cols) {
                         V4 t;
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) t[r] = (T)v[r];
+                        for (int e = 0; e < 4; ++e) t[e] = (T)value(p, k, e);
                         *reinterpret_cast<V4any*>(o) = t;
                     } else {
 #pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (j + r < g.cols) o[r] = (T)v[r];
+                        for (int e = 0; e < 4; ++e)
+                            if (j + e < g.cols) o[e] = (T)value(p, k, e);
                     }
                 }
             }
         return;
     }
-    const int64_t i1 = i0 + wi, j1 = j0 + wj;
-    if (g.part) {
-#pragma unroll
-        for (int q = 0; q < FJ; q += 2) {
-            const int64_t j = j1 + 16 * q + 8 * lg;
-#pragma unroll
-            for (int p = 0; p < FI; ++p) {
-                const int64_t i = i1 + 16 * p + li;
-                if (i >= g.rows || j >= g.cols) continue;
-                float* o = g.part + ((int64_t)part * g.rows + i) * g.cols + j;
-                float lo[4], hi[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    lo[e] = acc[p][q][e];
-                    hi[e] = acc[p][q + 1][e];
-                }
-                store_vec(o, g.cols - j, lo);
-                store_vec(o + 4, g.cols - j - 4, hi);
-            }
-        }
-        return;
-    }
     // A wave's results go through its own part of LDS, so that they are stored as whole rows of its block: z, then y.
-    constexpr int N = Vec<T>::N, kVecs = WC / N;
-    char* block = lds + wave * (WR * WC * (int)sizeof(T));
-    auto put = [&](int p, int q, const float* v) {
-        const int r = 16 * p + li;
+    if constexpr (!TT) {
+        constexpr int N = Vec<T>::N, kVecs = WC / N;
+        char* block = lds + wave * (WR * WC * (int)sizeof(T));
+        auto put = [&](int p, int k, const float* v) {
+            const int r = 16 * p + li;
 #pragma unroll
-        for (int e = 0; e < 8; e += N) {
-            typename Vec<T>::Packed t;
+            for (int e = 0; e < 8; e += N) {
+                typename Vec<T>::Packed t;
 #pragma unroll
-            for (int k = 0; k < N; ++k) t[k] = (T)v[e + k];
-            const int vec = (16 * q + 8 * lg + e) / N;
-            *reinterpret_cast<typename Vec<T>::Packed*>(block + r * (WC * (int)sizeof(T)) +
-                                                        (vec ^ (r & 7 & (kVecs - 1))) * 16) = t;
+                for (int u = 0; u < N; ++u) t[u] = (T)v[e + u];
+                const int vec = (column(k) + e) / N;
+                *reinterpret_cast<typename Vec<T>::Packed*>(block + r * (WC * (int)sizeof(T)) +
+                                                            (vec ^ (r & 7 & (kVecs - 1))) * 16) = t;
+            }
+        };
+        if (g.bias) {
+#pragma unroll
+            for (int k = 0; k < kGroups; ++k)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int64_t j = j1 + column(k) + e;
+                    const float bias = j < g.cols ? g.bias[j] : 0.f;
+#pragma unroll
+                    for (int p = 0; p < FI; ++p) acc[p][2 * k + e / 4][e & 3] += bias;
+                }
         }
-    };
-    barrier();   // all waves are done with the tiles
+        barrier();   // all waves are done with the tiles
+        if (g.z) {
 #pragma unroll
-    for (int q = 0; q < FJ; ++q) {
-        const int64_t j = j1 + 16 * (q & ~1) + 8 * lg + 4 * (q & 1);
+            for (int p = 0; p < FI; ++p)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float bias = g.bias && j + e < g.cols ? g.bias[j + e] : 0.f;
+                for (int k = 0; k < kGroups; ++k) {
+                    float v[8];
 #pragma unroll
-            for (int p = 0; p < FI; ++p) acc[p][q][e] += bias;
+                    for (int e = 0; e < 8; ++e) v[e] = value(p, k, e);
+                    put(p, k, v);
+                }
+            store_block<T, WR, WC>(block, (T*)g.z, g.ldz, i1, g.rows, j1, g.cols);
         }
-    }
-    if (g.z) {
 #pragma unroll
         for (int p = 0; p < FI; ++p)
 #pragma unroll
-            for (int q = 0; q < FJ; q += 2) {
+            for (int k = 0; k < kGroups; ++k) {
                 float v[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = acc[p][q + (e >> 2)][e & 3];
-                put(p, q, v);
+                for (int e = 0; e < 8; ++e) v[e] = value(p, k, e);
+                activate<8>(g.act, v);
+                const int64_t i = i1 + 16 * p + li, j = j1 + column(k);
+                if (g.residual && i < g.rows && j < g.cols) {
+                    const T* r = (const T*)g.residual + i * g.ldr + j;
+                    float t[8];
+#pragma unroll
+                    for (int e = 0; e < 8; e += N) load_vec(r + e, g.cols - j - e, t + e);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] += t[e];
+                }
+                put(p, k, v);
             }
-        store_block<T, WR, WC>(block, (T*)g.z, g.ldz, i1, g.rows, j1, g.cols);
+        store_block<T, WR, WC>(block, (T*)g.out, g.ldo, i1, g.rows, j1, g.cols);
     }
-#pragma unroll
-    for (int p = 0; p < FI; ++p)
-#pragma unroll
-        for (int q = 0; q < FJ; q += 2) {
-            float v[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = acc[p][q + (e >> 2)][e & 3];
-            activate<8>(g.act, v);
-            const int64_t i = i1 + 16 * p + li, j = j1 + 16 * q + 8 * lg;
-            if (g.residual && i < g.rows && j < g.cols) {
-                const T* r = (const T*)g.residual + i * g.ldr + j;
-                float t[8];
-#pragma unroll
-                for (int e = 0; e < 8; e += N) load_vec(r + e, g.cols - j - e, t + e);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] += t[e];
-            }
-            put(p, q, v);
-        }
-    store_block<T, WR, WC>(block, (T*)g.out, g.ldo, i1, g.rows, j1, g.cols);
 }
 
 // Few rows (NT, rows <= 16 MF): a workgroup takes 16 columns j and its waves share the sum; the weights go from
@@ -729,8 +765,8 @@ hipError_t run_gemm(const GemmArgs& g, hipStream_t s)
 template <typename T, bool TT, int BI, int BJ, int WI, int WJ>
 hipError_t run_any(bool fast, const GemmArgs& g, hipStream_t s)
 {
-    return fast ? run_gemm<T, Shape<TT, BI, BJ, WI, WJ, 2, 2, false, true>>(g, s)
-                : run_gemm<T, Shape<TT, BI, BJ, WI, WJ, 2, 2, false, false>>(g, s);
+    return fast ? run_gemm<T, Shape<TT, BI, BJ, WI, WJ, false, true>>(g, s)
+                : run_gemm<T, Shape<TT, BI, BJ, WI, WJ, false, false>>(g, s);
 }
 
 }  // namespace
@@ -739,7 +775,7 @@ template <typename T>
 hipError_t LinearOps<T>::gemm_nt(int tile, bool fast_a, const GemmArgs& g, hipStream_t s)
 {
     if (tile == kTile256) {   // fast_a, 16-bit
-        if constexpr (sizeof(T) == 2) return run_gemm<T, Shape<false, 256, 256, 2, 4, 2, 2, true, true>>(g, s);
+        if constexpr (sizeof(T) == 2) return run_gemm<T, Shape<false, 256, 256, 2, 4, true, true>>(g, s);
     }
     if (tile == kTile128) return run_any<T, false, 128, 128, 2, 2>(fast_a, g, s);
     if (tile == kTile128x64) return run_any<T, false, 128, 64, 4, 1>(fast_a, g, s);
@@ -750,7 +786,7 @@ template <typename T>
 hipError_t LinearOps<T>::gemm_tt(int tile, bool fast_b, const GemmArgs& g, hipStream_t s)
 {
     if (tile == kTile256) {   // fast_b, 16-bit
-        if constexpr (sizeof(T) == 2) return run_gemm<T, Shape<true, 256, 256, 2, 4, 2, 2, true, true>>(g, s);
+        if constexpr (sizeof(T) == 2) return run_gemm<T, Shape<true, 256, 256, 2, 4, true, true>>(g, s);
     }
     if (tile == kTile128) return run_any<T, true, 128, 128, 2, 2>(fast_b, g, s);
     return run_any<T, true, 64, 64, 2, 2>(fast_b, g, s);

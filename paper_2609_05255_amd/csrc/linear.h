@@ -17,7 +17,6 @@ struct GemmArgs {
     const void* b;
     int64_t lda, ldb;
     int64_t rows, cols, len;
-    int64_t a_rows, b_rows;        // stored rows of a and b (NT: rows, cols; TT: len)
     int64_t split_len;
     int32_t splits, planes;
     int64_t plane_stride;

@@ -161,8 +161,6 @@ hipError_t run_nt(int type, GemmArgs g, bool fast_a, float* part, hipStream_t s)
 {
     g.splits = g.planes = 1;
     g.split_len = g.len;
-    g.a_rows = g.rows;
-    g.b_rows = g.cols;
     if (g.rows <= kSkinnyRows) return LinearOps<T>::skinny(g, s);
     const Plan p = plan_nt(type, g.rows, g.cols, g.len, fast_a);
     g.splits = p.splits;
@@ -261,7 +259,7 @@ hipError_t linear_bwd(const gs_linear& p, const void* dy, int64_t lddy, const vo
         g.ldb = p.ldx;
         g.rows = p.n_out;
         g.cols = p.n_in;
-        g.len = g.a_rows = g.b_rows = p.rows;
+        g.len = p.rows;
         g.splits = plan.splits;
         g.split_len = plan.split_len;
         g.planes = planes;

@@ -249,3 +249,21 @@ def test_binding_refuses():
         gs.gs_linear_bwd(d["dy"], d["x"], d["w"], d["z"], None, torch.empty(16, 24, device="cuda"), None, ws[:256],
                          act="relu")
     assert e.value.status == gs.GS_ERR_CAPACITY
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("rows,n_in,n_out", [(4166, 520, 4104), (4100, 4104, 1032), (70, 4104, 4360), (300, 4096, 4608)])
+def test_largest_tiles(rows, n_in, n_out, dtype):
+    # products of enough tiles for the 256 x 256 ones: ends of rows, columns and sums inside a tile, an odd count of
+    # halves, sums shorter than the tiles on their way
+    d = make(rows, n_in, n_out, dtype, 17)
+    y, z = (torch.full_like(d["r"], float("nan")) for _ in range(2))
+    gs.gs_linear_fwd(d["x"], d["w"], d["bias"], y, space(d["x"], d["w"], "silu", None), act="silu", residual=d["r"], z=z)
+    check_forward(d, "silu", y, z)
+    for name, dw_type in (("tanh", dtype), ("gelu", torch.float32), ("none", torch.float32)):
+        dx = torch.full_like(d["x"], float("nan"))
+        dw = torch.full(d["w"].shape, float("nan"), dtype=dw_type, device="cuda")
+        db = torch.full((n_out,), float("nan"), device="cuda")
+        ws = space(d["x"], d["w"], name, dw_type)
+        gs.gs_linear_bwd(d["dy"], d["x"], d["w"], d["z"], dx, dw, db, ws, act=name)
+        check_backward(d, name, dx, dw, db)
