@@ -60,6 +60,25 @@ inline TileShape tile_shape(int tile)
     }
 }
 
+// A narrow layer's backward in one pass (narrow.h).
+struct NarrowArgs {
+    const void *dy, *z, *x, *w;
+    int64_t lddy, ldz, ldx, ldw, lddx, lddw;
+    int64_t rows;
+    int32_t out, in, act, dw_f32;
+    void* dx;                      // dx, dw, db: NULL where not wanted
+    void* dw;
+    float* db;
+    float* part;                   // [workgroups][narrow_part] dW [out][in], then db
+};
+__host__ __device__ inline int64_t narrow_part(int out, int in) { return (out * in + out + 3) / 4 * 4; }
+
+template <typename T>
+struct NarrowOps {   // T 16-bit
+    // fast: rows of dy, z and x are 16-byte aligned and whole 16-byte vectors
+    static hipError_t backward(const NarrowArgs& a, bool fast, int planes, int blocks, hipStream_t s);
+};
+
 // per type T (the files linear_*.hip)
 template <typename T>
 struct LinearOps {

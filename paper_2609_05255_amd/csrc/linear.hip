@@ -20,6 +20,9 @@ constexpr int kSlopeBlocks = 2048;
 constexpr int64_t kJoinSplitLen = 256;   // values of the sum in a split of a product of few tiles, at least
 constexpr int64_t kRowSplitLen = 512;    // rows in a split of dW's sum, at least
 
+constexpr int kNarrowMost = 128;         // inputs and outputs of a layer whose backward is one pass
+constexpr int kNarrowBlocks = 512;       // two workgroups per compute unit
+
 int elem(int type) { return type == GS_F32 ? 4 : 2; }
 int64_t vec(int type) { return 16 / elem(type); }
 int64_t padded(int type, int64_t n) { return div_up(n, vec(type)) * vec(type); }
@@ -124,6 +127,11 @@ FwdSpace fwd_space(void* base, int type, int64_t rows, int64_t in, int64_t out, 
     return f;
 }
 
+// A backward in one pass over the rows (narrow.h).
+bool narrow(int type, int64_t in, int64_t out) { return type != GS_F32 && in <= kNarrowMost && out <= kNarrowMost; }
+
+int narrow_blocks(int64_t rows) { return (int)std::max<int64_t>(1, std::min<int64_t>(div_up(rows, 64), kNarrowBlocks)); }
+
 struct BwdSpace {
     void* dz;
     void* wt;      // W transposed, [in][padded out]
@@ -136,6 +144,11 @@ BwdSpace bwd_space(void* base, int type, int act, int64_t rows, int64_t in, int6
 {
     Regions r{(char*)base};
     BwdSpace b = {};
+    if (narrow(type, in, out)) {
+        b.part = (float*)r.take(narrow_blocks(rows) * narrow_part((int)out, (int)in) * 4);
+        b.bytes = r.at;
+        return b;
+    }
     const int planes = planes_of(type, act, dw_type);
     if (need_dz) b.dz = r.take(planes * rows * padded(type, out) * elem(type));
     b.wt = r.take(in * padded(type, out) * elem(type));
@@ -209,6 +222,14 @@ hipError_t linear_bwd(const gs_linear& p, const void* dy, int64_t lddy, const vo
     const bool need_dz = p.act != GS_ACT_NONE || !fast(dy, lddy, p.n_out, p.type);
     const BwdSpace b = bwd_space(ws, p.type, p.act, p.rows, p.n_in, p.n_out, dw_type, need_dz);
     const int planes = dw ? planes_of(p.type, p.act, dw_type) : 1;
+    if constexpr (sizeof(T) == 2)
+        if (narrow(p.type, p.n_in, p.n_out)) {
+            const NarrowArgs a = {dy,   z,     p.x,  p.w,  lddy, ldz, p.ldx, p.ldw, lddx, lddw, p.rows, (int)p.n_out,
+                                  (int)p.n_in, p.act, dw_type == GS_F32, dx, dw,   db,    b.part};
+            const bool whole = fast(dy, lddy, p.n_out, p.type) && fast(p.x, p.ldx, p.n_in, p.type) &&
+                               (p.act == GS_ACT_NONE || fast(z, ldz, p.n_out, p.type));
+            return NarrowOps<T>::backward(a, whole, planes, narrow_blocks(p.rows), s);
+        }
     const int64_t ldo = need_dz ? padded(p.type, p.n_out) : lddy;
     const void* dz = need_dz ? b.dz : dy;
     hipError_t e = hipSuccess;

@@ -1,6 +1,7 @@
 // The linear operators' kernels for bf16 elements.
-#include "gemm.h"
+#include "narrow.h"
 
 namespace gsr {
 template struct LinearOps<bf16>;
+template struct NarrowOps<bf16>;
 }

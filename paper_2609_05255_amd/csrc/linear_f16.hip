@@ -1,6 +1,7 @@
 // The linear operators' kernels for f16 elements.
-#include "gemm.h"
+#include "narrow.h"
 
 namespace gsr {
 template struct LinearOps<f16>;
+template struct NarrowOps<f16>;
 }

@@ -267,3 +267,18 @@ def test_largest_tiles(rows, n_in, n_out, dtype):
         ws = space(d["x"], d["w"], name, dw_type)
         gs.gs_linear_bwd(d["dy"], d["x"], d["w"], d["z"], dx, dw, db, ws, act=name)
         check_backward(d, name, dx, dw, db)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("rows", [1, 63, 64, 65, 40_000])
+@pytest.mark.parametrize("n_in,n_out", [(64, 64), (65, 64), (64, 65), (128, 128), (129, 128), (128, 129), (17, 3), (3, 128)])
+def test_backward_on_both_sides_of_the_narrow_form(rows, n_in, n_out, dtype):
+    # one pass up to 128 inputs and outputs, separate products beyond; whole and part tiles of rows, fewer tiles than
+    # workgroups and more
+    d = make(rows, n_in, n_out, dtype, rows + n_in)
+    for name, dw_type in (("relu", torch.float32), ("silu", torch.float32), ("sigmoid", dtype)):
+        dx = torch.full_like(d["x"], float("nan"))
+        dw = torch.full(d["w"].shape, float("nan"), dtype=dw_type, device="cuda")
+        db = torch.full((n_out,), float("nan"), device="cuda")
+        gs.gs_linear_bwd(d["dy"], d["x"], d["w"], d["z"], dx, dw, db, space(d["x"], d["w"], name, dw_type), act=name)
+        check_backward(d, name, dx, dw, db)
