@@ -22,6 +22,8 @@
 // columns of one row and the epilogue moves whole 16-byte vectors.
 #pragma once
 
+#include <type_traits>
+
 #include "activation.h"
 #include "linear.h"
 
@@ -181,27 +183,27 @@ struct Tile {
         }
     };
 
-    // registers <- memory at any alignment, masked value by value at the ends
+    // registers <- memory at any alignment. Rows beyond the matrix read as its last one (NT: their results are never
+    // stored) or, along the sum, as zeros (TT).
     typedef typename Vec<T>::Packed Packed;
     static __device__ __forceinline__ void load_regs(Packed (&r)[kPasses], const T* p, int64_t ld, int64_t x0,
                                                      int64_t x_end, int64_t c0, int64_t c_end)
     {
         const int64_t r0 = TT ? c0 : x0, rows_end = TT ? c_end : x_end;
         const int64_t v0 = TT ? x0 : c0, v_end = TT ? x_end : c_end;
+        const bool whole = v0 + (TT ? X : kBK) <= v_end;   // no vector of the tile ends beyond the matrix
 #pragma unroll
         for (int k = 0; k < kPasses; ++k) {
             const int q = k * THREADS + threadIdx.x;
             const int64_t rr = r0 + row(q), v = v0 + (int64_t)vec(q) * kVec;
+            const T* src = p + (rr < rows_end ? rr : rows_end - 1) * ld + v;
             Packed t = {};
-            if (rr < rows_end) {
-                const T* src = p + rr * ld + v;
-                if (v + kVec <= v_end)
-                    t = *reinterpret_cast<const typename Vec<T>::Any*>(src);
-                else
-#pragma unroll
-                    for (int j = 0; j < kVec; ++j)
-                        if (v + j < v_end) t[j] = src[j];
+            if (whole) {
+                if (!TT || r0 < rows_end) t = *reinterpret_cast<const typename Vec<T>::Any*>(src);
+            } else if (r0 < rows_end) {
+                t = load_any(src, v_end - v);
             }
+            if (TT && rr >= rows_end) t = Packed{};
             r[k] = t;
         }
     }
@@ -255,13 +257,13 @@ __device__ __forceinline__ void tile_of(int64_t b, int64_t tiles_i, int64_t tile
     *tj = in / h;
 }
 
-// BI, BJ: the workgroup's tile; WI, WJ: its waves; AHEAD: fragments are read half a tile ahead of their MFMAs. FAST: the
+// BI, BJ: the workgroup's tile; WI, WJ: its waves; STAGES: tiles in the ring; AHEAD: fragments are read half a tile ahead of their MFMAs. FAST: the
 // operand that may be the caller's (A in NT, B in TT) is loaded asynchronously as well, as the other always is;
 // otherwise it goes through registers, at any alignment.
-template <bool TT_, int BI_, int BJ_, int WI_, int WJ_, bool AHEAD_, bool FAST_>
+template <bool TT_, int BI_, int BJ_, int WI_, int WJ_, int STAGES_, bool AHEAD_, bool FAST_>
 struct Shape {
     static constexpr bool TT = TT_, AHEAD = AHEAD_, FAST = FAST_;
-    static constexpr int BI = BI_, BJ = BJ_, WI = WI_, WJ = WJ_;
+    static constexpr int BI = BI_, BJ = BJ_, WI = WI_, WJ = WJ_, STAGES = STAGES_;
     static constexpr int THREADS = WI * WJ * 64;
 };
 
@@ -295,7 +297,7 @@ template <typename T, class S>
 __global__ __launch_bounds__(S::THREADS) void k_gemm(GemmArgs g)
 {
     constexpr bool TT = S::TT;
-    constexpr int BI = S::BI, BJ = S::BJ, WI = S::WI, WJ = S::WJ;
+    constexpr int BI = S::BI, BJ = S::BJ, WI = S::WI, WJ = S::WJ, kStages = S::STAGES;
     constexpr int WR = BI / WI, WC = BJ / WJ, FI = WR / 16, FJ = WC / 16;
     using Mm = Mma<T>;
     using TA = Tile<T, BI, TT, false, S::THREADS>;
@@ -304,8 +306,8 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(GemmArgs g)
     constexpr int kTileBytes = TA::kBytes + TB::kBytes;
     constexpr bool kAsyncA = S::FAST || TT, kAsyncB = S::FAST || !TT;
     static_assert(TT || FJ % 2 == 0, "columns interleave between pairs of fragments");
-    static_assert(TT || WI * WJ * WR * WC * (int)sizeof(T) <= 2 * kTileBytes, "the results pass through LDS");
-    __shared__ __attribute__((aligned(1024))) char lds[2 * kTileBytes + (S::AHEAD ? TA::kBytes : 0)];
+    static_assert(TT || WI * WJ * WR * WC * (int)sizeof(T) <= kStages * kTileBytes, "the results pass through LDS");
+    __shared__ __attribute__((aligned(1024))) char lds[kStages * kTileBytes + (S::AHEAD ? TA::kBytes : 0)];
 
     const int64_t tiles_i = (g.rows + BI - 1) / BI, tiles_j = (g.cols + BJ - 1) / BJ;
     int64_t ti, tj;
@@ -350,7 +352,7 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(GemmArgs g)
             // where tile t's own fragments have all been read. Behind each row of MFMAs stand a few reads and loads:
             // issued together they would hold the wave, and the MFMAs behind them, until the memory pipe takes them.
             constexpr int kHalf = kSteps / 2, kRows = kHalf * FI;   // rows of MFMAs in a half
-            static_assert(kRows == 2 * TA::kPasses && kRows == 2 * TB::kPasses &&
+            static_assert(kStages == 2 && kRows == 2 * TA::kPasses && kRows == 2 * TB::kPasses &&
                               kHalf * (FI + FJ) <= 2 * (kRows - 1), "the loads and reads of a half fit its rows");
             char* a_lds[3] = {lds, lds + TA::kBytes, lds + 2 * TA::kBytes};
             char* b_lds[2] = {lds + 3 * TA::kBytes, lds + 3 * TA::kBytes + TB::kBytes};
@@ -404,53 +406,64 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(GemmArgs g)
             }
         } else {
             Frag fa[kSteps][FI], fb[kSteps][FJ];
-            sa.load(lds);
-            sb.load(lds + TA::kBytes);
+            char* cur = lds;
+            char* to = lds;
+            for (int k = 0; k < kStages - 1; ++k, to += kTileBytes) {
+                sa.load(to);
+                sb.load(to + TA::kBytes);
+            }
             for (int t = 0; t < steps; ++t) {
-                char* cur = lds + (t & 1) * kTileBytes;
-                char* nxt = lds + ((t + 1) & 1) * kTileBytes;
-                wait_loads<0>();
+                wait_loads<(kStages - 2) * kLoads>();
                 barrier();   // tile t is here, and all waves are done with tile t - 1
-                sa.load(nxt);
-                sb.load(nxt + TA::kBytes);
+                sa.load(to);
+                sb.load(to + TA::kBytes);
                 read(cur, fa, fb);
                 multiply(fa, fb);
+                cur = cur + kTileBytes == lds + kStages * kTileBytes ? lds : cur + kTileBytes;
+                to = to + kTileBytes == lds + kStages * kTileBytes ? lds : to + kTileBytes;
             }
         }
         wait_loads<0>();   // nothing may still write to LDS
     } else {
+        // One operand through registers, kStages - 1 tiles ahead as the other in LDS. (The compiler's own waits for the
+        // registers count its loads alone, and so wait for some of the others too.)
+        constexpr int D = kStages - 1;
+        constexpr int kLoads = kAsyncA ? TA::kPasses : TB::kPasses;   // of a thread per tile, the asynchronous ones
+        using TR = std::conditional_t<kAsyncA, TB, TA>;               // the operand in registers
         Frag fa[kSteps][FI], fb[kSteps][FJ];
-        typename TA::Packed ra[kAsyncA ? 1 : TA::kPasses];
-        typename TB::Packed rb[kAsyncB ? 1 : TB::kPasses];
+        typename TR::Packed regs[D][TR::kPasses];
         typename TA::Source sa(a, g.lda, i0, g.rows, c_begin, c_end);
         typename TB::Source sb(b, g.ldb, j0, g.cols, c_begin, c_end);
-        auto fetch = [&](char* to, int64_t c0) {
-            if constexpr (kAsyncA)
+        int64_t c0 = c_begin;
+        auto fetch = [&](char* to, typename TR::Packed(&r)[TR::kPasses]) {
+            if constexpr (kAsyncA) {
                 sa.load(to);
-            else
-                TA::load_regs(ra, a, g.lda, i0, g.rows, c0, c_end);
-            if constexpr (kAsyncB)
+                TB::load_regs(r, b, g.ldb, j0, g.cols, c0 < c_end ? c0 : c_end, c_end);
+            } else {
+                TA::load_regs(r, a, g.lda, i0, g.rows, c0 < c_end ? c0 : c_end, c_end);
                 sb.load(to + TA::kBytes);
-            else
-                TB::load_regs(rb, b, g.ldb, j0, g.cols, c0, c_end);
+            }
+            c0 += kBK;
         };
-        auto settle = [&](char* to) {
-            if constexpr (!kAsyncA) TA::store_regs(to, ra);
-            if constexpr (!kAsyncB) TB::store_regs(to + TA::kBytes, rb);
-        };
+        auto stage = [&](int t) { return lds + (t % kStages) * kTileBytes; };
         if (steps > 0) {
-            fetch(lds, c_begin);
-            settle(lds);
+#pragma unroll
+            for (int k = 0; k < D; ++k) fetch(stage(k), regs[k]);
         }
-        for (int t = 0; t < steps; ++t) {
-            char* nxt = lds + ((t + 1) & 1) * kTileBytes;
-            wait_loads<0>();
-            __syncthreads();   // tile t has arrived, and the other is no longer read
-            if (t + 1 < steps) fetch(nxt, c_begin + (int64_t)(t + 1) * kBK);
-            read(lds + (t & 1) * kTileBytes, fa, fb);
-            multiply(fa, fb);
-            if (t + 1 < steps) settle(nxt);
+        for (int t0 = 0; t0 < steps; t0 += D) {
+#pragma unroll
+            for (int k = 0; k < D; ++k) {
+                const int t = t0 + k;
+                if (t >= steps) break;
+                TR::store_regs(stage(t) + (kAsyncA ? TA::kBytes : 0), regs[k]);
+                wait_loads<(D - 1) * (kLoads + TR::kPasses)>();
+                __syncthreads();   // tile t is here, and all waves are done with tile t - 1
+                fetch(stage(t + D), regs[k]);
+                read(stage(t), fa, fb);
+                multiply(fa, fb);
+            }
         }
+        wait_loads<0>();
     }
 
     // A lane's values of row i0 + wi + 16 p + li, in groups of 4 (TT) or 8 (NT) neighbouring columns: group k is
@@ -566,35 +579,46 @@ __global__ __launch_bounds__(kSkinnyWaves * 64) void k_skinny(GemmArgs g)
 {
     constexpr int N = Vec<T>::N;
     constexpr int kStep = 4 * N;                     // values of the sum per MFMA step
-    constexpr int kUnroll = 4;
+    constexpr int kUnroll = MF == 1 ? 8 : 4;         // steps whose loads are under way together
     __shared__ float sums[kSkinnyWaves][MF][16][17];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, lg = lane >> 4, li = lane & 15;
     const int64_t j0 = (int64_t)blockIdx.x * 16, i0 = (int64_t)blockIdx.y * (16 * MF);
-    const T* w = (const T*)g.b + (j0 + li < g.cols ? j0 + li : g.cols - 1) * g.ldb;
+    const T* w = (const T*)g.b + (j0 + li < g.cols ? j0 + li : g.cols - 1) * g.ldb + lg * N;
     const T* x[MF];
+    bool in[MF];   // (lanes of rows that do not exist load nothing)
 #pragma unroll
     for (int m = 0; m < MF; ++m) {
         const int64_t i = i0 + 16 * m + li;
-        x[m] = (const T*)g.a + (i < g.rows ? i : g.rows - 1) * g.lda;
+        in[m] = i < g.rows;
+        x[m] = (const T*)g.a + (in[m] ? i : 0) * g.lda + lg * N;
     }
     f32x4 acc[MF] = {};
     const int64_t steps = (g.len + kStep - 1) / kStep;
     const int64_t per = (steps + kSkinnyWaves - 1) / kSkinnyWaves;
     const int64_t s0 = wave * per, s1 = s0 + per < steps ? s0 + per : steps;
-    for (int64_t s = s0; s < s1; s += kUnroll) {
-        typename Vec<T>::Packed wv[kUnroll], xv[kUnroll][MF];
+    typedef typename Vec<T>::Packed Packed;
+    typedef typename Vec<T>::Any Any;
+    int64_t s = s0;
+    for (; s + kUnroll <= s1 && (s + kUnroll) * kStep <= g.len; s += kUnroll) {
+        Packed wv[kUnroll], xv[MF][kUnroll] = {};
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int64_t c = (s + u) * kStep + lg * N;
-            const int64_t left = s + u < s1 ? g.len - c : 0;
-            wv[u] = load_any(w + c, left);
+        for (int u = 0; u < kUnroll; ++u) wv[u] = *reinterpret_cast<const Any*>(w + (s + u) * kStep);
 #pragma unroll
-            for (int m = 0; m < MF; ++m) xv[u][m] = load_any(x[m] + c, left);
-        }
+        for (int m = 0; m < MF; ++m)
+            if (in[m])
+#pragma unroll
+                for (int u = 0; u < kUnroll; ++u) xv[m][u] = *reinterpret_cast<const Any*>(x[m] + (s + u) * kStep);
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u)
 #pragma unroll
-            for (int m = 0; m < MF; ++m) acc[m] = Mma<T>::mma(wv[u], xv[u][m], acc[m]);
+            for (int m = 0; m < MF; ++m) acc[m] = Mma<T>::mma(wv[u], xv[m][u], acc[m]);
+    }
+    for (; s < s1; ++s) {
+        const int64_t left = g.len - s * kStep - lg * N;
+        const Packed wv = load_any(w + s * kStep, left);
+#pragma unroll
+        for (int m = 0; m < MF; ++m)
+            acc[m] = Mma<T>::mma(wv, load_any(x[m] + s * kStep, in[m] ? left : 0), acc[m]);
     }
 #pragma unroll
     for (int m = 0; m < MF; ++m)
@@ -762,11 +786,11 @@ hipError_t run_gemm(const GemmArgs& g, hipStream_t s)
     return hipGetLastError();
 }
 
-template <typename T, bool TT, int BI, int BJ, int WI, int WJ>
+template <typename T, bool TT, int BI, int BJ, int WI, int WJ, int STAGES>
 hipError_t run_any(bool fast, const GemmArgs& g, hipStream_t s)
 {
-    return fast ? run_gemm<T, Shape<TT, BI, BJ, WI, WJ, false, true>>(g, s)
-                : run_gemm<T, Shape<TT, BI, BJ, WI, WJ, false, false>>(g, s);
+    return fast ? run_gemm<T, Shape<TT, BI, BJ, WI, WJ, STAGES, false, true>>(g, s)
+                : run_gemm<T, Shape<TT, BI, BJ, WI, WJ, STAGES, false, false>>(g, s);
 }
 
 }  // namespace
@@ -775,21 +799,21 @@ template <typename T>
 hipError_t LinearOps<T>::gemm_nt(int tile, bool fast_a, const GemmArgs& g, hipStream_t s)
 {
     if (tile == kTile256) {   // fast_a, 16-bit
-        if constexpr (sizeof(T) == 2) return run_gemm<T, Shape<false, 256, 256, 2, 4, true, true>>(g, s);
+        if constexpr (sizeof(T) == 2) return run_gemm<T, Shape<false, 256, 256, 2, 4, 2, true, true>>(g, s);
     }
-    if (tile == kTile128) return run_any<T, false, 128, 128, 2, 2>(fast_a, g, s);
-    if (tile == kTile128x64) return run_any<T, false, 128, 64, 4, 1>(fast_a, g, s);
-    return run_any<T, false, 64, 64, 2, 2>(fast_a, g, s);
+    if (tile == kTile128) return run_any<T, false, 128, 128, 2, 2, 2>(fast_a, g, s);
+    if (tile == kTile128x64) return run_any<T, false, 128, 64, 4, 1, 2>(fast_a, g, s);
+    return run_any<T, false, 64, 64, 2, 2, 4>(fast_a, g, s);
 }
 
 template <typename T>
 hipError_t LinearOps<T>::gemm_tt(int tile, bool fast_b, const GemmArgs& g, hipStream_t s)
 {
     if (tile == kTile256) {   // fast_b, 16-bit
-        if constexpr (sizeof(T) == 2) return run_gemm<T, Shape<true, 256, 256, 2, 4, true, true>>(g, s);
+        if constexpr (sizeof(T) == 2) return run_gemm<T, Shape<true, 256, 256, 2, 4, 2, true, true>>(g, s);
     }
-    if (tile == kTile128) return run_any<T, true, 128, 128, 2, 2>(fast_b, g, s);
-    return run_any<T, true, 64, 64, 2, 2>(fast_b, g, s);
+    if (tile == kTile128) return run_any<T, true, 128, 128, 2, 2, 2>(fast_b, g, s);
+    return run_any<T, true, 64, 64, 2, 2, 4>(fast_b, g, s);
 }
 
 template <typename T>

@@ -168,8 +168,14 @@ def _ptr(t):
     return C.c_void_p(t.data_ptr())
 
 
+# The current stream's handle without an object around it, where this torch has the call (0.1 us instead of 2.7)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream):
     if stream is None:
+        if _raw_stream is not None:
+            return C.c_void_p(_raw_stream(torch.cuda.current_device()))
         return C.c_void_p(torch.cuda.current_stream().cuda_stream)
     if isinstance(stream, torch.cuda.Stream):
         return C.c_void_p(stream.cuda_stream)

@@ -20,6 +20,11 @@ Learning rates per parameter channel (the row of the planar layout):
 The latents and the decoder weights have fp32 master copies here; each step
 writes their binary16 copies into the scene buffers the passes read, as the
 paper does for its decoder weights.
+
+With max_grad_norm, a step first takes the global norm of all the gradients and
+multiplies each by min(1, max_grad_norm / (norm + 1e-6)) as the update reads it
+(gs_grad_norm, then gs_adam_step_scaled): nothing is read back, and the
+gradients keep their values.
 """
 from __future__ import annotations
 
@@ -48,7 +53,7 @@ def camera_spacing(campos) -> float:
 
 class FusedAdam:
     def __init__(self, scene: gs.SceneTensors, frame: gs.Frame, kind: int, betas=(0.9, 0.999), eps: float = 1e-15,
-                 camera_dbar: float = LOBE_SPACING_REF):
+                 camera_dbar: float = LOBE_SPACING_REF, max_grad_norm: float | None = None):
         self.beta1, self.beta2, self.eps, self.t = betas[0], betas[1], eps, 0
         self.kind = kind
         self.groups = []
@@ -86,9 +91,20 @@ class FusedAdam:
             add(self.latent32, frame.dlatent, [LR_LATENT] * LATENT_DIM, half=scene.latent)
             add(self.mlp32, frame.dmlp_w, [LR_MLP], beta2=BETA2_MLP, half=scene.mlp_w)
 
+        self.max_grad_norm, self.clip = max_grad_norm, None
+        if max_grad_norm is not None:
+            self.grad_set = gs.GradSet([g["grad"] for g in self.groups])
+            self.clip = torch.zeros(2, device=scene.means.device)   # the last step's norm and coefficient
+            self.clip_ws = torch.empty(gs.gs_grad_workspace_size(self.grad_set), dtype=torch.uint8,
+                                       device=scene.means.device)
+
     def step(self, stream=None):
         self.t += 1
-        gs.gs_adam_step(self.groups, self.beta1, self.eps, self.t, stream)
+        if self.clip is None:
+            gs.gs_adam_step(self.groups, self.beta1, self.eps, self.t, stream)
+            return
+        gs.gs_grad_norm(self.grad_set, self.max_grad_norm, self.clip, self.clip_ws, stream)
+        gs.gs_adam_step(self.groups, self.beta1, self.eps, self.t, stream, grad_scale=self.clip[1:])
 
     def backward_step(self, frame: gs.Frame, cam: gs.Camera, scene: gs.SceneTensors, dL_dimage, sh_degree: int = 3,
                       grads: gs.Grads | None = None, stream=None):
@@ -97,6 +113,8 @@ class FusedAdam:
         without writing the gradients (pass `grads` to have them written as well)."""
         if self.kind != gs.GS_APP_SH3:
             raise ValueError("the step inside the backward is built for the SH3 appearance")
+        if self.clip is not None:
+            raise ValueError("clipping needs the gradients' norm before the step: backward, then step()")
         self.t += 1
         g = grads if grads is not None else gs.Grads()
         gs.gs_render_bwd_adam(cam, scene.gaussians(), scene.appearance(self.kind, sh_degree), frame.pre,
