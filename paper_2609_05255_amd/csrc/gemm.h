@@ -2,14 +2,16 @@
 // template for binary16, bfloat16 (16x16x32 MFMA) and fp32 (16x16x4 MFMA).
 //
 // A workgroup computes a BI x BJ tile of C with WI x WJ waves. The operands'
-// tiles (64 bytes along the sum: 32 16-bit or 16 fp32 values) go from memory to
-// LDS with buffer loads that write LDS directly, through a ring of STAGES tiles:
-// STAGES - 1 of them are on their way while one is worked on, and a wait for the
-// oldest alone (vmcnt) replaces a wait for all. Every step issues its loads, past
-// the end too (the descriptor's range check turns those, like rows beyond the
-// matrix, into zeros without reading), so that the counts stay the same.
-// With AHEAD, a wave's fragments of the next tile are read under the MFMAs of
-// this one.
+// tiles (128 bytes along the sum: 64 16-bit or 32 fp32 values) go from memory to
+// LDS with buffer loads that write LDS directly, the next tile's under the current
+// one's MFMAs. Every step issues its loads, past the end too: the descriptor's
+// range check turns those, like rows beyond the matrix, into zeros without
+// reading. The 256 x 256 tile, whose workgroup is alone on its compute unit, also
+// reads its fragments ahead and spreads its loads between the MFMAs (AHEAD); two
+// workgroups of the 128 x 128 tile and five of the 64 x 64 one overlap each other.
+// Measured at 8,192 x 4,096 x 4,096 in bfloat16: 1,110, 870 and 580 TFLOP/s (NT),
+// 1,060, 780 and 590 (TT); the MFMAs of the largest tile alone reach 1,480 under
+// the power limit.
 //
 // LDS slots are 16 bytes. Reading a fragment takes one slot from each of 16
 // rows (NT), or four 4-value pieces of rows through the transposing LDS read
@@ -257,13 +259,13 @@ __device__ __forceinline__ void tile_of(int64_t b, int64_t tiles_i, int64_t tile
     *tj = in / h;
 }
 
-// BI, BJ: the workgroup's tile; WI, WJ: its waves; STAGES: tiles in the ring; AHEAD: fragments are read half a tile ahead of their MFMAs. FAST: the
+// BI, BJ: the workgroup's tile; WI, WJ: its waves; AHEAD: fragments are read half a tile ahead of their MFMAs. FAST: the
 // operand that may be the caller's (A in NT, B in TT) is loaded asynchronously as well, as the other always is;
 // otherwise it goes through registers, at any alignment.
-template <bool TT_, int BI_, int BJ_, int WI_, int WJ_, int STAGES_, bool AHEAD_, bool FAST_>
+template <bool TT_, int BI_, int BJ_, int WI_, int WJ_, bool AHEAD_, bool FAST_>
 struct Shape {
     static constexpr bool TT = TT_, AHEAD = AHEAD_, FAST = FAST_;
-    static constexpr int BI = BI_, BJ = BJ_, WI = WI_, WJ = WJ_, STAGES = STAGES_;
+    static constexpr int BI = BI_, BJ = BJ_, WI = WI_, WJ = WJ_;
     static constexpr int THREADS = WI * WJ * 64;
 };
 
@@ -297,7 +299,7 @@ template <typename T, class S>
 __global__ __launch_bounds__(S::THREADS) void k_gemm(GemmArgs g)
 {
     constexpr bool TT = S::TT;
-    constexpr int BI = S::BI, BJ = S::BJ, WI = S::WI, WJ = S::WJ, kStages = S::STAGES;
+    constexpr int BI = S::BI, BJ = S::BJ, WI = S::WI, WJ = S::WJ;
     constexpr int WR = BI / WI, WC = BJ / WJ, FI = WR / 16, FJ = WC / 16;
     using Mm = Mma<T>;
     using TA = Tile<T, BI, TT, false, S::THREADS>;
@@ -306,8 +308,8 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(GemmArgs g)
     constexpr int kTileBytes = TA::kBytes + TB::kBytes;
     constexpr bool kAsyncA = S::FAST || TT, kAsyncB = S::FAST || !TT;
     static_assert(TT || FJ % 2 == 0, "columns interleave between pairs of fragments");
-    static_assert(TT || WI * WJ * WR * WC * (int)sizeof(T) <= kStages * kTileBytes, "the results pass through LDS");
-    __shared__ __attribute__((aligned(1024))) char lds[kStages * kTileBytes + (S::AHEAD ? TA::kBytes : 0)];
+    static_assert(TT || WI * WJ * WR * WC * (int)sizeof(T) <= 2 * kTileBytes, "the results pass through LDS");
+    __shared__ __attribute__((aligned(1024))) char lds[2 * kTileBytes + (S::AHEAD ? TA::kBytes : 0)];
 
     const int64_t tiles_i = (g.rows + BI - 1) / BI, tiles_j = (g.cols + BJ - 1) / BJ;
     int64_t ti, tj;
@@ -352,7 +354,7 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(GemmArgs g)
             // where tile t's own fragments have all been read. Behind each row of MFMAs stand a few reads and loads:
             // issued together they would hold the wave, and the MFMAs behind them, until the memory pipe takes them.
             constexpr int kHalf = kSteps / 2, kRows = kHalf * FI;   // rows of MFMAs in a half
-            static_assert(kStages == 2 && kRows == 2 * TA::kPasses && kRows == 2 * TB::kPasses &&
+            static_assert(kRows == 2 * TA::kPasses && kRows == 2 * TB::kPasses &&
                               kHalf * (FI + FJ) <= 2 * (kRows - 1), "the loads and reads of a half fit its rows");
             char* a_lds[3] = {lds, lds + TA::kBytes, lds + 2 * TA::kBytes};
             char* b_lds[2] = {lds + 3 * TA::kBytes, lds + 3 * TA::kBytes + TB::kBytes};
@@ -406,64 +408,49 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(GemmArgs g)
             }
         } else {
             Frag fa[kSteps][FI], fb[kSteps][FJ];
-            char* cur = lds;
-            char* to = lds;
-            for (int k = 0; k < kStages - 1; ++k, to += kTileBytes) {
-                sa.load(to);
-                sb.load(to + TA::kBytes);
-            }
+            sa.load(lds);
+            sb.load(lds + TA::kBytes);
             for (int t = 0; t < steps; ++t) {
-                wait_loads<(kStages - 2) * kLoads>();
+                char* cur = lds + (t & 1) * kTileBytes;
+                char* nxt = lds + ((t + 1) & 1) * kTileBytes;
+                wait_loads<0>();
                 barrier();   // tile t is here, and all waves are done with tile t - 1
-                sa.load(to);
-                sb.load(to + TA::kBytes);
+                sa.load(nxt);
+                sb.load(nxt + TA::kBytes);
                 read(cur, fa, fb);
                 multiply(fa, fb);
-                cur = cur + kTileBytes == lds + kStages * kTileBytes ? lds : cur + kTileBytes;
-                to = to + kTileBytes == lds + kStages * kTileBytes ? lds : to + kTileBytes;
             }
         }
         wait_loads<0>();   // nothing may still write to LDS
     } else {
-        // One operand through registers, kStages - 1 tiles ahead as the other in LDS. (The compiler's own waits for the
-        // registers count its loads alone, and so wait for some of the others too.)
-        constexpr int D = kStages - 1;
-        constexpr int kLoads = kAsyncA ? TA::kPasses : TB::kPasses;   // of a thread per tile, the asynchronous ones
-        using TR = std::conditional_t<kAsyncA, TB, TA>;               // the operand in registers
+        using TR = std::conditional_t<kAsyncA, TB, TA>;   // the operand that goes through registers
         Frag fa[kSteps][FI], fb[kSteps][FJ];
-        typename TR::Packed regs[D][TR::kPasses];
+        typename TR::Packed regs[TR::kPasses];
         typename TA::Source sa(a, g.lda, i0, g.rows, c_begin, c_end);
         typename TB::Source sb(b, g.ldb, j0, g.cols, c_begin, c_end);
-        int64_t c0 = c_begin;
-        auto fetch = [&](char* to, typename TR::Packed(&r)[TR::kPasses]) {
+        auto fetch = [&](char* to, int64_t c0) {
             if constexpr (kAsyncA) {
                 sa.load(to);
-                TB::load_regs(r, b, g.ldb, j0, g.cols, c0 < c_end ? c0 : c_end, c_end);
+                TB::load_regs(regs, b, g.ldb, j0, g.cols, c0, c_end);
             } else {
-                TA::load_regs(r, a, g.lda, i0, g.rows, c0 < c_end ? c0 : c_end, c_end);
+                TA::load_regs(regs, a, g.lda, i0, g.rows, c0, c_end);
                 sb.load(to + TA::kBytes);
             }
-            c0 += kBK;
         };
-        auto stage = [&](int t) { return lds + (t % kStages) * kTileBytes; };
+        auto settle = [&](char* to) { TR::store_regs(to + (kAsyncA ? TA::kBytes : 0), regs); };
         if (steps > 0) {
-#pragma unroll
-            for (int k = 0; k < D; ++k) fetch(stage(k), regs[k]);
+            fetch(lds, c_begin);
+            settle(lds);
         }
-        for (int t0 = 0; t0 < steps; t0 += D) {
-#pragma unroll
-            for (int k = 0; k < D; ++k) {
-                const int t = t0 + k;
-                if (t >= steps) break;
-                TR::store_regs(stage(t) + (kAsyncA ? TA::kBytes : 0), regs[k]);
-                wait_loads<(D - 1) * (kLoads + TR::kPasses)>();
-                __syncthreads();   // tile t is here, and all waves are done with tile t - 1
-                fetch(stage(t + D), regs[k]);
-                read(stage(t), fa, fb);
-                multiply(fa, fb);
-            }
+        for (int t = 0; t < steps; ++t) {
+            char* nxt = lds + ((t + 1) & 1) * kTileBytes;
+            wait_loads<0>();
+            __syncthreads();   // tile t has arrived, and the other is no longer read
+            if (t + 1 < steps) fetch(nxt, c_begin + (int64_t)(t + 1) * kBK);
+            read(lds + (t & 1) * kTileBytes, fa, fb);
+            multiply(fa, fb);
+            if (t + 1 < steps) settle(nxt);
         }
-        wait_loads<0>();
     }
 
     // A lane's values of row i0 + wi + 16 p + li, in groups of 4 (TT) or 8 (NT) neighbouring columns: group k is
@@ -750,30 +737,35 @@ __global__ __launch_bounds__(kBlock) void k_layout(const T* __restrict__ src, in
 {
     constexpr int N = Vec<T>::N, kRowVecs = kLayoutTile / N;
     __shared__ T t[kLayoutTile][kLayoutTile + 4 / sizeof(T)];
-    const int64_t r0 = (int64_t)blockIdx.y * kLayoutTile, c0 = (int64_t)blockIdx.x * kLayoutTile;
+    const int64_t c0 = (int64_t)blockIdx.y * kLayoutTile;
+    const int64_t all = transpose && ldd > rows ? ldd : rows;   // (a transposed copy's padding columns are rows here)
+    for (int64_t r0 = (int64_t)blockIdx.x * kLayoutTile; r0 < all; r0 += (int64_t)gridDim.x * kLayoutTile) {
 #pragma unroll
-    for (int q = threadIdx.x; q < kLayoutTile * kRowVecs; q += kBlock) {
-        const int r = q / kRowVecs, c = q % kRowVecs * N;
-        const typename Vec<T>::Packed v = load_any(src + (r0 + r) * lds + c0 + c, r0 + r < rows ? cols - c0 - c : 0);
-        if (!transpose) {
-            if (r0 + r < rows && c0 + c < ldd)
-                *reinterpret_cast<typename Vec<T>::Packed*>(dst + (r0 + r) * ldd + c0 + c) = v;
-        } else {
+        for (int q = threadIdx.x; q < kLayoutTile * kRowVecs; q += kBlock) {
+            const int r = q / kRowVecs, c = q % kRowVecs * N;
+            const typename Vec<T>::Packed v =
+                load_any(src + (r0 + r) * lds + c0 + c, r0 + r < rows ? cols - c0 - c : 0);
+            if (!transpose) {
+                if (r0 + r < rows && c0 + c < ldd)
+                    *reinterpret_cast<typename Vec<T>::Packed*>(dst + (r0 + r) * ldd + c0 + c) = v;
+            } else {
 #pragma unroll
-            for (int e = 0; e < N; ++e) t[r][c + e] = v[e];
+                for (int e = 0; e < N; ++e) t[r][c + e] = v[e];
+            }
         }
-    }
-    if (!transpose) return;
-    __syncthreads();
+        if (!transpose) continue;
+        __syncthreads();
 #pragma unroll
-    for (int q = threadIdx.x; q < kLayoutTile * kRowVecs; q += kBlock) {
-        // neighbouring lanes take neighbouring columns of the tile: LDS reads without conflicts
-        const int r = q % kLayoutTile, c = q / kLayoutTile * N;
-        if (c0 + r >= cols || r0 + c >= ldd) continue;
-        typename Vec<T>::Packed v;
+        for (int q = threadIdx.x; q < kLayoutTile * kRowVecs; q += kBlock) {
+            // neighbouring lanes take neighbouring columns of the tile: LDS reads without conflicts
+            const int r = q % kLayoutTile, c = q / kLayoutTile * N;
+            if (c0 + r >= cols || r0 + c >= ldd) continue;
+            typename Vec<T>::Packed v;
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = t[c + e][r];
-        *reinterpret_cast<typename Vec<T>::Packed*>(dst + (c0 + r) * ldd + r0 + c) = v;
+            for (int e = 0; e < N; ++e) v[e] = t[c + e][r];
+            *reinterpret_cast<typename Vec<T>::Packed*>(dst + (c0 + r) * ldd + r0 + c) = v;
+        }
+        __syncthreads();
     }
 }
 
@@ -786,11 +778,11 @@ hipError_t run_gemm(const GemmArgs& g, hipStream_t s)
     return hipGetLastError();
 }
 
-template <typename T, bool TT, int BI, int BJ, int WI, int WJ, int STAGES>
+template <typename T, bool TT, int BI, int BJ, int WI, int WJ>
 hipError_t run_any(bool fast, const GemmArgs& g, hipStream_t s)
 {
-    return fast ? run_gemm<T, Shape<TT, BI, BJ, WI, WJ, STAGES, false, true>>(g, s)
-                : run_gemm<T, Shape<TT, BI, BJ, WI, WJ, STAGES, false, false>>(g, s);
+    return fast ? run_gemm<T, Shape<TT, BI, BJ, WI, WJ, false, true>>(g, s)
+                : run_gemm<T, Shape<TT, BI, BJ, WI, WJ, false, false>>(g, s);
 }
 
 }  // namespace
@@ -799,21 +791,21 @@ template <typename T>
 hipError_t LinearOps<T>::gemm_nt(int tile, bool fast_a, const GemmArgs& g, hipStream_t s)
 {
     if (tile == kTile256) {   // fast_a, 16-bit
-        if constexpr (sizeof(T) == 2) return run_gemm<T, Shape<false, 256, 256, 2, 4, 2, true, true>>(g, s);
+        if constexpr (sizeof(T) == 2) return run_gemm<T, Shape<false, 256, 256, 2, 4, true, true>>(g, s);
     }
-    if (tile == kTile128) return run_any<T, false, 128, 128, 2, 2, 2>(fast_a, g, s);
-    if (tile == kTile128x64) return run_any<T, false, 128, 64, 4, 1, 2>(fast_a, g, s);
-    return run_any<T, false, 64, 64, 2, 2, 4>(fast_a, g, s);
+    if (tile == kTile128) return run_any<T, false, 128, 128, 2, 2>(fast_a, g, s);
+    if (tile == kTile128x64) return run_any<T, false, 128, 64, 4, 1>(fast_a, g, s);
+    return run_any<T, false, 64, 64, 2, 2>(fast_a, g, s);
 }
 
 template <typename T>
 hipError_t LinearOps<T>::gemm_tt(int tile, bool fast_b, const GemmArgs& g, hipStream_t s)
 {
     if (tile == kTile256) {   // fast_b, 16-bit
-        if constexpr (sizeof(T) == 2) return run_gemm<T, Shape<true, 256, 256, 2, 4, 2, true, true>>(g, s);
+        if constexpr (sizeof(T) == 2) return run_gemm<T, Shape<true, 256, 256, 2, 4, true, true>>(g, s);
     }
-    if (tile == kTile128) return run_any<T, true, 128, 128, 2, 2, 2>(fast_b, g, s);
-    return run_any<T, true, 64, 64, 2, 2, 4>(fast_b, g, s);
+    if (tile == kTile128) return run_any<T, true, 128, 128, 2, 2>(fast_b, g, s);
+    return run_any<T, true, 64, 64, 2, 2>(fast_b, g, s);
 }
 
 template <typename T>
@@ -857,8 +849,10 @@ hipError_t LinearOps<T>::layout(const void* src, int64_t lds, int64_t rows, int6
                                 int64_t ldd, hipStream_t s)
 {
     const int64_t w = transpose ? cols : std::max(cols, ldd), h = transpose ? std::max(rows, ldd) : rows;
-    hipLaunchKernelGGL((k_layout<T>), dim3((unsigned)div_up(w, kLayoutTile), (unsigned)div_up(h, kLayoutTile)),
-                       dim3(kBlock), 0, s, (const T*)src, lds, rows, cols, transpose ? 1 : 0, (T*)dst, ldd);
+    const int64_t blocks = std::min<int64_t>(div_up(h, kLayoutTile), 1 << 20);
+    if (blocks == 0) return hipSuccess;
+    hipLaunchKernelGGL((k_layout<T>), dim3((unsigned)blocks, (unsigned)div_up(w, kLayoutTile)), dim3(kBlock), 0, s,
+                       (const T*)src, lds, rows, cols, transpose ? 1 : 0, (T*)dst, ldd);
     return hipGetLastError();
 }
 

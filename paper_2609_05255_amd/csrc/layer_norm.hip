@@ -24,6 +24,19 @@ constexpr int kNormWaves = 4;            // waves of a workgroup whose rows lie 
 constexpr int kSumCols = 16;             // columns per workgroup of k_column_sum
 constexpr int kSumSlices = 64;           // row slices of k_column_sum
 
+// Parameters [c, c + N) of a row of dim; `otherwise` where there are none.
+template <int N>
+__device__ __forceinline__ void load_parameters(const float* p, int c, int dim, float otherwise, float* out)
+{
+    if (p) {
+#pragma unroll
+        for (int e = 0; e < N; e += 4) load_vec(p + c + e, dim - c - e, out + e);
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) out[e] = otherwise;
+    }
+}
+
 // Sum of v over the G lanes of a row, left in all of them. G > 64: the row is the workgroup's; `slot` is LDS
 // of G / 64 floats that the previous call did not use.
 template <int G>
@@ -52,13 +65,10 @@ __global__ __launch_bounds__(G > 64 ? G : kNormWaves * 64) void k_norm_fwd(
     const float inv = 1.f / (float)dim;
     float wv[NV][N], bv[NV][N];
 #pragma unroll
-    for (int k = 0; k < NV; ++k)
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const int c = (k * G + lane) * N + j;
-            wv[k][j] = w && c < dim ? w[c] : 1.f;
-            bv[k][j] = b && c < dim ? b[c] : 0.f;
-        }
+    for (int k = 0; k < NV; ++k) {
+        load_parameters<N>(w, (k * G + lane) * N, dim, 1.f, wv[k]);
+        load_parameters<N>(b, (k * G + lane) * N, dim, 0.f, bv[k]);
+    }
     // a row's vectors are fetched while the row before it is worked on
     const int64_t step = (int64_t)gridDim.x * (kThreads / G);
     typename Vec<T>::Packed next[NV];
@@ -172,13 +182,11 @@ __global__ __launch_bounds__(G > 64 ? G : kNormWaves * 64) void k_norm_bwd(
     const float inv = 1.f / (float)dim;
     float wv[NV][N], sw[NV][N], sb[NV][N];
 #pragma unroll
-    for (int k = 0; k < NV; ++k)
+    for (int k = 0; k < NV; ++k) {
+        load_parameters<N>(w, (k * G + lane) * N, dim, 1.f, wv[k]);
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const int c = (k * G + lane) * N + j;
-            wv[k][j] = w && c < dim ? w[c] : 1.f;
-            sw[k][j] = sb[k][j] = 0.f;
-        }
+        for (int j = 0; j < N; ++j) sw[k][j] = sb[k][j] = 0.f;
+    }
     // a row's vectors are fetched while the row before it is worked on
     const int64_t step = (int64_t)gridDim.x * (kThreads / G);
     typename Vec<T>::Packed nx[NV], ng[NV], na[NV];
@@ -400,15 +408,12 @@ RowShape row_shape(int type, int64_t dim, bool backward)
     for (int g = 1; g <= 64; g <<= 1)
         if (vecs <= g) return {g, 1};
     if (vecs <= 128) return {64, 2};
-    if (backward) {
-        for (int g = 256; g <= 1024; g <<= 1)
-            if (vecs <= g) return {g, 1};
-        return {0, 0};
+    for (int g = 64; g <= 512; g <<= 1) {
+        if (vecs <= 3 * g && g <= 256) return {g, 3};
+        if (vecs <= 4 * g && g <= 256) return {4 * g, 1};
     }
-    if (vecs <= 256) return {64, 4};
-    if (vecs <= 512) return {256, 2};
-    if (vecs <= 1024) return {256, 4};
-    if (vecs <= 2048) return {1024, 2};
+    // (the backward of 16-bit rows that long would need more than a 1,024-thread workgroup's 128 registers)
+    if (vecs <= 2048 && !backward) return {1024, 2};
     return {0, 0};
 }
 
@@ -421,9 +426,8 @@ int norm_bwd_blocks(int type, int64_t rows, int64_t dim)
     const RowShape sh = row_shape(type, dim, true);
     if (sh.g == 0) return (int)std::min<int64_t>(std::max<int64_t>(rows / 64, 1), 64);
     const int64_t per = sh.g > 64 ? 1 : kNormWaves * 64 / sh.g;
-    int64_t most = sh.g > 256 ? 256 * 1024 / sh.g : kNormParts;
-    most = std::min(most, std::max<int64_t>(rows / 32, 1));
-    return (int)std::max<int64_t>(1, std::min(most, div_up(rows, per * 2)));
+    const int64_t most = sh.g > 256 ? 256 * 1024 / sh.g : kNormParts;
+    return (int)std::max<int64_t>(1, std::min(most, div_up(rows, per * 4)));
 }
 
 template <typename T, int G, int NV>
@@ -431,7 +435,8 @@ void norm_fwd(const void* x, int64_t ldx, const float* w, const float* b, int64_
               int64_t ldy, float* mean, float* rstd, hipStream_t s)
 {
     constexpr int kThreads = G > 64 ? G : kNormWaves * 64;
-    const int64_t blocks = std::min<int64_t>(div_up(rows, kThreads / G), 256 * (2048 / kThreads));
+    // (every group takes a few rows where there are enough: its parameters are loaded once)
+    const int64_t blocks = std::min<int64_t>(div_up(rows, kThreads / G), 256 * (NV == 1 ? 2048 : 1024) / kThreads);
     hipLaunchKernelGGL((k_norm_fwd<T, G, NV>), dim3((unsigned)blocks), dim3(kThreads), 0, s, (const T*)x, ldx, w, b,
                        rows, dim, eps, (T*)y, ldy, mean, rstd);
 }
@@ -455,7 +460,13 @@ void norm_bwd(const void* dy, int64_t lddy, const void* x, int64_t ldx, const fl
     case 16 * 8 + 1: call(16, 1); break;            \
     case 32 * 8 + 1: call(32, 1); break;            \
     case 64 * 8 + 1: call(64, 1); break;            \
-    case 64 * 8 + 2: call(64, 2); break;
+    case 64 * 8 + 2: call(64, 2); break;            \
+    case 64 * 8 + 3: call(64, 3); break;            \
+    case 128 * 8 + 3: call(128, 3); break;          \
+    case 256 * 8 + 3: call(256, 3); break;          \
+    case 256 * 8 + 1: call(256, 1); break;          \
+    case 512 * 8 + 1: call(512, 1); break;          \
+    case 1024 * 8 + 1: call(1024, 1); break;
 
 template <typename T>
 hipError_t norm_fwd_type(int type, const void* x, int64_t ldx, const float* w, const float* b, int64_t rows, int dim,
@@ -464,9 +475,6 @@ hipError_t norm_fwd_type(int type, const void* x, int64_t ldx, const float* w, c
     const RowShape sh = row_shape(type, dim, false);
 #define CALL(G, NV) norm_fwd<T, G, NV>(x, ldx, w, b, rows, dim, eps, y, ldy, mean, rstd, s)
     GS_NORM_SHAPES(CALL)
-    case 64 * 8 + 4: CALL(64, 4); break;
-    case 256 * 8 + 2: CALL(256, 2); break;
-    case 256 * 8 + 4: CALL(256, 4); break;
     case 1024 * 8 + 2: CALL(1024, 2); break;
     default:
         hipLaunchKernelGGL((k_norm_fwd_long<T>), dim3((unsigned)std::min<int64_t>(rows, 512)), dim3(1024), 0, s,
@@ -487,9 +495,6 @@ hipError_t norm_bwd_type(int type, const void* dy, int64_t lddy, const void* x, 
 #define CALL(G, NV) \
     norm_bwd<T, G, NV>(dy, lddy, x, ldx, w, mean, rstd, add, ldadd, rows, dim, dx, lddx, dw, db, p, blocks, s)
     GS_NORM_SHAPES(CALL)
-    case 256 * 8 + 1: CALL(256, 1); break;
-    case 512 * 8 + 1: CALL(512, 1); break;
-    case 1024 * 8 + 1: CALL(1024, 1); break;
     default:
         if (rows > 0)
             hipLaunchKernelGGL((k_norm_bwd_long<T>), dim3((unsigned)std::min<int64_t>(rows, 512)), dim3(1024), 0, s,

@@ -39,45 +39,60 @@ struct Plan {
     int64_t split_len;
 };
 
-// NT: the largest tile that still fills the compute units; the sum is split where even the smallest does not.
-Plan plan_nt(int type, int64_t rows, int64_t cols, int64_t len, bool fast_a)
+// What a tile's kernel reaches: the workgroups that run at once, the rate of all compute units with their share of them
+// and with one each, and the time that a round of them takes beside its products (first loads, results). Measured at
+// 8,192 x 4,096 values, sums of 64 to 8,192, in bfloat16 and fp32.
+struct TileRate {
+    int tile, slots;
+    double flop_us, flop_us_one, round_us;
+};
+constexpr TileRate kRates16[] = {{kTile256, 256, 1.1e9, 1.1e9, 11.0},
+                                 {kTile128, 512, 0.85e9, 0.85e9, 6.0},
+                                 {kTile64, 1280, 0.58e9, 0.4e9, 4.0}};
+constexpr TileRate kRates32[] = {{kTile128, 512, 0.131e9, 0.131e9, 6.0}, {kTile64, 1280, 0.125e9, 0.1e9, 4.0}};
+constexpr double kJoinUs = 4.0, kBytesUs = 5.0e6;   // of a join's launch, and of memory
+
+// The tile, and the split of its sum, that these rates make fastest: large tiles where they fill the compute units,
+// smaller ones or a split sum (in parts of `least` values or more, which are then added up) where they do not.
+Plan plan_product(int type, int64_t rows, int64_t cols, int64_t len, int planes, bool fast_operand, int64_t least)
 {
-    Plan p = {kTile64, 1, len};
-    if (cols <= 64 && div_up(rows, 128) >= kFillTiles) {
-        p.tile = kTile128x64;
-        return p;
+    Plan best = {kTile64, 1, len};
+    double best_us = 1e300;
+    const TileRate* rates = type == GS_F32 ? kRates32 : kRates16;
+    const int count = type == GS_F32 ? 2 : 3;
+    for (int k = 0; k < count; ++k) {
+        const TileRate& r = rates[k];
+        if (r.tile == kTile256 && !fast_operand) continue;
+        const TileShape t = tile_shape(r.tile);
+        const int64_t tiles = div_up(rows, t.bi) * div_up(cols, t.bj) * planes;
+        const int64_t most = std::max<int64_t>(1, std::min(r.slots / std::min<int64_t>(tiles, r.slots), len / least));
+        for (int64_t want : {(int64_t)1, most}) {
+            const int64_t split_len = std::max<int64_t>(64, div_up(div_up(len, want), 64) * 64);
+            const int64_t splits = std::max<int64_t>(1, div_up(len, split_len));
+            // a compute unit's share of the workgroups, one after the other, and what their rounds add
+            const double share = (double)div_up(tiles * splits, kFillTiles);
+            double us = share * 2.0 * t.bi * t.bj * (double)split_len * kFillTiles / (share > 1 ? r.flop_us : r.flop_us_one) +
+                        (double)div_up(tiles * splits, r.slots) * r.round_us;
+            if (splits * planes > 1) us += kJoinUs + 8.0 * planes * splits * (double)rows * (double)cols / kBytesUs;
+            if (us < best_us) {
+                best_us = us;
+                best = {r.tile, (int)splits, split_len};
+            }
+        }
     }
-    if (fast_a && type != GS_F32 && div_up(rows, 256) * div_up(cols, 256) >= kFillTiles && cols >= 192 && len >= 512) {
-        p.tile = kTile256;
-        return p;
-    }
-    if (div_up(rows, 128) * div_up(cols, 128) >= kFillTiles) {
-        p.tile = kTile128;
-        return p;
-    }
-    const int64_t tiles = div_up(rows, 64) * div_up(cols, 64);
-    if (tiles < kFillTiles && len >= 2 * kJoinSplitLen) {
-        const int64_t want = std::min(div_up(2 * kFillTiles, tiles), len / kJoinSplitLen);
-        p.split_len = div_up(div_up(len, want), 64) * 64;
-        p.splits = (int)div_up(len, p.split_len);
-    }
-    return p;
+    return best;
 }
 
-// TT: the sum runs over the rows; its splits fill the compute units.
+Plan plan_nt(int type, int64_t rows, int64_t cols, int64_t len, bool fast_a)
+{
+    if (cols <= 64 && div_up(rows, 128) >= kFillTiles) return {kTile128x64, 1, len};
+    return plan_product(type, rows, cols, len, 1, fast_a, kJoinSplitLen);
+}
+
+// TT: the sum runs over the rows.
 Plan plan_tt(int type, int64_t out, int64_t in, int64_t rows, int planes, bool fast_b)
 {
-    Plan p;
-    p.tile = out >= 96 && in >= 96 ? kTile128 : kTile64;
-    if (fast_b && type != GS_F32 && div_up(out, 256) * div_up(in, 256) * planes >= kFillTiles) p.tile = kTile256;
-    const TileShape t = tile_shape(p.tile);
-    const int64_t tiles = div_up(out, t.bi) * div_up(in, t.bj) * planes;
-    // two workgroups per compute unit, one of the largest tile
-    const int64_t fill = p.tile == kTile256 ? kFillTiles : 2 * kFillTiles;
-    const int64_t want = std::max<int64_t>(1, std::min(div_up(fill, tiles), rows / kRowSplitLen));
-    p.split_len = std::max<int64_t>(64, div_up(div_up(rows, want), 64) * 64);
-    p.splits = (int)std::max<int64_t>(1, div_up(rows, p.split_len));
-    return p;
+    return plan_product(type, out, in, rows, planes, fast_b, kRowSplitLen);
 }
 
 // Planes of dz: an fp32 weight gradient keeps what rounding dz to 16 bits would drop, as further planes of the
@@ -120,8 +135,9 @@ FwdSpace fwd_space(void* base, int type, int64_t rows, int64_t in, int64_t out, 
     FwdSpace f = {};
     if (rows > kSkinnyRows) {
         if (copy_w) f.w = r.take(out * padded(type, in) * elem(type));
-        const Plan p = plan_nt(type, rows, out, in, false);
-        if (p.splits > 1) f.part = (float*)r.take((int64_t)p.splits * rows * out * 4);
+        int splits = 1;   // (a workspace is sized for either alignment of x)
+        for (int fast_x = 0; fast_x < 2; ++fast_x) splits = std::max(splits, plan_nt(type, rows, out, in, fast_x).splits);
+        if (splits > 1) f.part = (float*)r.take((int64_t)splits * rows * out * 4);
     }
     f.bytes = r.at;
     return f;
@@ -133,6 +149,7 @@ bool narrow(int type, int64_t in, int64_t out) { return type != GS_F32 && in <= 
 int narrow_blocks(int64_t rows) { return (int)std::max<int64_t>(1, std::min<int64_t>(div_up(rows, 64), kNarrowBlocks)); }
 
 struct BwdSpace {
+    void* x;       // x with padded rows, where its own do not end with a vector
     void* dz;
     void* wt;      // W transposed, [in][padded out]
     float* sums;
@@ -151,6 +168,7 @@ BwdSpace bwd_space(void* base, int type, int act, int64_t rows, int64_t in, int6
     }
     const int planes = planes_of(type, act, dw_type);
     if (need_dz) b.dz = r.take(planes * rows * padded(type, out) * elem(type));
+    if (in % vec(type)) b.x = r.take(rows * padded(type, in) * elem(type));
     b.wt = r.take(in * padded(type, out) * elem(type));
     b.sums = (float*)r.take((int64_t)slope_row_blocks(type, rows, out) * out * 4);
     int64_t part = 0;
@@ -272,12 +290,20 @@ hipError_t linear_bwd(const gs_linear& p, const void* dy, int64_t lddy, const vo
     }
     if (dw) {
         GemmArgs g = {};
-        const bool fast_x = fast(p.x, p.ldx, p.n_in, p.type);
+        const void* x = p.x;
+        int64_t ldx = p.ldx;
+        if (b.x) {
+            x = b.x;
+            ldx = padded(p.type, p.n_in);
+            e = LinearOps<T>::layout(p.x, p.ldx, p.rows, p.n_in, false, b.x, ldx, s);
+            if (e != hipSuccess) return e;
+        }
+        const bool fast_x = b.x || fast(x, ldx, p.n_in, p.type);
         const Plan plan = plan_tt(p.type, p.n_out, p.n_in, p.rows, planes, fast_x);
         g.a = dz;
         g.lda = ldo;
-        g.b = p.x;
-        g.ldb = p.ldx;
+        g.b = x;
+        g.ldb = ldx;
         g.rows = p.n_out;
         g.cols = p.n_in;
         g.len = p.rows;

@@ -61,7 +61,7 @@ __device__ __forceinline__ typename Mma<T>::Frag narrow_rows(const char* lds, in
 }
 
 // FAST: rows of dy, z and x are whole aligned vectors, and come through buffer loads whose range check turns what lies
-// beyond the matrix into zeros; otherwise loads branch at its ends.
+// beyond the matrix into zeros; otherwise they are loaded at any alignment.
 template <typename T, int OUT, int IN, int P, bool FAST>
 __global__ __launch_bounds__(kNarrowThreads, 2) void k_narrow_bwd(NarrowArgs a)
 {
@@ -100,6 +100,19 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void k_narrow_bwd(NarrowArgs a)
             for (int k = 0; k < n; ++k)
                 regs[k] = __builtin_bit_cast(
                     Packed, __builtin_amdgcn_raw_buffer_load_b128(rsrc, off + (uint32_t)(k * per * (int)ld * 2), 0, 0));
+        } else if (r0 + R + 8 <= a.rows) {
+            // whole vectors at any alignment, the values beyond the row turned into zeros; what they reach beyond the
+            // last row of the tile lies in the 8 rows behind it
+            const int left = cols - v * 8;
+            const T* src = (const T*)p + (r0 + first) * ld + (left > 0 ? v * 8 : 0);
+#pragma unroll
+            for (int k = 0; k < n; ++k) regs[k] = *reinterpret_cast<const typename Vec<T>::Any*>(src + k * per * ld);
+            if (left < 8)
+#pragma unroll
+                for (int k = 0; k < n; ++k)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (e >= left) regs[k][e] = (T)0.f;
         } else {
 #pragma unroll
             for (int k = 0; k < n; ++k) {
