@@ -4,9 +4,8 @@
 // A workgroup computes a BI x BJ tile of C with WI x WJ waves. The operands'
 // tiles (128 bytes along the sum: 64 16-bit or 32 fp32 values) go from memory to
 // LDS with buffer loads that write LDS directly, the next tile's under the current
-// one's MFMAs. Every step issues its loads, past the end too: the descriptor's
-// range check turns those, like rows beyond the matrix, into zeros without
-// reading. The 256 x 256 tile, whose workgroup is alone on its compute unit, also
+// one's MFMAs. What lies beyond a matrix the descriptor's range check turns into
+// zeros without reading. The 256 x 256 tile, whose workgroup is alone on its compute unit, also
 // reads its fragments ahead and spreads its loads between the MFMAs (AHEAD); two
 // workgroups of the 128 x 128 tile and five of the 64 x 64 one overlap each other.
 // Measured at 8,192 x 4,096 x 4,096 in bfloat16: 1,110, 870 and 580 TFLOP/s (NT),
@@ -267,6 +266,12 @@ struct Shape {
     static constexpr bool TT = TT_, AHEAD = AHEAD_, FAST = FAST_;
     static constexpr int BI = BI_, BJ = BJ_, WI = WI_, WJ = WJ_;
     static constexpr int THREADS = WI * WJ * 64;
+    // for a sum of so many tiles
+    static constexpr int lds_bytes(int64_t tiles, int size)
+    {
+        const int tile = (BI + BJ) * 128, results = TT ? 0 : BI * BJ * size;
+        return tiles > 1 || results > tile || AHEAD ? 2 * tile : tile;
+    }
 };
 
 // Stores a wave's WR x WC block of results whose 8-value groups are in LDS, whole rows of it at a time: row r's
@@ -308,8 +313,11 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(GemmArgs g)
     constexpr int kTileBytes = TA::kBytes + TB::kBytes;
     constexpr bool kAsyncA = S::FAST || TT, kAsyncB = S::FAST || !TT;
     static_assert(TT || FJ % 2 == 0, "columns interleave between pairs of fragments");
-    static_assert(TT || WI * WJ * WR * WC * (int)sizeof(T) <= 2 * kTileBytes, "the results pass through LDS");
-    __shared__ __attribute__((aligned(1024))) char lds[2 * kTileBytes + (S::AHEAD ? TA::kBytes : 0)];
+    static_assert(TT || BI * BJ * (int)sizeof(T) <= S::lds_bytes(1, sizeof(T)), "the results pass through LDS");
+    // (without AHEAD as much as the launch gives: two tiles, or one if the sum has no more, so that more workgroups fit)
+    extern __shared__ __attribute__((aligned(1024))) char lds_given[];
+    __shared__ __attribute__((aligned(1024))) char lds_ahead[S::AHEAD ? 2 * kTileBytes + TA::kBytes : 16];
+    char* lds = S::AHEAD ? lds_ahead : lds_given;
 
     const int64_t tiles_i = (g.rows + BI - 1) / BI, tiles_j = (g.cols + BJ - 1) / BJ;
     int64_t ti, tj;
@@ -415,8 +423,10 @@ __global__ __launch_bounds__(S::THREADS) void k_gemm(GemmArgs g)
                 char* nxt = lds + ((t + 1) & 1) * kTileBytes;
                 wait_loads<0>();
                 barrier();   // tile t is here, and all waves are done with tile t - 1
-                sa.load(nxt);
-                sb.load(nxt + TA::kBytes);
+                if (t + 1 < steps) {
+                    sa.load(nxt);
+                    sb.load(nxt + TA::kBytes);
+                }
                 read(cur, fa, fb);
                 multiply(fa, fb);
             }
@@ -773,7 +783,8 @@ template <typename T, class S>
 hipError_t run_gemm(const GemmArgs& g, hipStream_t s)
 {
     const int64_t tiles = div_up(g.rows, S::BI) * div_up(g.cols, S::BJ);
-    hipLaunchKernelGGL((k_gemm<T, S>), dim3((unsigned)tiles, (unsigned)(g.planes * g.splits)), dim3(S::THREADS), 0, s,
+    const int lds = S::AHEAD ? 0 : S::lds_bytes(div_up(g.split_len, 128 / (int)sizeof(T)), sizeof(T));
+    hipLaunchKernelGGL((k_gemm<T, S>), dim3((unsigned)tiles, (unsigned)(g.planes * g.splits)), dim3(S::THREADS), lds, s,
                        g);
     return hipGetLastError();
 }

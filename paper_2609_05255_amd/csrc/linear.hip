@@ -146,7 +146,12 @@ FwdSpace fwd_space(void* base, int type, int64_t rows, int64_t in, int64_t out, 
 // A backward in one pass over the rows (narrow.h).
 bool narrow(int type, int64_t in, int64_t out) { return type != GS_F32 && in <= kNarrowMost && out <= kNarrowMost; }
 
-int narrow_blocks(int64_t rows) { return (int)std::max<int64_t>(1, std::min<int64_t>(div_up(rows, 64), kNarrowBlocks)); }
+int narrow_blocks(int64_t rows, int64_t in, int64_t out)
+{
+    // (the smaller the layer, the more workgroups a compute unit holds)
+    const int64_t most = in > 64 && out > 64 ? kNarrowBlocks : 2 * kNarrowBlocks;
+    return (int)std::max<int64_t>(1, std::min<int64_t>(div_up(rows, 64), most));
+}
 
 struct BwdSpace {
     void* x;       // x with padded rows, where its own do not end with a vector
@@ -162,7 +167,7 @@ BwdSpace bwd_space(void* base, int type, int act, int64_t rows, int64_t in, int6
     Regions r{(char*)base};
     BwdSpace b = {};
     if (narrow(type, in, out)) {
-        b.part = (float*)r.take(narrow_blocks(rows) * narrow_part((int)out, (int)in) * 4);
+        b.part = (float*)r.take(narrow_blocks(rows, in, out) * narrow_part((int)out, (int)in) * 4);
         b.bytes = r.at;
         return b;
     }
@@ -246,7 +251,7 @@ hipError_t linear_bwd(const gs_linear& p, const void* dy, int64_t lddy, const vo
                                   (int)p.n_in, p.act, dw_type == GS_F32, dx, dw,   db,    b.part};
             const bool whole = fast(dy, lddy, p.n_out, p.type) && fast(p.x, p.ldx, p.n_in, p.type) &&
                                (p.act == GS_ACT_NONE || fast(z, ldz, p.n_out, p.type));
-            return NarrowOps<T>::backward(a, whole, planes, narrow_blocks(p.rows), s);
+            return NarrowOps<T>::backward(a, whole, planes, narrow_blocks(p.rows, p.n_in, p.n_out), s);
         }
     const int64_t ldo = need_dz ? padded(p.type, p.n_out) : lddy;
     const void* dz = need_dz ? b.dz : dy;

@@ -3,7 +3,7 @@
 //   dz = dy act'(z), dx = dz W, dW = dz^T x, db = column sums of dz
 //
 // Bound by HBM: dy, z and x are read once and dx is written once, where separate products would write dz and read it
-// twice. W and 64 rows of dz and x are in LDS; a workgroup takes 64 rows at a time and keeps its dW and db in registers
+// twice. W and some rows of dz and x are in LDS; a workgroup takes 32 to 128 rows at a time and keeps its dW and db in registers
 // over all of them, so that both products come from the same tile: dx sums over dz's columns, dW over its rows. The
 // next rows are fetched into registers under the products. Each workgroup writes its dW and db once; k_narrow_join adds
 // them up in a fixed order.
@@ -22,8 +22,14 @@ namespace gsr {
 
 namespace {
 
-constexpr int kNarrowRows = 64;
 constexpr int kNarrowThreads = 256;
+
+// Rows of a workgroup's tile: as many as leave room for two workgroups on a compute unit, in LDS and in registers.
+constexpr int narrow_tile_rows(int out, int in, int planes, bool fast)
+{
+    if (out == 128 && in == 128) return planes == 1 && fast ? 64 : 32;
+    return out >= 64 || in >= 64 ? 64 : 128;
+}
 
 __device__ __forceinline__ int narrow_hash(int row) { return (row & 6) | ((row >> 3) & 1); }
 
@@ -65,24 +71,28 @@ __device__ __forceinline__ typename Mma<T>::Frag narrow_rows(const char* lds, in
 template <typename T, int OUT, int IN, int P, bool FAST>
 __global__ __launch_bounds__(kNarrowThreads, 2) void k_narrow_bwd(NarrowArgs a)
 {
-    constexpr int R = kNarrowRows, VO = OUT / 8, VI = IN / 8;
+    constexpr int R = narrow_tile_rows(OUT, IN, P, FAST), VO = OUT / 8, VI = IN / 8;
     constexpr int NO = R * VO / kNarrowThreads, NI = R * VI / kNarrowThreads;   // vectors of a thread
-    constexpr int FO = OUT / 32, FI = IN / 32, FX = IN / 16;                    // fragments of a wave: dW's rows, columns; dx's columns
-    constexpr int kDz = R * OUT * 2, kX = R * IN * 2, kW = OUT * IN * 2;
+    constexpr int FO = OUT / 32, FI = IN / 32;                                  // fragments of a wave's part of dW
+    // dx: a wave takes 16 rows and all columns at a time, or with 32 rows half of the columns
+    constexpr int kBlocksX = R < 64 ? 1 : R / 64, FX = IN / 16 / (R < 64 ? 2 : 1);
+    // (rows of 128 bytes at least)
+    constexpr int kDz = R * (OUT < 64 ? 64 : OUT) * 2, kX = R * (IN < 64 ? 64 : IN) * 2;
+    constexpr int kW = OUT * (IN < 64 ? 64 : IN) * 2, kBlock16 = 16 * FX * 16 * 2;
     typedef typename Mma<T>::Frag Frag;
     typedef typename Vec<T>::Packed Packed;
-    __shared__ __attribute__((aligned(1024))) char lds[P * kDz + kX + kW + R * IN * 2];
+    __shared__ __attribute__((aligned(1024))) char lds[P * kDz + kX + kW + 4 * kBlock16];
     char* lds_dz = lds;
     char* lds_x = lds + P * kDz;
     char* lds_w = lds_x + kX;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lg = lane >> 4, li = lane & 15;
-    char* block = lds_w + kW + wave * (16 * IN * 2);   // a wave's 16 rows of dx on their way out
+    char* block = lds_w + kW + wave * kBlock16;   // a wave's 16 rows of dx on their way out
 
     if (a.dx)
 #pragma unroll
-        for (int k = 0; k < OUT * VI / kNarrowThreads; ++k) {
-            const int q = k * kNarrowThreads + tid, r = q / VI, v = q % VI;
+        for (int q = tid; q < OUT * VI; q += kNarrowThreads) {
+            const int r = q / VI, v = q % VI;
             *reinterpret_cast<Packed*>(lds_w + narrow_at(OUT, r, v)) =
                 load_any((const T*)a.w + r * a.ldw + v * 8, r < a.out ? a.in - v * 8 : 0);
         }
@@ -130,7 +140,7 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void k_narrow_bwd(NarrowArgs a)
     float db[8] = {};
     const int wo = (wave >> 1) * (OUT / 32), wn = (wave & 1) * (IN / 32);   // first groups of 16 of the wave's part of dW
     const int64_t tiles = (a.rows + R - 1) / R;
-    if (tiles > 0) fetch((int64_t)blockIdx.x * R);   // (no more workgroups than tiles)
+    if (blockIdx.x < tiles) fetch((int64_t)blockIdx.x * R);
     for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
 #pragma unroll
         for (int k = 0; k < NO; ++k) {
@@ -164,25 +174,30 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void k_narrow_bwd(NarrowArgs a)
                 *reinterpret_cast<Packed*>(lds_x + narrow_at(R, ri + k * (kNarrowThreads / VI), vi)) = rx[k];
         __syncthreads();
         if (t + gridDim.x < tiles) fetch((t + gridDim.x) * R);
-        if (a.dx) {
-            f32x4 acc[FX] = {};
+        if (a.dx)
 #pragma unroll
-            for (int s = 0; s < OUT / 32; ++s) {
-                const Frag f = narrow_rows<T>(lds_dz, R, wave * 16, s);
+            for (int k = 0; k < kBlocksX; ++k) {
+                const int row = 16 * (R < 64 ? wave & 1 : wave * kBlocksX + k), group = R < 64 ? (wave >> 1) * FX : 0;
+                f32x4 acc[FX] = {};
 #pragma unroll
-                for (int n = 0; n < FX; ++n) acc[n] = Mma<T>::mma(narrow_columns<T>(lds_w, OUT, n, 32 * s), f, acc[n]);
+                for (int s = 0; s < OUT / 32; ++s) {
+                    const Frag f = narrow_rows<T>(lds_dz, R, row, s);
+#pragma unroll
+                    for (int n = 0; n < FX; ++n)
+                        acc[n] = Mma<T>::mma(narrow_columns<T>(lds_w, OUT, group + n, 32 * s), f, acc[n]);
+                }
+                // acc[n][r]: row li, column 16 (group + n) + 4 lg + r
+#pragma unroll
+                for (int n = 0; n < FX; ++n) {
+                    typedef T V4 __attribute__((ext_vector_type(4)));
+                    V4 h;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) h[e] = (T)acc[n][e];
+                    *reinterpret_cast<V4*>(block + li * (FX * 32) + ((2 * n + (lg >> 1)) ^ (li & 7 & (2 * FX - 1))) * 16 +
+                                           (lg & 1) * 8) = h;
+                }
+                store_block<T, 16, FX * 16>(block, (T*)a.dx, a.lddx, t * R + row, a.rows, 16 * group, a.in);
             }
-            // acc[n][r]: row li, column 16 n + 4 lg + r
-#pragma unroll
-            for (int n = 0; n < FX; ++n) {
-                typedef T V4 __attribute__((ext_vector_type(4)));
-                V4 h;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) h[e] = (T)acc[n][e];
-                *reinterpret_cast<V4*>(block + li * (IN * 2) + ((2 * n + (lg >> 1)) ^ (li & 7)) * 16 + (lg & 1) * 8) = h;
-            }
-            store_block<T, 16, IN>(block, (T*)a.dx, a.lddx, t * R + wave * 16, a.rows, 0, a.in);
-        }
         if (a.dw) {
 #pragma unroll
             for (int p = 0; p < P; ++p)
@@ -216,6 +231,7 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void k_narrow_bwd(NarrowArgs a)
                 if (i < a.out) store_vec(part + i * a.in + j, a.in - j, v);
             }
     if (!a.db) return;
+    static_assert(kNarrowThreads / VO * OUT * 4 <= (int)sizeof(lds), "the sums fit");
     float* s = reinterpret_cast<float*>(lds);   // [kNarrowThreads / VO][OUT]
 #pragma unroll
     for (int e = 0; e < 8; ++e) s[ro * OUT + vo * 8 + e] = db[e];
@@ -276,11 +292,21 @@ void run_narrow(const NarrowArgs& a, int planes, int blocks, hipStream_t s)
 template <typename T, bool FAST>
 void run_narrow(const NarrowArgs& a, int planes, int blocks, hipStream_t s)
 {
-    if (a.out <= 64)
-        a.in <= 64 ? run_narrow<T, 64, 64, FAST>(a, planes, blocks, s) : run_narrow<T, 64, 128, FAST>(a, planes, blocks, s);
+    auto with_out = [&](auto out) {
+        constexpr int OUT = decltype(out)::value;
+        if (a.in <= 32)
+            run_narrow<T, OUT, 32, FAST>(a, planes, blocks, s);
+        else if (a.in <= 64)
+            run_narrow<T, OUT, 64, FAST>(a, planes, blocks, s);
+        else
+            run_narrow<T, OUT, 128, FAST>(a, planes, blocks, s);
+    };
+    if (a.out <= 32)
+        with_out(std::integral_constant<int, 32>());
+    else if (a.out <= 64)
+        with_out(std::integral_constant<int, 64>());
     else
-        a.in <= 64 ? run_narrow<T, 128, 64, FAST>(a, planes, blocks, s)
-                   : run_narrow<T, 128, 128, FAST>(a, planes, blocks, s);
+        with_out(std::integral_constant<int, 128>());
 }
 
 }  // namespace
