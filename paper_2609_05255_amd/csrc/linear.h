@@ -60,7 +60,7 @@ inline TileShape tile_shape(int tile)
     }
 }
 
-// A narrow layer's backward in one pass (narrow.h).
+// A narrow layer in one pass (narrow.h).
 struct NarrowArgs {
     const void *dy, *z, *x, *w;
     int64_t lddy, ldz, ldx, ldw, lddx, lddw;
@@ -75,6 +75,8 @@ __host__ __device__ inline int64_t narrow_part(int out, int in) { return (out * 
 
 template <typename T>
 struct NarrowOps {   // T 16-bit
+    // fast: rows of x are 16-byte aligned and whole 16-byte vectors
+    static hipError_t forward(const GemmArgs& g, bool fast, int blocks, hipStream_t s);
     // fast: rows of dy, z and x are 16-byte aligned and whole 16-byte vectors
     static hipError_t backward(const NarrowArgs& a, bool fast, int planes, int blocks, hipStream_t s);
 };

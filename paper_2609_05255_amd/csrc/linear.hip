@@ -123,6 +123,16 @@ struct Regions {
     }
 };
 
+// Layers that one pass over the rows takes (narrow.h).
+bool narrow(int type, int64_t in, int64_t out) { return type != GS_F32 && in <= kNarrowMost && out <= kNarrowMost; }
+
+int narrow_blocks(int64_t rows, int64_t in, int64_t out)
+{
+    // (the smaller the layer, the more workgroups a compute unit holds)
+    const int64_t most = in > 64 && out > 64 ? kNarrowBlocks : 2 * kNarrowBlocks;
+    return (int)std::max<int64_t>(1, std::min<int64_t>(div_up(rows, 64), most));
+}
+
 struct FwdSpace {
     void* w;       // W with padded rows, where its own cannot be read in vectors
     float* part;
@@ -133,7 +143,7 @@ FwdSpace fwd_space(void* base, int type, int64_t rows, int64_t in, int64_t out, 
 {
     Regions r{(char*)base};
     FwdSpace f = {};
-    if (rows > kSkinnyRows) {
+    if (rows > kSkinnyRows && !narrow(type, in, out)) {
         if (copy_w) f.w = r.take(out * padded(type, in) * elem(type));
         int splits = 1;   // (a workspace is sized for either alignment of x)
         for (int fast_x = 0; fast_x < 2; ++fast_x) splits = std::max(splits, plan_nt(type, rows, out, in, fast_x).splits);
@@ -141,16 +151,6 @@ FwdSpace fwd_space(void* base, int type, int64_t rows, int64_t in, int64_t out, 
     }
     f.bytes = r.at;
     return f;
-}
-
-// A backward in one pass over the rows (narrow.h).
-bool narrow(int type, int64_t in, int64_t out) { return type != GS_F32 && in <= kNarrowMost && out <= kNarrowMost; }
-
-int narrow_blocks(int64_t rows, int64_t in, int64_t out)
-{
-    // (the smaller the layer, the more workgroups a compute unit holds)
-    const int64_t most = in > 64 && out > 64 ? kNarrowBlocks : 2 * kNarrowBlocks;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(div_up(rows, 64), most));
 }
 
 struct BwdSpace {
@@ -235,7 +235,11 @@ hipError_t linear_fwd(const gs_linear& p, const void* residual, int64_t ldr, voi
     g.ldo = ldy;
     g.z = z;
     g.ldz = ldz;
-    return run_nt<T>(p.type, g, fast(p.x, p.ldx, p.n_in, p.type), f.part, s);
+    const bool fast_x = fast(p.x, p.ldx, p.n_in, p.type);
+    if constexpr (sizeof(T) == 2)
+        if (p.rows > kSkinnyRows && narrow(p.type, p.n_in, p.n_out))
+            return NarrowOps<T>::forward(g, fast_x, (int)std::min<int64_t>(div_up(p.rows, 64), 4 * kFillTiles), s);
+    return run_nt<T>(p.type, g, fast_x, f.part, s);
 }
 
 template <typename T>

@@ -1,4 +1,5 @@
-// Backward of a linear layer of up to 128 inputs and outputs in one pass over the rows (16-bit types).
+// A linear layer of up to 128 inputs and outputs in one pass over the rows (16-bit types): its backward, and below it
+// its forward.
 //
 //   dz = dy act'(z), dx = dz W, dW = dz^T x, db = column sums of dz
 //
@@ -279,6 +280,119 @@ __global__ __launch_bounds__(kBlock) void k_narrow_join(NarrowArgs a, int parts)
     }
 }
 
+// Forward of such a layer. W is in LDS; a wave takes 16 rows at a time and goes through them without a barrier: x comes
+// from memory in the layout of the MFMAs' fragments, the next rows' while these are worked on, and the results leave
+// through the wave's part of LDS as whole rows. Bound by HBM.
+template <typename T, int OUT, int IN, bool FAST>
+__global__ __launch_bounds__(kNarrowThreads) void k_narrow_fwd(GemmArgs g)
+{
+    constexpr int FJ = OUT / 16, KS = IN / 32, kRow = (IN < 64 ? 64 : IN) * 2, kBlock16 = 16 * OUT * 2;
+    typedef typename Mma<T>::Frag Frag;
+    typedef typename Vec<T>::Packed Packed;
+    using W = Tile<T, OUT < 32 ? 32 : OUT, false, true, 64>;   // for its hash of a row
+    __shared__ __attribute__((aligned(1024))) char lds[OUT * kRow + 4 * kBlock16];
+    __shared__ float bias[OUT];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lg = lane >> 4, li = lane & 15, in = (int)g.len, out = (int)g.cols;
+    char* block = lds + OUT * kRow + wave * kBlock16;
+    auto at = [](int row, int v) { return (v >> 3) * OUT * 128 + row * 128 + ((v & 7) ^ W::hash(row)) * 16; };
+    for (int q = tid; q < OUT * (IN / 8); q += kNarrowThreads) {
+        const int r = q / (IN / 8), v = q % (IN / 8);
+        *reinterpret_cast<Packed*>(lds + at(r, v)) = load_any((const T*)g.b + r * g.ldb + v * 8, r < out ? in - v * 8 : 0);
+    }
+    for (int c = tid; c < OUT; c += kNarrowThreads) bias[c] = g.bias && c < out ? g.bias[c] : 0.f;
+    __syncthreads();
+
+    const int64_t blocks = (g.rows + 15) / 16, step = (int64_t)gridDim.x * 4;
+    Packed next[KS];
+    auto fetch = [&](int64_t b) {
+        const int64_t r = b * 16 + li < g.rows ? b * 16 + li : g.rows - 1;   // (rows beyond are not stored)
+        const T* src = (const T*)g.a + r * g.lda + lg * 8;
+        if (FAST || b * 16 + 24 <= g.rows) {
+            // whole vectors; what they reach beyond the last row (not FAST) lies in the 8 rows behind it
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const int left = in - 32 * s - lg * 8;
+                Packed t = {};
+                if (left > 0) t = *reinterpret_cast<const typename Vec<T>::Any*>(src + 32 * s);
+                if (!FAST)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (e >= left) t[e] = (T)0.f;
+                next[s] = t;
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < KS; ++s) next[s] = load_any(src + 32 * s, in - 32 * s - lg * 8);
+        }
+    };
+    const int64_t first = (int64_t)blockIdx.x * 4 + wave;
+    if (first < blocks) fetch(first);
+    for (int64_t b = first; b < blocks; b += step) {
+        Frag x[KS];
+#pragma unroll
+        for (int s = 0; s < KS; ++s) x[s] = next[s];
+        if (b + step < blocks) fetch(b + step);
+        const int64_t i = b * 16 + li;
+        Packed r[FJ / 2];   // the residual, 8 columns of row i each
+        if (g.residual)
+#pragma unroll
+            for (int q = 0; q < FJ / 2; ++q) {
+                const int j = 32 * q + 8 * lg;
+                r[q] = load_any((const T*)g.residual + i * g.ldr + j, i < g.rows ? out - j : 0);
+            }
+        f32x4 acc[FJ] = {};
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int f = 0; f < FJ; ++f) {
+                // columns of f, f + 1 interleave in fours: a lane ends up with 8 neighbouring ones
+                const int row = 32 * (f >> 1) + 4 * (f & 1) + 8 * (li >> 2) + (li & 3);
+                const Frag w = *reinterpret_cast<const Frag*>(lds + at(row, 4 * s + lg));
+                acc[f] = Mma<T>::mma(w, x[s], acc[f]);
+            }
+        float v[FJ / 2][8];
+#pragma unroll
+        for (int q = 0; q < FJ / 2; ++q)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[q][e] = acc[2 * q + e / 4][e & 3] + bias[32 * q + 8 * lg + e];
+        auto put = [&]() {
+#pragma unroll
+            for (int q = 0; q < FJ / 2; ++q) {
+                Packed t;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) t[e] = (T)v[q][e];
+                *reinterpret_cast<Packed*>(block + li * (OUT * 2) + ((4 * q + lg) ^ (li & 7 & (OUT / 8 - 1))) * 16) = t;
+            }
+        };
+        if (g.z) {
+            put();
+            store_block<T, 16, OUT>(block, (T*)g.z, g.ldz, b * 16, g.rows, 0, out);
+        }
+#pragma unroll
+        for (int q = 0; q < FJ / 2; ++q) {
+            activate<8>(g.act, v[q]);
+            if (g.residual)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[q][e] += (float)r[q][e];
+        }
+        put();
+        store_block<T, 16, OUT>(block, (T*)g.out, g.ldo, b * 16, g.rows, 0, out);
+    }
+}
+
+// Calls f with the number of columns that a narrow kernel is built for: 32, 64 or 128.
+template <typename F>
+void with_width(int n, F f)
+{
+    if (n <= 32)
+        f(std::integral_constant<int, 32>());
+    else if (n <= 64)
+        f(std::integral_constant<int, 64>());
+    else
+        f(std::integral_constant<int, 128>());
+}
+
 template <typename T, int OUT, int IN, bool FAST>
 void run_narrow(const NarrowArgs& a, int planes, int blocks, hipStream_t s)
 {
@@ -292,21 +406,11 @@ void run_narrow(const NarrowArgs& a, int planes, int blocks, hipStream_t s)
 template <typename T, bool FAST>
 void run_narrow(const NarrowArgs& a, int planes, int blocks, hipStream_t s)
 {
-    auto with_out = [&](auto out) {
-        constexpr int OUT = decltype(out)::value;
-        if (a.in <= 32)
-            run_narrow<T, OUT, 32, FAST>(a, planes, blocks, s);
-        else if (a.in <= 64)
-            run_narrow<T, OUT, 64, FAST>(a, planes, blocks, s);
-        else
-            run_narrow<T, OUT, 128, FAST>(a, planes, blocks, s);
-    };
-    if (a.out <= 32)
-        with_out(std::integral_constant<int, 32>());
-    else if (a.out <= 64)
-        with_out(std::integral_constant<int, 64>());
-    else
-        with_out(std::integral_constant<int, 128>());
+    with_width(a.out, [&](auto out) {
+        with_width(a.in, [&](auto in) {
+            run_narrow<T, decltype(out)::value, decltype(in)::value, FAST>(a, planes, blocks, s);
+        });
+    });
 }
 
 }  // namespace
@@ -319,6 +423,21 @@ hipError_t NarrowOps<T>::backward(const NarrowArgs& a, bool fast, int planes, in
     if (e != hipSuccess || !(a.dw || a.db)) return e;
     hipLaunchKernelGGL((k_narrow_join<T>), dim3((unsigned)div_up(a.out * a.in + a.out, 64)), dim3(kBlock), 0, s, a,
                        blocks);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t NarrowOps<T>::forward(const GemmArgs& g, bool fast, int blocks, hipStream_t s)
+{
+    with_width((int)g.cols, [&](auto out) {
+        with_width((int)g.len, [&](auto in) {
+            constexpr int OUT = decltype(out)::value, IN = decltype(in)::value;
+            if (fast)
+                hipLaunchKernelGGL((k_narrow_fwd<T, OUT, IN, true>), dim3(blocks), dim3(kNarrowThreads), 0, s, g);
+            else
+                hipLaunchKernelGGL((k_narrow_fwd<T, OUT, IN, false>), dim3(blocks), dim3(kNarrowThreads), 0, s, g);
+        });
+    });
     return hipGetLastError();
 }
 

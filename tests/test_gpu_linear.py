@@ -282,3 +282,17 @@ def test_backward_on_both_sides_of_the_narrow_form(rows, n_in, n_out, dtype):
         db = torch.full((n_out,), float("nan"), device="cuda")
         gs.gs_linear_bwd(d["dy"], d["x"], d["w"], d["z"], dx, dw, db, space(d["x"], d["w"], name, dw_type), act=name)
         check_backward(d, name, dx, dw, db)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("rows", [65, 79, 80, 20_011])
+@pytest.mark.parametrize("n_in,n_out", [(32, 32), (33, 31), (64, 128), (128, 64), (128, 128), (127, 125), (128, 129), (8, 3)])
+def test_forward_on_both_sides_of_the_narrow_form(rows, n_in, n_out, dtype):
+    d = make(rows, n_in, n_out, dtype, rows + n_in)
+    y, z = (torch.full_like(d["r"], float("nan")) for _ in range(2))
+    ws = space(d["x"], d["w"], "gelu", None)
+    gs.gs_linear_fwd(d["x"], d["w"], d["bias"], y, ws, act="gelu", residual=d["r"], z=z)
+    check_forward(d, "gelu", y, z)
+    wide, s = strided(torch.zeros_like(d["r"]), 3), {k: strided(v, 5, 1) if v.dim() == 2 else v for k, v in d.items()}
+    gs.gs_linear_fwd(s["x"], s["w"], d["bias"], wide, ws, act="tanh", residual=s["r"])
+    check_forward(d, "tanh", wide)
