@@ -793,7 +793,7 @@ gs_status gs_linear_fwd(const gs_linear* p, const void* residual, int64_t ldr, v
     if (residual && (st = check_matrix("residual", residual, p->rows, p->n_out, ldr, p->type)) != GS_OK) return st;
     if (z && (st = check_matrix("z", z, p->rows, p->n_out, ldz, p->type)) != GS_OK) return st;
     if (p->rows == 0) return ok();
-    if ((st = check_workspace(workspace, workspace_bytes, linear_fwd_workspace(*p))) != GS_OK) return st;
+    if ((st = check_workspace(workspace, workspace_bytes, linear_fwd_workspace(*p, z != nullptr))) != GS_OK) return st;
     hipStream_t s = static_cast<hipStream_t>(stream);
     timing_begin(GS_KERNEL_LINEAR_FWD, s);
     GS_HIP(launch_linear_fwd(*p, residual, ldr, y, ldy, z, ldz, workspace, s));

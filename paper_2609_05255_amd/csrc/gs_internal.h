@@ -210,7 +210,7 @@ hipError_t launch_layer_norm_bwd(int type, const void* dy, int64_t lddy, const v
                                  const float* mean, const float* rstd, const void* add, int64_t ldadd, int64_t rows,
                                  int dim, void* dx, int64_t lddx, float* dw, float* db, float* part, hipStream_t s);
 size_t linear_workspace(int type, int act, int64_t rows, int64_t in, int64_t out, int dw_type);   // -1: forward only
-size_t linear_fwd_workspace(const gs_linear& p);
+size_t linear_fwd_workspace(const gs_linear& p, bool z);
 size_t linear_bwd_workspace(const gs_linear& p, const void* dy, int64_t lddy, int dw_type);
 bool linear_grid_fits(int64_t rows, int64_t cols);
 hipError_t launch_linear_fwd(const gs_linear& p, const void* residual, int64_t ldr, void* y, int64_t ldy, void* z,

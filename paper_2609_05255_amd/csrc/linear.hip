@@ -133,17 +133,24 @@ int narrow_blocks(int64_t rows, int64_t in, int64_t out)
     return (int)std::max<int64_t>(1, std::min<int64_t>(div_up(rows, 64), most));
 }
 
+// The forward in that form, but where z and y are wider than x and more than the 256 MB cache holds: there the tiles'
+// larger blocks of writes are faster (3,000,000 x 64 x 128 with z: 338 us against 393; 100,000 rows: 20 against 17).
+bool narrow_forward(int type, int64_t rows, int64_t in, int64_t out, bool z)
+{
+    return narrow(type, in, out) && !(z && out > in && 4 * rows * out > ((int64_t)256 << 20));
+}
+
 struct FwdSpace {
     void* w;       // W with padded rows, where its own cannot be read in vectors
     float* part;
     size_t bytes;
 };
 
-FwdSpace fwd_space(void* base, int type, int64_t rows, int64_t in, int64_t out, bool copy_w)
+FwdSpace fwd_space(void* base, int type, int64_t rows, int64_t in, int64_t out, bool copy_w, bool z)
 {
     Regions r{(char*)base};
     FwdSpace f = {};
-    if (rows > kSkinnyRows && !narrow(type, in, out)) {
+    if (rows > kSkinnyRows && !narrow_forward(type, rows, in, out, z)) {
         if (copy_w) f.w = r.take(out * padded(type, in) * elem(type));
         int splits = 1;   // (a workspace is sized for either alignment of x)
         for (int fast_x = 0; fast_x < 2; ++fast_x) splits = std::max(splits, plan_nt(type, rows, out, in, fast_x).splits);
@@ -212,7 +219,7 @@ hipError_t linear_fwd(const gs_linear& p, const void* residual, int64_t ldr, voi
                       int64_t ldz, void* ws, hipStream_t s)
 {
     const bool copy_w = !fast(p.w, p.ldw, p.n_in, p.type);
-    const FwdSpace f = fwd_space(ws, p.type, p.rows, p.n_in, p.n_out, copy_w);
+    const FwdSpace f = fwd_space(ws, p.type, p.rows, p.n_in, p.n_out, copy_w, z != nullptr);
     GemmArgs g = {};
     g.a = p.x;
     g.lda = p.ldx;
@@ -237,7 +244,7 @@ hipError_t linear_fwd(const gs_linear& p, const void* residual, int64_t ldr, voi
     g.ldz = ldz;
     const bool fast_x = fast(p.x, p.ldx, p.n_in, p.type);
     if constexpr (sizeof(T) == 2)
-        if (p.rows > kSkinnyRows && narrow(p.type, p.n_in, p.n_out))
+        if (p.rows > kSkinnyRows && narrow_forward(p.type, p.rows, p.n_in, p.n_out, z != nullptr))
             return NarrowOps<T>::forward(g, fast_x, (int)std::min<int64_t>(div_up(p.rows, 64), 4 * kFillTiles), s);
     return run_nt<T>(p.type, g, fast_x, f.part, s);
 }
@@ -332,9 +339,9 @@ hipError_t linear_bwd(const gs_linear& p, const void* dy, int64_t lddy, const vo
 
 }  // namespace
 
-size_t linear_fwd_workspace(const gs_linear& p)
+size_t linear_fwd_workspace(const gs_linear& p, bool z)
 {
-    return fwd_space(nullptr, p.type, p.rows, p.n_in, p.n_out, !fast(p.w, p.ldw, p.n_in, p.type)).bytes;
+    return fwd_space(nullptr, p.type, p.rows, p.n_in, p.n_out, !fast(p.w, p.ldw, p.n_in, p.type), z).bytes;
 }
 
 size_t linear_bwd_workspace(const gs_linear& p, const void* dy, int64_t lddy, int dw_type)
@@ -345,7 +352,7 @@ size_t linear_bwd_workspace(const gs_linear& p, const void* dy, int64_t lddy, in
 
 size_t linear_workspace(int type, int act, int64_t rows, int64_t in, int64_t out, int dw_type)
 {
-    const size_t fwd = fwd_space(nullptr, type, rows, in, out, true).bytes;
+    const size_t fwd = fwd_space(nullptr, type, rows, in, out, true, true).bytes;
     return dw_type < 0 ? fwd : std::max(fwd, bwd_space(nullptr, type, act, rows, in, out, dw_type, true).bytes);
 }
 

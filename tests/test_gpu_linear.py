@@ -296,3 +296,18 @@ def test_forward_on_both_sides_of_the_narrow_form(rows, n_in, n_out, dtype):
     wide, s = strided(torch.zeros_like(d["r"]), 3), {k: strided(v, 5, 1) if v.dim() == 2 else v for k, v in d.items()}
     gs.gs_linear_fwd(s["x"], s["w"], d["bias"], wide, ws, act="tanh", residual=s["r"])
     check_forward(d, "tanh", wide)
+
+
+def test_forward_of_more_than_the_cache_holds():
+    # the widening layer that goes through tiles where it keeps z (rows compared in a few places)
+    d = make(1_100_003, 32, 64, torch.float16, 3)
+    y, z = (torch.full_like(d["r"], float("nan")) for _ in range(2))
+    ws = space(d["x"], d["w"], "relu", None)
+    gs.gs_linear_fwd(d["x"], d["w"], d["bias"], y, ws, act="relu", residual=d["r"], z=z)
+    plain = torch.full_like(y, float("nan"))
+    gs.gs_linear_fwd(d["x"], d["w"], d["bias"], plain, ws, act="relu", residual=d["r"])
+    for rows in (slice(0, 2000), slice(550_000, 552_000), slice(-2000, None)):
+        part = {k: v[rows] if v.shape[0] == 1_100_003 else v for k, v in d.items()}
+        check_forward(part, "relu", y[rows], z[rows])
+        check_forward(part, "relu", plain[rows])
+    assert torch.isfinite(y).all() and torch.isfinite(plain).all()
