@@ -90,9 +90,9 @@ struct LinearOps {
     static hipError_t skinny(const GemmArgs& g, hipStream_t s);
     static hipError_t slope(const SlopeArgs& p, hipStream_t s);
     static hipError_t join(const GemmArgs& g, float plane_scale, hipStream_t s);   // adds the parts up, with the epilogue
-    // dst[c][r] (ldd) = src[r][c], or dst[r][c]; zero in the padding columns
-    static hipError_t layout(const void* src, int64_t lds, int64_t rows, int64_t cols, bool transpose, void* dst,
-                             int64_t ldd, hipStream_t s);
+    // dst[c][r] (ldd) = src[r][c], r < 2^20; zero in the padding columns
+    static hipError_t transpose(const void* src, int64_t lds, int64_t rows, int64_t cols, void* dst, int64_t ldd,
+                                hipStream_t s);
 };
 
 }  // namespace gsr

@@ -48,8 +48,14 @@ struct TileRate {
 };
 constexpr TileRate kRates16[] = {{kTile256, 256, 1.1e9, 1.1e9, 11.0},
                                  {kTile128, 512, 0.85e9, 0.85e9, 6.0},
-                                 {kTile64, 1280, 0.58e9, 0.4e9, 4.0}};
+                                 {kTile64, 1280, 0.58e9, 0.25e9, 4.0}};
 constexpr TileRate kRates32[] = {{kTile128, 512, 0.131e9, 0.131e9, 6.0}, {kTile64, 1280, 0.125e9, 0.1e9, 4.0}};
+// An operand that goes through registers slows a product down (20,003 x 777 x 999 in binary16: 90 us against 79), which
+// is about what a copy of it with aligned rows would take.
+constexpr double kSlowRate = 0.85;
+// Sums from which the largest tile can pay: with short ones its workgroup, alone on its compute unit, hides neither its
+// first loads nor its results (7,133 x 48 x 1,424 in binary16: 16 us against 12 with the 128 x 128 tile).
+constexpr int64_t k256Len = 512;
 constexpr double kJoinUs = 4.0, kBytesUs = 5.0e6;   // of a join's launch, and of memory
 
 // The tile, and the split of its sum, that these rates make fastest: large tiles where they fill the compute units,
@@ -62,7 +68,7 @@ Plan plan_product(int type, int64_t rows, int64_t cols, int64_t len, int planes,
     const int count = type == GS_F32 ? 2 : 3;
     for (int k = 0; k < count; ++k) {
         const TileRate& r = rates[k];
-        if (r.tile == kTile256 && !fast_operand) continue;
+        if (r.tile == kTile256 && (!fast_operand || len < k256Len)) continue;
         const TileShape t = tile_shape(r.tile);
         const int64_t tiles = div_up(rows, t.bi) * div_up(cols, t.bj) * planes;
         const int64_t most = std::max<int64_t>(1, std::min(r.slots / std::min<int64_t>(tiles, r.slots), len / least));
@@ -71,7 +77,8 @@ Plan plan_product(int type, int64_t rows, int64_t cols, int64_t len, int planes,
             const int64_t splits = std::max<int64_t>(1, div_up(len, split_len));
             // a compute unit's share of the workgroups, one after the other, and what their rounds add
             const double share = (double)div_up(tiles * splits, kFillTiles);
-            double us = share * 2.0 * t.bi * t.bj * (double)split_len * kFillTiles / (share > 1 ? r.flop_us : r.flop_us_one) +
+            const double rate = (share > 1 ? r.flop_us : r.flop_us_one) * (fast_operand ? 1.0 : kSlowRate);
+            double us = share * 2.0 * t.bi * t.bj * (double)split_len * kFillTiles / rate +
                         (double)div_up(tiles * splits, r.slots) * r.round_us;
             if (splits * planes > 1) us += kJoinUs + 8.0 * planes * splits * (double)rows * (double)cols / kBytesUs;
             if (us < best_us) {
@@ -107,8 +114,29 @@ float plane_scale(int type) { return type == GS_F16 ? 1.f / 2048.f : 1.f / 256.f
 
 int slope_row_blocks(int type, int64_t rows, int64_t cols)
 {
-    const int64_t blocks_x = div_up(div_up(cols, vec(type)), 64);
-    return (int)std::max<int64_t>(1, std::min(div_up(kSlopeBlocks, blocks_x), div_up(rows, 32)));
+    // up to 64 lanes along a row, and two rows of a thread at least: few rows need the workgroups more than long
+    // columns (891 x 1,936 in binary16: 7 us against 14 with eight rows of a thread)
+    const int64_t vecs = div_up(cols, vec(type)), blocks_x = div_up(vecs, 64);
+    int64_t lanes = 1;
+    while (lanes < 64 && lanes < vecs) lanes <<= 1;
+    return (int)std::max<int64_t>(1, std::min(div_up(kSlopeBlocks, blocks_x), div_up(rows, 2 * kBlock / lanes)));
+}
+
+// dst [rows][padded cols]: a copy whose rows are whole aligned vectors, zero in the padding columns.
+template <typename T>
+hipError_t copy_rows(int type, const void* src, int64_t lds, int64_t rows, int64_t cols, void* dst, hipStream_t s)
+{
+    SlopeArgs a = {};
+    a.dy = src;
+    a.lddy = lds;
+    a.rows = rows;
+    a.cols = cols;
+    a.act = GS_ACT_NONE;
+    a.planes = 1;
+    a.out = dst;
+    a.ldo = padded(type, cols);
+    a.row_blocks = slope_row_blocks(type, rows, cols);
+    return LinearOps<T>::slope(a, s);
 }
 
 // Workspace: regions taken in order, 256-byte aligned.
@@ -218,7 +246,7 @@ template <typename T>
 hipError_t linear_fwd(const gs_linear& p, const void* residual, int64_t ldr, void* y, int64_t ldy, void* z,
                       int64_t ldz, void* ws, hipStream_t s)
 {
-    const bool copy_w = !fast(p.w, p.ldw, p.n_in, p.type);
+    const bool copy_w = !fast(p.w, p.ldw, p.n_in, p.type), fast_x = fast(p.x, p.ldx, p.n_in, p.type);
     const FwdSpace f = fwd_space(ws, p.type, p.rows, p.n_in, p.n_out, copy_w, z != nullptr);
     GemmArgs g = {};
     g.a = p.x;
@@ -228,7 +256,7 @@ hipError_t linear_fwd(const gs_linear& p, const void* residual, int64_t ldr, voi
     if (f.w) {
         g.b = f.w;
         g.ldb = padded(p.type, p.n_in);
-        const hipError_t e = LinearOps<T>::layout(p.w, p.ldw, p.n_out, p.n_in, false, f.w, g.ldb, s);
+        const hipError_t e = copy_rows<T>(p.type, p.w, p.ldw, p.n_out, p.n_in, f.w, s);
         if (e != hipSuccess) return e;
     }
     g.rows = p.rows;
@@ -242,7 +270,6 @@ hipError_t linear_fwd(const gs_linear& p, const void* residual, int64_t ldr, voi
     g.ldo = ldy;
     g.z = z;
     g.ldz = ldz;
-    const bool fast_x = fast(p.x, p.ldx, p.n_in, p.type);
     if constexpr (sizeof(T) == 2)
         if (p.rows > kSkinnyRows && narrow_forward(p.type, p.rows, p.n_in, p.n_out, z != nullptr))
             return NarrowOps<T>::forward(g, fast_x, (int)std::min<int64_t>(div_up(p.rows, 64), 4 * kFillTiles), s);
@@ -290,7 +317,7 @@ hipError_t linear_bwd(const gs_linear& p, const void* dy, int64_t lddy, const vo
     if (dx && p.rows > 0) {
         GemmArgs g = {};
         const int64_t ldt = padded(p.type, p.n_out);
-        e = LinearOps<T>::layout(p.w, p.ldw, p.n_out, p.n_in, true, b.wt, ldt, s);
+        e = LinearOps<T>::transpose(p.w, p.ldw, p.n_out, p.n_in, b.wt, ldt, s);
         if (e != hipSuccess) return e;
         g.a = dz;
         g.lda = ldo;
@@ -311,7 +338,7 @@ hipError_t linear_bwd(const gs_linear& p, const void* dy, int64_t lddy, const vo
         if (b.x) {
             x = b.x;
             ldx = padded(p.type, p.n_in);
-            e = LinearOps<T>::layout(p.x, p.ldx, p.rows, p.n_in, false, b.x, ldx, s);
+            e = copy_rows<T>(p.type, p.x, p.ldx, p.rows, p.n_in, b.x, s);
             if (e != hipSuccess) return e;
         }
         const bool fast_x = b.x || fast(x, ldx, p.n_in, p.type);
