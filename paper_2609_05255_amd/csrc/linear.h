@@ -45,20 +45,8 @@ struct SlopeArgs {
     int32_t row_blocks;
 };
 
-enum { kTile256 = 0, kTile128, kTile64, kTile128x64 };
-
-struct TileShape {
-    int bi, bj, threads;
-};
-inline TileShape tile_shape(int tile)
-{
-    switch (tile) {
-    case kTile256: return {256, 256, 512};
-    case kTile128: return {128, 128, 256};
-    case kTile64: return {64, 64, 256};
-    default: return {128, 64, 256};
-    }
-}
+// Tiles of a product (rows x columns; By: so many groups of waves share its sum)
+enum { kTile256 = 0, kTile128, kTile64, kTile64By4, kTile128x64 };
 
 // A narrow layer in one pass (narrow.h).
 struct NarrowArgs {

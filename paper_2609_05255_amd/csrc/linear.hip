@@ -39,23 +39,27 @@ struct Plan {
     int64_t split_len;
 };
 
-// What a tile's kernel reaches: the workgroups that run at once, the rate of all compute units with their share of them
-// and with one each, and the time that a round of them takes beside its products (first loads, results). Measured at
-// 8,192 x 4,096 values, sums of 64 to 8,192, in bfloat16 and fp32.
+// What a tile's kernel reaches: its rows and columns, the workgroups that run at once, the rate of all compute units with
+// their share of them and with one each, the time that a round of them takes beside its products (first loads,
+// results), and the shortest sum that it is taken for. Measured at 8,192 x 4,096 and at 1,024 to 4,096 x 1,024 values,
+// sums of 64 to 8,192, in bfloat16 and fp32.
+// The largest tile's workgroup, alone on its compute unit, hides neither its first loads nor its results: short sums
+// are left to smaller ones (7,133 x 48 x 1,424 in binary16: 16 us against 12).
 struct TileRate {
-    int tile, slots;
+    int tile, size, slots;
     double flop_us, flop_us_one, round_us;
+    int64_t least;
 };
-constexpr TileRate kRates16[] = {{kTile256, 256, 1.1e9, 1.1e9, 11.0},
-                                 {kTile128, 512, 0.85e9, 0.85e9, 6.0},
-                                 {kTile64, 1280, 0.58e9, 0.25e9, 4.0}};
-constexpr TileRate kRates32[] = {{kTile128, 512, 0.131e9, 0.131e9, 6.0}, {kTile64, 1280, 0.125e9, 0.1e9, 4.0}};
+constexpr TileRate kRates16[] = {{kTile256, 256, 256, 1.1e9, 1.1e9, 11.0, 512},
+                                 {kTile128, 128, 512, 0.85e9, 0.85e9, 6.0, 0},
+                                 {kTile64By4, 64, 256, 0.45e9, 0.45e9, 3.5, 1024},
+                                 {kTile64, 64, 1280, 0.58e9, 0.28e9, 4.0, 0}};
+constexpr TileRate kRates32[] = {{kTile128, 128, 512, 0.131e9, 0.112e9, 6.0, 0},
+                                 {kTile64By4, 64, 256, 0.105e9, 0.105e9, 3.5, 512},
+                                 {kTile64, 64, 1280, 0.115e9, 0.09e9, 4.0, 0}};
 // An operand that goes through registers slows a product down (20,003 x 777 x 999 in binary16: 90 us against 79), which
 // is about what a copy of it with aligned rows would take.
 constexpr double kSlowRate = 0.85;
-// Sums from which the largest tile can pay: with short ones its workgroup, alone on its compute unit, hides neither its
-// first loads nor its results (7,133 x 48 x 1,424 in binary16: 16 us against 12 with the 128 x 128 tile).
-constexpr int64_t k256Len = 512;
 constexpr double kJoinUs = 4.0, kBytesUs = 5.0e6;   // of a join's launch, and of memory
 
 // The tile, and the split of its sum, that these rates make fastest: large tiles where they fill the compute units,
@@ -65,20 +69,20 @@ Plan plan_product(int type, int64_t rows, int64_t cols, int64_t len, int planes,
     Plan best = {kTile64, 1, len};
     double best_us = 1e300;
     const TileRate* rates = type == GS_F32 ? kRates32 : kRates16;
-    const int count = type == GS_F32 ? 2 : 3;
+    const int count = type == GS_F32 ? 3 : 4;
     for (int k = 0; k < count; ++k) {
         const TileRate& r = rates[k];
-        if (r.tile == kTile256 && (!fast_operand || len < k256Len)) continue;
-        const TileShape t = tile_shape(r.tile);
-        const int64_t tiles = div_up(rows, t.bi) * div_up(cols, t.bj) * planes;
+        if (!fast_operand && (r.tile == kTile256 || r.tile == kTile64By4)) continue;
+        const int64_t tiles = div_up(rows, r.size) * div_up(cols, r.size) * planes;
         const int64_t most = std::max<int64_t>(1, std::min(r.slots / std::min<int64_t>(tiles, r.slots), len / least));
         for (int64_t want : {(int64_t)1, most}) {
             const int64_t split_len = std::max<int64_t>(64, div_up(div_up(len, want), 64) * 64);
             const int64_t splits = std::max<int64_t>(1, div_up(len, split_len));
+            if (split_len < r.least) continue;
             // a compute unit's share of the workgroups, one after the other, and what their rounds add
             const double share = (double)div_up(tiles * splits, kFillTiles);
             const double rate = (share > 1 ? r.flop_us : r.flop_us_one) * (fast_operand ? 1.0 : kSlowRate);
-            double us = share * 2.0 * t.bi * t.bj * (double)split_len * kFillTiles / rate +
+            double us = share * 2.0 * r.size * r.size * (double)split_len * kFillTiles / rate +
                         (double)div_up(tiles * splits, r.slots) * r.round_us;
             if (splits * planes > 1) us += kJoinUs + 8.0 * planes * splits * (double)rows * (double)cols / kBytesUs;
             if (us < best_us) {

@@ -269,6 +269,22 @@ def test_largest_tiles(rows, n_in, n_out, dtype):
         check_backward(d, name, dx, dw, db)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,n_in,n_out", [(1000, 2064, 968), (70, 1032, 2048), (2100, 1000, 960), (1025, 136, 520)])
+def test_sums_shared_within_a_workgroup(rows, n_in, n_out, dtype):
+    # products of about one tile for each compute unit, with long sums: parts of unequal length, ends inside a tile
+    d = make(rows, n_in, n_out, dtype, 23)
+    y, z = (torch.full_like(d["r"], float("nan")) for _ in range(2))
+    gs.gs_linear_fwd(d["x"], d["w"], d["bias"], y, space(d["x"], d["w"], "gelu", None), act="gelu", residual=d["r"], z=z)
+    check_forward(d, "gelu", y, z)
+    for name, dw_type in (("relu", dtype), ("silu", torch.float32)):
+        dx = torch.full_like(d["x"], float("nan"))
+        dw = torch.full(d["w"].shape, float("nan"), dtype=dw_type, device="cuda")
+        db = torch.full((n_out,), float("nan"), device="cuda")
+        gs.gs_linear_bwd(d["dy"], d["x"], d["w"], d["z"], dx, dw, db, space(d["x"], d["w"], name, dw_type), act=name)
+        check_backward(d, name, dx, dw, db)
+
+
 @pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
 @pytest.mark.parametrize("rows", [1, 63, 64, 65, 40_000])
 @pytest.mark.parametrize("n_in,n_out", [(64, 64), (65, 64), (64, 65), (128, 128), (129, 128), (128, 129), (17, 3), (3, 128)])
