@@ -724,24 +724,25 @@ __global__ __launch_bounds__(kBlock) void k_join(GemmArgs g, float plane_scale, 
     }
 }
 
-// dz (in planes) and its column sums; or a copy with aligned rows. A thread takes a vector of columns and every
-// gridDim.y * rows-per-workgroup'th row, kSlopeRows of them in flight together. Bound by memory: 137,428 x 256 in
-// bfloat16 with relu takes 45 us, 4.7 TB/s.
+// What a product's operands need before it, in one launch, as none of it needs the rest: dz (in planes) with its column
+// sums, W transposed, and a copy of a matrix with aligned rows. Workgroups of the two forms alternate in proportion, so
+// that dz's arithmetic (the slope of gelu) runs while W is on its way.
 constexpr float kBf16Plane = 1.f / 256.f, kF16Plane = 1.f / 2048.f;
-constexpr int kSlopeRows = 4;
+constexpr int kSlopeRows = 4, kTransposeTile = 64;
 
+// A thread takes a vector of columns and every row_blocks * slices'th row, kSlopeRows of them in flight together. Bound
+// by memory: 137,428 x 256 in bfloat16 with relu takes 45 us, 4.7 TB/s.
 template <typename T>
-__global__ __launch_bounds__(kBlock) void k_slope(SlopeArgs p, int lanes)
+__device__ __forceinline__ void slope_rows(const SlopeArgs& p, int64_t bx, int64_t by, char* lds)
 {
     constexpr int N = Vec<T>::N;
-    __shared__ float s[kBlock][N + 1];
-    const int lane = threadIdx.x % lanes, slice = threadIdx.x / lanes, slices = kBlock / lanes;
-    const int64_t c = ((int64_t)blockIdx.x * lanes + lane) * N;
+    const int lanes = p.lanes, lane = threadIdx.x % lanes, slice = threadIdx.x / lanes, slices = kBlock / lanes;
+    const int64_t c = (bx * lanes + lane) * N;
     const int64_t left = p.cols - c;
     float sum[N] = {};
-    const int64_t step = (int64_t)gridDim.y * slices;
+    const int64_t step = (int64_t)p.row_blocks * slices;
     if (c < p.ldo || left > 0)
-        for (int64_t r0 = (int64_t)blockIdx.y * slices + slice; r0 < p.rows; r0 += kSlopeRows * step) {
+        for (int64_t r0 = by * slices + slice; r0 < p.rows; r0 += kSlopeRows * step) {
             typename Vec<T>::Packed dy[kSlopeRows], zs[kSlopeRows];
 #pragma unroll
             for (int u = 0; u < kSlopeRows; ++u) {
@@ -782,47 +783,65 @@ __global__ __launch_bounds__(kBlock) void k_slope(SlopeArgs p, int lanes)
             }
         }
     if (!p.sums) return;
+    float(*s)[N + 1] = reinterpret_cast<float(*)[N + 1]>(lds);
 #pragma unroll
     for (int j = 0; j < N; ++j) s[threadIdx.x][j] = sum[j];
     __syncthreads();
     for (int k = threadIdx.x; k < lanes * N; k += kBlock) {
-        const int64_t col = (int64_t)blockIdx.x * lanes * N + k;
+        const int64_t col = bx * lanes * N + k;
         if (col >= p.cols) continue;
         float t = 0.f;
         for (int q = 0; q < slices; ++q) t += s[q * lanes + k / N][k % N];
-        p.sums[(int64_t)blockIdx.y * p.cols + col] = t;
+        p.sums[by * p.cols + col] = t;
     }
 }
 
 // dst[c][r] = src[r][c], 64 x 64 tiles through LDS, whole 16-byte vectors in and out. dst: aligned rows of ldd values, a
 // multiple of a vector, all written (padding: zero).
-constexpr int kLayoutTile = 64;
-
 template <typename T>
-__global__ __launch_bounds__(kBlock) void k_transpose(const T* __restrict__ src, int64_t lds, int64_t rows,
-                                                      int64_t cols, T* __restrict__ dst, int64_t ldd)
+__device__ __forceinline__ void transpose_tile(const TransposeArgs& p, int64_t bx, int64_t by, char* lds)
 {
-    constexpr int N = Vec<T>::N, kRowVecs = kLayoutTile / N;
-    __shared__ T t[kLayoutTile][kLayoutTile + 4 / sizeof(T)];
-    const int64_t r0 = (int64_t)blockIdx.y * kLayoutTile, c0 = (int64_t)blockIdx.x * kLayoutTile;
+    constexpr int N = Vec<T>::N, kRowVecs = kTransposeTile / N, kRow = kTransposeTile + 4 / sizeof(T);
+    T(*t)[kRow] = reinterpret_cast<T(*)[kRow]>(lds);
+    const int64_t r0 = by * kTransposeTile, c0 = bx * kTransposeTile;
 #pragma unroll
-    for (int q = threadIdx.x; q < kLayoutTile * kRowVecs; q += kBlock) {
+    for (int q = threadIdx.x; q < kTransposeTile * kRowVecs; q += kBlock) {
         const int r = q / kRowVecs, c = q % kRowVecs * N;
-        const typename Vec<T>::Packed v = load_any(src + (r0 + r) * lds + c0 + c, r0 + r < rows ? cols - c0 - c : 0);
+        const typename Vec<T>::Packed v =
+            load_any((const T*)p.src + (r0 + r) * p.lds + c0 + c, r0 + r < p.rows ? p.cols - c0 - c : 0);
 #pragma unroll
         for (int e = 0; e < N; ++e) t[r][c + e] = v[e];
     }
     __syncthreads();
 #pragma unroll
-    for (int q = threadIdx.x; q < kLayoutTile * kRowVecs; q += kBlock) {
+    for (int q = threadIdx.x; q < kTransposeTile * kRowVecs; q += kBlock) {
         // neighbouring lanes take neighbouring columns of the tile: LDS reads without conflicts
-        const int r = q % kLayoutTile, c = q / kLayoutTile * N;
-        if (c0 + r >= cols || r0 + c >= ldd) continue;
+        const int r = q % kTransposeTile, c = q / kTransposeTile * N;
+        if (c0 + r >= p.cols || r0 + c >= p.ldd) continue;
         typename Vec<T>::Packed v;
 #pragma unroll
         for (int e = 0; e < N; ++e) v[e] = t[c + e][r];
-        *reinterpret_cast<typename Vec<T>::Packed*>(dst + (c0 + r) * ldd + r0 + c) = v;
+        *reinterpret_cast<typename Vec<T>::Packed*>((T*)p.dst + (c0 + r) * p.ldd + r0 + c) = v;
     }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_prepare(PrepareArgs a)
+{
+    constexpr int kSums = kBlock * (Vec<T>::N + 1) * 4, kTile = kTransposeTile * (kTransposeTile * sizeof(T) + 4);
+    __shared__ __attribute__((aligned(16))) char lds[kSums > kTile ? kSums : kTile];
+    // of blocks 0 .. b, about b * tiles / all transpose
+    const uint64_t all = gridDim.x, b = blockIdx.x, tiles = a.tiles;
+    const int64_t before = b * tiles / all;
+    if ((int64_t)((b + 1) * tiles / all) > before) {
+        transpose_tile<T>(a.transpose, before % a.tiles_x, before / a.tiles_x, lds);
+        return;
+    }
+    int64_t k = (int64_t)b - before;
+    const bool copy = k >= a.slope_blocks;
+    if (copy) k -= a.slope_blocks;
+    const SlopeArgs& p = copy ? a.copy : a.slope;
+    slope_rows<T>(p, k / p.row_blocks, k % p.row_blocks, lds);
 }
 
 template <typename T, class S>
@@ -881,13 +900,28 @@ hipError_t LinearOps<T>::skinny(const GemmArgs& g, hipStream_t s)
 }
 
 template <typename T>
-hipError_t LinearOps<T>::slope(const SlopeArgs& p, hipStream_t s)
+hipError_t LinearOps<T>::prepare(const SlopeArgs* slope, const SlopeArgs* copy, const TransposeArgs* transpose,
+                                 hipStream_t s)
 {
-    const int64_t vecs = div_up(p.ldo > p.cols ? p.ldo : p.cols, Vec<T>::N);
-    int lanes = 1;
-    while (lanes < 64 && lanes < vecs) lanes <<= 1;
-    hipLaunchKernelGGL((k_slope<T>), dim3((unsigned)div_up(vecs, lanes), (unsigned)p.row_blocks), dim3(kBlock), 0, s, p,
-                       lanes);
+    PrepareArgs a = {};
+    auto blocks = [](const SlopeArgs& from, SlopeArgs& to) -> int64_t {
+        to = from;
+        const int64_t vecs = div_up(std::max(to.ldo, to.cols), Vec<T>::N);
+        to.lanes = 1;
+        while (to.lanes < 64 && to.lanes < vecs) to.lanes <<= 1;
+        return div_up(vecs, to.lanes) * to.row_blocks;
+    };
+    int64_t all = 0;
+    if (slope) all += a.slope_blocks = blocks(*slope, a.slope);
+    if (copy) all += blocks(*copy, a.copy);
+    if (transpose) {
+        a.transpose = *transpose;
+        a.tiles_x = div_up(transpose->cols, kTransposeTile);
+        a.tiles = a.tiles_x * div_up(std::max(transpose->rows, transpose->ldd), kTransposeTile);
+        all += a.tiles;
+    }
+    if (all == 0) return hipSuccess;
+    hipLaunchKernelGGL((k_prepare<T>), dim3((unsigned)all), dim3(kBlock), 0, s, a);
     return hipGetLastError();
 }
 
@@ -900,16 +934,6 @@ hipError_t LinearOps<T>::join(const GemmArgs& g, float plane_scale, hipStream_t 
     while (slices < 32 && places * slices < 1024 * kBlock && g.splits >= 8 * slices) slices *= 2;
     hipLaunchKernelGGL((k_join<T>), dim3((unsigned)div_up(places, kBlock / slices)), dim3(kBlock), 0, s, g, plane_scale,
                        slices);
-    return hipGetLastError();
-}
-
-template <typename T>
-hipError_t LinearOps<T>::transpose(const void* src, int64_t lds, int64_t rows, int64_t cols, void* dst, int64_t ldd,
-                                   hipStream_t s)
-{
-    hipLaunchKernelGGL((k_transpose<T>),
-                       dim3((unsigned)div_up(cols, kLayoutTile), (unsigned)div_up(std::max(rows, ldd), kLayoutTile)),
-                       dim3(kBlock), 0, s, (const T*)src, lds, rows, cols, (T*)dst, ldd);
     return hipGetLastError();
 }
 

@@ -43,6 +43,21 @@ struct SlopeArgs {
     int64_t plane_stride;
     float* sums;                   // [workgroups along the rows][cols], or NULL
     int32_t row_blocks;
+    int32_t lanes;                 // of a workgroup along a row (set by prepare)
+};
+
+// dst[c][r] (ldd) = src[r][c] (lds), zero in the padding columns.
+struct TransposeArgs {
+    const void* src;
+    int64_t lds, rows, cols;
+    void* dst;
+    int64_t ldd;
+};
+
+struct PrepareArgs {
+    SlopeArgs slope, copy;
+    TransposeArgs transpose;
+    int64_t slope_blocks, tiles_x, tiles;
 };
 
 // Tiles of a product (rows x columns; By: so many groups of waves share its sum)
@@ -76,11 +91,10 @@ struct LinearOps {
     static hipError_t gemm_nt(int tile, bool fast_a, const GemmArgs& g, hipStream_t s);
     static hipError_t gemm_tt(int tile, bool fast_b, const GemmArgs& g, hipStream_t s);
     static hipError_t skinny(const GemmArgs& g, hipStream_t s);
-    static hipError_t slope(const SlopeArgs& p, hipStream_t s);
+    // those that are wanted (not NULL) of dz, a matrix copied (dz without an activation) and W transposed, in one launch
+    static hipError_t prepare(const SlopeArgs* slope, const SlopeArgs* copy, const TransposeArgs* transpose,
+                              hipStream_t s);
     static hipError_t join(const GemmArgs& g, float plane_scale, hipStream_t s);   // adds the parts up, with the epilogue
-    // dst[c][r] (ldd) = src[r][c], r < 2^20; zero in the padding columns
-    static hipError_t transpose(const void* src, int64_t lds, int64_t rows, int64_t cols, void* dst, int64_t ldd,
-                                hipStream_t s);
 };
 
 }  // namespace gsr

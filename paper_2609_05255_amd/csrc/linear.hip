@@ -127,8 +127,7 @@ int slope_row_blocks(int type, int64_t rows, int64_t cols)
 }
 
 // dst [rows][padded cols]: a copy whose rows are whole aligned vectors, zero in the padding columns.
-template <typename T>
-hipError_t copy_rows(int type, const void* src, int64_t lds, int64_t rows, int64_t cols, void* dst, hipStream_t s)
+SlopeArgs copy_of(int type, const void* src, int64_t lds, int64_t rows, int64_t cols, void* dst)
 {
     SlopeArgs a = {};
     a.dy = src;
@@ -140,7 +139,7 @@ hipError_t copy_rows(int type, const void* src, int64_t lds, int64_t rows, int64
     a.out = dst;
     a.ldo = padded(type, cols);
     a.row_blocks = slope_row_blocks(type, rows, cols);
-    return LinearOps<T>::slope(a, s);
+    return a;
 }
 
 // Workspace: regions taken in order, 256-byte aligned.
@@ -260,7 +259,8 @@ hipError_t linear_fwd(const gs_linear& p, const void* residual, int64_t ldr, voi
     if (f.w) {
         g.b = f.w;
         g.ldb = padded(p.type, p.n_in);
-        const hipError_t e = copy_rows<T>(p.type, p.w, p.ldw, p.n_out, p.n_in, f.w, s);
+        const SlopeArgs copy = copy_of(p.type, p.w, p.ldw, p.n_out, p.n_in, f.w);
+        const hipError_t e = LinearOps<T>::prepare(nullptr, &copy, nullptr, s);
         if (e != hipSuccess) return e;
     }
     g.rows = p.rows;
@@ -297,32 +297,33 @@ hipError_t linear_bwd(const gs_linear& p, const void* dy, int64_t lddy, const vo
         }
     const int64_t ldo = need_dz ? padded(p.type, p.n_out) : lddy;
     const void* dz = need_dz ? b.dz : dy;
-    hipError_t e = hipSuccess;
+    const int64_t ldt = padded(p.type, p.n_out);
+    SlopeArgs slope = {}, copy = {};
     if (need_dz || db) {
-        SlopeArgs a = {};
-        a.dy = dy;
-        a.lddy = lddy;
-        a.z = z;
-        a.ldz = ldz;
-        a.rows = p.rows;
-        a.cols = p.n_out;
-        a.act = p.act;
-        a.planes = planes;
-        a.out = need_dz ? b.dz : nullptr;
-        a.ldo = need_dz ? ldo : 0;
-        a.plane_stride = p.rows * ldo;
-        a.row_blocks = slope_row_blocks(p.type, p.rows, p.n_out);
-        a.sums = db ? (a.row_blocks == 1 ? db : b.sums) : nullptr;
-        e = LinearOps<T>::slope(a, s);
-        if (e == hipSuccess && db && a.row_blocks > 1)
-            e = launch_column_sum(b.sums, a.row_blocks, p.n_out, p.n_out, db, nullptr, s);
-        if (e != hipSuccess) return e;
+        slope.dy = dy;
+        slope.lddy = lddy;
+        slope.z = z;
+        slope.ldz = ldz;
+        slope.rows = p.rows;
+        slope.cols = p.n_out;
+        slope.act = p.act;
+        slope.planes = planes;
+        slope.out = need_dz ? b.dz : nullptr;
+        slope.ldo = need_dz ? ldo : 0;
+        slope.plane_stride = p.rows * ldo;
+        slope.row_blocks = slope_row_blocks(p.type, p.rows, p.n_out);
+        slope.sums = db ? (slope.row_blocks == 1 ? db : b.sums) : nullptr;
     }
-    if (dx && p.rows > 0) {
+    const bool copy_x = dw && b.x, want_dx = dx && p.rows > 0;
+    if (copy_x) copy = copy_of(p.type, p.x, p.ldx, p.rows, p.n_in, b.x);
+    const TransposeArgs transpose = {p.w, p.ldw, p.n_out, p.n_in, b.wt, ldt};
+    hipError_t e = LinearOps<T>::prepare(need_dz || db ? &slope : nullptr, copy_x ? &copy : nullptr,
+                                         want_dx ? &transpose : nullptr, s);
+    if (e == hipSuccess && db && slope.row_blocks > 1)
+        e = launch_column_sum(b.sums, slope.row_blocks, p.n_out, p.n_out, db, nullptr, s);
+    if (e != hipSuccess) return e;
+    if (want_dx) {
         GemmArgs g = {};
-        const int64_t ldt = padded(p.type, p.n_out);
-        e = LinearOps<T>::transpose(p.w, p.ldw, p.n_out, p.n_in, b.wt, ldt, s);
-        if (e != hipSuccess) return e;
         g.a = dz;
         g.lda = ldo;
         g.b = b.wt;
@@ -337,15 +338,9 @@ hipError_t linear_bwd(const gs_linear& p, const void* dy, int64_t lddy, const vo
     }
     if (dw) {
         GemmArgs g = {};
-        const void* x = p.x;
-        int64_t ldx = p.ldx;
-        if (b.x) {
-            x = b.x;
-            ldx = padded(p.type, p.n_in);
-            e = copy_rows<T>(p.type, p.x, p.ldx, p.rows, p.n_in, b.x, s);
-            if (e != hipSuccess) return e;
-        }
-        const bool fast_x = b.x || fast(x, ldx, p.n_in, p.type);
+        const void* x = copy_x ? b.x : p.x;
+        const int64_t ldx = copy_x ? padded(p.type, p.n_in) : p.ldx;
+        const bool fast_x = copy_x || fast(x, ldx, p.n_in, p.type);
         const Plan plan = plan_tt(p.type, p.n_out, p.n_in, p.rows, planes, fast_x);
         g.a = dz;
         g.lda = ldo;
