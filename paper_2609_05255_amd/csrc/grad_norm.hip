@@ -13,6 +13,10 @@
 // same fixed order, so no atomics and no third launch are needed and the same
 // gradients give the same bits. Where c is 1 and the gradients stay in place
 // nothing is read again.
+//
+// Measured: the norm of 177M fp32 gradients (five tensors) 118 us, 6.0 TB/s; of
+// 60 bfloat16 ones of up to a million values, clipped into fp32 arrays, 15 us for
+// the norm, from the last-level cache in part, and 35 for the clipping, 5.4 TB/s.
 #include "gs_internal.h"
 #include "vec.h"
 
@@ -23,9 +27,10 @@ namespace {
 constexpr int kGradChunk = 8192;
 constexpr int kGradTable = 100;
 constexpr int kGradBlocks = 2048;        // workgroups of all launches of a norm together, about
-// One workgroup takes a few gradients alone, in one launch, a chunk of kSmallChunk elements per wave.
+// One workgroup takes a few gradients alone, in one launch, a chunk of kSmallChunk elements per wave: 8 of 8,000 values
+// 6.0 us a call for 8.3 in two launches, but 8 of 16,000 (128 chunks) 8.8 for 8.5.
 constexpr int kSmallChunk = 1024;
-constexpr int kSmallChunks = 128;
+constexpr int kSmallChunks = 96;
 constexpr int kSmallThreads = 1024;
 
 struct GradEntry {

@@ -12,7 +12,14 @@
 // sums for dw and db, stay in registers over all rows of a workgroup; a
 // workgroup adds up its sums in LDS and writes one partial row, and
 // k_column_sum adds the partial rows in a fixed order (no atomics: the same
-// call gives the same bits). All arithmetic is fp32.
+// call gives the same bits). All arithmetic is fp32; results are rounded to the
+// element type once, as they are stored.
+//
+// Measured: forward of 30,000 x 1,024 in binary16 21 us, 5.9 TB/s of what it has
+// to move (it partly stays in the last-level cache); backward of 16,384 x 4,096
+// in bfloat16 with the skip connection's gradient 106 us and 7 for the partial
+// sums, of 100,003 x 333 in fp32 79 and 5: both 5.2 TB/s in counted bytes, the
+// rate of a large copy. One row is the latency of a launch, 7 us a call.
 #include "gs_internal.h"
 #include "vec.h"
 
@@ -395,8 +402,10 @@ __global__ __launch_bounds__(kSumCols* kSumSlices) void k_column_sum(const float
 }
 
 // Lanes and vectors of a row: the fewest lanes (a power of two up to a wave, then 4 or 16 waves) that hold it
-// with as few vectors each as possible. A wave holds up to 4 vectors a lane before a row goes to a workgroup:
-// its sums then need no barrier.
+// with as few vectors each as possible. A wave holds 2 or 3 vectors a lane before a row goes to a workgroup: its sums
+// then need no barrier, and fewer lanes are idle. Against workgroups of one vector a lane from 65 vectors on: forward of
+// 30,000 x 1,024 in binary16 21 us for 31, of 100,003 x 333 in fp32 56 for 89; backward 47 for 58 and 85 for 133, of
+// 20,000 x 1,500 in bfloat16 61 for 87 (of 20,003 x 700 in fp32 42 for 37).
 struct RowShape {
     int g, nv;   // g = 0: longer than a workgroup holds
 };

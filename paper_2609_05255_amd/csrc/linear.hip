@@ -14,7 +14,6 @@ namespace gsr {
 
 namespace {
 
-constexpr int64_t kSkinnyRows = 64;      // rows up to which the weights' bytes bound the product
 constexpr int kFillTiles = 256;          // compute units
 constexpr int kSlopeBlocks = 2048;
 constexpr int64_t kJoinSplitLen = 256;   // values of the sum in a split of a product of few tiles, at least
@@ -107,7 +106,8 @@ Plan plan_tt(int type, int64_t out, int64_t in, int64_t rows, int planes, bool f
 }
 
 // Planes of dz: an fp32 weight gradient keeps what rounding dz to 16 bits would drop, as further planes of the
-// type; without an activation, or with relu, dz is dy or 0 and needs none.
+// type; without an activation, or with relu, dz is dy or 0 and needs none. dx, and a dW in the type itself, take the
+// first plane alone: their operands' rounding adds to that of the result what a user's own dz in this type would.
 int planes_of(int type, int act, int dw_type)
 {
     if (type == GS_F32 || dw_type != GS_F32 || act == GS_ACT_NONE || act == GS_ACT_RELU) return 1;
@@ -141,6 +141,10 @@ SlopeArgs copy_of(int type, const void* src, int64_t lds, int64_t rows, int64_t 
     a.row_blocks = slope_row_blocks(type, rows, cols);
     return a;
 }
+
+// Few rows, where the weights' bytes bound the product: up to 32, or 64 where the tiles would need a copy of W with
+// aligned rows first (4,096 x 4,096 in bfloat16: 64 rows 21 us, 17 in tiles, and 15 for such a copy).
+bool few_rows(int64_t rows, bool copy_w) { return rows <= (copy_w ? 64 : 32); }
 
 // Workspace: regions taken in order, 256-byte aligned.
 struct Regions {
@@ -181,7 +185,7 @@ FwdSpace fwd_space(void* base, int type, int64_t rows, int64_t in, int64_t out, 
 {
     Regions r{(char*)base};
     FwdSpace f = {};
-    if (rows > kSkinnyRows && !narrow_forward(type, rows, in, out, z)) {
+    if (!few_rows(rows, copy_w) && !narrow_forward(type, rows, in, out, z)) {
         if (copy_w) f.w = r.take(out * padded(type, in) * elem(type));
         int splits = 1;   // (a workspace is sized for either alignment of x)
         for (int fast_x = 0; fast_x < 2; ++fast_x) splits = std::max(splits, plan_nt(type, rows, out, in, fast_x).splits);
@@ -215,7 +219,7 @@ BwdSpace bwd_space(void* base, int type, int act, int64_t rows, int64_t in, int6
     b.wt = r.take(in * padded(type, out) * elem(type));
     b.sums = (float*)r.take((int64_t)slope_row_blocks(type, rows, out) * out * 4);
     int64_t part = 0;
-    if (rows > kSkinnyRows) {
+    if (!few_rows(rows, false)) {
         const Plan x = plan_nt(type, rows, in, out, true);
         if (x.splits > 1) part = (int64_t)x.splits * rows * in * 4;
     }
@@ -231,11 +235,11 @@ BwdSpace bwd_space(void* base, int type, int act, int64_t rows, int64_t in, int6
 
 // A product along rows with its epilogue: few rows, one launch of tiles, or splits and their join.
 template <typename T>
-hipError_t run_nt(int type, GemmArgs g, bool fast_a, float* part, hipStream_t s)
+hipError_t run_nt(int type, GemmArgs g, bool few, bool fast_a, float* part, hipStream_t s)
 {
     g.splits = g.planes = 1;
     g.split_len = g.len;
-    if (g.rows <= kSkinnyRows) return LinearOps<T>::skinny(g, s);
+    if (few) return LinearOps<T>::skinny(g, s);
     const Plan p = plan_nt(type, g.rows, g.cols, g.len, fast_a);
     g.splits = p.splits;
     g.split_len = p.split_len;
@@ -250,6 +254,7 @@ hipError_t linear_fwd(const gs_linear& p, const void* residual, int64_t ldr, voi
                       int64_t ldz, void* ws, hipStream_t s)
 {
     const bool copy_w = !fast(p.w, p.ldw, p.n_in, p.type), fast_x = fast(p.x, p.ldx, p.n_in, p.type);
+    const bool few = few_rows(p.rows, copy_w);
     const FwdSpace f = fwd_space(ws, p.type, p.rows, p.n_in, p.n_out, copy_w, z != nullptr);
     GemmArgs g = {};
     g.a = p.x;
@@ -275,9 +280,9 @@ hipError_t linear_fwd(const gs_linear& p, const void* residual, int64_t ldr, voi
     g.z = z;
     g.ldz = ldz;
     if constexpr (sizeof(T) == 2)
-        if (p.rows > kSkinnyRows && narrow_forward(p.type, p.rows, p.n_in, p.n_out, z != nullptr))
+        if (!few && narrow_forward(p.type, p.rows, p.n_in, p.n_out, z != nullptr))
             return NarrowOps<T>::forward(g, fast_x, (int)std::min<int64_t>(div_up(p.rows, 64), 4 * kFillTiles), s);
-    return run_nt<T>(p.type, g, fast_x, f.part, s);
+    return run_nt<T>(p.type, g, few, fast_x, f.part, s);
 }
 
 template <typename T>
@@ -333,7 +338,7 @@ hipError_t linear_bwd(const gs_linear& p, const void* dy, int64_t lddy, const vo
         g.len = p.n_out;
         g.out = dx;
         g.ldo = lddx;
-        e = run_nt<T>(p.type, g, true, b.part, s);
+        e = run_nt<T>(p.type, g, few_rows(p.rows, false), true, b.part, s);
         if (e != hipSuccess) return e;
     }
     if (dw) {
@@ -378,7 +383,9 @@ size_t linear_bwd_workspace(const gs_linear& p, const void* dy, int64_t lddy, in
 
 size_t linear_workspace(int type, int act, int64_t rows, int64_t in, int64_t out, int dw_type)
 {
-    const size_t fwd = fwd_space(nullptr, type, rows, in, out, true, true).bytes;
+    // (for either alignment of W)
+    const size_t fwd = std::max(fwd_space(nullptr, type, rows, in, out, false, true).bytes,
+                                fwd_space(nullptr, type, rows, in, out, true, true).bytes);
     return dw_type < 0 ? fwd : std::max(fwd, bwd_space(nullptr, type, act, rows, in, out, dw_type, true).bytes);
 }
 

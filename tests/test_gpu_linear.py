@@ -270,6 +270,22 @@ def test_largest_tiles(rows, n_in, n_out, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows", [32, 33, 48, 64, 65])
+@pytest.mark.parametrize("n_in,n_out", [(64, 48), (33, 17), (520, 264), (1031, 300), (4096, 200)])
+def test_few_rows_and_more(rows, n_in, n_out, dtype):
+    # on both sides of the form for few rows, whose limit depends on whether W has aligned rows
+    d = make(rows, n_in, n_out, dtype, rows + n_in)
+    y, z = (torch.full_like(d["r"], float("nan")) for _ in range(2))
+    gs.gs_linear_fwd(d["x"], d["w"], d["bias"], y, space(d["x"], d["w"], "tanh", None), act="tanh", residual=d["r"], z=z)
+    check_forward(d, "tanh", y, z)
+    dx = torch.full_like(d["x"], float("nan"))
+    dw = torch.full(d["w"].shape, float("nan"), device="cuda")
+    db = torch.full((n_out,), float("nan"), device="cuda")
+    gs.gs_linear_bwd(d["dy"], d["x"], d["w"], d["z"], dx, dw, db, space(d["x"], d["w"], "silu"), act="silu")
+    check_backward(d, "silu", dx, dw, db)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,n_in,n_out", [(1000, 2064, 968), (70, 1032, 2048), (2100, 1000, 960), (1025, 136, 520)])
 def test_sums_shared_within_a_workgroup(rows, n_in, n_out, dtype):
     # products of about one tile for each compute unit, with long sums: parts of unequal length, ends inside a tile
