@@ -337,8 +337,7 @@ __global__ __launch_bounds__(S::THREADS * S::WAYS) void k_gemm(GemmArgs g)
     int64_t ti, tj;
     tile_of(blockIdx.x, tiles_i, tiles_j, &ti, &tj);
     const int64_t i0 = ti * BI, j0 = tj * BJ;
-    const int part = blockIdx.y, plane = part / g.splits, split = part - plane * g.splits;
-    int64_t c_begin = split * g.split_len;
+    int64_t c_begin = blockIdx.y * g.split_len;
     int64_t c_end = c_begin + g.split_len < g.len ? c_begin + g.split_len : g.len;
     int steps = c_end > c_begin ? (int)((c_end - c_begin + kBK - 1) / kBK) : 0;
     if constexpr (S::WAYS > 1) {
@@ -347,7 +346,6 @@ __global__ __launch_bounds__(S::THREADS * S::WAYS) void k_gemm(GemmArgs g)
         c_begin += group * ((int64_t)steps * kBK);
         c_end = c_begin + (int64_t)steps * kBK < c_end ? c_begin + (int64_t)steps * kBK : c_end;
     }
-    const T* a = (const T*)g.a + plane * g.plane_stride;
     const T* b = (const T*)g.b;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x % S::THREADS >> 6);
     const int wi = (wave / WJ) * WR, wj = (wave % WJ) * WC;
@@ -372,117 +370,127 @@ __global__ __launch_bounds__(S::THREADS * S::WAYS) void k_gemm(GemmArgs g)
 #pragma unroll
                 for (int q = 0; q < FJ; ++q) acc[p][q] = Mm::mma(fb[s][q], fa[s][p], acc[p][q]);
     };
-    if constexpr (S::FAST) {
-        constexpr int kLoads = TA::kPasses + TB::kPasses;   // of a thread per tile
-        typename TA::Source sa(a, g.lda, i0, g.rows, c_begin, c_end);
-        typename TB::Source sb(b, g.ldb, j0, g.cols, c_begin, c_end);
-        if constexpr (S::AHEAD) {
-            // Three tiles of A and two of B in LDS, each of two halves along the sum. While a half's MFMAs run, the next
-            // half's fragments are read; A's tile t + 2 is loaded under the first half of tile t, B's under the second,
-            // where tile t's own fragments have all been read. Behind each row of MFMAs stand a few reads and loads:
-            // issued together they would hold the wave, and the MFMAs behind them, until the memory pipe takes them.
-            constexpr int kHalf = kSteps / 2, kRows = kHalf * FI;   // rows of MFMAs in a half
-            static_assert(kRows == 2 * TA::kPasses && kRows == 2 * TB::kPasses &&
-                              kHalf * (FI + FJ) <= 2 * (kRows - 1), "the loads and reads of a half fit its rows");
-            char* a_lds[3] = {lds, lds + TA::kBytes, lds + 2 * TA::kBytes};
-            char* b_lds[2] = {lds + 3 * TA::kBytes, lds + 3 * TA::kBytes + TB::kBytes};
-            Frag fa[2][kHalf][FI], fb[2][kHalf][FJ];
-            for (int k = 0; k < 2; ++k) {
-                sa.load(a_lds[k]);
-                sb.load(b_lds[k]);
+    // A's planes, the least significant one first, whose sums are scaled into the next one's
+    for (int plane = (TT ? g.planes : 1) - 1; plane >= 0; --plane) {
+        const T* a = (const T*)g.a + (TT ? plane * g.plane_stride : 0);
+        if constexpr (S::FAST) {
+            constexpr int kLoads = TA::kPasses + TB::kPasses;   // of a thread per tile
+            typename TA::Source sa(a, g.lda, i0, g.rows, c_begin, c_end);
+            typename TB::Source sb(b, g.ldb, j0, g.cols, c_begin, c_end);
+            if constexpr (S::AHEAD) {
+                // Three tiles of A and two of B in LDS, each of two halves along the sum. While a half's MFMAs run, the next
+                // half's fragments are read; A's tile t + 2 is loaded under the first half of tile t, B's under the second,
+                // where tile t's own fragments have all been read. Behind each row of MFMAs stand a few reads and loads:
+                // issued together they would hold the wave, and the MFMAs behind them, until the memory pipe takes them.
+                constexpr int kHalf = kSteps / 2, kRows = kHalf * FI;   // rows of MFMAs in a half
+                static_assert(kRows == 2 * TA::kPasses && kRows == 2 * TB::kPasses &&
+                                  kHalf * (FI + FJ) <= 2 * (kRows - 1), "the loads and reads of a half fit its rows");
+                char* a_lds[3] = {lds, lds + TA::kBytes, lds + 2 * TA::kBytes};
+                char* b_lds[2] = {lds + 3 * TA::kBytes, lds + 3 * TA::kBytes + TB::kBytes};
+                Frag fa[2][kHalf][FI], fb[2][kHalf][FJ];
+                for (int k = 0; k < 2; ++k) {
+                    sa.load(a_lds[k]);
+                    sb.load(b_lds[k]);
+                }
+                wait_loads<kLoads>();
+                barrier();
+                auto fetch = [&](const char* from_a, const char* from_b, int half, int k, Frag(&na)[kHalf][FI],
+                                 Frag(&nb)[kHalf][FJ]) {
+                    const int s = k / (FI + FJ), f = k % (FI + FJ);
+                    if (s >= kHalf) return;
+                    if (f < FJ)
+                        nb[s][f] = TB::frag(from_b, wj, f, half * kHalf + s);
+                    else
+                        na[s][f - FJ] = TA::frag(from_a, wi, f - FJ, half * kHalf + s);
+                };
+#pragma unroll
+                for (int k = 0; k < 2 * kRows; ++k) fetch(a_lds[0], b_lds[0], 0, k, fa[0], fb[0]);
+                auto half = [&](const Frag(&ma)[kHalf][FI], const Frag(&mb)[kHalf][FJ], const char* from_a,
+                                const char* from_b, int h, Frag(&na)[kHalf][FI], Frag(&nb)[kHalf][FJ], auto load) {
+#pragma unroll
+                    for (int u = 0; u < kRows; ++u) {
+                        const int s = u / FI, p = u % FI;
+#pragma unroll
+                        for (int q = 0; q < FJ; ++q) acc[p][q] = Mm::mma(mb[s][q], ma[s][p], acc[p][q]);
+                        __builtin_amdgcn_sched_barrier(0);
+                        fetch(from_a, from_b, h, 2 * u, na, nb);
+                        fetch(from_a, from_b, h, 2 * u + 1, na, nb);
+                        if (u % 2 == 0) load(u / 2);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                };
+                for (int t = 0; t < steps; ++t) {
+                    half(fa[0], fb[0], a_lds[0], b_lds[0], 1, fa[1], fb[1], [&](int k) { sa.pass(a_lds[2], k); });
+                    sa.advance();
+                    __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): this wave has tile t's fragments
+                    wait_loads<TA::kPasses>();
+                    barrier();                            // as all have, and tile t + 1 is here
+                    half(fa[1], fb[1], a_lds[1], b_lds[1], 0, fa[0], fb[0], [&](int k) { sb.pass(b_lds[0], k); });
+                    sb.advance();
+                    char* x = a_lds[0];
+                    a_lds[0] = a_lds[1];
+                    a_lds[1] = a_lds[2];
+                    a_lds[2] = x;
+                    x = b_lds[0];
+                    b_lds[0] = b_lds[1];
+                    b_lds[1] = x;
+                }
+            } else {
+                Frag fa[kSteps][FI], fb[kSteps][FJ];
+                sa.load(lds);
+                sb.load(lds + TA::kBytes);
+                for (int t = 0; t < steps; ++t) {
+                    char* cur = lds + (t & 1) * kTileBytes;
+                    char* nxt = lds + ((t + 1) & 1) * kTileBytes;
+                    wait_loads<0>();
+                    barrier();   // tile t is here, and all waves are done with tile t - 1
+                    if (t + 1 < steps) {
+                        sa.load(nxt);
+                        sb.load(nxt + TA::kBytes);
+                    }
+                    read(cur, fa, fb);
+                    multiply(fa, fb);
+                }
             }
-            wait_loads<kLoads>();
-            barrier();
-            auto fetch = [&](const char* from_a, const char* from_b, int half, int k, Frag(&na)[kHalf][FI],
-                             Frag(&nb)[kHalf][FJ]) {
-                const int s = k / (FI + FJ), f = k % (FI + FJ);
-                if (s >= kHalf) return;
-                if (f < FJ)
-                    nb[s][f] = TB::frag(from_b, wj, f, half * kHalf + s);
-                else
-                    na[s][f - FJ] = TA::frag(from_a, wi, f - FJ, half * kHalf + s);
-            };
-#pragma unroll
-            for (int k = 0; k < 2 * kRows; ++k) fetch(a_lds[0], b_lds[0], 0, k, fa[0], fb[0]);
-            auto half = [&](const Frag(&ma)[kHalf][FI], const Frag(&mb)[kHalf][FJ], const char* from_a,
-                            const char* from_b, int h, Frag(&na)[kHalf][FI], Frag(&nb)[kHalf][FJ], auto load) {
-#pragma unroll
-                for (int u = 0; u < kRows; ++u) {
-                    const int s = u / FI, p = u % FI;
-#pragma unroll
-                    for (int q = 0; q < FJ; ++q) acc[p][q] = Mm::mma(mb[s][q], ma[s][p], acc[p][q]);
-                    __builtin_amdgcn_sched_barrier(0);
-                    fetch(from_a, from_b, h, 2 * u, na, nb);
-                    fetch(from_a, from_b, h, 2 * u + 1, na, nb);
-                    if (u % 2 == 0) load(u / 2);
-                    __builtin_amdgcn_sched_barrier(0);
+            wait_loads<0>();   // nothing may still write to LDS
+        } else {
+            using TR = std::conditional_t<kAsyncA, TB, TA>;   // the operand that goes through registers
+            Frag fa[kSteps][FI], fb[kSteps][FJ];
+            typename TR::Packed regs[TR::kPasses];
+            typename TA::Source sa(a, g.lda, i0, g.rows, c_begin, c_end);
+            typename TB::Source sb(b, g.ldb, j0, g.cols, c_begin, c_end);
+            auto fetch = [&](char* to, int64_t c0) {
+                if constexpr (kAsyncA) {
+                    sa.load(to);
+                    TB::load_regs(regs, b, g.ldb, j0, g.cols, c0, c_end);
+                } else {
+                    TA::load_regs(regs, a, g.lda, i0, g.rows, c0, c_end);
+                    sb.load(to + TA::kBytes);
                 }
             };
-            for (int t = 0; t < steps; ++t) {
-                half(fa[0], fb[0], a_lds[0], b_lds[0], 1, fa[1], fb[1], [&](int k) { sa.pass(a_lds[2], k); });
-                sa.advance();
-                __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): this wave has tile t's fragments
-                wait_loads<TA::kPasses>();
-                barrier();                            // as all have, and tile t + 1 is here
-                half(fa[1], fb[1], a_lds[1], b_lds[1], 0, fa[0], fb[0], [&](int k) { sb.pass(b_lds[0], k); });
-                sb.advance();
-                char* x = a_lds[0];
-                a_lds[0] = a_lds[1];
-                a_lds[1] = a_lds[2];
-                a_lds[2] = x;
-                x = b_lds[0];
-                b_lds[0] = b_lds[1];
-                b_lds[1] = x;
+            auto settle = [&](char* to) { TR::store_regs(to + (kAsyncA ? TA::kBytes : 0), regs); };
+            if (steps > 0) {
+                fetch(lds, c_begin);
+                settle(lds);
             }
-        } else {
-            Frag fa[kSteps][FI], fb[kSteps][FJ];
-            sa.load(lds);
-            sb.load(lds + TA::kBytes);
             for (int t = 0; t < steps; ++t) {
-                char* cur = lds + (t & 1) * kTileBytes;
                 char* nxt = lds + ((t + 1) & 1) * kTileBytes;
                 wait_loads<0>();
-                barrier();   // tile t is here, and all waves are done with tile t - 1
-                if (t + 1 < steps) {
-                    sa.load(nxt);
-                    sb.load(nxt + TA::kBytes);
-                }
-                read(cur, fa, fb);
+                __syncthreads();   // tile t has arrived, and the other is no longer read
+                if (t + 1 < steps) fetch(nxt, c_begin + (int64_t)(t + 1) * kBK);
+                read(lds + (t & 1) * kTileBytes, fa, fb);
                 multiply(fa, fb);
+                if (t + 1 < steps) settle(nxt);
             }
         }
-        wait_loads<0>();   // nothing may still write to LDS
-    } else {
-        using TR = std::conditional_t<kAsyncA, TB, TA>;   // the operand that goes through registers
-        Frag fa[kSteps][FI], fb[kSteps][FJ];
-        typename TR::Packed regs[TR::kPasses];
-        typename TA::Source sa(a, g.lda, i0, g.rows, c_begin, c_end);
-        typename TB::Source sb(b, g.ldb, j0, g.cols, c_begin, c_end);
-        auto fetch = [&](char* to, int64_t c0) {
-            if constexpr (kAsyncA) {
-                sa.load(to);
-                TB::load_regs(regs, b, g.ldb, j0, g.cols, c0, c_end);
-            } else {
-                TA::load_regs(regs, a, g.lda, i0, g.rows, c0, c_end);
-                sb.load(to + TA::kBytes);
-            }
-        };
-        auto settle = [&](char* to) { TR::store_regs(to + (kAsyncA ? TA::kBytes : 0), regs); };
-        if (steps > 0) {
-            fetch(lds, c_begin);
-            settle(lds);
-        }
-        for (int t = 0; t < steps; ++t) {
-            char* nxt = lds + ((t + 1) & 1) * kTileBytes;
-            wait_loads<0>();
-            __syncthreads();   // tile t has arrived, and the other is no longer read
-            if (t + 1 < steps) fetch(nxt, c_begin + (int64_t)(t + 1) * kBK);
-            read(lds + (t & 1) * kTileBytes, fa, fb);
-            multiply(fa, fb);
-            if (t + 1 < steps) settle(nxt);
+        if (plane > 0) {
+            barrier();   // all waves are done with the tiles
+#pragma unroll
+            for (int p = 0; p < FI; ++p)
+#pragma unroll
+                for (int q = 0; q < FJ; ++q) acc[p][q] *= g.plane_scale;
         }
     }
-
     if constexpr (S::WAYS > 1) {
         // The groups' sums meet behind the LDS that the first group's results pass through; in the order of the groups.
         constexpr int kResults = BI * BJ * 4, kWave = FI * FJ * 64 * 16;
@@ -515,7 +523,7 @@ __global__ __launch_bounds__(S::THREADS * S::WAYS) void k_gemm(GemmArgs g)
     auto value = [&](int p, int k, int e) -> float { return acc[p][(k * kGroup + e) / 4][e & 3]; };
     const int64_t i1 = i0 + wi, j1 = j0 + wj;
     if (TT || g.part) {
-        float* out = g.part ? g.part + (int64_t)part * g.rows * g.cols : (float*)g.out;
+        float* out = g.part ? g.part + (int64_t)blockIdx.y * g.rows * g.cols : (float*)g.out;
         const int64_t ldo = g.part ? g.cols : g.ldo;
 #pragma unroll
         for (int p = 0; p < FI; ++p)
@@ -687,7 +695,7 @@ __global__ __launch_bounds__(kSkinnyWaves * 64) void k_skinny(GemmArgs g)
 // kBlock / slices places; `slices` threads share a place's parts and meet in LDS. Bound by reading the parts: 4 to 9 us
 // for the splits that the plan makes.
 template <typename T>
-__global__ __launch_bounds__(kBlock) void k_join(GemmArgs g, float plane_scale, int slices)
+__global__ __launch_bounds__(kBlock) void k_join(GemmArgs g, int slices)
 {
     __shared__ f32x4 sums[kBlock];
     const int64_t quads = (g.cols + 3) / 4, total = g.rows * quads;
@@ -696,19 +704,16 @@ __global__ __launch_bounds__(kBlock) void k_join(GemmArgs g, float plane_scale, 
     const int64_t k = (int64_t)blockIdx.x * places + place;
     const int64_t i = k / quads, j = (k - i * quads) * 4, left = g.cols - j;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    if (k < total)
-        for (int p = g.planes - 1; p >= 0; --p) {
-            const float* part = g.part + (int64_t)p * g.splits * size + i * g.cols + j;
-            f32x4 t = {0.f, 0.f, 0.f, 0.f};
+    if (k < total) {
+        const float* part = g.part + i * g.cols + j;
 #pragma unroll 8
-            for (int s = slice; s < g.splits; s += slices) {
-                float u[4];
-                load_vec(part + (int64_t)s * size, left, u);
+        for (int s = slice; s < g.splits; s += slices) {
+            float u[4];
+            load_vec(part + (int64_t)s * size, left, u);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) t[e] += u[e];
-            }
-            v = v * plane_scale + t;
+            for (int e = 0; e < 4; ++e) v[e] += u[e];
         }
+    }
     if (slices > 1) {
         sums[threadIdx.x] = v;
         __syncthreads();
@@ -855,8 +860,7 @@ hipError_t run_gemm(const GemmArgs& g, hipStream_t s)
 {
     const int64_t tiles = div_up(g.rows, S::BI) * div_up(g.cols, S::BJ);
     const int lds = S::STATIC_LDS ? 0 : S::lds_bytes(div_up(g.split_len, 128 / (int)sizeof(T)), sizeof(T));
-    hipLaunchKernelGGL((k_gemm<T, S>), dim3((unsigned)tiles, (unsigned)(g.planes * g.splits)), dim3(S::THREADS * S::WAYS), lds,
-                       s, g);
+    hipLaunchKernelGGL((k_gemm<T, S>), dim3((unsigned)tiles, (unsigned)g.splits), dim3(S::THREADS * S::WAYS), lds, s, g);
     return hipGetLastError();
 }
 
@@ -932,14 +936,13 @@ hipError_t LinearOps<T>::prepare(const SlopeArgs* slope, const SlopeArgs* copy, 
 }
 
 template <typename T>
-hipError_t LinearOps<T>::join(const GemmArgs& g, float plane_scale, hipStream_t s)
+hipError_t LinearOps<T>::join(const GemmArgs& g, hipStream_t s)
 {
     // enough workgroups to fill the compute units, at least 4 parts a thread
     const int64_t places = g.rows * div_up(g.cols, 4);
     int slices = 1;
     while (slices < 32 && places * slices < 1024 * kBlock && g.splits >= 8 * slices) slices *= 2;
-    hipLaunchKernelGGL((k_join<T>), dim3((unsigned)div_up(places, kBlock / slices)), dim3(kBlock), 0, s, g, plane_scale,
-                       slices);
+    hipLaunchKernelGGL((k_join<T>), dim3((unsigned)div_up(places, kBlock / slices)), dim3(kBlock), 0, s, g, slices);
     return hipGetLastError();
 }
 

@@ -10,8 +10,8 @@ namespace gsr {
 // One product C[i][j] = sum over c of A(i, c) B(j, c), i < rows, j < cols, c < len.
 // NT: A(i, c) = a[i lda + c], B(j, c) = b[j ldb + c] (both contiguous along the sum).
 // TT: A(i, c) = a[c lda + i], B(j, c) = b[c ldb + j] (both contiguous across it).
-// The sum may be split: part z = plane * splits + split covers c in [split * split_len, ...) of A plane
-// `plane` (a + plane * plane_stride).
+// The sum may be split: part `split` covers c in [split * split_len, ...). In TT A may be given in planes (a + plane *
+// plane_stride), whose products are added up with the factors plane_scale^plane.
 struct GemmArgs {
     const void* a;
     const void* b;
@@ -20,6 +20,7 @@ struct GemmArgs {
     int64_t split_len;
     int32_t splits, planes;
     int64_t plane_stride;
+    float plane_scale;
     // epilogue: out = act(C + bias) + residual, z = C + bias
     const float* bias;
     const void* residual;
@@ -28,7 +29,7 @@ struct GemmArgs {
     int64_t ldr, ldo, ldz;
     int32_t act;
     int32_t out_f32;               // out is fp32 whatever the type (residual, z: unused)
-    float* part;                   // [planes * splits][rows][cols] fp32 instead of the epilogue, or NULL
+    float* part;                   // [splits][rows][cols] fp32 instead of the epilogue, or NULL
 };
 
 // dz = dy act'(z) of [rows][cols], as `planes` planes of the element type whose sum it is (plane k scaled by
@@ -94,7 +95,7 @@ struct LinearOps {
     // those that are wanted (not NULL) of dz, a matrix copied (dz without an activation) and W transposed, in one launch
     static hipError_t prepare(const SlopeArgs* slope, const SlopeArgs* copy, const TransposeArgs* transpose,
                               hipStream_t s);
-    static hipError_t join(const GemmArgs& g, float plane_scale, hipStream_t s);   // adds the parts up, with the epilogue
+    static hipError_t join(const GemmArgs& g, hipStream_t s);   // adds the parts up, with the epilogue
 };
 
 }  // namespace gsr

@@ -17,7 +17,7 @@ namespace {
 constexpr int kFillTiles = 256;          // compute units
 constexpr int kSlopeBlocks = 2048;
 constexpr int64_t kJoinSplitLen = 256;   // values of the sum in a split of a product of few tiles, at least
-constexpr int64_t kRowSplitLen = 512;    // rows in a split of dW's sum, at least
+constexpr int64_t kRowSplitLen = 512;    // rows (of all planes) in a split of dW's sum, at least
 
 constexpr int kNarrowMost = 128;         // inputs and outputs of a layer whose backward is one pass
 constexpr int kNarrowBlocks = 512;       // two workgroups per compute unit
@@ -72,7 +72,7 @@ Plan plan_product(int type, int64_t rows, int64_t cols, int64_t len, int planes,
     for (int k = 0; k < count; ++k) {
         const TileRate& r = rates[k];
         if (!fast_operand && (r.tile == kTile256 || r.tile == kTile64By4)) continue;
-        const int64_t tiles = div_up(rows, r.size) * div_up(cols, r.size) * planes;
+        const int64_t tiles = div_up(rows, r.size) * div_up(cols, r.size);
         const int64_t most = std::max<int64_t>(1, std::min(r.slots / std::min<int64_t>(tiles, r.slots), len / least));
         for (int64_t want : {(int64_t)1, most}) {
             const int64_t split_len = std::max<int64_t>(64, div_up(div_up(len, want), 64) * 64);
@@ -81,9 +81,9 @@ Plan plan_product(int type, int64_t rows, int64_t cols, int64_t len, int planes,
             // a compute unit's share of the workgroups, one after the other, and what their rounds add
             const double share = (double)div_up(tiles * splits, kFillTiles);
             const double rate = (share > 1 ? r.flop_us : r.flop_us_one) * (fast_operand ? 1.0 : kSlowRate);
-            double us = share * 2.0 * r.size * r.size * (double)split_len * kFillTiles / rate +
+            double us = share * 2.0 * r.size * r.size * (double)split_len * planes * kFillTiles / rate +
                         (double)div_up(tiles * splits, r.slots) * r.round_us;
-            if (splits * planes > 1) us += kJoinUs + 8.0 * planes * splits * (double)rows * (double)cols / kBytesUs;
+            if (splits > 1) us += kJoinUs + 8.0 * splits * (double)rows * (double)cols / kBytesUs;
             if (us < best_us) {
                 best_us = us;
                 best = {r.tile, (int)splits, split_len};
@@ -102,7 +102,7 @@ Plan plan_nt(int type, int64_t rows, int64_t cols, int64_t len, bool fast_a)
 // TT: the sum runs over the rows.
 Plan plan_tt(int type, int64_t out, int64_t in, int64_t rows, int planes, bool fast_b)
 {
-    return plan_product(type, out, in, rows, planes, fast_b, kRowSplitLen);
+    return plan_product(type, out, in, rows, planes, fast_b, kRowSplitLen / planes);
 }
 
 // Planes of dz: an fp32 weight gradient keeps what rounding dz to 16 bits would drop, as further planes of the
@@ -226,7 +226,7 @@ BwdSpace bwd_space(void* base, int type, int act, int64_t rows, int64_t in, int6
     // (a workspace is sized for either operand's alignment)
     for (int fast_x = 0; fast_x < 2; ++fast_x) {
         const Plan w = plan_tt(type, out, in, rows, planes, fast_x != 0);
-        if (w.splits * planes > 1) part = std::max(part, (int64_t)w.splits * planes * out * in * 4);
+        if (w.splits > 1) part = std::max(part, (int64_t)w.splits * out * in * 4);
     }
     b.part = (float*)r.take(part);
     b.bytes = r.at;
@@ -246,7 +246,7 @@ hipError_t run_nt(int type, GemmArgs g, bool few, bool fast_a, float* part, hipS
     g.part = p.splits > 1 ? part : nullptr;
     const hipError_t e = LinearOps<T>::gemm_nt(p.tile, fast_a, g, s);
     if (e != hipSuccess || p.splits == 1) return e;
-    return LinearOps<T>::join(g, 1.f, s);
+    return LinearOps<T>::join(g, s);
 }
 
 template <typename T>
@@ -358,12 +358,13 @@ hipError_t linear_bwd(const gs_linear& p, const void* dy, int64_t lddy, const vo
         g.split_len = plan.split_len;
         g.planes = planes;
         g.plane_stride = p.rows * ldo;
+        g.plane_scale = plane_scale(p.type);
         g.out = dw;
         g.ldo = lddw;
         g.out_f32 = dw_type == GS_F32;
-        g.part = plan.splits * planes > 1 ? b.part : nullptr;
+        g.part = plan.splits > 1 ? b.part : nullptr;
         e = LinearOps<T>::gemm_tt(plan.tile, fast_x, g, s);
-        if (e == hipSuccess && g.part) e = LinearOps<T>::join(g, plane_scale(p.type), s);
+        if (e == hipSuccess && g.part) e = LinearOps<T>::join(g, s);
     }
     return e;
 }
