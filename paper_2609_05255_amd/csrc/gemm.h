@@ -632,13 +632,13 @@ __global__ __launch_bounds__(kSkinnyWaves * 64) void k_skinny(GemmArgs g)
     constexpr int kUnroll = MF == 1 ? 8 : 4;         // steps whose loads are under way together
     __shared__ float sums[kSkinnyWaves][MF][16][17];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, lg = lane >> 4, li = lane & 15;
-    const int64_t j0 = (int64_t)blockIdx.x * 16, i0 = (int64_t)blockIdx.y * (16 * MF);
+    const int64_t j0 = (int64_t)blockIdx.x * 16;
     const T* w = (const T*)g.b + (j0 + li < g.cols ? j0 + li : g.cols - 1) * g.ldb + lg * N;
     const T* x[MF];
     bool in[MF];   // (lanes of rows that do not exist load nothing)
 #pragma unroll
     for (int m = 0; m < MF; ++m) {
-        const int64_t i = i0 + 16 * m + li;
+        const int64_t i = 16 * m + li;
         in[m] = i < g.rows;
         x[m] = (const T*)g.a + (in[m] ? i : 0) * g.lda + lg * N;
     }
@@ -677,7 +677,7 @@ __global__ __launch_bounds__(kSkinnyWaves * 64) void k_skinny(GemmArgs g)
     __syncthreads();
     for (int k = threadIdx.x; k < MF * 256; k += kSkinnyWaves * 64) {
         const int m = k >> 8, ii = (k >> 4) & 15, jj = k & 15;
-        const int64_t i = i0 + 16 * m + ii, j = j0 + jj;
+        const int64_t i = 16 * m + ii, j = j0 + jj;
         if (i >= g.rows || j >= g.cols) continue;
         float v = g.bias ? g.bias[j] : 0.f;
         float t = 0.f;
@@ -899,13 +899,11 @@ hipError_t LinearOps<T>::gemm_tt(int tile, bool fast_b, const GemmArgs& g, hipSt
 template <typename T>
 hipError_t LinearOps<T>::skinny(const GemmArgs& g, hipStream_t s)
 {
-    const unsigned x = (unsigned)div_up(g.cols, 16);
+    const dim3 grid((unsigned)div_up(g.cols, 16));
     if (g.rows <= 16)
-        hipLaunchKernelGGL((k_skinny<T, 1>), dim3(x, 1), dim3(kSkinnyWaves * 64), 0, s, g);
-    else if (g.rows <= 32)
-        hipLaunchKernelGGL((k_skinny<T, 2>), dim3(x, 1), dim3(kSkinnyWaves * 64), 0, s, g);
-    else
-        hipLaunchKernelGGL((k_skinny<T, 4>), dim3(x, (unsigned)div_up(g.rows, 64)), dim3(kSkinnyWaves * 64), 0, s, g);
+        hipLaunchKernelGGL((k_skinny<T, 1>), grid, dim3(kSkinnyWaves * 64), 0, s, g);
+    else   // up to 32
+        hipLaunchKernelGGL((k_skinny<T, 2>), grid, dim3(kSkinnyWaves * 64), 0, s, g);
     return hipGetLastError();
 }
 

@@ -17,6 +17,9 @@ namespace {
 constexpr int kFillTiles = 256;          // compute units
 constexpr int kSlopeBlocks = 2048;
 constexpr int64_t kJoinSplitLen = 256;   // values of the sum in a split of a product of few tiles, at least
+// Rows up to which the weights' bytes bound the product (4,096 x 4,096 in bfloat16: 64 rows 21 us, 16 in tiles; 70 and
+// 39, with a copy of W first, where its rows are not aligned).
+constexpr int64_t kFewRows = 32;
 constexpr int64_t kRowSplitLen = 512;    // rows (of all planes) in a split of dW's sum, at least
 
 constexpr int kNarrowMost = 128;         // inputs and outputs of a layer whose backward is one pass
@@ -142,10 +145,6 @@ SlopeArgs copy_of(int type, const void* src, int64_t lds, int64_t rows, int64_t 
     return a;
 }
 
-// Few rows, where the weights' bytes bound the product: up to 32, or 64 where the tiles would need a copy of W with
-// aligned rows first (4,096 x 4,096 in bfloat16: 64 rows 21 us, 17 in tiles, and 15 for such a copy).
-bool few_rows(int64_t rows, bool copy_w) { return rows <= (copy_w ? 64 : 32); }
-
 // Workspace: regions taken in order, 256-byte aligned.
 struct Regions {
     char* base;
@@ -185,7 +184,7 @@ FwdSpace fwd_space(void* base, int type, int64_t rows, int64_t in, int64_t out, 
 {
     Regions r{(char*)base};
     FwdSpace f = {};
-    if (!few_rows(rows, copy_w) && !narrow_forward(type, rows, in, out, z)) {
+    if (rows > kFewRows && !narrow_forward(type, rows, in, out, z)) {
         if (copy_w) f.w = r.take(out * padded(type, in) * elem(type));
         int splits = 1;   // (a workspace is sized for either alignment of x)
         for (int fast_x = 0; fast_x < 2; ++fast_x) splits = std::max(splits, plan_nt(type, rows, out, in, fast_x).splits);
@@ -219,7 +218,7 @@ BwdSpace bwd_space(void* base, int type, int act, int64_t rows, int64_t in, int6
     b.wt = r.take(in * padded(type, out) * elem(type));
     b.sums = (float*)r.take((int64_t)slope_row_blocks(type, rows, out) * out * 4);
     int64_t part = 0;
-    if (!few_rows(rows, false)) {
+    if (rows > kFewRows) {
         const Plan x = plan_nt(type, rows, in, out, true);
         if (x.splits > 1) part = (int64_t)x.splits * rows * in * 4;
     }
@@ -235,11 +234,11 @@ BwdSpace bwd_space(void* base, int type, int act, int64_t rows, int64_t in, int6
 
 // A product along rows with its epilogue: few rows, one launch of tiles, or splits and their join.
 template <typename T>
-hipError_t run_nt(int type, GemmArgs g, bool few, bool fast_a, float* part, hipStream_t s)
+hipError_t run_nt(int type, GemmArgs g, bool fast_a, float* part, hipStream_t s)
 {
     g.splits = g.planes = 1;
     g.split_len = g.len;
-    if (few) return LinearOps<T>::skinny(g, s);
+    if (g.rows <= kFewRows) return LinearOps<T>::skinny(g, s);
     const Plan p = plan_nt(type, g.rows, g.cols, g.len, fast_a);
     g.splits = p.splits;
     g.split_len = p.split_len;
@@ -254,7 +253,6 @@ hipError_t linear_fwd(const gs_linear& p, const void* residual, int64_t ldr, voi
                       int64_t ldz, void* ws, hipStream_t s)
 {
     const bool copy_w = !fast(p.w, p.ldw, p.n_in, p.type), fast_x = fast(p.x, p.ldx, p.n_in, p.type);
-    const bool few = few_rows(p.rows, copy_w);
     const FwdSpace f = fwd_space(ws, p.type, p.rows, p.n_in, p.n_out, copy_w, z != nullptr);
     GemmArgs g = {};
     g.a = p.x;
@@ -280,9 +278,9 @@ hipError_t linear_fwd(const gs_linear& p, const void* residual, int64_t ldr, voi
     g.z = z;
     g.ldz = ldz;
     if constexpr (sizeof(T) == 2)
-        if (!few && narrow_forward(p.type, p.rows, p.n_in, p.n_out, z != nullptr))
+        if (p.rows > kFewRows && narrow_forward(p.type, p.rows, p.n_in, p.n_out, z != nullptr))
             return NarrowOps<T>::forward(g, fast_x, (int)std::min<int64_t>(div_up(p.rows, 64), 4 * kFillTiles), s);
-    return run_nt<T>(p.type, g, few, fast_x, f.part, s);
+    return run_nt<T>(p.type, g, fast_x, f.part, s);
 }
 
 template <typename T>
@@ -338,7 +336,7 @@ hipError_t linear_bwd(const gs_linear& p, const void* dy, int64_t lddy, const vo
         g.len = p.n_out;
         g.out = dx;
         g.ldo = lddx;
-        e = run_nt<T>(p.type, g, few_rows(p.rows, false), true, b.part, s);
+        e = run_nt<T>(p.type, g, true, b.part, s);
         if (e != hipSuccess) return e;
     }
     if (dw) {
@@ -384,9 +382,7 @@ size_t linear_bwd_workspace(const gs_linear& p, const void* dy, int64_t lddy, in
 
 size_t linear_workspace(int type, int act, int64_t rows, int64_t in, int64_t out, int dw_type)
 {
-    // (for either alignment of W)
-    const size_t fwd = std::max(fwd_space(nullptr, type, rows, in, out, false, true).bytes,
-                                fwd_space(nullptr, type, rows, in, out, true, true).bytes);
+    const size_t fwd = fwd_space(nullptr, type, rows, in, out, true, true).bytes;
     return dw_type < 0 ? fwd : std::max(fwd, bwd_space(nullptr, type, act, rows, in, out, dw_type, true).bytes);
 }
 

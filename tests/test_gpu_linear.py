@@ -273,7 +273,7 @@ def test_largest_tiles(rows, n_in, n_out, dtype):
 @pytest.mark.parametrize("rows", [32, 33, 48, 64, 65])
 @pytest.mark.parametrize("n_in,n_out", [(64, 48), (33, 17), (520, 264), (1031, 300), (4096, 200)])
 def test_few_rows_and_more(rows, n_in, n_out, dtype):
-    # on both sides of the form for few rows, whose limit depends on whether W has aligned rows
+    # on both sides of the form for few rows, with W's rows aligned and not
     d = make(rows, n_in, n_out, dtype, rows + n_in)
     y, z = (torch.full_like(d["r"], float("nan")) for _ in range(2))
     gs.gs_linear_fwd(d["x"], d["w"], d["bias"], y, space(d["x"], d["w"], "tanh", None), act="tanh", residual=d["r"], z=z)
