@@ -622,9 +622,43 @@ __global__ __launch_bounds__(S::THREADS * S::WAYS) void k_gemm(GemmArgs g)
 // memory to registers once, 16 bytes per lane and load, eight loads (or four, with more rows) under way together, and
 // the waves' sums meet in LDS. Bound by reading the weights: one row of 4,096 x 4,096 in bfloat16 takes 8.4 us a call,
 // 4.0 TB/s, where an empty launch takes 4.3.
+// ODD: 16-bit values at odd element addresses, whose vectors are loaded as the five aligned words that they lie in (no
+// further than these, so never beyond a word that holds a value) and shifted: one row of 4,095 x 4,096 in bfloat16 takes
+// 12.6 us, 16 rows 16.3; loaded as they are 17.3 and 28.8.
 constexpr int kSkinnyWaves = 8;
 
-template <typename T, int MF>
+// A whole vector on its way.
+template <typename T, bool ODD>
+struct Flight {
+    typename Vec<T>::Packed v;
+    __device__ __forceinline__ void load(const T* p) { v = *reinterpret_cast<const typename Vec<T>::Any*>(p); }
+    __device__ __forceinline__ typename Vec<T>::Packed value(const T*) const { return v; }
+};
+
+template <typename T>
+struct Flight<T, true> {
+    typedef u32x4 Words __attribute__((aligned(4)));
+    u32x4 v;
+    uint32_t next;   // the word behind them, where the vector reaches into it
+    __device__ __forceinline__ void load(const T* p)
+    {
+        const uint64_t at = reinterpret_cast<uint64_t>(p);
+        const uint32_t* q = reinterpret_cast<const uint32_t*>(at & ~(uint64_t)3);
+        v = *reinterpret_cast<const Words*>(q);
+        next = q[at & 2 ? 4 : 3];
+    }
+    // (p: any vector of the same row)
+    __device__ __forceinline__ typename Vec<T>::Packed value(const T* p) const
+    {
+        const uint32_t shift = (reinterpret_cast<uint64_t>(p) & 2) * 8;
+        u32x4 t;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) t[e] = __builtin_amdgcn_alignbit(e < 3 ? v[e + 1] : next, v[e], shift);
+        return __builtin_bit_cast(typename Vec<T>::Packed, t);
+    }
+};
+
+template <typename T, int MF, bool ODD>
 __global__ __launch_bounds__(kSkinnyWaves * 64) void k_skinny(GemmArgs g)
 {
     constexpr int N = Vec<T>::N;
@@ -647,28 +681,33 @@ __global__ __launch_bounds__(kSkinnyWaves * 64) void k_skinny(GemmArgs g)
     const int64_t per = (steps + kSkinnyWaves - 1) / kSkinnyWaves;
     const int64_t s0 = wave * per, s1 = s0 + per < steps ? s0 + per : steps;
     typedef typename Vec<T>::Packed Packed;
-    typedef typename Vec<T>::Any Any;
+    const int64_t left = g.len - lg * N;
     int64_t s = s0;
-    for (; s + kUnroll <= s1 && (s + kUnroll) * kStep <= g.len; s += kUnroll) {
-        Packed wv[kUnroll], xv[MF][kUnroll] = {};
+    auto steps_from = [&](auto whole) {
+        Flight<T, ODD> wv[kUnroll] = {}, xv[MF][kUnroll] = {};
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) wv[u] = *reinterpret_cast<const Any*>(w + (s + u) * kStep);
+        for (int u = 0; u < kUnroll; ++u)
+            if (whole(u)) wv[u].load(w + (s + u) * kStep);
 #pragma unroll
         for (int m = 0; m < MF; ++m)
             if (in[m])
 #pragma unroll
-                for (int u = 0; u < kUnroll; ++u) xv[m][u] = *reinterpret_cast<const Any*>(x[m] + (s + u) * kStep);
+                for (int u = 0; u < kUnroll; ++u)
+                    if (whole(u)) xv[m][u].load(x[m] + (s + u) * kStep);
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u)
 #pragma unroll
-            for (int m = 0; m < MF; ++m) acc[m] = Mma<T>::mma(wv[u], xv[m][u], acc[m]);
-    }
-    for (; s < s1; ++s) {
-        const int64_t left = g.len - s * kStep - lg * N;
-        const Packed wv = load_any(w + s * kStep, left);
+            for (int m = 0; m < MF; ++m) acc[m] = Mma<T>::mma(wv[u].value(w), xv[m][u].value(x[m]), acc[m]);
+    };
+    for (; s + kUnroll <= s1 && (s + kUnroll) * kStep <= g.len; s += kUnroll) steps_from([](int) { return true; });
+    // those left, of which the sum's last ones may lie in part beyond it
+    for (; s < s1; s += kUnroll) steps_from([&](int u) { return s + u < s1 && left - (s + u) * kStep >= N; });
+    // the vector that the sum ends in
+    if (s1 == steps && s0 < s1 && g.len % N) {
+        const int64_t at = (steps - 1) * kStep, end = left - at < N ? left - at : 0;
+        const Packed wv = load_any(w + at, end);
 #pragma unroll
-        for (int m = 0; m < MF; ++m)
-            acc[m] = Mma<T>::mma(wv, load_any(x[m] + s * kStep, in[m] ? left : 0), acc[m]);
+        for (int m = 0; m < MF; ++m) acc[m] = Mma<T>::mma(wv, load_any(x[m] + at, in[m] ? end : 0), acc[m]);
     }
 #pragma unroll
     for (int m = 0; m < MF; ++m)
@@ -900,10 +939,14 @@ template <typename T>
 hipError_t LinearOps<T>::skinny(const GemmArgs& g, hipStream_t s)
 {
     const dim3 grid((unsigned)div_up(g.cols, 16));
-    if (g.rows <= 16)
-        hipLaunchKernelGGL((k_skinny<T, 1>), grid, dim3(kSkinnyWaves * 64), 0, s, g);
-    else   // up to 32
-        hipLaunchKernelGGL((k_skinny<T, 2>), grid, dim3(kSkinnyWaves * 64), 0, s, g);
+    auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kSkinnyWaves * 64), 0, s, g); };
+    if constexpr (sizeof(T) == 2) {
+        if ((((uintptr_t)g.a | (uintptr_t)g.b) & 2) || ((g.lda | g.ldb) & 1)) {
+            run(g.rows <= 16 ? k_skinny<T, 1, true> : k_skinny<T, 2, true>);
+            return hipGetLastError();
+        }
+    }
+    run(g.rows <= 16 ? k_skinny<T, 1, false> : k_skinny<T, 2, false>);   // (up to 32 rows)
     return hipGetLastError();
 }
 

@@ -286,6 +286,19 @@ def test_few_rows_and_more(rows, n_in, n_out, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows", [1, 16, 31])
+@pytest.mark.parametrize("n_in", [7, 31, 256, 1027, 2304, 4099])
+@pytest.mark.parametrize("pad,offset", [(0, 0), (1, 0), (2, 1), (8, 1)])
+def test_few_rows_at_any_address(rows, n_in, pad, offset, dtype):
+    # rows of x and W at even and odd addresses, sums that end anywhere in a vector or a step; what lies between is NaN
+    d = make(rows, n_in, 37, dtype, n_in)
+    x, w = strided(d["x"], pad, offset), strided(d["w"], pad, offset)
+    y, z = (torch.full_like(d["r"], float("nan")) for _ in range(2))
+    gs.gs_linear_fwd(x, w, d["bias"], y, space(x, w, "sigmoid", None), act="sigmoid", residual=d["r"], z=z)
+    check_forward(d, "sigmoid", y, z)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,n_in,n_out", [(1000, 2064, 968), (70, 1032, 2048), (2100, 1000, 960), (1025, 136, 520)])
 def test_sums_shared_within_a_workgroup(rows, n_in, n_out, dtype):
     # products of about one tile for each compute unit, with long sums: parts of unequal length, ends inside a tile
