@@ -20,7 +20,7 @@ constexpr int64_t kJoinSplitLen = 256;   // values of the sum in a split of a pr
 // Rows up to which the weights' bytes bound the product (4,096 x 4,096 in bfloat16: 64 rows 21 us, 16 in tiles; 70 and
 // 39, with a copy of W first, where its rows are not aligned).
 constexpr int64_t kFewRows = 32;
-constexpr int64_t kRowSplitLen = 512;    // rows (of all planes) in a split of dW's sum, at least
+constexpr int64_t kRowSplitLen = 128;    // rows in a split of dW's sum, at least
 
 constexpr int kNarrowMost = 128;         // inputs and outputs of a layer whose backward is one pass
 constexpr int kNarrowBlocks = 512;       // two workgroups per compute unit
@@ -41,24 +41,27 @@ struct Plan {
     int64_t split_len;
 };
 
-// What a tile's kernel reaches: its rows and columns, the workgroups that run at once, the rate of all compute units with
-// their share of them and with one each, the time that a round of them takes beside its products (first loads,
-// results), and the shortest sum that it is taken for. Measured at 8,192 x 4,096 and at 1,024 to 4,096 x 1,024 values,
-// sums of 64 to 8,192, in bfloat16 and fp32.
+// What a tile's kernel reaches: its rows and columns, the workgroups of it that a compute unit holds, the rate of all
+// compute units with that many of them, and with one each, the time that a round of them takes beside its products
+// (first loads, results), and the shortest sum that it is taken for. Measured in bfloat16 and fp32 at 8,192 x 4,096 and
+// at 13 products between 1,384 x 816 x 2,592 and 24,981 x 768 x 1,680 (us: 64 x 64, 128 x 64, 128 x 128, 256 x 256):
+//   5,049 x 360 x 1,716     20   23   28   43        4,000 x 1,024 x 1,024   16   14   16   28
+//   1,500 x 3,000 x 1,500   39   36   30   39        8,299 x 928 x 4,016    148  136  126   89
 // The largest tile's workgroup, alone on its compute unit, hides neither its first loads nor its results: short sums
 // are left to smaller ones (7,133 x 48 x 1,424 in binary16: 16 us against 12).
 struct TileRate {
-    int tile, size, slots;
+    int tile, rows, cols, held;
     double flop_us, flop_us_one, round_us;
     int64_t least;
 };
-constexpr TileRate kRates16[] = {{kTile256, 256, 256, 1.1e9, 1.1e9, 11.0, 512},
-                                 {kTile128, 128, 512, 0.85e9, 0.85e9, 6.0, 0},
-                                 {kTile64By4, 64, 256, 0.45e9, 0.45e9, 3.5, 1024},
-                                 {kTile64, 64, 1280, 0.58e9, 0.28e9, 4.0, 0}};
-constexpr TileRate kRates32[] = {{kTile128, 128, 512, 0.131e9, 0.112e9, 6.0, 0},
-                                 {kTile64By4, 64, 256, 0.105e9, 0.105e9, 3.5, 512},
-                                 {kTile64, 64, 1280, 0.115e9, 0.09e9, 4.0, 0}};
+constexpr TileRate kRates16[] = {{kTile256, 256, 256, 1, 1.25e9, 1.6e9, 16.0, 512},
+                                 {kTile128, 128, 128, 2, 0.95e9, 0.75e9, 6.0, 0},
+                                 {kTile128x64, 128, 64, 3, 0.7e9, 0.42e9, 5.0, 0},
+                                 {kTile64By4, 64, 64, 1, 0.45e9, 0.45e9, 3.5, 1024},
+                                 {kTile64, 64, 64, 5, 0.5e9, 0.28e9, 4.0, 0}};
+constexpr TileRate kRates32[] = {{kTile128, 128, 128, 2, 0.131e9, 0.112e9, 6.0, 0},
+                                 {kTile64By4, 64, 64, 1, 0.105e9, 0.105e9, 3.5, 512},
+                                 {kTile64, 64, 64, 5, 0.115e9, 0.09e9, 4.0, 0}};
 // An operand that goes through registers slows a product down (20,003 x 777 x 999 in binary16: 90 us against 79), which
 // is about what a copy of it with aligned rows would take.
 constexpr double kSlowRate = 0.85;
@@ -66,31 +69,36 @@ constexpr double kJoinUs = 4.0, kBytesUs = 5.0e6;   // of a join's launch, and o
 
 // The tile, and the split of its sum, that these rates make fastest: large tiles where they fill the compute units,
 // smaller ones or a split sum (in parts of `least` values or more, which are then added up) where they do not.
-Plan plan_product(int type, int64_t rows, int64_t cols, int64_t len, int planes, bool fast_operand, int64_t least)
+Plan plan_product(int type, bool tt, int64_t rows, int64_t cols, int64_t len, int planes, bool fast_operand,
+                  int64_t least)
 {
     Plan best = {kTile64, 1, len};
     double best_us = 1e300;
     const TileRate* rates = type == GS_F32 ? kRates32 : kRates16;
-    const int count = type == GS_F32 ? 3 : 4;
+    const int count = type == GS_F32 ? 3 : 5;
     for (int k = 0; k < count; ++k) {
         const TileRate& r = rates[k];
         if (!fast_operand && (r.tile == kTile256 || r.tile == kTile64By4)) continue;
-        const int64_t tiles = div_up(rows, r.size) * div_up(cols, r.size);
-        const int64_t most = std::max<int64_t>(1, std::min(r.slots / std::min<int64_t>(tiles, r.slots), len / least));
-        for (int64_t want : {(int64_t)1, most}) {
+        if (tt && r.tile == kTile128x64) continue;
+        const int64_t tiles = div_up(rows, r.rows) * div_up(cols, r.cols), slots = r.held * kFillTiles;
+        const int64_t most = std::max<int64_t>(1, std::min(slots / std::min(tiles, slots), len / least));
+        for (int64_t want = most;; want = want > 1 && want < 4 ? 1 : want / 2) {
             const int64_t split_len = std::max<int64_t>(64, div_up(div_up(len, want), 64) * 64);
             const int64_t splits = std::max<int64_t>(1, div_up(len, split_len));
-            if (split_len < r.least) continue;
-            // a compute unit's share of the workgroups, one after the other, and what their rounds add
-            const double share = (double)div_up(tiles * splits, kFillTiles);
-            const double rate = (share > 1 ? r.flop_us : r.flop_us_one) * (fast_operand ? 1.0 : kSlowRate);
-            double us = share * 2.0 * r.size * r.size * (double)split_len * planes * kFillTiles / rate +
-                        (double)div_up(tiles * splits, r.slots) * r.round_us;
-            if (splits > 1) us += kJoinUs + 8.0 * splits * (double)rows * (double)cols / kBytesUs;
-            if (us < best_us) {
-                best_us = us;
-                best = {r.tile, (int)splits, split_len};
+            if (split_len >= r.least) {
+                // a compute unit's workgroups, `held` at a time, the last ones perhaps alone
+                const int64_t share = div_up(tiles * splits, kFillTiles), rounds = div_up(share, r.held);
+                const bool alone = (share - 1) % r.held == 0;
+                const double unit = 2.0 * r.rows * r.cols * (double)split_len * planes * kFillTiles;
+                double us = unit * ((double)(share - alone) / r.flop_us + alone / r.flop_us_one) /
+                                (fast_operand ? 1.0 : kSlowRate) + (double)rounds * r.round_us;
+                if (splits > 1) us += kJoinUs + 8.0 * splits * (double)rows * (double)cols / kBytesUs;
+                if (us < best_us) {
+                    best_us = us;
+                    best = {r.tile, (int)splits, split_len};
+                }
             }
+            if (want == 1) break;
         }
     }
     return best;
@@ -99,13 +107,13 @@ Plan plan_product(int type, int64_t rows, int64_t cols, int64_t len, int planes,
 Plan plan_nt(int type, int64_t rows, int64_t cols, int64_t len, bool fast_a)
 {
     if (cols <= 64 && div_up(rows, 128) >= kFillTiles) return {kTile128x64, 1, len};
-    return plan_product(type, rows, cols, len, 1, fast_a, kJoinSplitLen);
+    return plan_product(type, false, rows, cols, len, 1, fast_a, kJoinSplitLen);
 }
 
 // TT: the sum runs over the rows.
 Plan plan_tt(int type, int64_t out, int64_t in, int64_t rows, int planes, bool fast_b)
 {
-    return plan_product(type, out, in, rows, planes, fast_b, kRowSplitLen / planes);
+    return plan_product(type, true, out, in, rows, planes, fast_b, kRowSplitLen);
 }
 
 // Planes of dz: an fp32 weight gradient keeps what rounding dz to 16 bits would drop, as further planes of the
