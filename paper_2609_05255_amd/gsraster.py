@@ -385,6 +385,8 @@ def _vector(name, t, n):
 def _space(workspace):
     if workspace is None:
         return None, 0
+    if not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError("workspace: a contiguous tensor on the GPU expected")
     return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 

@@ -180,3 +180,11 @@ def test_binding_refuses(gs):
         gs.GradSet([], out=[None])
     with pytest.raises(ValueError, match="grad_scale"):
         gs.gs_adam_step([], 0.9, 1e-8, 1, grad_scale=torch.ones(1))
+
+
+def test_binding_refuses_workspaces(gs):
+    # a host array, which a kernel could not write
+    for bad in (torch.zeros(512, dtype=torch.uint8), torch.zeros(64, 8, dtype=torch.uint8)[:, :4]):
+        with pytest.raises(ValueError, match="workspace"):
+            gs._space(bad)
+    assert gs._space(None) == (None, 0)
