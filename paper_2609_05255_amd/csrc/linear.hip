@@ -81,6 +81,8 @@ Plan plan_product(int type, bool tt, int64_t rows, int64_t cols, int64_t len, in
         if (!fast_operand && (r.tile == kTile256 || r.tile == kTile64By4)) continue;
         if (tt && r.tile == kTile128x64) continue;
         const int64_t tiles = div_up(rows, r.rows) * div_up(cols, r.cols), slots = r.held * kFillTiles;
+        // (work items of a launch are counted in 32 bits; linear_grid_fits holds for tiles of 128)
+        if (tiles * (r.tile == kTile64By4 ? 1024 : r.tile == kTile256 ? 512 : 256) >> 32) continue;
         const int64_t most = std::max<int64_t>(1, std::min(slots / std::min(tiles, slots), len / least));
         for (int64_t want = most;; want = want > 1 && want < 4 ? 1 : want / 2) {
             const int64_t split_len = std::max<int64_t>(64, div_up(div_up(len, want), 64) * 64);
