@@ -15,8 +15,8 @@
 // value 4 t + e of lane group g is row (dW) or column (dx) 16 t + 4 g + e of its 32.
 //
 // P planes of dz: dz rounded to T (all that dx takes, as it is rounded to T itself), then what that leaves, so that an
-// fp32 dW keeps 22 bits or more. In binary16 the
-// second plane is scaled by 2^11 against underflow, and x by 2^-11 (exact down to 2^-25) where it meets it.
+// fp32 dW keeps 22 bits or more. In binary16 the second plane is scaled by 2^11 against underflow; its products of 32
+// rows are summed apart and join dW's sums times 2^-11 in fp32 (scaling x instead would round every x below 2^-3).
 #pragma once
 
 #include "gemm.h"
@@ -166,7 +166,7 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void k_narrow_bwd(NarrowArgs a)
                     h[e] = (T)v[e];
                     // what the plane leaves; an infinite or undefined value is the first plane's alone
                     const float rest = v[e] - (float)h[e];
-                    v[e] = fabsf(rest) < __builtin_inff() ? (__is_same(T, f16) ? rest * 2048.f : rest) : 0.f;
+                    v[e] = fabsf(rest) < __builtin_inff() ? (__is_same(T, f16) ? rest * (1.f / kF16Plane) : rest) : 0.f;
                 }
                 *reinterpret_cast<Packed*>(lds_dz + p * kDz + narrow_at(R, r, vo)) = h;
             }
@@ -210,14 +210,19 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void k_narrow_bwd(NarrowArgs a)
 #pragma unroll
                     for (int n = 0; n < FO; ++n) fz[n] = narrow_columns<T>(lds_dz + p * kDz, R, wo + n, 32 * s);
 #pragma unroll
-                    for (int n = 0; n < FI; ++n) {
-                        fx[n] = narrow_columns<T>(lds_x, R, wn + n, 32 * s);
-                        if (__is_same(T, f16) && p == 1) fx[n] *= (T)(1.f / 2048.f);
-                    }
+                    for (int n = 0; n < FI; ++n) fx[n] = narrow_columns<T>(lds_x, R, wn + n, 32 * s);
 #pragma unroll
                     for (int m = 0; m < FO; ++m)
 #pragma unroll
-                        for (int n = 0; n < FI; ++n) dw[m][n] = Mma<T>::mma(fx[n], fz[m], dw[m][n]);
+                        for (int n = 0; n < FI; ++n) {
+                            if (__is_same(T, f16) && p == 1) {
+                                const f32x4 low = Mma<T>::mma(fx[n], fz[m], f32x4{});
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) dw[m][n][e] = fmaf(low[e], kF16Plane, dw[m][n][e]);
+                            } else {
+                                dw[m][n] = Mma<T>::mma(fx[n], fz[m], dw[m][n]);
+                            }
+                        }
                 }
         }
         __syncthreads();   // LDS is free again

@@ -1,0 +1,34 @@
+"""The linear backward's fp32 weight gradient where dz is kept in planes of a 16-bit type (an activation with a smooth
+slope): operands far from size 1, on both sides of the narrow form. Bounds as in test_gpu_linear.py; with few rows the
+sum's own share of them lies well below the 2^-12 that a lost plane would leave."""
+import pytest
+import torch
+
+from paper_2609_05255_amd import gsraster as gs
+from test_gpu_linear import check_backward, make, space
+
+pytestmark = pytest.mark.gpu
+
+HALF_TYPES = [torch.float16, torch.bfloat16]
+# (rows, inputs, outputs): the narrow form's widths with whole and part tiles of rows, then tiles
+LAYERS = [(64, 128, 128), (65, 64, 64), (40, 17, 40), (33, 127, 31), (300, 32, 128), (64, 129, 128), (64, 256, 200),
+          (300, 72, 400), (48, 1032, 520)]
+
+
+def backward(d, name):
+    n_out, n_in = d["w"].shape
+    dx = torch.full_like(d["x"], float("nan"))
+    dw = torch.full((n_out, n_in), float("nan"), device="cuda")
+    db = torch.full((n_out,), float("nan"), device="cuda")
+    gs.gs_linear_bwd(d["dy"], d["x"], d["w"], d["z"], dx, dw, db, space(d["x"], d["w"], name), act=name)
+    return dx, dw, db
+
+
+@pytest.mark.parametrize("dtype", HALF_TYPES)
+@pytest.mark.parametrize("size", [1e-2, 1e-3, 1e-4, 100.0])
+@pytest.mark.parametrize("rows,n_in,n_out", LAYERS)
+def test_weight_gradient_of_inputs_of_any_size(rows, n_in, n_out, size, dtype):
+    d = make(rows, n_in, n_out, dtype, rows + n_in)
+    d["x"] = (d["x"].float() * size).to(dtype)
+    for name in ("gelu", "silu"):
+        check_backward(d, name, *backward(d, name))
