@@ -508,7 +508,8 @@ gs_status gs_linear_fwd(const gs_linear* p, const void* residual, int64_t ldr, v
  * overwritten and may each be NULL. For dx, and for dw in a 16-bit type, dz is
  * rounded to p->type; for dw in fp32 it is kept to 22 bits or more (a dz beyond the
  * type's range counts as infinite). The same call gives the same bits.
- * workspace: gs_linear_workspace_size bytes, 256-byte aligned.
+ * workspace: gs_linear_workspace_size bytes, 256-byte aligned; without dw, the size for
+ * either dw_type is enough.
  */
 gs_status gs_linear_bwd(const gs_linear* p, const void* dy, int64_t lddy, const void* z, int64_t ldz, void* dx,
                         int64_t lddx, void* dw, int64_t lddw, int32_t dw_type, float* db, void* workspace,

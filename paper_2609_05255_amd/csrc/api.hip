@@ -812,7 +812,8 @@ gs_status gs_linear_bwd(const gs_linear* p, const void* dy, int64_t lddy, const 
     if (dx && (st = check_matrix("dx", dx, p->rows, p->n_in, lddx, p->type)) != GS_OK) return st;
     GS_CHECK(dw_type == GS_F32 || dw_type == p->type, "dw_type %d: fp32 or the layer's type", dw_type);
     if (dw && (st = check_matrix("dw", dw, p->n_out, p->n_in, lddw, dw_type)) != GS_OK) return st;
-    if ((st = check_workspace(workspace, workspace_bytes, linear_bwd_workspace(*p, dy, lddy, dw_type))) != GS_OK)
+    if ((st = check_workspace(workspace, workspace_bytes, linear_bwd_workspace(*p, dy, lddy, dw ? dw_type : -1))) !=
+        GS_OK)
         return st;
     hipStream_t s = static_cast<hipStream_t>(stream);
     timing_begin(GS_KERNEL_LINEAR_BWD, s);

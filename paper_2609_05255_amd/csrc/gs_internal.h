@@ -211,7 +211,7 @@ hipError_t launch_layer_norm_bwd(int type, const void* dy, int64_t lddy, const v
                                  int dim, void* dx, int64_t lddx, float* dw, float* db, float* part, hipStream_t s);
 size_t linear_workspace(int type, int act, int64_t rows, int64_t in, int64_t out, int dw_type);   // -1: forward only
 size_t linear_fwd_workspace(const gs_linear& p, bool z);
-size_t linear_bwd_workspace(const gs_linear& p, const void* dy, int64_t lddy, int dw_type);
+size_t linear_bwd_workspace(const gs_linear& p, const void* dy, int64_t lddy, int dw_type);   // -1: without dW
 bool linear_grid_fits(int64_t rows, int64_t cols);
 hipError_t launch_linear_fwd(const gs_linear& p, const void* residual, int64_t ldr, void* y, int64_t ldy, void* z,
                              int64_t ldz, void* ws, hipStream_t s);

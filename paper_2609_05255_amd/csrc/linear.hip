@@ -118,9 +118,10 @@ Plan plan_tt(int type, int64_t out, int64_t in, int64_t rows, int planes, bool f
     return plan_product(type, true, out, in, rows, planes, fast_b, kRowSplitLen);
 }
 
-// Planes of dz: an fp32 weight gradient keeps what rounding dz to 16 bits would drop, as further planes of the
-// type; without an activation, or with relu, dz is dy or 0 and needs none. dx, and a dW in the type itself, take the
-// first plane alone: their operands' rounding adds to that of the result what a user's own dz in this type would.
+// Planes of dz (dw_type: -1 without dW): an fp32 weight gradient keeps what rounding dz to 16 bits would drop, as
+// further planes of the type; without an activation, or with relu, dz is dy or 0 and needs none. dx, and a dW in the
+// type itself, take the first plane alone: their operands' rounding adds to that of the result what a user's own dz in
+// this type would.
 int planes_of(int type, int act, int dw_type)
 {
     if (type == GS_F32 || dw_type != GS_F32 || act == GS_ACT_NONE || act == GS_ACT_RELU) return 1;
@@ -213,6 +214,7 @@ struct BwdSpace {
     size_t bytes;
 };
 
+// dw_type: -1 without dW. Whatever the calls that a layer's workspace was sized for, one without dW needs no more.
 BwdSpace bwd_space(void* base, int type, int act, int64_t rows, int64_t in, int64_t out, int dw_type, bool need_dz)
 {
     Regions r{(char*)base};
@@ -222,9 +224,10 @@ BwdSpace bwd_space(void* base, int type, int act, int64_t rows, int64_t in, int6
         b.bytes = r.at;
         return b;
     }
+    const bool want_dw = dw_type >= 0;
     const int planes = planes_of(type, act, dw_type);
     if (need_dz) b.dz = r.take(planes * rows * padded(type, out) * elem(type));
-    if (in % vec(type)) b.x = r.take(rows * padded(type, in) * elem(type));
+    if (want_dw && in % vec(type)) b.x = r.take(rows * padded(type, in) * elem(type));
     b.wt = r.take(in * padded(type, out) * elem(type));
     b.sums = (float*)r.take((int64_t)slope_row_blocks(type, rows, out) * out * 4);
     int64_t part = 0;
@@ -233,7 +236,7 @@ BwdSpace bwd_space(void* base, int type, int act, int64_t rows, int64_t in, int6
         if (x.splits > 1) part = (int64_t)x.splits * rows * in * 4;
     }
     // (a workspace is sized for either operand's alignment)
-    for (int fast_x = 0; fast_x < 2; ++fast_x) {
+    for (int fast_x = 0; want_dw && fast_x < 2; ++fast_x) {
         const Plan w = plan_tt(type, out, in, rows, planes, fast_x != 0);
         if (w.splits > 1) part = std::max(part, (int64_t)w.splits * out * in * 4);
     }
@@ -298,8 +301,8 @@ hipError_t linear_bwd(const gs_linear& p, const void* dy, int64_t lddy, const vo
                       int64_t lddx, void* dw, int64_t lddw, int dw_type, float* db, void* ws, hipStream_t s)
 {
     const bool need_dz = p.act != GS_ACT_NONE || !fast(dy, lddy, p.n_out, p.type);
-    const BwdSpace b = bwd_space(ws, p.type, p.act, p.rows, p.n_in, p.n_out, dw_type, need_dz);
-    const int planes = dw ? planes_of(p.type, p.act, dw_type) : 1;
+    const BwdSpace b = bwd_space(ws, p.type, p.act, p.rows, p.n_in, p.n_out, dw ? dw_type : -1, need_dz);
+    const int planes = planes_of(p.type, p.act, dw ? dw_type : -1);
     if constexpr (sizeof(T) == 2)
         if (narrow(p.type, p.n_in, p.n_out)) {
             const NarrowArgs a = {dy,   z,     p.x,  p.w,  lddy, ldz, p.ldx, p.ldw, lddx, lddw, p.rows, (int)p.n_out,
@@ -327,7 +330,7 @@ hipError_t linear_bwd(const gs_linear& p, const void* dy, int64_t lddy, const vo
         slope.row_blocks = slope_row_blocks(p.type, p.rows, p.n_out);
         slope.sums = db ? (slope.row_blocks == 1 ? db : b.sums) : nullptr;
     }
-    const bool copy_x = dw && b.x, want_dx = dx && p.rows > 0;
+    const bool copy_x = b.x != nullptr, want_dx = dx && p.rows > 0;
     if (copy_x) copy = copy_of(p.type, p.x, p.ldx, p.rows, p.n_in, b.x);
     const TransposeArgs transpose = {p.w, p.ldw, p.n_out, p.n_in, b.wt, ldt};
     hipError_t e = LinearOps<T>::prepare(need_dz || db ? &slope : nullptr, copy_x ? &copy : nullptr,

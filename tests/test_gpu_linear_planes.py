@@ -32,3 +32,19 @@ def test_weight_gradient_of_inputs_of_any_size(rows, n_in, n_out, size, dtype):
     d["x"] = (d["x"].float() * size).to(dtype)
     for name in ("gelu", "silu"):
         check_backward(d, name, *backward(d, name))
+
+
+@pytest.mark.parametrize("dtype", HALF_TYPES)
+@pytest.mark.parametrize("rows,n_in,n_out", [(300, 48, 40), (500, 256, 200), (333, 203, 150), (20, 300, 72)])
+def test_outputs_left_out_with_workspaces_for_either_type(rows, n_in, n_out, dtype):
+    d = make(rows, n_in, n_out, dtype, rows)
+    for dw_type in (torch.float32, dtype):
+        ws = space(d["x"], d["w"], "gelu", dw_type)
+        dx, db = torch.empty_like(d["x"]), torch.empty(n_out, device="cuda")
+        dw = torch.empty(n_out, n_in, dtype=dw_type, device="cuda")
+        for keep in range(8):
+            outs = [t if keep >> k & 1 else None for k, t in enumerate((dx, dw, db))]
+            for t in (dx, dw, db):
+                t.fill_(float("nan"))
+            gs.gs_linear_bwd(d["dy"], d["x"], d["w"], d["z"], *outs, ws, act="gelu")
+            check_backward(d, "gelu", *outs)
