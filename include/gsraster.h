@@ -514,7 +514,8 @@ gs_status gs_linear_fwd(const gs_linear* p, const void* residual, int64_t ldr, v
 gs_status gs_linear_bwd(const gs_linear* p, const void* dy, int64_t lddy, const void* z, int64_t ldz, void* dx,
                         int64_t lddx, void* dw, int64_t lddw, int32_t dw_type, float* db, void* workspace,
                         size_t workspace_bytes, void* stream);
-/* Bytes for the forward and the backward of a layer; dw_type -1: for the forward alone. */
+/* Bytes for the forward and the backward of a layer; dw_type -1: for the forward alone.
+ * The size for an fp32 dw is enough for one in the layer's type too. */
 gs_status gs_linear_workspace_size(int32_t type, int32_t act, int64_t rows, int64_t n_in, int64_t n_out, int32_t dw_type,
                                    size_t* bytes);
 

@@ -396,7 +396,10 @@ size_t linear_bwd_workspace(const gs_linear& p, const void* dy, int64_t lddy, in
 size_t linear_workspace(int type, int act, int64_t rows, int64_t in, int64_t out, int dw_type)
 {
     const size_t fwd = fwd_space(nullptr, type, rows, in, out, true, true).bytes;
-    return dw_type < 0 ? fwd : std::max(fwd, bwd_space(nullptr, type, act, rows, in, out, dw_type, true).bytes);
+    if (dw_type < 0) return fwd;
+    // (fewer planes of dz can mean more splits of dW: the size for an fp32 dW does for one in the type as well)
+    return std::max({fwd, bwd_space(nullptr, type, act, rows, in, out, dw_type, true).bytes,
+                     bwd_space(nullptr, type, act, rows, in, out, type, true).bytes});
 }
 
 // Work items of a launch are counted in 32 bits.

@@ -437,7 +437,7 @@ def _activation(act) -> int:
 
 def gs_linear_workspace_size(x, w, act: str = "none", dw_type=torch.float32) -> int:
     """Workspace bytes of gs_linear_fwd and gs_linear_bwd for these shapes; dw_type: the weight gradient's type
-    (None: for the forward alone)."""
+    (float32: enough for one of x's type too; None: for the forward alone)."""
     rows, n_in = _shape("x", x)
     n_out = _shape("w", w)[0]
     out = C.c_size_t(0)

@@ -53,3 +53,26 @@ def test_without_a_weight_gradient(gs, type_, act, layer, odd):
         for dw_type in {F32, type_}:
             assert accepts(gs, type_, act, layer, False, dw_type, have, odd), (sized_for, dw_type)
         assert accepts(gs, type_, act, layer, True, sized_for, have, odd)
+
+
+# with gelu in binary16 the product of the first plane alone is split further than that of both: 2763 x 2922 -> 71 and
+# 5581 x 1426 -> 66 needed more for a binary16 dw than for an fp32 one
+@pytest.mark.parametrize("layer", LAYERS)
+@pytest.mark.parametrize("act", [NONE, RELU, GELU])
+@pytest.mark.parametrize("type_", [F16, BF16])
+@pytest.mark.parametrize("odd", [False, True])
+def test_the_size_for_an_fp32_weight_gradient_does_for_both_types(gs, type_, act, layer, odd):
+    assert size(gs, type_, act, layer, F32) >= size(gs, type_, act, layer, type_)
+    assert accepts(gs, type_, act, layer, True, type_, size(gs, type_, act, layer, F32), odd)
+
+
+def test_general_layers_keep_dz_in_planes(gs):
+    # beyond the narrow form's 128 columns the workspace holds dz, once more for each further plane of an fp32 dw
+    plane = 1000 * 200 * 2
+    for type_, planes in ((F16, 2), (BF16, 3)):
+        for act, kept in ((GELU, planes), (RELU, 1)):
+            assert size(gs, type_, act, (1000, 256, 200), F32) >= kept * plane + 256 * 200 * 2
+        one, more = (size(gs, type_, GELU, (1000, 256, 200), t) for t in (type_, F32))
+        assert one >= plane + 256 * 200 * 2 and more - one >= (planes - 1) * plane - 256 * 200 * 4
+    # the narrow form keeps none: parts of dW and db alone, alike for either type of dw
+    assert size(gs, F16, GELU, (1000, 64, 48), F32) == size(gs, F16, GELU, (1000, 64, 48), F16)
