@@ -93,17 +93,26 @@ class FusedAdam:
 
         self.max_grad_norm, self.clip = max_grad_norm, None
         if max_grad_norm is not None:
-            self.grad_set = gs.GradSet([g["grad"] for g in self.groups])
             self.clip = torch.zeros(2, device=scene.means.device)   # the last step's norm and coefficient
-            self.clip_ws = torch.empty(gs.gs_grad_workspace_size(self.grad_set), dtype=torch.uint8,
-                                       device=scene.means.device)
+            self.clip_ws = torch.empty(self._clip_size(self._grad_set()), dtype=torch.uint8, device=scene.means.device)
+
+    def _grad_set(self):
+        return gs.GradSet([g["grad"] for g in self.groups])
+
+    def _clip_size(self, grads):
+        return max(gs.gs_grad_workspace_size(grads), 1)
 
     def step(self, stream=None):
         self.t += 1
         if self.clip is None:
             gs.gs_adam_step(self.groups, self.beta1, self.eps, self.t, stream)
             return
-        gs.gs_grad_norm(self.grad_set, self.max_grad_norm, self.clip, self.clip_ws, stream)
+        # the groups as they are now, as the step reads them: a caller may have put other tensors in
+        grads = self._grad_set()
+        if self._clip_size(grads) > self.clip_ws.numel():
+            torch.cuda.synchronize(self.clip.device)   # an earlier step may still use the smaller one
+            self.clip_ws = torch.empty(self._clip_size(grads), dtype=torch.uint8, device=self.clip.device)
+        gs.gs_grad_norm(grads, self.max_grad_norm, self.clip, self.clip_ws, stream)
         gs.gs_adam_step(self.groups, self.beta1, self.eps, self.t, stream, grad_scale=self.clip[1:])
 
     def backward_step(self, frame: gs.Frame, cam: gs.Camera, scene: gs.SceneTensors, dL_dimage, sh_degree: int = 3,
