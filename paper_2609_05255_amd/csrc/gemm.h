@@ -488,7 +488,14 @@ __global__ __launch_bounds__(S::THREADS * S::WAYS) void k_gemm(GemmArgs g)
 #pragma unroll
             for (int p = 0; p < FI; ++p)
 #pragma unroll
-                for (int q = 0; q < FJ; ++q) acc[p][q] *= g.plane_scale;
+                for (int q = 0; q < FJ; ++q)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        // (where B has an infinite or undefined value, the first plane alone says what becomes of it:
+                        // what it makes of a lower plane's zeros and signs is left out)
+                        const float v = acc[p][q][e];
+                        acc[p][q][e] = fabsf(v) < __builtin_inff() ? v * g.plane_scale : 0.f;
+                    }
         }
     }
     if constexpr (S::WAYS > 1) {

@@ -17,6 +17,8 @@
 // P planes of dz: dz rounded to T (all that dx takes, as it is rounded to T itself), then what that leaves, so that an
 // fp32 dW keeps 22 bits or more. In binary16 the second plane is scaled by 2^11 against underflow; its products of 32
 // rows are summed apart and join dW's sums times 2^-11 in fp32 (scaling x instead would round every x below 2^-3).
+// An infinite or undefined x counts as 0 beside the lower planes, whose zeros and signs say nothing about its product
+// with dz; a lane looks for one in its fragments of x.
 #pragma once
 
 #include "gemm.h"
@@ -67,6 +69,26 @@ __device__ __forceinline__ typename Mma<T>::Frag narrow_rows(const char* lds, in
     typename Mma<T>::Frag out;
     __builtin_memcpy(&out, both, 16);
     return out;
+}
+
+// The halves of a word of two 16-bit values whose exponents are all ones (infinite or undefined): their highest bits.
+template <typename T>
+__device__ __forceinline__ uint32_t not_finite(uint32_t w)
+{
+    return ((w & 0x7FFF7FFFu) + (__is_same(T, f16) ? 0x04000400u : 0x00800080u)) & 0x80008000u;
+}
+
+// v with such values as 0
+template <typename T, typename V>
+__device__ __forceinline__ V finite_of(V v)
+{
+    u32x4 w = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t one = not_finite<T>(w[e]) >> 15;
+        w[e] &= ~((one << 16) - one);
+    }
+    return __builtin_bit_cast(V, w);
 }
 
 // FAST: rows of dy, z and x are whole aligned vectors, and come through buffer loads whose range check turns what lies
@@ -203,14 +225,25 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void k_narrow_bwd(NarrowArgs a)
             }
         if (a.dw) {
 #pragma unroll
-            for (int p = 0; p < P; ++p)
+            for (int s = 0; s < R / 32; ++s) {
+                Frag fx[FI];
 #pragma unroll
-                for (int s = 0; s < R / 32; ++s) {
-                    Frag fz[FO], fx[FI];
+                for (int n = 0; n < FI; ++n) fx[n] = narrow_columns<T>(lds_x, R, wn + n, 32 * s);
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    Frag fz[FO];
 #pragma unroll
                     for (int n = 0; n < FO; ++n) fz[n] = narrow_columns<T>(lds_dz + p * kDz, R, wo + n, 32 * s);
+                    if (p == 1) {
+                        uint32_t found = 0;   // values that are not finite
 #pragma unroll
-                    for (int n = 0; n < FI; ++n) fx[n] = narrow_columns<T>(lds_x, R, wn + n, 32 * s);
+                        for (int n = 0; n < FI; ++n)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) found |= not_finite<T>(__builtin_bit_cast(u32x4, fx[n])[e]);
+                        if (found)
+#pragma unroll
+                            for (int n = 0; n < FI; ++n) fx[n] = finite_of<T>(fx[n]);
+                    }
 #pragma unroll
                     for (int m = 0; m < FO; ++m)
 #pragma unroll
@@ -224,6 +257,7 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void k_narrow_bwd(NarrowArgs a)
                             }
                         }
                 }
+            }
         }
         __syncthreads();   // LDS is free again
     }

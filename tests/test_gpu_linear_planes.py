@@ -48,3 +48,28 @@ def test_outputs_left_out_with_workspaces_for_either_type(rows, n_in, n_out, dty
                 t.fill_(float("nan"))
             gs.gs_linear_bwd(d["dy"], d["x"], d["w"], d["z"], *outs, ws, act="gelu")
             check_backward(d, "gelu", *outs)
+
+
+@pytest.mark.parametrize("dtype", HALF_TYPES)
+@pytest.mark.parametrize("rows,n_in,n_out", LAYERS + [(70, 1032, 2048), (2100, 1000, 960), (4100, 264, 1040)])
+def test_infinite_and_undefined_inputs(rows, n_in, n_out, dtype):
+    # an x that is not finite meets its column of dw alone, and that with the sign of its products with dz: what it makes
+    # of the lower planes' zeros and signs must not show
+    d = make(rows, n_in, n_out, dtype, 3 * rows + n_in)
+    d["dy"] = (d["dy"].sign() * (0.02 + d["dy"].abs().float())).to(dtype)
+    d["z"] = (d["z"].abs().float() + 0.5).to(dtype)   # slopes between 0.7 and 1.2
+    d["dy"][5, 3] = 0.0
+    up, down, none = 7, n_in - 1, n_in // 2
+    d["x"][5, up] = float("inf")
+    d["x"][rows - 1, down] = float("-inf")
+    d["x"][11, none] = float("nan")
+    for name in ("gelu", "silu"):
+        dx, dw, db = backward(d, name)
+        sign = d["dy"].float().sign()
+        want = sign[5] * float("inf")   # (0 times infinity is undefined)
+        assert torch.equal(dw[:, up].isnan(), want.isnan()) and bool(want.isnan()[3])
+        assert torch.equal(dw[:, up].nan_to_num(nan=0.0), want.nan_to_num(nan=0.0))
+        assert torch.equal(dw[:, down], -sign[rows - 1] * float("inf"))
+        assert torch.isnan(dw[:, none]).all()
+        keep = [c for c in range(n_in) if c not in (up, down, none)]
+        check_backward({**d, "x": d["x"][:, keep], "w": d["w"][:, keep]}, name, dx[:, keep], dw[:, keep], db)
