@@ -503,7 +503,8 @@ gs_status gs_linear_fwd(const gs_linear* p, const void* residual, int64_t ldr, v
 /*
  * gs_linear_bwd -- dz = dy act'(z), dx = dz w, dw = dz^T x, db = sum over rows of dz
  * (the residual's gradient is dy itself). p->bias is not read.
- * z: as gs_linear_fwd wrote it (not read for GS_ACT_NONE). dx: [rows][n_in]; dw:
+ * z: as gs_linear_fwd wrote it (not read for GS_ACT_NONE); where it is infinite, beyond
+ * the type's range, act' is its limit there. dx: [rows][n_in]; dw:
  * [n_out][n_in] of dw_type, GS_F32 or p->type; db: [n_out] fp32. dx, dw and db are
  * overwritten and may each be NULL. For dx, and for dw in a 16-bit type, dz is
  * rounded to p->type; for dw in fp32 it is kept to 22 bits or more (a dz beyond the

@@ -76,7 +76,8 @@ __device__ __forceinline__ void activate(int act, float* v)
     }
 }
 
-// v[k] *= act'(z[k])
+// v[k] *= act'(z[k]). A stored z may be infinite where the type's range ends before that of the layer's own sums: the
+// slope there is its limit, so z counts as bounded where it is multiplied by what has long become 0.
 template <int N>
 __device__ __forceinline__ void times_slope(int act, float* v, const float* z)
 {
@@ -90,14 +91,14 @@ __device__ __forceinline__ void times_slope(int act, float* v, const float* z)
         for (int k = 0; k < N; ++k) {
             float density;
             const float phi = normal_cdf(z[k], &density);
-            v[k] *= fmaf(z[k], density, phi);
+            v[k] *= fmaf(__builtin_amdgcn_fmed3f(z[k], -64.f, 64.f), density, phi);
         }
         break;
     case GS_ACT_SILU:
 #pragma unroll
         for (int k = 0; k < N; ++k) {
             const float p = logistic(z[k]);
-            v[k] *= p * fmaf(z[k], 1.f - p, 1.f);
+            v[k] *= p * fmaf(__builtin_amdgcn_fmed3f(z[k], -128.f, 128.f), 1.f - p, 1.f);
         }
         break;
     case GS_ACT_TANH:
