@@ -222,7 +222,7 @@ __global__ __launch_bounds__(G > 64 ? G : kNormWaves * 64) void k_norm_bwd(
 #pragma unroll
             for (int j = 0; j < N; ++j) {
                 xh[k][j] = (float)nx[k][j];
-                g[k][j] = (float)ng[k][j];   // 0 beyond the row, and with it all that such a place adds
+                g[k][j] = (float)ng[k][j];   // 0 beyond the row, and with it what such a place adds
             }
         }
         if (r + step < rows) fetch(r + step);
@@ -230,7 +230,8 @@ __global__ __launch_bounds__(G > 64 ? G : kNormWaves * 64) void k_norm_bwd(
         for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                xh[k][j] = (xh[k][j] - mu) * rs;
+                // (beyond the row 0 as well: the mean times rstd can be infinite where no x of the row is far from it)
+                xh[k][j] = (k * G + lane) * N + j < dim ? (xh[k][j] - mu) * rs : 0.f;
                 sb[k][j] += g[k][j];
                 sw[k][j] += g[k][j] * xh[k][j];
                 g[k][j] *= wv[k][j];
