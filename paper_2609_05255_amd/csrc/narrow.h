@@ -15,8 +15,9 @@
 // value 4 t + e of lane group g is row (dW) or column (dx) 16 t + 4 g + e of its 32.
 //
 // P planes of dz: dz rounded to T (all that dx takes, as it is rounded to T itself), then what that leaves, so that an
-// fp32 dW keeps 22 bits or more. In binary16 the second plane is scaled by 2^11 against underflow; its products of 32
-// rows are summed apart and join dW's sums times 2^-11 in fp32 (scaling x instead would round every x below 2^-3).
+// fp32 dW keeps 22 bits or more. In binary16 the second plane is scaled by 2^11 against underflow (below |dz| = 2^-14 dz
+// is kept to within 2^-36, which is fewer bits); its products of 32 rows are summed apart and join dW's sums times 2^-11
+// in fp32 (scaling x instead would round every x below 2^-3).
 // An infinite or undefined x counts as 0 beside the lower planes, whose zeros and signs say nothing about its product
 // with dz; a lane looks for one in its fragments of x.
 #pragma once

@@ -5,7 +5,8 @@ import pytest
 import torch
 
 from paper_2609_05255_amd import gsraster as gs
-from test_gpu_linear import check_backward, make, space
+from rows_reference import assert_close, slope, sum_bound
+from test_gpu_linear import ACT_ERROR, check_backward, make, space
 
 pytestmark = pytest.mark.gpu
 
@@ -73,3 +74,17 @@ def test_infinite_and_undefined_inputs(rows, n_in, n_out, dtype):
         assert torch.isnan(dw[:, none]).all()
         keep = [c for c in range(n_in) if c not in (up, down, none)]
         check_backward({**d, "x": d["x"][:, keep], "w": d["w"][:, keep]}, name, dx[:, keep], dw[:, keep], db)
+
+
+@pytest.mark.parametrize("dtype", HALF_TYPES)
+@pytest.mark.parametrize("size", [1e-4, 1e-6, 1e-7])
+@pytest.mark.parametrize("rows,n_in,n_out", LAYERS)
+def test_weight_gradient_of_small_gradients(rows, n_in, n_out, size, dtype):
+    # dz is kept to 22 bits, in binary16 to within 2^-36 where it is small (2^-14 and less)
+    d = make(rows, n_in, n_out, dtype, 5 * rows + n_in)
+    d["dy"] = (d["dy"].float() * (10 * size)).to(dtype)
+    x, dy, z = (d[k].double() for k in ("x", "dy", "z"))
+    dz = dy * slope("gelu", z)
+    lost = 2.0 ** -22 * dz.abs() + (2.0 ** -36 if dtype == torch.float16 else 0.0) + dy.abs() * ACT_ERROR * (1 + z.abs())
+    dw = backward(d, "gelu")[1]
+    assert_close("dw", dw, dz.t() @ x, sum_bound(rows) * (dz.abs().t() @ x.abs()) + lost.t() @ x.abs(), torch.float32)
