@@ -80,9 +80,12 @@ __device__ __forceinline__ void wait_loads()
     asm volatile("" ::: "memory");
 }
 
+// (behind a barrier LDS that a wave has read is written again: its reads have ended before it, by this wait and not only
+// where their use happens to stand in front of the barrier)
 __device__ __forceinline__ void barrier()
 {
     asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
@@ -422,9 +425,8 @@ __global__ __launch_bounds__(S::THREADS * S::WAYS) void k_gemm(GemmArgs g)
                 for (int t = 0; t < steps; ++t) {
                     half(fa[0], fb[0], a_lds[0], b_lds[0], 1, fa[1], fb[1], [&](int k) { sa.pass(a_lds[2], k); });
                     sa.advance();
-                    __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): this wave has tile t's fragments
                     wait_loads<TA::kPasses>();
-                    barrier();                            // as all have, and tile t + 1 is here
+                    barrier();   // all waves have tile t's fragments, and tile t + 1 is here
                     half(fa[1], fb[1], a_lds[1], b_lds[1], 0, fa[0], fb[0], [&](int k) { sb.pass(b_lds[0], k); });
                     sb.advance();
                     char* x = a_lds[0];
