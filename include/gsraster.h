@@ -506,7 +506,8 @@ gs_status gs_linear_fwd(const gs_linear* p, const void* residual, int64_t ldr, v
  * z: as gs_linear_fwd wrote it (not read for GS_ACT_NONE); where it is infinite, beyond
  * the type's range, act' is its limit there. dx: [rows][n_in]; dw:
  * [n_out][n_in] of dw_type, GS_F32 or p->type; db: [n_out] fp32. dx, dw and db are
- * overwritten and may each be NULL. For dx, and for dw in a 16-bit type, dz is
+ * overwritten and may each be NULL (dx: GS_ERR_UNSUPPORTED if n_in times n_out exceed
+ * the grid, about 2^36 values). For dx, and for dw in a 16-bit type, dz is
  * rounded to p->type; for dw in fp32 it is kept to 22 bits or more, in binary16 from
  * |dz| = 2^-14 on and to within 2^-36 below (a dz beyond the type's range counts as
  * infinite). The same call gives the same bits.

@@ -810,6 +810,9 @@ gs_status gs_linear_bwd(const gs_linear* p, const void* dy, int64_t lddy, const 
     if ((st = check_matrix("dy", dy, p->rows, p->n_out, lddy, p->type)) != GS_OK) return st;
     if (p->act != GS_ACT_NONE && (st = check_matrix("z", z, p->rows, p->n_out, ldz, p->type)) != GS_OK) return st;
     if (dx && (st = check_matrix("dx", dx, p->rows, p->n_in, lddx, p->type)) != GS_OK) return st;
+    if (dx && !linear_dx_fits(p->n_in, p->n_out))
+        return fail(GS_ERR_UNSUPPORTED, "dx against %lld x %lld weights exceeds the grid", (long long)p->n_out,
+                    (long long)p->n_in);
     GS_CHECK(dw_type == GS_F32 || dw_type == p->type, "dw_type %d: fp32 or the layer's type", dw_type);
     if (dw && (st = check_matrix("dw", dw, p->n_out, p->n_in, lddw, dw_type)) != GS_OK) return st;
     if ((st = check_workspace(workspace, workspace_bytes, linear_bwd_workspace(*p, dy, lddy, dw ? dw_type : -1))) !=

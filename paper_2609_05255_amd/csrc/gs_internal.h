@@ -213,6 +213,7 @@ size_t linear_workspace(int type, int act, int64_t rows, int64_t in, int64_t out
 size_t linear_fwd_workspace(const gs_linear& p, bool z);
 size_t linear_bwd_workspace(const gs_linear& p, const void* dy, int64_t lddy, int dw_type);   // -1: without dW
 bool linear_grid_fits(int64_t rows, int64_t cols);
+bool linear_dx_fits(int64_t in, int64_t out);
 hipError_t launch_linear_fwd(const gs_linear& p, const void* residual, int64_t ldr, void* y, int64_t ldy, void* z,
                              int64_t ldz, void* ws, hipStream_t s);
 hipError_t launch_linear_bwd(const gs_linear& p, const void* dy, int64_t lddy, const void* z, int64_t ldz, void* dx,

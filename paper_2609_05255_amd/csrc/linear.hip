@@ -408,6 +408,12 @@ bool linear_grid_fits(int64_t rows, int64_t cols)
     return div_up(rows, 128) * div_up(cols, cols <= 64 ? 64 : 128) * 256 < ((int64_t)1 << 32);
 }
 
+// The launch that transposes W for dx, beside dz and x of up to 2^12 workgroups each.
+bool linear_dx_fits(int64_t in, int64_t out)
+{
+    return (div_up(in, 64) * div_up(out, 64) + 8192) * kBlock < ((int64_t)1 << 32);
+}
+
 hipError_t launch_linear_fwd(const gs_linear& p, const void* residual, int64_t ldr, void* y, int64_t ldy, void* z,
                              int64_t ldz, void* ws, hipStream_t s)
 {

@@ -76,3 +76,15 @@ def test_general_layers_keep_dz_in_planes(gs):
         assert one >= plane + 256 * 200 * 2 and more - one >= (planes - 1) * plane - 256 * 200 * 4
     # the narrow form keeps none: parts of dW and db alone, alike for either type of dw
     assert size(gs, F16, GELU, (1000, 64, 48), F32) == size(gs, F16, GELU, (1000, 64, 48), F16)
+
+
+def test_weights_too_large_to_transpose_are_refused(gs):
+    # 2^18 x 2^18: the launch that transposes W for dx would have 2^32 work items; without dx there is none
+    n = 1 << 18
+    p = gs.Linear(BF16, NONE, 1, n, n, FAKE, FAKE, None, n, n)
+
+    def call(dx):
+        return gs.lib().gs_linear_bwd(C.byref(p), FAKE, n, None, 0, dx, n, None, n, F32, FAKE, FAKE + 8, 1 << 50, None)
+
+    assert call(FAKE) == gs.GS_ERR_UNSUPPORTED
+    assert call(None) == gs.GS_ERR_INVALID_ARG and b"aligned" in gs.lib().gs_last_error()
