@@ -17,8 +17,10 @@ namespace {
 constexpr int kFillTiles = 256;          // compute units
 constexpr int kSlopeBlocks = 2048;
 constexpr int64_t kJoinSplitLen = 256;   // values of the sum in a split of a product of few tiles, at least
-// Rows up to which the weights' bytes bound the product (4,096 x 4,096 in bfloat16: 64 rows 21 us, 16 in tiles; 70 and
-// 39, with a copy of W first, where its rows are not aligned).
+// Rows up to which the weights' bytes bound the product. The form for few rows and tiles, us a call in bfloat16:
+//   4,096 x 4,096: 17 rows 10.5 and 12.2, 32 rows 12.9 and 13.4 (64 rows, when it was built for them, 21 and 16)
+//   2,048 x 2,048: 32 rows 7.4 and 10.3; 512 x 512: 6.8 and 7.3; 2,048 x 2,048 in fp32: 13.2 and 14.0
+//   4,095 x 4,096, whose rows tiles copy first: 32 rows 18.7 and 33
 constexpr int64_t kFewRows = 32;
 constexpr int64_t kRowSplitLen = 128;    // rows in a split of dW's sum, at least
 
@@ -178,11 +180,17 @@ int narrow_blocks(int64_t rows, int64_t in, int64_t out)
     return (int)std::max<int64_t>(1, std::min<int64_t>(div_up(rows, 64), most));
 }
 
-// The forward in that form, but where z and y are wider than x and more than the 256 MB cache holds: there the tiles'
-// larger blocks of writes are faster (3,000,000 x 64 x 128 with z: 338 us against 393; 100,000 rows: 20 against 17).
-bool narrow_forward(int type, int64_t rows, int64_t in, int64_t out, bool z)
+// The forward in that form, but where little is read and computed for z and y, which are more than the 256 MB cache holds:
+// there the tiles' larger blocks of writes are faster. In binary16 with z, us in this form and in tiles:
+//   64 -> 128, relu: 100,000 rows 14 and 18, 300,000 33 and 36, 540,000 81 and 71, 1,000,000 131 and 120
+//   1,000,000 rows, relu: 40 -> 128 127 and 113, 64 -> 100 170 and 140, 32 -> 64 61 and 62, 64 -> 72 99 and 96;
+//     more than 64 inputs: 96 -> 128 138 and 153; rows of x that are not aligned: 60 -> 128 151 and 180
+//   1,000,000 x 64 -> 128, gelu: 141 and 151
+bool narrow_forward(int type, int act, int64_t rows, int64_t in, int64_t out, bool z, bool fast_x)
 {
-    return narrow(type, in, out) && !(z && out > in && 4 * rows * out > ((int64_t)256 << 20));
+    const bool writes = z && out > in && 4 * rows * out > ((int64_t)256 << 20);
+    const bool little = fast_x && in <= 64 && (act == GS_ACT_NONE || act == GS_ACT_RELU);
+    return narrow(type, in, out) && !(writes && little);
 }
 
 struct FwdSpace {
@@ -191,11 +199,12 @@ struct FwdSpace {
     size_t bytes;
 };
 
-FwdSpace fwd_space(void* base, int type, int64_t rows, int64_t in, int64_t out, bool copy_w, bool z)
+FwdSpace fwd_space(void* base, int type, int act, int64_t rows, int64_t in, int64_t out, bool copy_w, bool z,
+                   bool aligned_x)
 {
     Regions r{(char*)base};
     FwdSpace f = {};
-    if (rows > kFewRows && !narrow_forward(type, rows, in, out, z)) {
+    if (rows > kFewRows && !narrow_forward(type, act, rows, in, out, z, aligned_x)) {
         if (copy_w) f.w = r.take(out * padded(type, in) * elem(type));
         int splits = 1;   // (a workspace is sized for either alignment of x)
         for (int fast_x = 0; fast_x < 2; ++fast_x) splits = std::max(splits, plan_nt(type, rows, out, in, fast_x).splits);
@@ -266,7 +275,7 @@ hipError_t linear_fwd(const gs_linear& p, const void* residual, int64_t ldr, voi
                       int64_t ldz, void* ws, hipStream_t s)
 {
     const bool copy_w = !fast(p.w, p.ldw, p.n_in, p.type), fast_x = fast(p.x, p.ldx, p.n_in, p.type);
-    const FwdSpace f = fwd_space(ws, p.type, p.rows, p.n_in, p.n_out, copy_w, z != nullptr);
+    const FwdSpace f = fwd_space(ws, p.type, p.act, p.rows, p.n_in, p.n_out, copy_w, z != nullptr, fast_x);
     GemmArgs g = {};
     g.a = p.x;
     g.lda = p.ldx;
@@ -291,7 +300,7 @@ hipError_t linear_fwd(const gs_linear& p, const void* residual, int64_t ldr, voi
     g.z = z;
     g.ldz = ldz;
     if constexpr (sizeof(T) == 2)
-        if (p.rows > kFewRows && narrow_forward(p.type, p.rows, p.n_in, p.n_out, z != nullptr))
+        if (p.rows > kFewRows && narrow_forward(p.type, p.act, p.rows, p.n_in, p.n_out, z != nullptr, fast_x))
             return NarrowOps<T>::forward(g, fast_x, (int)std::min<int64_t>(div_up(p.rows, 64), 4 * kFillTiles), s);
     return run_nt<T>(p.type, g, fast_x, f.part, s);
 }
@@ -384,7 +393,8 @@ hipError_t linear_bwd(const gs_linear& p, const void* dy, int64_t lddy, const vo
 
 size_t linear_fwd_workspace(const gs_linear& p, bool z)
 {
-    return fwd_space(nullptr, p.type, p.rows, p.n_in, p.n_out, !fast(p.w, p.ldw, p.n_in, p.type), z).bytes;
+    return fwd_space(nullptr, p.type, p.act, p.rows, p.n_in, p.n_out, !fast(p.w, p.ldw, p.n_in, p.type), z,
+                     fast(p.x, p.ldx, p.n_in, p.type)).bytes;
 }
 
 size_t linear_bwd_workspace(const gs_linear& p, const void* dy, int64_t lddy, int dw_type)
@@ -395,7 +405,7 @@ size_t linear_bwd_workspace(const gs_linear& p, const void* dy, int64_t lddy, in
 
 size_t linear_workspace(int type, int act, int64_t rows, int64_t in, int64_t out, int dw_type)
 {
-    const size_t fwd = fwd_space(nullptr, type, rows, in, out, true, true).bytes;
+    const size_t fwd = fwd_space(nullptr, type, act, rows, in, out, true, true, true).bytes;
     if (dw_type < 0) return fwd;
     // (fewer planes of dz can mean more splits of dW: the size for an fp32 dW does for one in the type as well)
     return std::max({fwd, bwd_space(nullptr, type, act, rows, in, out, dw_type, true).bytes,

@@ -58,3 +58,17 @@ def test_infinite_gradient(rows, n_in, n_out, dtype):
         check_backward({**clean, "dy": clean["dy"][keep], "z": d["z"][keep], "x": d["x"][keep]}, name, dx[keep], None, None)
         check_backward({**clean, "dy": clean["dy"][:, cols], "z": d["z"][:, cols], "w": d["w"][cols]}, name, None,
                        dw[cols], db[cols])
+
+
+# more z and y than the cache holds, in the narrow form and in tiles: by the activation, the inputs' width and x's alignment
+@pytest.mark.parametrize("rows,n_in,n_out,name,pad", [(1_100_003, 32, 64, "gelu", 0), (1_100_003, 32, 64, "relu", 4),
+                                                      (1_100_003, 32, 64, "none", 8), (600_001, 72, 120, "relu", 0),
+                                                      (1_500_001, 17, 45, "relu", 0)])
+def test_forward_of_more_than_the_cache_holds(rows, n_in, n_out, name, pad):
+    d = make(rows, n_in, n_out, torch.float16, 3)
+    x = strided(d["x"], pad) if pad else d["x"]
+    y, z = (torch.full_like(d["r"], float("nan")) for _ in range(2))
+    gs.gs_linear_fwd(x, d["w"], d["bias"], y, space(d["x"], d["w"], name, None), act=name, residual=d["r"], z=z)
+    for part in (slice(0, 2000), slice(rows // 2, rows // 2 + 2000), slice(rows - 2000, rows)):
+        check_forward({k: v[part] if v.shape[0] == rows else v for k, v in d.items()}, name, y[part], z[part])
+    assert torch.isfinite(y).all() and torch.isfinite(z).all()
