@@ -77,7 +77,8 @@ __device__ __forceinline__ void activate(int act, float* v)
 }
 
 // v[k] *= act'(z[k]). A stored z may be infinite where the type's range ends before that of the layer's own sums: the
-// slope there is its limit, so z counts as bounded where it is multiplied by what has long become 0.
+// slope there is its limit, where the formula has infinity times 0. (Chosen by a comparison: bounding z instead takes
+// registers for the bounds, which cost the narrow backward of 128 x 128 with relu 20 of 204 us.)
 template <int N>
 __device__ __forceinline__ void times_slope(int act, float* v, const float* z)
 {
@@ -91,14 +92,14 @@ __device__ __forceinline__ void times_slope(int act, float* v, const float* z)
         for (int k = 0; k < N; ++k) {
             float density;
             const float phi = normal_cdf(z[k], &density);
-            v[k] *= fmaf(__builtin_amdgcn_fmed3f(z[k], -64.f, 64.f), density, phi);
+            v[k] *= fabsf(z[k]) < __builtin_inff() ? fmaf(z[k], density, phi) : phi;
         }
         break;
     case GS_ACT_SILU:
 #pragma unroll
         for (int k = 0; k < N; ++k) {
             const float p = logistic(z[k]);
-            v[k] *= p * fmaf(__builtin_amdgcn_fmed3f(z[k], -128.f, 128.f), 1.f - p, 1.f);
+            v[k] *= fabsf(z[k]) < __builtin_inff() ? p * fmaf(z[k], 1.f - p, 1.f) : p;
         }
         break;
     case GS_ACT_TANH:
