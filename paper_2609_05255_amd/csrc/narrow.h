@@ -8,7 +8,7 @@
 // registers over all of them, so that both products come from the same tile: dx sums over dz's columns, dW over its
 // rows. The next rows are fetched into registers under the products. Each workgroup writes its dW and db once;
 // k_narrow_join adds them up in a fixed order. Measured: 1,000,000 x 128 x 128 in binary16 with relu 196 and 8 us, 5.0
-// TB/s of what it has to move (separate products: 392).
+// TB/s of what it has to move (separate products: 392); with gelu and an fp32 dW, in planes, 256 and 8 (bfloat16 270).
 //
 // LDS layout of each matrix: blocks of 64 columns, rows of 128 bytes, 16-byte slots XOR-ed with a hash of the row, so
 // that the transposing reads (dW's operands, W) and the row reads (dz in dx) are free of bank conflicts. A fragment's
