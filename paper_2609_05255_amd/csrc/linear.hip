@@ -405,7 +405,8 @@ size_t linear_bwd_workspace(const gs_linear& p, const void* dy, int64_t lddy, in
 
 size_t linear_workspace(int type, int act, int64_t rows, int64_t in, int64_t out, int dw_type)
 {
-    const size_t fwd = fwd_space(nullptr, type, act, rows, in, out, true, true, true).bytes;
+    // (the forward that needs most: with z, W and x as they may come, whatever the activation)
+    const size_t fwd = fwd_space(nullptr, type, GS_ACT_NONE, rows, in, out, true, true, true).bytes;
     if (dw_type < 0) return fwd;
     // (fewer planes of dz can mean more splits of dW: the size for an fp32 dW does for one in the type as well)
     return std::max({fwd, bwd_space(nullptr, type, act, rows, in, out, dw_type, true).bytes,

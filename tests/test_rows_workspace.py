@@ -88,3 +88,9 @@ def test_weights_too_large_to_transpose_are_refused(gs):
 
     assert call(FAKE) == gs.GS_ERR_UNSUPPORTED
     assert call(None) == gs.GS_ERR_INVALID_ARG and b"aligned" in gs.lib().gs_last_error()
+
+
+@pytest.mark.parametrize("layer", LAYERS + [(1_100_000, 30, 63), (3_000_000, 64, 128)])
+@pytest.mark.parametrize("type_", [F32, F16, BF16])
+def test_the_forward_needs_the_same_for_any_activation(gs, type_, layer):
+    assert len({size(gs, type_, act, layer, -1) for act in range(6)}) == 1
