@@ -553,6 +553,104 @@ gs_status gs_grad_workspace_size(const gs_grad_tensor* tensors, int32_t count, s
 gs_status gs_adam_step_scaled(const gs_adam_tensor* tensors, int32_t count, float beta1, float eps, int64_t step,
                               const float* grad_scale, void* stream);
 
+/* ---- Codebooks and mixtures of decoders ---------------------------------------------
+ * Rows that share entries of a codebook, and rows that go to some of several experts.
+ * Both rest on the rows' order by a key (gs_sort_rows), whose arrays stay on the device:
+ * nothing is read back. Matrices are as for the row operators above. */
+#define GS_MAX_EXPERTS 1024                     /* experts of a router or a mixture, at most */
+#define GS_MAX_CHOICES 16                       /* experts of a row, at most */
+
+/* Positions 0 .. count - 1 in the order of their groups (device arrays, caller-owned). */
+typedef struct gs_row_order {
+    int64_t count;            /* positions: rows, or rows times the choices of each */
+    int64_t groups;           /* codebook entries or experts */
+    int32_t* order;           /* [count] positions by (group, position), those without a group last */
+    int32_t* sorted;          /* [count] the groups of these positions, `groups` for none; or NULL */
+    int32_t* place;           /* [count] where each position is in `order`, -1 without a group; or NULL */
+    int32_t* offsets;         /* [groups + 1] first place of each group; offsets[groups]: places in use */
+} gs_row_order;
+
+/*
+ * gs_sort_rows -- fills the arrays of `order` from the positions' groups, stably: within a
+ * group the order is that of the positions. group_of: [count] int32; a value outside
+ * [0, groups) is no group.
+ * Limits: 0 <= count < 2^31, 1 <= groups < 2^31 - 1.
+ * workspace: gs_sort_rows_workspace_size bytes, 256-byte aligned; NULL where that is 0.
+ */
+gs_status gs_sort_rows(const int32_t* group_of, const gs_row_order* order, void* workspace, size_t workspace_bytes,
+                       void* stream);
+gs_status gs_sort_rows_workspace_size(int64_t count, int64_t groups, size_t* bytes);
+
+/*
+ * gs_embedding_fwd -- y[i] = scale table[index[i]]: table [entries][dim], y [rows][dim] of
+ * one type, index [rows] int32. A row whose index is outside [0, entries) is zero. The
+ * product is taken in fp32 and rounded once.
+ * Limits: 0 <= rows < 2^31, 1 <= entries < 2^31 - 1, 1 <= dim <= GS_MAX_DIM.
+ */
+gs_status gs_embedding_fwd(int32_t type, int64_t rows, int64_t dim, int64_t entries, const void* table, int64_t ldt,
+                           const int32_t* index, float scale, void* y, int64_t ldy, void* stream);
+/*
+ * gs_embedding_bwd -- the table's gradient: dtable[v] = scale times the sum of dy[i] over the
+ * rows i whose index is v, overwritten, zero for an entry without rows. order: the rows
+ * sorted by index (gs_sort_rows with count = rows of dy, groups = entries; `sorted` is
+ * needed, place is not); an order may serve as long as the indices stay the same.
+ * dtable: [entries][dim] of dtable_type, GS_F32 or `type`. Sums are fp32 in a fixed
+ * order: the same call gives the same bits.
+ * workspace: gs_embedding_workspace_size bytes, 256-byte aligned.
+ */
+gs_status gs_embedding_bwd(int32_t type, int64_t dim, const void* dy, int64_t lddy, const gs_row_order* order,
+                           float scale, void* dtable, int64_t lddt, int32_t dtable_type, void* workspace,
+                           size_t workspace_bytes, void* stream);
+gs_status gs_embedding_workspace_size(int32_t type, int64_t rows, int64_t dim, size_t* bytes);
+
+/*
+ * gs_route_fwd -- the k experts of each row's largest logits, in falling order (the lower
+ * expert of equal ones first), and their weights: the softmax over the chosen logits
+ * (normalise != 0) or over all of the row's. An expert whose logit is -infinity is never
+ * chosen: where fewer than k are left, the rest of the choices are expert -1 with weight 0.
+ * An undefined logit counts as the largest; where one is undefined or +infinity the row's
+ * weights may be undefined, its experts are not.
+ * logits: [rows][experts]; expert: [rows][k] int32, weight: [rows][k] fp32.
+ * Limits: 0 <= rows, rows k < 2^31, 1 <= experts <= GS_MAX_EXPERTS, 1 <= k <= experts and
+ * <= GS_MAX_CHOICES.
+ */
+gs_status gs_route_fwd(int32_t type, int64_t rows, int64_t experts, int32_t k, const void* logits, int64_t ldl,
+                       int32_t normalise, int32_t* expert, float* weight, void* stream);
+/*
+ * gs_route_bwd -- the logits' gradient from that of the weights, dweight [rows][k] fp32
+ * (not read for choices that are -1); logits, expert and weight as gs_route_fwd took and wrote them.
+ * With inner = sum of dweight weight: normalised, weight (dweight - inner) at the chosen
+ * experts and 0 elsewhere (logits: not read, may be NULL); otherwise p (dweight - inner)
+ * at these and -p inner elsewhere, p the softmax of the row. dlogits: [rows][experts].
+ */
+gs_status gs_route_bwd(int32_t type, int64_t rows, int64_t experts, int32_t k, const float* dweight, const void* logits,
+                       int64_t ldl, const int32_t* expert, const float* weight, int32_t normalise, void* dlogits,
+                       int64_t lddl, void* stream);
+
+/*
+ * Rows to their experts and back. order: rows times k positions (k = order->count / rows,
+ * at most GS_MAX_CHOICES), position i k + j being the j-th choice of row i, sorted by expert; p below is
+ * a place in that order. Places from offsets[groups] on are in no use: rows of xs and dys there stay as they are, and
+ * rows of dxs and ys are not read. Choices of no expert add nothing. Sums are fp32, in the order of the choices.
+ * gs_dispatch_fwd: xs[p] = x[order[p] / k]; x [rows][dim], xs [count][dim].
+ * gs_dispatch_bwd: dx[i] = sum over j of dxs[place[i k + j]] [+ add[i]].
+ * gs_combine_fwd: y[i] = sum over j of weight[i][j] ys[place[i k + j]] [+ residual[i]].
+ * gs_combine_bwd: dys[p] = weight[order[p]] dy[order[p] / k], dweight[i][j] = dy[i] . ys[place[i k + j]], 0 for no
+ * expert (the residual's gradient is dy itself).
+ * weight, dweight: [rows][k] fp32. Limits: 0 <= rows, count < 2^31, 1 <= dim <= GS_MAX_DIM.
+ */
+gs_status gs_dispatch_fwd(int32_t type, int64_t rows, int64_t dim, const void* x, int64_t ldx, const gs_row_order* order,
+                          void* xs, int64_t ldxs, void* stream);
+gs_status gs_dispatch_bwd(int32_t type, int64_t rows, int64_t dim, const void* dxs, int64_t lddxs,
+                          const gs_row_order* order, const void* add, int64_t ldadd, void* dx, int64_t lddx,
+                          void* stream);
+gs_status gs_combine_fwd(int32_t type, int64_t rows, int64_t dim, const void* ys, int64_t ldys,
+                         const gs_row_order* order, const float* weight, const void* residual, int64_t ldr, void* y,
+                         int64_t ldy, void* stream);
+gs_status gs_combine_bwd(int32_t type, int64_t rows, int64_t dim, const void* dy, int64_t lddy, const void* ys,
+                         int64_t ldys, const gs_row_order* order, const float* weight, void* dys, int64_t lddys,
+                         float* dweight, void* stream);
+
 /* Workspace bytes needed by any rasterizer call for these sizes (host only). */
 gs_status gs_workspace_size(int64_t n, int32_t width, int32_t height, uint64_t capacity, int32_t kind,
                             size_t* bytes);
@@ -572,7 +670,9 @@ enum {
     GS_KERNEL_BLOCK_ENTRIES, GS_KERNEL_BLOCK_SORT, GS_KERNEL_TILE_LISTS, GS_KERNEL_BLEND_FWD,
     GS_KERNEL_BWD_PREP, GS_KERNEL_BLEND_BWD, GS_KERNEL_PREPROCESS_BWD, GS_KERNEL_MLP_REDUCE,
     GS_KERNEL_ADAM, GS_KERNEL_NEURAL_FOLD, GS_KERNEL_LAYER_NORM_FWD, GS_KERNEL_LAYER_NORM_BWD, GS_KERNEL_LINEAR_FWD,
-    GS_KERNEL_LINEAR_BWD, GS_KERNEL_GRAD_NORM, GS_KERNEL_COUNT
+    GS_KERNEL_LINEAR_BWD, GS_KERNEL_GRAD_NORM, GS_KERNEL_SORT_ROWS, GS_KERNEL_EMBEDDING_FWD, GS_KERNEL_EMBEDDING_BWD,
+    GS_KERNEL_ROUTE_FWD, GS_KERNEL_ROUTE_BWD, GS_KERNEL_DISPATCH_FWD, GS_KERNEL_DISPATCH_BWD, GS_KERNEL_COMBINE_FWD,
+    GS_KERNEL_COMBINE_BWD, GS_KERNEL_EXPERTS_FWD, GS_KERNEL_EXPERTS_BWD, GS_KERNEL_COUNT
 };   /* GS_KERNEL_BWD_PREP: the backward's accumulator clear and its tile order.
       * gs_bin_sort of few Gaussians (its method's second form) has no block
       * entries: GS_KERNEL_ENTRY_OFFSETS, _BLOCK_ENTRIES and _BLOCK_SORT count

@@ -167,7 +167,9 @@ void resolve_pending(gs_timer* t)
 const char* const kKernelNames[GS_KERNEL_COUNT] = {
     "preprocess", "pair_count", "depth_sort", "entry_offsets", "block_entries", "block_sort", "tile_lists",
     "blend_fwd", "bwd_prep", "blend_bwd", "preprocess_bwd", "mlp_reduce", "adam", "neural_fold",
-    "layer_norm_fwd", "layer_norm_bwd", "linear_fwd", "linear_bwd", "grad_norm"};
+    "layer_norm_fwd", "layer_norm_bwd", "linear_fwd", "linear_bwd", "grad_norm", "sort_rows", "embedding_fwd",
+    "embedding_bwd", "route_fwd", "route_bwd", "dispatch_fwd", "dispatch_bwd", "combine_fwd", "combine_bwd",
+    "experts_fwd", "experts_bwd"};
 
 }  // namespace
 
@@ -717,9 +719,228 @@ gs_status grad_clip(const gs_grad_tensor* tensors, int32_t count, float max_norm
     return ok();
 }
 
+// A launch between the timer's events.
+template <typename F>
+gs_status timed(int kernel, void* stream, F launch)
+{
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    timing_begin(kernel, s);
+    GS_HIP(launch(s));
+    timing_end(kernel, s);
+    return ok();
+}
+
+gs_status check_ints(const char* name, const void* p, int64_t count)
+{
+    GS_CHECK(count == 0 || p != nullptr, "%s is NULL", name);
+    GS_CHECK(((uintptr_t)p & 3) == 0, "%s is not aligned to its element type", name);
+    return GS_OK;
+}
+
+gs_status check_order(const gs_row_order* o)
+{
+    gs_status st;
+    GS_CHECK(o != nullptr, "order is NULL");
+    GS_CHECK(o->count >= 0 && o->count < ((int64_t)1 << 31), "count = %lld out of range [0, 2^31)", (long long)o->count);
+    GS_CHECK(o->groups >= 1 && o->groups < ((int64_t)1 << 31) - 1, "groups = %lld out of range [1, 2^31 - 1)",
+             (long long)o->groups);
+    if ((st = check_ints("order", o->order, o->count)) != GS_OK) return st;
+    if ((st = check_ints("offsets", o->offsets, 1)) != GS_OK) return st;
+    GS_CHECK((((uintptr_t)o->sorted | (uintptr_t)o->place) & 3) == 0, "sorted or place is not aligned to its element type");
+    return GS_OK;
+}
+
+gs_status check_entries(int64_t entries)
+{
+    GS_CHECK(entries >= 1 && entries < ((int64_t)1 << 31) - 1, "entries = %lld out of range [1, 2^31 - 1)",
+             (long long)entries);
+    return GS_OK;
+}
+
+gs_status check_route(int32_t type, int64_t rows, int64_t experts, int32_t k, const int32_t* expert, const float* weight)
+{
+    gs_status st;
+    if ((st = check_rows(type, rows)) != GS_OK) return st;
+    GS_CHECK(experts >= 1 && experts <= GS_MAX_EXPERTS, "experts = %lld outside [1, %d]", (long long)experts,
+             GS_MAX_EXPERTS);
+    GS_CHECK(k >= 1 && k <= experts && k <= GS_MAX_CHOICES, "k = %d outside [1, %lld]", k,
+             (long long)std::min<int64_t>(experts, GS_MAX_CHOICES));
+    GS_CHECK(rows * k < ((int64_t)1 << 31), "%lld rows of %d choices: fewer than 2^31 expected", (long long)rows, k);
+    if ((st = check_ints("expert", expert, rows)) != GS_OK) return st;
+    return check_ints("weight", weight, rows);
+}
+
+// What the moves of rows to experts and back share; `sorted` rows are order->count.
+gs_status check_move(int32_t type, int64_t rows, int64_t dim, const gs_row_order* o, bool place)
+{
+    gs_status st;
+    if ((st = check_rows(type, rows)) != GS_OK) return st;
+    if ((st = check_dim("dim", dim)) != GS_OK) return st;
+    if ((st = check_order(o)) != GS_OK) return st;
+    GS_CHECK(rows == 0 ? o->count == 0 : o->count % rows == 0 && o->count / rows >= 1 && o->count / rows <= GS_MAX_CHOICES,
+             "%lld places are not 1 to %d choices of each of %lld rows", (long long)o->count, GS_MAX_CHOICES,
+             (long long)rows);
+    return place ? check_ints("place", o->place, rows) : GS_OK;
+}
+
 }  // namespace
 
 extern "C" {
+
+gs_status gs_sort_rows_workspace_size(int64_t count, int64_t groups, size_t* bytes)
+{
+    GS_CHECK(bytes != nullptr, "bytes is NULL");
+    GS_CHECK(count >= 0 && count < ((int64_t)1 << 31), "count = %lld out of range [0, 2^31)", (long long)count);
+    GS_CHECK(groups >= 1 && groups < ((int64_t)1 << 31) - 1, "groups = %lld out of range [1, 2^31 - 1)",
+             (long long)groups);
+    *bytes = sort_rows_workspace(count, groups);
+    return ok();
+}
+
+gs_status gs_sort_rows(const int32_t* group_of, const gs_row_order* order, void* workspace, size_t workspace_bytes,
+                       void* stream)
+{
+    gs_status st;
+    if ((st = check_order(order)) != GS_OK) return st;
+    if ((st = check_ints("group_of", group_of, order->count)) != GS_OK) return st;
+    if ((st = check_workspace(workspace, workspace_bytes, sort_rows_workspace(order->count, order->groups))) != GS_OK)
+        return st;
+    return timed(GS_KERNEL_SORT_ROWS, stream, [&](hipStream_t s) { return launch_sort_rows(group_of, *order, workspace, s); });
+}
+
+gs_status gs_embedding_fwd(int32_t type, int64_t rows, int64_t dim, int64_t entries, const void* table, int64_t ldt,
+                           const int32_t* index, float scale, void* y, int64_t ldy, void* stream)
+{
+    gs_status st;
+    if ((st = check_rows(type, rows)) != GS_OK) return st;
+    if ((st = check_dim("dim", dim)) != GS_OK) return st;
+    if ((st = check_entries(entries)) != GS_OK) return st;
+    if ((st = check_matrix("table", table, entries, dim, ldt, type)) != GS_OK) return st;
+    if ((st = check_ints("index", index, rows)) != GS_OK) return st;
+    if ((st = check_matrix("y", y, rows, dim, ldy, type)) != GS_OK) return st;
+    if (rows == 0) return ok();
+    return timed(GS_KERNEL_EMBEDDING_FWD, stream, [&](hipStream_t s) {
+        return launch_embedding_fwd(type, table, ldt, entries, index, scale, rows, dim, y, ldy, s);
+    });
+}
+
+gs_status gs_embedding_workspace_size(int32_t type, int64_t rows, int64_t dim, size_t* bytes)
+{
+    gs_status st;
+    GS_CHECK(bytes != nullptr, "bytes is NULL");
+    if ((st = check_rows(type, rows)) != GS_OK) return st;
+    if ((st = check_dim("dim", dim)) != GS_OK) return st;
+    *bytes = embedding_workspace(type, rows, dim);
+    return ok();
+}
+
+gs_status gs_embedding_bwd(int32_t type, int64_t dim, const void* dy, int64_t lddy, const gs_row_order* order,
+                           float scale, void* dtable, int64_t lddt, int32_t dtable_type, void* workspace,
+                           size_t workspace_bytes, void* stream)
+{
+    gs_status st;
+    if ((st = check_order(order)) != GS_OK) return st;
+    if ((st = check_rows(type, order->count)) != GS_OK) return st;
+    if ((st = check_dim("dim", dim)) != GS_OK) return st;
+    if ((st = check_ints("sorted", order->sorted, order->count)) != GS_OK) return st;
+    if ((st = check_matrix("dy", dy, order->count, dim, lddy, type)) != GS_OK) return st;
+    GS_CHECK(dtable_type == GS_F32 || dtable_type == type, "dtable_type %d: fp32 or the type of dy", dtable_type);
+    if ((st = check_matrix("dtable", dtable, order->groups, dim, lddt, dtable_type)) != GS_OK) return st;
+    if ((st = check_workspace(workspace, workspace_bytes, embedding_workspace(type, order->count, dim))) != GS_OK) return st;
+    return timed(GS_KERNEL_EMBEDDING_BWD, stream, [&](hipStream_t s) {
+        return launch_embedding_bwd(type, dy, lddy, *order, scale, dim, dtable, lddt, dtable_type == GS_F32,
+                                    (float*)workspace, s);
+    });
+}
+
+gs_status gs_route_fwd(int32_t type, int64_t rows, int64_t experts, int32_t k, const void* logits, int64_t ldl,
+                       int32_t normalise, int32_t* expert, float* weight, void* stream)
+{
+    gs_status st;
+    if ((st = check_route(type, rows, experts, k, expert, weight)) != GS_OK) return st;
+    if ((st = check_matrix("logits", logits, rows, experts, ldl, type)) != GS_OK) return st;
+    if (rows == 0) return ok();
+    return timed(GS_KERNEL_ROUTE_FWD, stream, [&](hipStream_t s) {
+        return launch_route_fwd(type, rows, (int)experts, k, logits, ldl, normalise, expert, weight, s);
+    });
+}
+
+gs_status gs_route_bwd(int32_t type, int64_t rows, int64_t experts, int32_t k, const float* dweight, const void* logits,
+                       int64_t ldl, const int32_t* expert, const float* weight, int32_t normalise, void* dlogits,
+                       int64_t lddl, void* stream)
+{
+    gs_status st;
+    if ((st = check_route(type, rows, experts, k, expert, weight)) != GS_OK) return st;
+    if ((st = check_ints("dweight", dweight, rows)) != GS_OK) return st;
+    if (!normalise && (st = check_matrix("logits", logits, rows, experts, ldl, type)) != GS_OK) return st;
+    if ((st = check_matrix("dlogits", dlogits, rows, experts, lddl, type)) != GS_OK) return st;
+    if (rows == 0) return ok();
+    return timed(GS_KERNEL_ROUTE_BWD, stream, [&](hipStream_t s) {
+        return launch_route_bwd(type, rows, (int)experts, k, dweight, logits, ldl, expert, weight, normalise, dlogits, lddl,
+                                s);
+    });
+}
+
+gs_status gs_dispatch_fwd(int32_t type, int64_t rows, int64_t dim, const void* x, int64_t ldx, const gs_row_order* order,
+                          void* xs, int64_t ldxs, void* stream)
+{
+    gs_status st;
+    if ((st = check_move(type, rows, dim, order, false)) != GS_OK) return st;
+    if ((st = check_matrix("x", x, rows, dim, ldx, type)) != GS_OK) return st;
+    if ((st = check_matrix("xs", xs, order->count, dim, ldxs, type)) != GS_OK) return st;
+    if (rows == 0) return ok();
+    return timed(GS_KERNEL_DISPATCH_FWD, stream, [&](hipStream_t s) {
+        return launch_dispatch_fwd(type, x, ldx, *order, (int)(order->count / rows), dim, xs, ldxs, s);
+    });
+}
+
+gs_status gs_dispatch_bwd(int32_t type, int64_t rows, int64_t dim, const void* dxs, int64_t lddxs,
+                          const gs_row_order* order, const void* add, int64_t ldadd, void* dx, int64_t lddx,
+                          void* stream)
+{
+    gs_status st;
+    if ((st = check_move(type, rows, dim, order, true)) != GS_OK) return st;
+    if ((st = check_matrix("dxs", dxs, order->count, dim, lddxs, type)) != GS_OK) return st;
+    if (add && (st = check_matrix("add", add, rows, dim, ldadd, type)) != GS_OK) return st;
+    if ((st = check_matrix("dx", dx, rows, dim, lddx, type)) != GS_OK) return st;
+    if (rows == 0) return ok();
+    return timed(GS_KERNEL_DISPATCH_BWD, stream, [&](hipStream_t s) {
+        return launch_sum_choices(type, dxs, lddxs, *order, nullptr, add, ldadd, rows, dim, dx, lddx, s);
+    });
+}
+
+gs_status gs_combine_fwd(int32_t type, int64_t rows, int64_t dim, const void* ys, int64_t ldys,
+                         const gs_row_order* order, const float* weight, const void* residual, int64_t ldr, void* y,
+                         int64_t ldy, void* stream)
+{
+    gs_status st;
+    if ((st = check_move(type, rows, dim, order, true)) != GS_OK) return st;
+    if ((st = check_matrix("ys", ys, order->count, dim, ldys, type)) != GS_OK) return st;
+    if ((st = check_ints("weight", weight, rows)) != GS_OK) return st;
+    if (residual && (st = check_matrix("residual", residual, rows, dim, ldr, type)) != GS_OK) return st;
+    if ((st = check_matrix("y", y, rows, dim, ldy, type)) != GS_OK) return st;
+    if (rows == 0) return ok();
+    return timed(GS_KERNEL_COMBINE_FWD, stream, [&](hipStream_t s) {
+        return launch_sum_choices(type, ys, ldys, *order, weight, residual, ldr, rows, dim, y, ldy, s);
+    });
+}
+
+gs_status gs_combine_bwd(int32_t type, int64_t rows, int64_t dim, const void* dy, int64_t lddy, const void* ys,
+                         int64_t ldys, const gs_row_order* order, const float* weight, void* dys, int64_t lddys,
+                         float* dweight, void* stream)
+{
+    gs_status st;
+    if ((st = check_move(type, rows, dim, order, true)) != GS_OK) return st;
+    if ((st = check_matrix("dy", dy, rows, dim, lddy, type)) != GS_OK) return st;
+    if ((st = check_matrix("ys", ys, order->count, dim, ldys, type)) != GS_OK) return st;
+    if ((st = check_ints("weight", weight, rows)) != GS_OK) return st;
+    if ((st = check_matrix("dys", dys, order->count, dim, lddys, type)) != GS_OK) return st;
+    if ((st = check_ints("dweight", dweight, rows)) != GS_OK) return st;
+    if (rows == 0) return ok();
+    return timed(GS_KERNEL_COMBINE_BWD, stream, [&](hipStream_t s) {
+        return launch_combine_bwd(type, dy, lddy, ys, ldys, *order, weight, rows, dim, dys, lddys, dweight, s);
+    });
+}
 
 gs_status gs_layer_norm_fwd(int32_t type, int64_t rows, int64_t dim, const void* x, int64_t ldx, const float* w,
                             const float* b, float eps, void* y, int64_t ldy, float* mean, float* rstd, void* stream)

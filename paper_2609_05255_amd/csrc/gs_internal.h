@@ -221,6 +221,28 @@ hipError_t launch_linear_bwd(const gs_linear& p, const void* dy, int64_t lddy, c
 int64_t grad_parts(const gs_grad_tensor* tensors, int count);   // fp64 partial sums of a norm
 hipError_t launch_grad_clip(const gs_grad_tensor* tensors, int count, float max_norm, float* result, double* part,
                             bool scale, hipStream_t s);
+// Codebooks and mixtures (sort_rows.hip, move_rows.hip, route.hip, experts.hip).
+size_t sort_rows_workspace(int64_t count, int64_t groups);
+hipError_t launch_sort_rows(const int32_t* group_of, const gs_row_order& o, void* ws, hipStream_t s);
+hipError_t launch_embedding_fwd(int type, const void* table, int64_t ldt, int64_t entries, const int32_t* index,
+                                float scale, int64_t rows, int64_t dim, void* y, int64_t ldy, hipStream_t s);
+size_t embedding_workspace(int type, int64_t count, int64_t dim);
+hipError_t launch_embedding_bwd(int type, const void* dy, int64_t lddy, const gs_row_order& o, float scale, int64_t dim,
+                                void* dtable, int64_t lddt, int out_f32, float* part, hipStream_t s);
+hipError_t launch_route_fwd(int type, int64_t rows, int experts, int k, const void* logits, int64_t ldl, int normalise,
+                            int32_t* expert, float* weight, hipStream_t s);
+hipError_t launch_route_bwd(int type, int64_t rows, int experts, int k, const float* dweight, const void* logits,
+                            int64_t ldl, const int32_t* expert, const float* weight, int normalise, void* dlogits,
+                            int64_t ldd, hipStream_t s);
+hipError_t launch_dispatch_fwd(int type, const void* x, int64_t ldx, const gs_row_order& o, int k, int64_t dim, void* xs,
+                               int64_t ldxs, hipStream_t s);
+// dst[i] = sum over the choices of row i of weight (NULL: 1) src[place], plus add (or NULL)
+hipError_t launch_sum_choices(int type, const void* src, int64_t lds, const gs_row_order& o, const float* weight,
+                              const void* add, int64_t ldadd, int64_t rows, int64_t dim, void* dst, int64_t ldd,
+                              hipStream_t s);
+hipError_t launch_combine_bwd(int type, const void* dy, int64_t lddy, const void* ys, int64_t ldys, const gs_row_order& o,
+                              const float* weight, int64_t rows, int64_t dim, void* dys, int64_t lddys, float* dweight,
+                              hipStream_t s);
 hipError_t launch_mlp_eval(const uint16_t* x, int64_t rows, const uint16_t* w, float* out, hipStream_t s);
 hipError_t launch_neural_fold(const uint16_t* features, const uint16_t* w, int64_t n, uint16_t* preact,
                               hipStream_t s);

@@ -1,0 +1,548 @@
+// Rows copied to where an index says and added up on their way back: embedding lookup, rows moved to experts and their
+// results combined, and the gradients of these.
+//
+//   lookup   y[i] = s table[index[i]], zero without an entry;  dtable[v] = s sum of dy[i] over index[i] = v
+//   dispatch xs[p] = x[order[p] / k];                          dx[i] = sum over j of dxs[place[i k + j]] [+ add]
+//   combine  y[i] = sum over j of w[i k + j] ys[place[i k + j]] [+ residual]
+//            dys[p] = w[order[p]] dy[order[p] / k],            dw[i k + j] = <dy[i], ys[place[i k + j]]>
+//
+// All are bound by HBM: every row is read once and written once, in vectors of 16 bytes at any alignment, a group of
+// lanes for each row, several rows of a group under way together. Sums are fp32 and have a fixed order: no atomics, the
+// same call gives the same bits. Results are rounded to the element type once, as they are stored.
+#include <type_traits>
+
+#include "gs_internal.h"
+#include "vec.h"
+
+namespace gsr {
+
+namespace {
+
+// Lanes that share a row of `vecs` vectors: a power of two up to a wave.
+int row_lanes(int64_t vecs)
+{
+    int g = 1;
+    while (g < 64 && g < vecs) g <<= 1;
+    return g;
+}
+
+template <typename F>
+void with_lanes(int g, F f)
+{
+    switch (g) {
+    case 1: f(std::integral_constant<int, 1>()); break;
+    case 2: f(std::integral_constant<int, 2>()); break;
+    case 4: f(std::integral_constant<int, 4>()); break;
+    case 8: f(std::integral_constant<int, 8>()); break;
+    case 16: f(std::integral_constant<int, 16>()); break;
+    case 32: f(std::integral_constant<int, 32>()); break;
+    default: f(std::integral_constant<int, 64>());
+    }
+}
+
+constexpr int64_t kMoveBlocks = 256 * 8;   // workgroups that take rows in turn
+
+int64_t move_blocks(int64_t rows, int g, int fly)
+{
+    return std::max<int64_t>(1, std::min<int64_t>(div_up(rows, (int64_t)kBlock / g * fly), kMoveBlocks));
+}
+
+// The stored vector as it is, or its first `left` elements.
+template <typename T>
+__device__ __forceinline__ void put_vec(T* p, int64_t left, typename Vec<T>::Packed v)
+{
+    constexpr int N = Vec<T>::N;
+    if (left >= N) {
+        *reinterpret_cast<typename Vec<T>::Any*>(p) = v;
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (j < left) p[j] = v[j];
+    }
+}
+
+// ---- one row to one row -----------------------------------------------------
+
+struct GatherArgs {
+    const void* src;
+    void* dst;
+    int64_t lds, ldd, rows, dim;
+    const int32_t* index;
+    const int32_t* used;   // dispatch: how many rows there are
+    int64_t entries;       // lookup: rows of src
+    int32_t k;             // dispatch: choices of a row
+    float scale;
+};
+
+constexpr int kGatherRows = 4;   // of a group under way together
+
+// LOOKUP: an index outside [0, entries) gives a row of zeros. Otherwise index[p] / k is the row, below *used.
+template <typename T, int G, bool LOOKUP>
+__global__ __launch_bounds__(kBlock) void k_gather(GatherArgs a)
+{
+    constexpr int N = Vec<T>::N, U = kGatherRows, kGroups = kBlock / G;
+    typedef typename Vec<T>::Packed Packed;
+    const int lane = threadIdx.x & (G - 1);
+    const int64_t rows = LOOKUP ? a.rows : min((int64_t)*a.used, a.rows);
+    const int64_t step = (int64_t)gridDim.x * kGroups;
+    for (int64_t r0 = (int64_t)blockIdx.x * kGroups + threadIdx.x / G; r0 < rows; r0 += U * step) {
+        const T* from[U];
+        bool in[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t r = r0 + u * step;
+            const int32_t i = r < rows ? a.index[r] : -1;
+            if (LOOKUP) {
+                in[u] = i >= 0 && i < a.entries;
+                from[u] = (const T*)a.src + (in[u] ? i : 0) * a.lds;
+            } else {
+                in[u] = i >= 0 && i < a.rows;
+                from[u] = (const T*)a.src + (in[u] ? (uint32_t)i / (uint32_t)a.k : 0) * a.lds;
+            }
+        }
+        for (int64_t c = (int64_t)lane * N; c < a.dim; c += G * N) {
+            const int64_t left = a.dim - c;
+            Packed v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = load_any(from[u] + c, in[u] ? left : 0);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t r = r0 + u * step;
+                if (r >= rows) break;
+                T* to = (T*)a.dst + r * a.ldd + c;
+                if (LOOKUP) {
+                    float f[N];
+#pragma unroll
+                    for (int e = 0; e < N; ++e) f[e] = in[u] ? (float)v[u][e] * a.scale : 0.f;
+                    store_vec(to, left, f);
+                } else {
+                    put_vec(to, left, v[u]);
+                }
+            }
+        }
+    }
+}
+
+// ---- the choices of a row added up ------------------------------------------
+
+struct SumArgs {
+    const void* src;       // [sorted rows][dim]
+    const void* add;       // [rows][dim] or NULL
+    void* dst;
+    const float* weight;   // [rows][k], or NULL: 1
+    const int32_t* place;
+    const int32_t* used;
+    int64_t lds, ldadd, ldd, rows, dim;
+    int32_t k;
+};
+
+constexpr int kSumChoices = 4;   // under way together
+
+template <typename T, int G>
+__global__ __launch_bounds__(kBlock) void k_sum_choices(SumArgs a)
+{
+    constexpr int N = Vec<T>::N, U = kSumChoices, kGroups = kBlock / G;
+    typedef typename Vec<T>::Packed Packed;
+    const int lane = threadIdx.x & (G - 1);
+    const int64_t used = min((int64_t)*a.used, a.rows * a.k);
+    const int64_t step = (int64_t)gridDim.x * kGroups;
+    for (int64_t r = (int64_t)blockIdx.x * kGroups + threadIdx.x / G; r < a.rows; r += step) {
+        const int32_t* place = a.place + r * a.k;
+        const float* weight = a.weight ? a.weight + r * a.k : nullptr;
+        for (int64_t c = (int64_t)lane * N; c < a.dim; c += G * N) {
+            const int64_t left = a.dim - c;
+            float sum[N] = {};
+            if (a.add) load_vec((const T*)a.add + r * a.ldadd + c, left, sum);
+            for (int j0 = 0; j0 < a.k; j0 += U) {
+                Packed v[U];
+                bool in[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int32_t p = j0 + u < a.k ? place[j0 + u] : -1;
+                    in[u] = p >= 0 && p < used;
+                    v[u] = load_any((const T*)a.src + (in[u] ? p : 0) * a.lds + c, in[u] ? left : 0);
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    if (!in[u]) continue;
+                    const float w = weight ? weight[j0 + u] : 1.f;
+#pragma unroll
+                    for (int e = 0; e < N; ++e) sum[e] = fmaf(w, (float)v[u][e], sum[e]);
+                }
+            }
+            store_vec((T*)a.dst + r * a.ldd + c, left, sum);
+        }
+    }
+}
+
+// ---- the gradients of a combination -----------------------------------------
+
+struct CombineBwdArgs {
+    const void *dy, *ys;
+    void* dys;
+    const float* weight;
+    float* dweight;
+    const int32_t* place;
+    const int32_t* used;
+    int64_t lddy, ldys, lddys, rows, dim;
+    int32_t k;
+};
+
+template <typename T, int G>
+__global__ __launch_bounds__(kBlock) void k_combine_bwd(CombineBwdArgs a)
+{
+    constexpr int N = Vec<T>::N, U = kSumChoices, kGroups = kBlock / G;
+    typedef typename Vec<T>::Packed Packed;
+    const int lane = threadIdx.x & (G - 1);
+    const int64_t used = min((int64_t)*a.used, a.rows * a.k);
+    const int64_t step = (int64_t)gridDim.x * kGroups;
+    for (int64_t r = (int64_t)blockIdx.x * kGroups + threadIdx.x / G; r < a.rows; r += step) {
+        const int64_t at = r * a.k;
+        for (int j0 = 0; j0 < a.k; j0 += U) {
+            int32_t p[U];
+            float w[U], dot[U] = {};
+            bool in[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                p[u] = j0 + u < a.k ? a.place[at + j0 + u] : -1;
+                in[u] = p[u] >= 0 && p[u] < used;
+                p[u] = in[u] ? p[u] : 0;
+                w[u] = in[u] ? a.weight[at + j0 + u] : 0.f;
+            }
+            for (int64_t c = (int64_t)lane * N; c < a.dim; c += G * N) {
+                const int64_t left = a.dim - c;
+                float g[N];
+                load_vec((const T*)a.dy + r * a.lddy + c, left, g);
+                Packed v[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) v[u] = load_any((const T*)a.ys + p[u] * a.ldys + c, in[u] ? left : 0);
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    if (!in[u]) continue;
+                    float o[N];
+#pragma unroll
+                    for (int e = 0; e < N; ++e) {
+                        dot[u] = fmaf(g[e], (float)v[u][e], dot[u]);
+                        o[e] = g[e] * w[u];
+                    }
+                    store_vec((T*)a.dys + p[u] * a.lddys + c, left, o);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const float d = lane_sum<G>(dot[u]);
+                if (lane == 0 && j0 + u < a.k) a.dweight[at + j0 + u] = d;
+            }
+        }
+    }
+}
+
+// ---- the gradient of a lookup -----------------------------------------------
+//
+// The sorted positions are cut into equal parts, whatever the entries' shares are: a group of lanes sums a part of its
+// workgroup's, a row after the other, and writes the entries that begin and end in it. What an entry has in several
+// groups meets in LDS, and what it has in several workgroups in k_join_entries, both in the sorted order. Columns beyond
+// 64 vectors are other workgroups'.
+
+struct EntriesArgs {
+    const void* dy;
+    void* dtable;
+    int64_t lddy, lddt, dim, entries, count;
+    const int32_t *order, *sorted, *offsets;
+    float scale;
+    float* part;           // [workgroups][2][dim]: sums of the first entry, if it began before, and of the last, if it
+                           // began here and does not end here
+    int32_t per;           // positions of a group of lanes
+    int32_t out_f32;
+};
+
+constexpr int kEntryRows = 8;   // of a group under way together
+
+template <typename T>
+__device__ __forceinline__ void store_entry(const EntriesArgs& a, int64_t v, int64_t c, float value)
+{
+    if (a.out_f32)
+        ((float*)a.dtable)[v * a.lddt + c] = value * a.scale;
+    else
+        ((T*)a.dtable)[v * a.lddt + c] = (T)(value * a.scale);
+}
+
+template <typename T, int G>
+__global__ __launch_bounds__(kBlock) void k_sum_entries(EntriesArgs a)
+{
+    constexpr int N = Vec<T>::N, U = kEntryRows, kGroups = kBlock / G, kCols = G * N;
+    typedef typename Vec<T>::Packed Packed;
+    // a group's sums of its first entry, and of its last where that is another one
+    __shared__ float sums[kGroups][2][kCols];
+    __shared__ int32_t keys[kGroups][2];
+    const int lane = threadIdx.x & (G - 1), group = threadIdx.x / G;
+    const int64_t c = (int64_t)blockIdx.y * kCols + lane * N, left = a.dim - c;
+    const int64_t used = min((int64_t)a.offsets[a.entries], a.count);
+    const int64_t w0 = (int64_t)blockIdx.x * kGroups * a.per;
+    const int64_t w1 = w0 + kGroups * a.per < used ? w0 + kGroups * a.per : used;
+    const int64_t p0 = w0 + (int64_t)group * a.per, p1 = p0 + a.per < w1 ? p0 + a.per : w1;
+    int32_t first = -1, key = -1;
+    float sum[N] = {};
+    for (int64_t p = p0; p < p1; p += U) {
+        Packed v[U];
+        int32_t k[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const bool in = p + u < p1;
+            const uint32_t i = in ? (uint32_t)a.order[p + u] : 0;
+            k[u] = in && i < a.count ? a.sorted[p + u] : -1;
+            v[u] = load_any((const T*)a.dy + (int64_t)i * a.lddy + c, k[u] >= 0 ? left : 0);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (k[u] < 0 || k[u] >= a.entries) continue;
+            if (k[u] != key) {
+                if (key == first) {   // (nothing yet, or the first entry)
+                    if (key < 0)
+                        first = k[u];
+                    else
+#pragma unroll
+                        for (int e = 0; e < N; ++e) sums[group][0][lane * N + e] = sum[e];
+                } else {
+#pragma unroll
+                    for (int e = 0; e < N; ++e)
+                        if (e < left) store_entry<T>(a, key, c + e, sum[e]);
+                }
+                key = k[u];
+#pragma unroll
+                for (int e = 0; e < N; ++e) sum[e] = 0.f;
+            }
+#pragma unroll
+            for (int e = 0; e < N; ++e) sum[e] += (float)v[u][e];
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) sums[group][key == first ? 0 : 1][lane * N + e] = sum[e];
+    if (lane == 0) {
+        keys[group][0] = first;
+        keys[group][1] = key;
+    }
+    __syncthreads();
+    if (w0 >= w1) return;
+    const bool before = w0 > 0 && a.sorted[w0 - 1] == a.sorted[w0];
+    const bool behind = w1 < used && a.sorted[w1] == a.sorted[w1 - 1];
+    const int32_t w_first = keys[0][0];
+    float* part = a.part + (int64_t)blockIdx.x * 2 * a.dim;
+    for (int col = threadIdx.x; col < kCols; col += kBlock) {
+        const int64_t cc = (int64_t)blockIdx.y * kCols + col;
+        if (cc >= a.dim) break;
+        int32_t at = w_first;
+        float t = 0.f;
+        auto finish = [&](bool last) {
+            if (at == w_first && before)
+                part[cc] = t;
+            else if (last && behind)
+                part[a.dim + cc] = t;
+            else
+                store_entry<T>(a, at, cc, t);
+        };
+        for (int g = 0; g < kGroups; ++g) {
+            const int32_t k0 = keys[g][0], k1 = keys[g][1];
+            if (k0 < 0) break;
+            if (k0 != at) {
+                finish(false);
+                at = k0;
+                t = 0.f;
+            }
+            t += sums[g][0][col];
+            if (k1 != k0) {
+                finish(false);
+                at = k1;
+                t = sums[g][1][col];
+            }
+        }
+        finish(true);
+    }
+}
+
+// Entries that workgroups of k_sum_entries share, a workgroup for each that such an entry begins in, and 16 columns; and
+// zeros for the entries that have no rows (the other workgroups).
+constexpr int kJoinCols = 16, kJoinSlices = kBlock / kJoinCols;
+constexpr int64_t kZeroBlocks = 4096;
+
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_join_entries(EntriesArgs a, int64_t parts, int64_t span)
+{
+    const int64_t first_col = (int64_t)blockIdx.y * kJoinCols * 16;
+    const int64_t end_col = min(a.dim, first_col + kJoinCols * 16);
+    if (blockIdx.x >= parts) {
+        // a wave looks at 64 entries and clears the empty ones' columns
+        const int lane = threadIdx.x & 63;
+        const int64_t step = (gridDim.x - parts) * kBlock;
+        for (int64_t v0 = (blockIdx.x - parts) * kBlock + (threadIdx.x & ~63); v0 < a.entries; v0 += step) {
+            const int64_t v = v0 + lane;
+            uint64_t empty = __ballot(v < a.entries && a.offsets[v] == a.offsets[v + 1]);
+            for (; empty; empty &= empty - 1)
+                for (int64_t c = first_col + lane; c < end_col; c += 64)
+                    store_entry<T>(a, v0 + __builtin_ctzll(empty), c, 0.f);
+        }
+        return;
+    }
+    __shared__ float s[kJoinSlices][kJoinCols];
+    const int64_t used = min((int64_t)a.offsets[a.entries], a.count);
+    const int64_t w0 = (int64_t)blockIdx.x * span, w1 = w0 + span;
+    if (w1 >= used) return;
+    const int32_t key = a.sorted[w1 - 1];
+    if (key != a.sorted[w1]) return;                                       // it ends here
+    if (a.sorted[w0] == key && w0 > 0 && a.sorted[w0 - 1] == key) return;   // it began before
+    if (key < 0 || key >= a.entries) return;
+    const int64_t last = min((int64_t)a.offsets[key + 1] - 1, used - 1) / span;
+    const int col = threadIdx.x % kJoinCols, slice = threadIdx.x / kJoinCols;
+    for (int64_t c0 = first_col; c0 < end_col; c0 += kJoinCols) {
+        const int64_t c = c0 + col;
+        float t = 0.f;
+        if (c < a.dim) {
+            if (slice == 0) t = a.part[((int64_t)blockIdx.x * 2 + 1) * a.dim + c];
+#pragma unroll 4
+            for (int64_t b = blockIdx.x + 1 + slice; b <= last; b += kJoinSlices) t += a.part[b * 2 * a.dim + c];
+        }
+        s[slice][col] = t;
+        __syncthreads();
+        if (slice == 0 && c < a.dim) {
+#pragma unroll
+            for (int k = 1; k < kJoinSlices; ++k) t += s[k][col];
+            store_entry<T>(a, key, c, t);
+        }
+        __syncthreads();
+    }
+}
+
+struct EntriesPlan {
+    int lanes;
+    int64_t per, span, parts;   // positions of a group and of a workgroup, workgroups
+};
+
+EntriesPlan entries_plan(int type, int64_t count, int64_t dim)
+{
+    EntriesPlan p;
+    p.lanes = row_lanes(div_up(dim, type == GS_F32 ? 4 : 8));
+    const int64_t groups = kBlock / p.lanes, all = kMoveBlocks * groups;
+    p.per = std::max<int64_t>(kEntryRows, div_up(div_up(count, all), kEntryRows) * kEntryRows);
+    p.span = p.per * groups;
+    p.parts = std::max<int64_t>(1, div_up(count, p.span));
+    return p;
+}
+
+template <typename T>
+hipError_t gather(bool lookup, const GatherArgs& a, hipStream_t s)
+{
+    const int g = row_lanes(div_up(a.dim, Vec<T>::N));
+    const dim3 grid((unsigned)move_blocks(a.rows, g, kGatherRows));
+    with_lanes(g, [&](auto lanes) {
+        constexpr int G = decltype(lanes)::value;
+        if (lookup)
+            hipLaunchKernelGGL((k_gather<T, G, true>), grid, dim3(kBlock), 0, s, a);
+        else
+            hipLaunchKernelGGL((k_gather<T, G, false>), grid, dim3(kBlock), 0, s, a);
+    });
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t sum_choices(const SumArgs& a, hipStream_t s)
+{
+    const int g = row_lanes(div_up(a.dim, Vec<T>::N));
+    with_lanes(g, [&](auto lanes) {
+        hipLaunchKernelGGL((k_sum_choices<T, decltype(lanes)::value>), dim3((unsigned)move_blocks(a.rows, g, 1)),
+                           dim3(kBlock), 0, s, a);
+    });
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t combine_bwd(const CombineBwdArgs& a, hipStream_t s)
+{
+    const int g = row_lanes(div_up(a.dim, Vec<T>::N));
+    with_lanes(g, [&](auto lanes) {
+        hipLaunchKernelGGL((k_combine_bwd<T, decltype(lanes)::value>), dim3((unsigned)move_blocks(a.rows, g, 1)),
+                           dim3(kBlock), 0, s, a);
+    });
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t embedding_bwd(int type, const EntriesArgs& args, hipStream_t s)
+{
+    EntriesArgs a = args;
+    const EntriesPlan p = entries_plan(type, a.count, a.dim);
+    a.per = (int32_t)p.per;
+    hipError_t e = hipSuccess;
+    if (a.count > 0) {
+        with_lanes(p.lanes, [&](auto lanes) {
+            constexpr int G = decltype(lanes)::value;
+            hipLaunchKernelGGL((k_sum_entries<T, G>), dim3((unsigned)p.parts, (unsigned)div_up(a.dim, G * Vec<T>::N)),
+                               dim3(kBlock), 0, s, a);
+        });
+        e = hipGetLastError();
+    }
+    if (e != hipSuccess) return e;
+    const int64_t parts = a.count > 0 ? p.parts : 0;
+    hipLaunchKernelGGL((k_join_entries<T>), dim3((unsigned)(parts + std::min(div_up(a.entries, kBlock), kZeroBlocks)),
+                                                 (unsigned)div_up(a.dim, kJoinCols * 16)),
+                       dim3(kBlock), 0, s, a, parts, p.span);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_embedding_fwd(int type, const void* table, int64_t ldt, int64_t entries, const int32_t* index,
+                                float scale, int64_t rows, int64_t dim, void* y, int64_t ldy, hipStream_t s)
+{
+    const GatherArgs a = {table, y, ldt, ldy, rows, dim, index, nullptr, entries, 1, scale};
+    if (type == GS_F16) return gather<f16>(true, a, s);
+    if (type == GS_BF16) return gather<bf16>(true, a, s);
+    return gather<float>(true, a, s);
+}
+
+hipError_t launch_dispatch_fwd(int type, const void* x, int64_t ldx, const gs_row_order& o, int k, int64_t dim, void* xs,
+                               int64_t ldxs, hipStream_t s)
+{
+    const GatherArgs a = {x, xs, ldx, ldxs, o.count, dim, o.order, o.offsets + o.groups, 0, k, 1.f};
+    if (type == GS_F16) return gather<f16>(false, a, s);
+    if (type == GS_BF16) return gather<bf16>(false, a, s);
+    return gather<float>(false, a, s);
+}
+
+hipError_t launch_sum_choices(int type, const void* src, int64_t lds, const gs_row_order& o, const float* weight,
+                              const void* add, int64_t ldadd, int64_t rows, int64_t dim, void* dst, int64_t ldd,
+                              hipStream_t s)
+{
+    const SumArgs a = {src,   add, dst,  weight, o.place, o.offsets + o.groups, lds,
+                       ldadd, ldd, rows, dim,    (int32_t)(o.count / rows)};
+    if (type == GS_F16) return sum_choices<f16>(a, s);
+    if (type == GS_BF16) return sum_choices<bf16>(a, s);
+    return sum_choices<float>(a, s);
+}
+
+hipError_t launch_combine_bwd(int type, const void* dy, int64_t lddy, const void* ys, int64_t ldys, const gs_row_order& o,
+                              const float* weight, int64_t rows, int64_t dim, void* dys, int64_t lddys, float* dweight,
+                              hipStream_t s)
+{
+    const CombineBwdArgs a = {dy,    ys,   dys,  weight, dweight, o.place, o.offsets + o.groups, lddy, ldys,
+                              lddys, rows, dim, (int32_t)(o.count / rows)};
+    if (type == GS_F16) return combine_bwd<f16>(a, s);
+    if (type == GS_BF16) return combine_bwd<bf16>(a, s);
+    return combine_bwd<float>(a, s);
+}
+
+size_t embedding_workspace(int type, int64_t count, int64_t dim)
+{
+    return count > 0 ? (size_t)entries_plan(type, count, dim).parts * 2 * (size_t)dim * sizeof(float) : 0;
+}
+
+hipError_t launch_embedding_bwd(int type, const void* dy, int64_t lddy, const gs_row_order& o, float scale, int64_t dim,
+                                void* dtable, int64_t lddt, int out_f32, float* part, hipStream_t s)
+{
+    const EntriesArgs a = {dy,       dtable,   lddy,      lddt,  dim,  o.groups, o.count,
+                           o.order, o.sorted, o.offsets, scale, part, 0,        out_f32};
+    if (type == GS_F16) return embedding_bwd<f16>(type, a, s);
+    if (type == GS_BF16) return embedding_bwd<bf16>(type, a, s);
+    return embedding_bwd<float>(type, a, s);
+}
+
+}  // namespace gsr

@@ -25,14 +25,13 @@
 // With few Gaussians one workgroup sorts them by depth in LDS, and each block
 // finds its own entries among all of them (k_small_depth_sort, k_small_counts, k_small_lists).
 #include "gs_internal.h"
+#include "wave.h"
 
 namespace gsr {
 
 namespace {
 
 constexpr int kDupItems = kDupChunk / kBlock;              // 4 per thread
-
-__device__ __forceinline__ uint64_t lanemask_lt() { return (1ull << __lane_id()) - 1ull; }
 
 // Exclusive scan of one u32 per thread over the 256-thread workgroup.
 __device__ __forceinline__ uint32_t block_excl_scan(uint32_t v, uint32_t* lds4, uint32_t* total)
@@ -83,24 +82,6 @@ __device__ __forceinline__ T wg_excl_scan_1024(T v, T* lds16, T* total)
     __syncthreads();
     *total = tot;
     return before + x - v;
-}
-
-// Lanes of this wave holding the same kBits-bit digit (restricted to valid lanes).
-template <int kBits>
-__device__ __forceinline__ uint64_t match_digit(uint32_t d, bool valid)
-{
-    const uint64_t v = __ballot(valid);
-    uint32_t lo = (uint32_t)v, hi = (uint32_t)(v >> 32);
-#pragma unroll
-    for (int b = 0; b < kBits; ++b) {
-        const uint32_t bit = (d >> b) & 1u;
-        const uint64_t bm = __ballot(bit);
-        const uint32_t s = 0u - bit;   // all ones where this lane's bit is set
-        // keep the lanes whose bit equals ours: bm where set, ~bm where clear
-        lo &= ~((uint32_t)bm ^ s);
-        hi &= ~((uint32_t)(bm >> 32) ^ s);
-    }
-    return ((uint64_t)hi << 32) | lo;
 }
 
 // Digit counts of each workgroup's keys, one row of R counts per workgroup, and

@@ -33,7 +33,9 @@ def neural_weight_count(arch=None) -> int:
     return 32 * width + (layers - 1) * width * width + 3 * width
 KERNEL_NAMES = ["preprocess", "pair_count", "depth_sort", "entry_offsets", "block_entries", "block_sort", "tile_lists",
                 "blend_fwd", "bwd_prep", "blend_bwd", "preprocess_bwd", "mlp_reduce", "adam", "neural_fold",
-                "layer_norm_fwd", "layer_norm_bwd", "linear_fwd", "linear_bwd", "grad_norm"]
+                "layer_norm_fwd", "layer_norm_bwd", "linear_fwd", "linear_bwd", "grad_norm", "sort_rows", "embedding_fwd",
+                "embedding_bwd", "route_fwd", "route_bwd", "dispatch_fwd", "dispatch_bwd", "combine_fwd", "combine_bwd",
+                "experts_fwd", "experts_bwd"]
 TYPE_IDS = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}   # GS_F32, GS_F16, GS_BF16
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3, "tanh": 4, "sigmoid": 5}   # GS_ACT_*
 ADAM_MAX_TENSORS = 8
@@ -100,6 +102,11 @@ class GradTensor(C.Structure):
     _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("type", C.c_int32)]
 
 
+class RowOrderArrays(C.Structure):
+    _fields_ = [("count", C.c_int64), ("groups", C.c_int64), ("order", C.c_void_p), ("sorted", C.c_void_p),
+                ("place", C.c_void_p), ("offsets", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -133,6 +140,18 @@ def lib() -> C.CDLL:
         L.gs_grad_norm.argtypes = [P(GradTensor), i32, C.c_float, vp, vp, sz, vp]
         L.gs_grad_clip.argtypes = [P(GradTensor), i32, C.c_float, vp, vp, sz, vp]
         L.gs_grad_workspace_size.argtypes = [P(GradTensor), i32, P(sz)]
+        O = P(RowOrderArrays)
+        L.gs_sort_rows.argtypes = [vp, O, vp, sz, vp]
+        L.gs_sort_rows_workspace_size.argtypes = [i64, i64, P(sz)]
+        L.gs_embedding_fwd.argtypes = [i32, i64, i64, i64, vp, i64, vp, C.c_float, vp, i64, vp]
+        L.gs_embedding_bwd.argtypes = [i32, i64, vp, i64, O, C.c_float, vp, i64, i32, vp, sz, vp]
+        L.gs_embedding_workspace_size.argtypes = [i32, i64, i64, P(sz)]
+        L.gs_route_fwd.argtypes = [i32, i64, i64, i32, vp, i64, i32, vp, vp, vp]
+        L.gs_route_bwd.argtypes = [i32, i64, i64, i32, vp, vp, i64, vp, vp, i32, vp, i64, vp]
+        L.gs_dispatch_fwd.argtypes = [i32, i64, i64, vp, i64, O, vp, i64, vp]
+        L.gs_dispatch_bwd.argtypes = [i32, i64, i64, vp, i64, O, vp, i64, vp, i64, vp]
+        L.gs_combine_fwd.argtypes = [i32, i64, i64, vp, i64, O, vp, vp, i64, vp, i64, vp]
+        L.gs_combine_bwd.argtypes = [i32, i64, i64, vp, i64, vp, i64, O, vp, vp, i64, vp, vp]
         L.gs_render_bwd_adam.argtypes = [P(Camera), P(Gaussians), P(Appearance), P(Preprocessed), vp, vp, vp, vp,
                                          vp, P(Grads), P(AdamTensor), C.c_float, C.c_float, i64, vp, sz, vp]
         L.gs_timer_create.argtypes = [P(vp)]
@@ -144,7 +163,9 @@ def lib() -> C.CDLL:
                   "gs_render_bwd", "gs_render_bwd_adam", "gs_workspace_size", "gs_mlp_eval", "gs_neural_fold",
                   "gs_adam_step", "gs_adam_step_scaled", "gs_layer_norm_fwd", "gs_layer_norm_bwd",
                   "gs_layer_norm_workspace_size", "gs_linear_fwd", "gs_linear_bwd", "gs_linear_workspace_size",
-                  "gs_grad_norm", "gs_grad_clip", "gs_grad_workspace_size", "gs_timer_create", "gs_timer_destroy", "gs_timer_attach", "gs_timer_reset",
+                  "gs_grad_norm", "gs_grad_clip", "gs_grad_workspace_size", "gs_sort_rows", "gs_sort_rows_workspace_size",
+                  "gs_embedding_fwd", "gs_embedding_bwd", "gs_embedding_workspace_size", "gs_route_fwd", "gs_route_bwd",
+                  "gs_dispatch_fwd", "gs_dispatch_bwd", "gs_combine_fwd", "gs_combine_bwd", "gs_timer_create", "gs_timer_destroy", "gs_timer_attach", "gs_timer_reset",
                   "gs_timer_read"):
             getattr(L, f).restype = C.c_int
         L.gs_last_error.restype = C.c_char_p
@@ -520,6 +541,180 @@ def gs_grad_clip(grads: GradSet, max_norm: float, result, workspace, stream=None
     ws, ws_bytes = _space(workspace)
     _check(lib().gs_grad_clip(grads.array, len(grads.grads), max_norm, _vector("result", result, 2), ws, ws_bytes,
                               _stream(stream)))
+
+
+# ---- codebooks and mixtures: rows by key, lookup, routing, rows to experts and back ----
+
+
+def _array(name, t, shape, dtype):
+    """Address of a contiguous array of this shape and type on the GPU."""
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError("%s: %s of %s, a contiguous %s of %s on the GPU expected" % (name, tuple(t.shape), t.dtype,
+                                                                                      tuple(shape), dtype))
+    return t.data_ptr()
+
+
+def _one_device(*tensors):
+    """The launches go to the current device: all tensors (None: left out) have to be there."""
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.is_cuda and t.get_device() != device:
+            raise ValueError("a tensor on %s while the current device is %d" % (t.device, device))
+
+
+class RowOrder:
+    """The order of `count` positions by their group (gs_row_order): int32 tensors order, sorted, place and offsets,
+    which gs_sort_rows fills. sorted is what gs_embedding_bwd needs, place what rows on their way back from experts do;
+    either may be left out."""
+
+    def __init__(self, count: int, groups: int, device="cuda", sorted: bool = True, place: bool = True):
+        ints = lambda n: torch.empty(n, dtype=torch.int32, device=device)  # noqa: E731
+        self.count, self.groups = int(count), int(groups)
+        self.order, self.offsets = ints(self.count), ints(self.groups + 1)
+        self.sorted = ints(self.count) if sorted else None
+        self.place = ints(self.count) if place else None
+
+    def arrays(self) -> RowOrderArrays:
+        n, i32 = self.count, torch.int32
+        _one_device(self.order, self.sorted, self.place, self.offsets)
+        return RowOrderArrays(n, self.groups, _array("order", self.order, (n,), i32),
+                              None if self.sorted is None else _array("sorted", self.sorted, (n,), i32),
+                              None if self.place is None else _array("place", self.place, (n,), i32),
+                              _array("offsets", self.offsets, (self.groups + 1,), i32))
+
+
+def gs_sort_rows_workspace_size(order: RowOrder) -> int:
+    out = C.c_size_t(0)
+    _check(lib().gs_sort_rows_workspace_size(order.count, order.groups, C.byref(out)))
+    return out.value
+
+
+def gs_sort_rows(group_of, order: RowOrder, workspace=None, stream=None):
+    """Fills `order` from the groups of its positions (a contiguous int32 tensor of order.count values, of any shape);
+    values outside [0, order.groups) are no group."""
+    if group_of.numel() != order.count:
+        raise ValueError("group_of: %d values, %d expected" % (group_of.numel(), order.count))
+    _one_device(group_of, workspace)
+    ws, ws_bytes = _space(workspace)
+    _check(lib().gs_sort_rows(_array("group_of", group_of, group_of.shape, torch.int32), C.byref(order.arrays()), ws,
+                              ws_bytes, _stream(stream)))
+
+
+def gs_embedding_fwd(table, index, scale: float, y, stream=None):
+    """y[i] = scale * table[index[i]] (matrices of one type, index int32 [rows]); zero where the index is none of the
+    table's."""
+    entries, dim = _shape("table", table)
+    rows = index.numel()
+    _one_device(table, index, y)
+    pt, ldt = _matrix("table", table, entries, dim, table.dtype)
+    py, ldy = _matrix("y", y, rows, dim, table.dtype)
+    _check(lib().gs_embedding_fwd(_type_id(table), rows, dim, entries, pt, ldt,
+                                  _array("index", index, (rows,), torch.int32), scale, py, ldy, _stream(stream)))
+
+
+def gs_embedding_workspace_size(dy) -> int:
+    """Workspace bytes of gs_embedding_bwd for dy's shape and type."""
+    rows, dim = _shape("dy", dy)
+    out = C.c_size_t(0)
+    _check(lib().gs_embedding_workspace_size(_type_id(dy), rows, dim, C.byref(out)))
+    return out.value
+
+
+def gs_embedding_bwd(dy, order: RowOrder, scale: float, dtable, workspace, stream=None):
+    """dtable[v] = scale times the sum of dy's rows with index v, dtable float32 or of dy's type; order: the rows sorted
+    by index, with `sorted`."""
+    rows, dim = _shape("dy", dy)
+    if rows != order.count:
+        raise ValueError("dy: %d rows, %d sorted" % (rows, order.count))
+    _one_device(dy, dtable, workspace)
+    pdy, lddy = _matrix("dy", dy, rows, dim, dy.dtype)
+    out_type = torch.float32 if dtable.dtype == torch.float32 else dy.dtype
+    pdt, lddt = _matrix("dtable", dtable, order.groups, dim, out_type)
+    ws, ws_bytes = _space(workspace)
+    _check(lib().gs_embedding_bwd(_type_id(dy), dim, pdy, lddy, C.byref(order.arrays()), scale, pdt, lddt,
+                                  TYPE_IDS[out_type], ws, ws_bytes, _stream(stream)))
+
+
+def gs_route_fwd(logits, expert, weight, normalise: bool = True, stream=None):
+    """The experts (int32 [rows][k]) of each row's k largest logits and their weights (float32 [rows][k]): the softmax
+    over the chosen ones (normalise) or over all."""
+    rows, experts = _shape("logits", logits)
+    k = _shape("expert", expert)[1]
+    _one_device(logits, expert, weight)
+    pl, ldl = _matrix("logits", logits, rows, experts, logits.dtype)
+    _check(lib().gs_route_fwd(_type_id(logits), rows, experts, k, pl, ldl, int(normalise),
+                              _array("expert", expert, (rows, k), torch.int32),
+                              _array("weight", weight, (rows, k), torch.float32), _stream(stream)))
+
+
+def gs_route_bwd(dweight, logits, expert, weight, dlogits, normalise: bool = True, stream=None):
+    """The logits' gradient from that of the weights; logits, expert and weight as gs_route_fwd took and wrote them."""
+    rows, experts = _shape("dlogits", dlogits)
+    k = _shape("expert", expert)[1]
+    t = dlogits.dtype
+    _one_device(dweight, logits, expert, weight, dlogits)
+    pl, ldl = (None, 0) if logits is None else _matrix("logits", logits, rows, experts, t)
+    pd, ldd = _matrix("dlogits", dlogits, rows, experts, t)
+    _check(lib().gs_route_bwd(_type_id(dlogits), rows, experts, k,
+                              _array("dweight", dweight, (rows, k), torch.float32), pl, ldl,
+                              _array("expert", expert, (rows, k), torch.int32),
+                              _array("weight", weight, (rows, k), torch.float32), int(normalise), pd, ldd,
+                              _stream(stream)))
+
+
+def _choices(name, t, rows, order: RowOrder):
+    """Address of a float32 [rows][choices] array."""
+    if rows == 0:
+        return None
+    return _array(name, t, (rows, order.count // rows), torch.float32)
+
+
+def gs_dispatch_fwd(x, order: RowOrder, xs, stream=None):
+    """xs[p] = x[order[p] // k]: x [rows][dim] copied to where its k choices are sorted; xs [order.count][dim], rows
+    behind the last place in use stay as they are."""
+    rows, dim = _shape("x", x)
+    _one_device(x, xs)
+    px, ldx = _matrix("x", x, rows, dim, x.dtype)
+    pxs, ldxs = _matrix("xs", xs, order.count, dim, x.dtype)
+    _check(lib().gs_dispatch_fwd(_type_id(x), rows, dim, px, ldx, C.byref(order.arrays()), pxs, ldxs, _stream(stream)))
+
+
+def gs_dispatch_bwd(dxs, order: RowOrder, dx, add=None, stream=None):
+    """dx[i] = the sum of dxs over the places of row i's choices, plus `add`, a gradient of dx's shape."""
+    rows, dim = _shape("dx", dx)
+    t = dx.dtype
+    _one_device(dxs, dx, add)
+    ps, lds = _matrix("dxs", dxs, order.count, dim, t)
+    pa, lda = (None, 0) if add is None else _matrix("add", add, rows, dim, t)
+    pd, ldd = _matrix("dx", dx, rows, dim, t)
+    _check(lib().gs_dispatch_bwd(_type_id(dx), rows, dim, ps, lds, C.byref(order.arrays()), pa, lda, pd, ldd,
+                                 _stream(stream)))
+
+
+def gs_combine_fwd(ys, order: RowOrder, weight, y, residual=None, stream=None):
+    """y[i] = the sum over row i's choices of weight (float32 [rows][k]) times their rows of ys, plus the residual."""
+    rows, dim = _shape("y", y)
+    t = y.dtype
+    _one_device(ys, weight, y, residual)
+    ps, lds = _matrix("ys", ys, order.count, dim, t)
+    pr, ldr = (None, 0) if residual is None else _matrix("residual", residual, rows, dim, t)
+    py, ldy = _matrix("y", y, rows, dim, t)
+    _check(lib().gs_combine_fwd(_type_id(y), rows, dim, ps, lds, C.byref(order.arrays()),
+                                _choices("weight", weight, rows, order), pr, ldr, py, ldy, _stream(stream)))
+
+
+def gs_combine_bwd(dy, ys, order: RowOrder, weight, dys, dweight, stream=None):
+    """Backward of gs_combine_fwd: dys of ys's shape (rows behind the last place in use stay as they are) and dweight
+    (float32 [rows][k])."""
+    rows, dim = _shape("dy", dy)
+    t = dy.dtype
+    _one_device(dy, ys, weight, dys, dweight)
+    pdy, lddy = _matrix("dy", dy, rows, dim, t)
+    ps, lds = _matrix("ys", ys, order.count, dim, t)
+    pd, ldd = _matrix("dys", dys, order.count, dim, t)
+    _check(lib().gs_combine_bwd(_type_id(dy), rows, dim, pdy, lddy, ps, lds, C.byref(order.arrays()),
+                                _choices("weight", weight, rows, order), pd, ldd,
+                                _choices("dweight", dweight, rows, order), _stream(stream)))
 
 
 class Timer:

@@ -1,0 +1,196 @@
+"""Rows to experts and back (gs_dispatch_*, gs_combine_*) against 64 bits: copies bit for bit, sums of a row's choices in
+fp32, at widths on both sides of every change of the rows' spread over lanes, with choices of no expert, unused places
+whose rows stay as they are, strides and alignments."""
+import pytest
+import torch
+
+from paper_2609_05255_amd import gsraster as gs
+from mixture_reference import gathered, sort_rows
+from rows_reference import U32, assert_close, strided, sum_bound
+
+pytestmark = pytest.mark.gpu
+
+TYPES = [torch.float32, torch.float16, torch.bfloat16]
+NAN = float("nan")
+
+
+def normal(seed, *shape, dtype=torch.float32):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.randn(*shape, generator=g, device="cuda").to(dtype)
+
+
+def make_order(rows, k, experts, seed, dropped=True):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    expert = torch.randint(0, experts, (rows, k), generator=g, device="cuda")
+    if dropped:
+        expert = torch.where(torch.rand(rows, k, generator=g, device="cuda") < 0.15, -1, expert)
+    o = gs.RowOrder(rows * k, experts, sorted=False)
+    gs.gs_sort_rows(expert.int(), o, torch.empty(max(gs.gs_sort_rows_workspace_size(o), 1), dtype=torch.uint8,
+                                                 device="cuda"))
+    order, _, place, offsets = sort_rows(expert, experts)
+    assert torch.equal(o.order.cpu().long(), order) and torch.equal(o.place.cpu().long(), place)
+    return o, int(offsets[-1])
+
+
+SHAPES = [(1, 1, 1, 1), (1, 2, 256, 8), (5, 1, 3, 2), (9, 3, 8, 4), (100, 2, 9, 16), (33, 4, 17, 5), (65, 5, 40, 7),
+          (200, 2, 64, 16), (31, 16, 33, 20), (50, 2, 100, 256), (20, 3, 255, 3), (17, 2, 512, 8), (9, 4, 513, 4),
+          (8, 2, 1000, 8), (4, 7, 2049, 2), (3, 2, 4096, 5), (20_011, 2, 24, 37), (9000, 2, 128, 16)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,k,dim,experts", SHAPES)
+def test_dispatch(rows, k, dim, experts, dtype):
+    o, used = make_order(rows, k, experts, rows)
+    x = normal(1, rows, dim, dtype=dtype)
+    xs = torch.full((rows * k, dim), NAN, dtype=dtype, device="cuda")
+    gs.gs_dispatch_fwd(x, o, xs)
+    assert torch.equal(xs[:used], x[o.order[:used].long() // k])
+    assert torch.isnan(xs[used:]).all()   # unused places stay as they are
+    dxs = normal(2, rows * k, dim, dtype=dtype)
+    dxs[used:] = NAN                       # and are not read
+    for add in (None, normal(3, rows, dim, dtype=dtype)):
+        dx = torch.full((rows, dim), NAN, dtype=dtype, device="cuda")
+        gs.gs_dispatch_bwd(dxs, o, dx, add=add)
+        v = gathered(dxs, o.place, k)
+        a = torch.zeros(rows, dim, dtype=torch.float64) if add is None else add.double().cpu()
+        assert_close("dx", dx, v.sum(1) + a, (k + 1) * U32 * (v.abs().sum(1) + a.abs()), dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,k,dim,experts", SHAPES)
+def test_combine(rows, k, dim, experts, dtype):
+    o, used = make_order(rows, k, experts, rows + 1)
+    ys, w = normal(4, rows * k, dim, dtype=dtype), normal(5, rows, k)
+    ys[used:] = NAN
+    wd = w.double().cpu().unsqueeze(2)
+    for r in (None, normal(6, rows, dim, dtype=dtype)):
+        y = torch.full((rows, dim), NAN, dtype=dtype, device="cuda")
+        gs.gs_combine_fwd(ys, o, w, y, residual=r)
+        v = gathered(ys, o.place, k) * wd
+        a = torch.zeros(rows, dim, dtype=torch.float64) if r is None else r.double().cpu()
+        assert_close("y", y, v.sum(1) + a, (k + 1) * U32 * (v.abs().sum(1) + a.abs()), dtype)
+    dy = normal(7, rows, dim, dtype=dtype)
+    dys = torch.full((rows * k, dim), NAN, dtype=dtype, device="cuda")
+    dw = torch.full((rows, k), NAN, device="cuda")
+    gs.gs_combine_bwd(dy, ys, o, w, dys, dw)
+    assert torch.isnan(dys[used:]).all()
+    order = o.order[:used].cpu().long()
+    ref = w.double().cpu().view(-1, 1)[order] * dy.double().cpu()[order // k]
+    assert_close("dys", dys[:used], ref, U32 * ref.abs(), dtype)
+    prod = gathered(ys, o.place, k) * dy.double().cpu().unsqueeze(1)
+    assert_close("dweight", dw, prod.sum(2), sum_bound(dim) * prod.abs().sum(2), torch.float32)
+    assert not dw[o.place.view(rows, k) < 0].any()
+
+
+def test_no_expert_at_all():
+    o = gs.RowOrder(6, 4, sorted=False)
+    gs.gs_sort_rows(torch.full((3, 2), -1, dtype=torch.int32, device="cuda"), o)
+    x, xs = torch.ones(3, 5, device="cuda"), torch.full((6, 5), 9.0, device="cuda")
+    gs.gs_dispatch_fwd(x, o, xs)
+    assert (xs == 9).all()
+    y, w = torch.full((3, 5), NAN, device="cuda"), torch.full((3, 2), NAN, device="cuda")
+    gs.gs_combine_fwd(torch.full((6, 5), NAN, device="cuda"), o, w, y)
+    assert not y.any()
+    gs.gs_combine_fwd(torch.full((6, 5), NAN, device="cuda"), o, w, y, residual=x)
+    assert torch.equal(y, x)
+    dw = torch.full((3, 2), NAN, device="cuda")
+    gs.gs_combine_bwd(x, xs, o, w, xs, dw)
+    assert not dw.any() and (xs == 9).all()
+
+
+def test_special_values_stay_in_their_rows():
+    o, used = make_order(50, 2, 4, 9, dropped=False)
+    ys, w = normal(1, 100, 40), normal(2, 50, 2)
+    p = int(o.place[2 * 7])   # row 7's first choice
+    ys[p, 3], w[20, 1] = float("inf"), NAN
+    y = torch.empty(50, 40, device="cuda")
+    gs.gs_combine_fwd(ys, o, w, y)
+    bad = torch.zeros(50, 40, dtype=torch.bool, device="cuda")
+    bad[7, 3], bad[20] = True, True
+    assert torch.equal(~torch.isfinite(y), bad)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("pad,offset", [(1, 0), (0, 1), (5, 3), (8, 8)])
+def test_strides(dtype, pad, offset):
+    rows, k, dim = 101, 2, 45
+    o, used = make_order(rows, k, 6, 4)
+    x, ys, w = normal(1, rows, dim, dtype=dtype), normal(2, rows * k, dim, dtype=dtype), normal(3, rows, k)
+    far = lambda t: strided(t, pad, offset)  # noqa: E731
+    outs = []
+    for change in (lambda t: t, far):
+        xs, dys = (change(torch.zeros(rows * k, dim, dtype=dtype, device="cuda")) for _ in range(2))
+        dx, y = (change(torch.zeros(rows, dim, dtype=dtype, device="cuda")) for _ in range(2))
+        dw = torch.zeros(rows, k, device="cuda")
+        gs.gs_dispatch_fwd(change(x), o, xs)
+        gs.gs_dispatch_bwd(change(ys), o, dx, add=change(x))
+        gs.gs_combine_fwd(change(ys), o, w, y, residual=change(x))
+        gs.gs_combine_bwd(change(x), change(ys), o, w, dys, dw)
+        outs.append([xs, dx, y, dys, dw])
+        for t in (xs, dx, y, dys):
+            if change is far and pad:
+                b = t._base
+                between = torch.ones_like(b, dtype=torch.bool)
+                between[offset:].view(t.shape[0], dim + pad)[:, :dim] = False
+                assert torch.isnan(b[between]).all()
+    for a, b in zip(*outs):
+        assert torch.equal(a, b)
+
+
+def test_gradients_against_differences():
+    """combine is linear in ys and in the weights, dispatch in x."""
+    rows, k, dim = 12, 3, 7
+    o, used = make_order(rows, k, 4, 2)
+    ys, w, c = normal(1, rows * k, dim), normal(2, rows, k), normal(3, rows, dim)
+    dys, dw = torch.zeros_like(ys), torch.empty_like(w)
+    gs.gs_combine_bwd(c, ys, o, w, dys, dw)
+
+    def value(ys, w):
+        y = torch.empty(rows, dim, device="cuda")
+        gs.gs_combine_fwd(ys, o, w, y)
+        return float((y.double() * c.double()).sum())
+
+    size = 8 * U32 * float((gathered(ys, o.place, k).abs().sum(1) + 3).mul(c.abs().double().cpu()).sum()) * 4
+    for p, j in ((0, 0), (used - 1, 3), (used // 2, 6)):
+        up, down = ys.clone(), ys.clone()
+        up[p, j] += 1.0
+        down[p, j] -= 1.0
+        assert abs((value(up, w) - value(down, w)) / 2 - float(dys[p, j])) <= size
+    for r, j in ((0, 0), (5, 2), (11, 1)):
+        up, down = w.clone(), w.clone()
+        up[r, j] += 1.0
+        down[r, j] -= 1.0
+        assert abs((value(ys, up) - value(ys, down)) / 2 - float(dw[r, j])) <= size
+
+
+def test_more_rows_than_the_grid_holds():
+    rows, k, dim = 300_001, 2, 16
+    o, used = make_order(rows, k, 16, 5)
+    x = normal(1, rows, dim, dtype=torch.float16)
+    xs = torch.zeros(rows * k, dim, dtype=torch.float16, device="cuda")
+    gs.gs_dispatch_fwd(x, o, xs)
+    at = o.order[:used].long() // k
+    assert torch.equal(xs[:used], x[at])
+    dx = torch.empty_like(x)
+    gs.gs_dispatch_bwd(xs, o, dx)
+    count = (o.place.view(rows, k) >= 0).sum(1, keepdim=True)
+    assert torch.equal(dx, x * count)   # exact: once or twice a binary16 value
+
+
+def test_a_long_sorted_matrix():
+    """Places whose rows begin more than 2^31 values behind the first."""
+    rows, k, dim = 2 ** 20 + 3, 2, 1032
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("6.5 GB of rows")
+    expert = torch.zeros(rows, k, dtype=torch.int32, device="cuda")
+    expert[:, 1] = 1
+    o = gs.RowOrder(rows * k, 2, sorted=False)
+    gs.gs_sort_rows(expert, o, torch.empty(gs.gs_sort_rows_workspace_size(o), dtype=torch.uint8, device="cuda"))
+    x = torch.zeros(rows, dim, dtype=torch.bfloat16, device="cuda")
+    x[-1], x[0] = 5.0, 2.0
+    xs = torch.empty(rows * k, dim, dtype=torch.bfloat16, device="cuda")
+    gs.gs_dispatch_fwd(x, o, xs)
+    assert (xs[-1] == 5).all() and (xs[rows] == 2).all() and int(torch.count_nonzero(xs)) == 4 * dim
+    y, w = torch.empty_like(x), torch.full((rows, k), 0.5, device="cuda")
+    gs.gs_combine_fwd(xs, o, w, y)
+    assert torch.equal(y, x)
