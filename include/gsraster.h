@@ -651,6 +651,42 @@ gs_status gs_combine_bwd(int32_t type, int64_t rows, int64_t dim, const void* dy
                          int64_t ldys, const gs_row_order* order, const float* weight, void* dys, int64_t lddys,
                          float* dweight, void* stream);
 
+/* The layer of each expert of a mixture over rows sorted by expert. */
+typedef struct gs_experts {
+    gs_linear layer;          /* rows: those of x, y, ...; w: the first expert's; bias: [experts][n_out], or NULL */
+    int64_t experts;
+    int64_t w_stride;         /* elements from an expert's w to the next one's */
+    const int32_t* offsets;   /* [experts + 1] device array: expert e's rows are offsets[e] .. offsets[e + 1] - 1,
+                               * as gs_sort_rows writes it (never falling, offsets[experts] <= rows) */
+} gs_experts;
+
+/*
+ * gs_experts_fwd -- z = x w_e^T + bias_e, y = act(z) for the rows of every expert e, as
+ * gs_linear_fwd does for one layer. Rows from offsets[experts] on are neither read nor
+ * written, and the weights of an expert without rows are not read.
+ * Limits: those of gs_linear_fwd, 1 <= experts <= GS_MAX_EXPERTS (GS_ERR_UNSUPPORTED if
+ * rows times n_out or n_in exceed the grid: about 2^36 values).
+ * workspace: gs_experts_workspace_size bytes, 256-byte aligned; NULL where that is 0.
+ */
+gs_status gs_experts_fwd(const gs_experts* p, void* y, int64_t ldy, void* z, int64_t ldz, void* workspace,
+                         size_t workspace_bytes, void* stream);
+/*
+ * gs_experts_bwd -- dz = dy act'(z), dx = dz w_e for the rows of every expert e, dw_e = dz^T x
+ * and db_e = sum of dz over its rows, zero for an expert without rows: as gs_linear_bwd for
+ * one layer, with its types and precisions (in binary16 an x or w below 2^-14 counts as
+ * 2^-14 in how finely its products' sums are kept, as the matrix cores take it). dw: [experts][n_out][n_in] with row stride lddw
+ * and dw_stride from an expert to the next, db: [experts][n_out]; dx, dw and db are
+ * overwritten (dx: the experts' rows) and may each be NULL. The same call gives the same bits.
+ * workspace: gs_experts_workspace_size bytes, 256-byte aligned.
+ */
+gs_status gs_experts_bwd(const gs_experts* p, const void* dy, int64_t lddy, const void* z, int64_t ldz, void* dx,
+                         int64_t lddx, void* dw, int64_t lddw, int64_t dw_stride, int32_t dw_type, float* db,
+                         void* workspace, size_t workspace_bytes, void* stream);
+/* Bytes for the forward and the backward; dw_type -1: for the forward alone. The size for an
+ * fp32 dw is enough for one in the layer's type, and for a backward without dw. */
+gs_status gs_experts_workspace_size(int32_t type, int32_t act, int64_t rows, int64_t experts, int64_t n_in, int64_t n_out,
+                                    int32_t dw_type, size_t* bytes);
+
 /* Workspace bytes needed by any rasterizer call for these sizes (host only). */
 gs_status gs_workspace_size(int64_t n, int32_t width, int32_t height, uint64_t capacity, int32_t kind,
                             size_t* bytes);

@@ -783,9 +783,78 @@ gs_status check_move(int32_t type, int64_t rows, int64_t dim, const gs_row_order
     return place ? check_ints("place", o->place, rows) : GS_OK;
 }
 
+gs_status check_experts(const gs_experts* p)
+{
+    gs_status st;
+    GS_CHECK(p != nullptr, "the layer is NULL");
+    if ((st = check_linear(&p->layer)) != GS_OK) return st;
+    GS_CHECK(p->experts >= 1 && p->experts <= GS_MAX_EXPERTS, "experts = %lld outside [1, %d]", (long long)p->experts,
+             GS_MAX_EXPERTS);
+    GS_CHECK(p->w_stride >= 0 && p->w_stride < ((int64_t)1 << 48), "w_stride = %lld out of range", (long long)p->w_stride);
+    if ((st = check_ints("offsets", p->offsets, 1)) != GS_OK) return st;
+    if (!experts_grid_fits(p->layer.rows, p->experts, p->layer.n_in, p->layer.n_out))
+        return fail(GS_ERR_UNSUPPORTED, "%lld rows of %lld and %lld values for %lld experts exceed the grid",
+                    (long long)p->layer.rows, (long long)p->layer.n_in, (long long)p->layer.n_out, (long long)p->experts);
+    return GS_OK;
+}
+
 }  // namespace
 
 extern "C" {
+
+gs_status gs_experts_workspace_size(int32_t type, int32_t act, int64_t rows, int64_t experts, int64_t n_in, int64_t n_out,
+                                    int32_t dw_type, size_t* bytes)
+{
+    gs_status st;
+    GS_CHECK(bytes != nullptr, "bytes is NULL");
+    if ((st = check_rows(type, rows)) != GS_OK) return st;
+    GS_CHECK(act >= GS_ACT_NONE && act <= GS_ACT_SIGMOID, "unknown activation %d", act);
+    GS_CHECK(experts >= 1 && experts <= GS_MAX_EXPERTS, "experts = %lld outside [1, %d]", (long long)experts,
+             GS_MAX_EXPERTS);
+    if ((st = check_dim("n_in", n_in)) != GS_OK) return st;
+    if ((st = check_dim("n_out", n_out)) != GS_OK) return st;
+    GS_CHECK(dw_type == -1 || dw_type == GS_F32 || dw_type == type, "dw_type %d: fp32, the layer's type or -1", dw_type);
+    *bytes = experts_workspace(type, act, rows, experts, n_in, n_out, dw_type);
+    return ok();
+}
+
+gs_status gs_experts_fwd(const gs_experts* p, void* y, int64_t ldy, void* z, int64_t ldz, void* workspace,
+                         size_t workspace_bytes, void* stream)
+{
+    gs_status st;
+    if ((st = check_experts(p)) != GS_OK) return st;
+    const gs_linear& l = p->layer;
+    if ((st = check_matrix("y", y, l.rows, l.n_out, ldy, l.type)) != GS_OK) return st;
+    if (z && (st = check_matrix("z", z, l.rows, l.n_out, ldz, l.type)) != GS_OK) return st;
+    if (l.rows == 0) return ok();
+    if ((st = check_workspace(workspace, workspace_bytes, experts_fwd_workspace(*p))) != GS_OK) return st;
+    return timed(GS_KERNEL_EXPERTS_FWD, stream,
+                 [&](hipStream_t s) { return launch_experts_fwd(*p, y, ldy, z, ldz, workspace, s); });
+}
+
+gs_status gs_experts_bwd(const gs_experts* p, const void* dy, int64_t lddy, const void* z, int64_t ldz, void* dx,
+                         int64_t lddx, void* dw, int64_t lddw, int64_t dw_stride, int32_t dw_type, float* db,
+                         void* workspace, size_t workspace_bytes, void* stream)
+{
+    gs_status st;
+    if ((st = check_experts(p)) != GS_OK) return st;
+    const gs_linear& l = p->layer;
+    if ((st = check_matrix("dy", dy, l.rows, l.n_out, lddy, l.type)) != GS_OK) return st;
+    if (l.act != GS_ACT_NONE && (st = check_matrix("z", z, l.rows, l.n_out, ldz, l.type)) != GS_OK) return st;
+    if (dx && (st = check_matrix("dx", dx, l.rows, l.n_in, lddx, l.type)) != GS_OK) return st;
+    GS_CHECK(dw_type == GS_F32 || dw_type == l.type, "dw_type %d: fp32 or the layer's type", dw_type);
+    if (dw) {
+        if ((st = check_matrix("dw", dw, l.n_out, l.n_in, lddw, dw_type)) != GS_OK) return st;
+        GS_CHECK(p->experts == 1 || (dw_stride >= (l.n_out - 1) * lddw + l.n_in && dw_stride < ((int64_t)1 << 48)),
+                 "dw_stride = %lld: an expert's gradient would overlap the next", (long long)dw_stride);
+    }
+    GS_CHECK(((uintptr_t)db & 3) == 0, "db is not aligned to its element type");
+    if ((st = check_workspace(workspace, workspace_bytes, experts_bwd_workspace(*p, dy, lddy, dw ? dw_type : -1))) != GS_OK)
+        return st;
+    return timed(GS_KERNEL_EXPERTS_BWD, stream, [&](hipStream_t s) {
+        return launch_experts_bwd(*p, dy, lddy, z, ldz, dx, lddx, dw, lddw, dw_stride, dw_type, db, workspace, s);
+    });
+}
 
 gs_status gs_sort_rows_workspace_size(int64_t count, int64_t groups, size_t* bytes)
 {

@@ -1,0 +1,186 @@
+// Kernels of a mixture's layers beside the products of gemm.h and narrow.h.
+#pragma once
+
+#include "narrow.h"
+
+namespace gsr {
+
+namespace {
+
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_mix_prepare(MixPrepareArgs a)
+{
+    constexpr int kSums = kBlock * (Vec<T>::N + 1) * 4, kTile = kTransposeTile * (kTransposeTile * sizeof(T) + 4);
+    __shared__ __attribute__((aligned(16))) char lds[kSums > kTile ? kSums : kTile];
+    int64_t b = blockIdx.x;
+    if (b < a.slope_blocks) {
+        const int64_t unit = b / a.slope_x;
+        const MixUnit u = mix_unit(a.mix, a.mix.size, 0, unit);
+        if (u.expert < 0) return;
+        const int64_t first = u.first + u.unit * a.mix.size, left = u.rows - u.unit * a.mix.size;
+        SlopeArgs p = a.slope;
+        p.rows = left < a.mix.size ? left : a.mix.size;
+        p.row_blocks = 1;
+        p.dy = (const T*)p.dy + first * p.lddy;
+        if (p.act != GS_ACT_NONE) p.z = (const T*)p.z + first * p.ldz;
+        if (p.out) p.out = (T*)p.out + first * p.ldo;
+        if (p.sums) p.sums += unit * p.cols;
+        slope_rows<T>(p, b % a.slope_x, 0, lds);
+        return;
+    }
+    b -= a.slope_blocks;
+    if (b < a.copy_blocks) {
+        slope_rows<T>(a.copy, b / a.copy.row_blocks, b % a.copy.row_blocks, lds);
+        return;
+    }
+    b -= a.copy_blocks;
+    const int64_t e = b / a.weight_blocks;
+    b -= e * a.weight_blocks;
+    if (mix_offset(a.mix, (int)e + 1) <= mix_offset(a.mix, (int)e)) return;   // nobody reads its weights
+    if (a.transpose.src) {
+        TransposeArgs p = a.transpose;
+        const int64_t tiles_x = (p.cols + kTransposeTile - 1) / kTransposeTile;
+        p.src = (const T*)p.src + e * a.mix.w_stride;
+        p.dst = (T*)p.dst + e * a.w_out;
+        transpose_tile<T>(p, b % tiles_x, b / tiles_x, lds);
+    } else {
+        SlopeArgs p = a.weights;
+        p.dy = (const T*)p.dy + e * a.mix.w_stride;
+        p.out = (T*)p.out + e * a.w_out;
+        slope_rows<T>(p, b / p.row_blocks, b % p.row_blocks, lds);
+    }
+}
+
+// Adds up the parts of an expert's dW where it has several; blockIdx.y is the expert.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_mix_join(GemmArgs g)
+{
+    const MixUnit u = mix_expert(g.mix, (int)g.split_len, 1, blockIdx.y);
+    if (u.units < 2) return;
+    const int64_t quads = (g.cols + 3) / 4, size = g.rows * g.cols;
+    const int64_t before = mix_parts_before(g.mix, (int)g.split_len, u.expert);
+    const int64_t units = min(u.units, g.mix.limit - before);
+    const float* parts = g.part + before * size;
+    for (int64_t k = (int64_t)blockIdx.x * kBlock + threadIdx.x; k < g.rows * quads; k += (int64_t)gridDim.x * kBlock) {
+        const int64_t i = k / quads, j = (k - i * quads) * 4, left = g.cols - j;
+        const float* part = parts + i * g.cols + j;
+        float v[4] = {};
+#pragma unroll 8
+        for (int64_t s = 0; s < units; ++s) {
+            float p[4];
+            load_vec(part + s * size, left, p);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += p[e];
+        }
+        const int64_t o = u.expert * g.mix.dw_stride + i * g.ldo + j;
+        if (g.out_f32) {
+            store_vec((float*)g.out + o, left, v);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (e < left) ((T*)g.out)[o + e] = (T)v[e];
+        }
+    }
+}
+
+// blockIdx.y is the expert; 16 columns, 16 threads share one's units
+__global__ __launch_bounds__(kBlock) void k_mix_sums(Mix mix, const float* __restrict__ part, int64_t cols,
+                                                     float* __restrict__ db)
+{
+    __shared__ float s[16][16];
+    const MixUnit u = mix_expert(mix, mix.size, 0, blockIdx.y);
+    const int col = threadIdx.x & 15, slice = threadIdx.x >> 4;
+    const int64_t c = (int64_t)blockIdx.x * 16 + col;
+    float t = 0.f;
+    if (c < cols)
+#pragma unroll 8
+        for (int64_t k = slice; k < min(u.units, mix.limit - u.before); k += 16) t += part[(u.before + k) * cols + c];
+    s[slice][col] = t;
+    __syncthreads();
+    if (slice != 0 || c >= cols) return;
+#pragma unroll
+    for (int k = 1; k < 16; ++k) t += s[k][col];
+    db[u.expert * cols + c] = t;
+}
+
+}  // namespace
+
+template <typename T>
+hipError_t MixtureOps<T>::gemm_nt(int tile, bool fast_a, const GemmArgs& g, hipStream_t s)
+{
+    return run_nt<T, true>(tile, fast_a, g, s);
+}
+
+template <typename T>
+hipError_t MixtureOps<T>::gemm_tt(int tile, bool fast_b, const GemmArgs& g, hipStream_t s)
+{
+    const hipError_t e = run_tt<T, true>(tile, fast_b, g, s);
+    if (e != hipSuccess || !g.part) return e;
+    const int64_t blocks = std::min<int64_t>(div_up(g.rows * div_up(g.cols, 4), kBlock), 4096);
+    hipLaunchKernelGGL((k_mix_join<T>), dim3((unsigned)blocks, (unsigned)g.mix.experts), dim3(kBlock), 0, s, g);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t MixtureOps<T>::skinny(const GemmArgs& g, hipStream_t s)
+{
+    return run_skinny<T, true>(g, s);
+}
+
+template <typename T>
+hipError_t MixtureOps<T>::prepare(const Mix& mix, int64_t units, const SlopeArgs* slope, const SlopeArgs* copy,
+                                  const SlopeArgs* weights, const TransposeArgs* transpose, int64_t w_out,
+                                  hipStream_t s)
+{
+    MixPrepareArgs a = {};
+    a.mix = mix;
+    a.w_out = w_out;
+    a.slope_x = a.weight_blocks = 1;
+    auto lanes = [](const SlopeArgs& from, SlopeArgs& to) -> int64_t {   // workgroups across
+        to = from;
+        const int64_t vecs = div_up(std::max(to.ldo, to.cols), Vec<T>::N);
+        to.lanes = 1;
+        while (to.lanes < 64 && to.lanes < vecs) to.lanes <<= 1;
+        return div_up(vecs, to.lanes);
+    };
+    int64_t all = 0;
+    if (slope) {
+        a.slope_x = lanes(*slope, a.slope);
+        all += a.slope_blocks = a.slope_x * units;
+    }
+    if (copy) all += a.copy_blocks = lanes(*copy, a.copy) * copy->row_blocks;
+    if (weights) all += (a.weight_blocks = lanes(*weights, a.weights) * weights->row_blocks) * mix.experts;
+    if (transpose) {
+        a.transpose = *transpose;
+        a.weight_blocks = div_up(transpose->cols, kTransposeTile) *
+                          div_up(std::max(transpose->rows, transpose->ldd), kTransposeTile);
+        all += a.weight_blocks * mix.experts;
+    }
+    if (all == 0) return hipSuccess;
+    hipLaunchKernelGGL((k_mix_prepare<T>), dim3((unsigned)all), dim3(kBlock), 0, s, a);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t MixtureOps<T>::sums(const Mix& mix, const float* part, int64_t cols, float* db, hipStream_t s)
+{
+    hipLaunchKernelGGL(k_mix_sums, dim3((unsigned)div_up(cols, 16), (unsigned)mix.experts), dim3(kBlock), 0, s, mix, part,
+                       cols, db);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t MixtureOps<T>::narrow_fwd(const GemmArgs& g, bool fast, int64_t units, hipStream_t s)
+{
+    if constexpr (sizeof(T) == 2) return run_narrow_fwd<T, true>(g, fast, (int)units, s);
+    return hipErrorInvalidValue;
+}
+
+template <typename T>
+hipError_t MixtureOps<T>::narrow_bwd(const NarrowArgs& a, bool fast, int planes, int64_t units, hipStream_t s)
+{
+    if constexpr (sizeof(T) == 2) return run_narrow_bwd<T, true>(a, fast, planes, (int)units, s);
+    return hipErrorInvalidValue;
+}
+
+}  // namespace gsr

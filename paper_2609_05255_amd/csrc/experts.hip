@@ -1,0 +1,330 @@
+// The layers of a mixture's experts over rows that are sorted by expert: plans, workspaces, launches.
+//
+//   fwd: z = x W_e^T + b_e, y = act(z)                          for the rows of expert e
+//   bwd: dz = dy act'(z), dx = dz W_e, dW_e = dz^T x, db_e = column sums of dz, both over the expert's rows
+//
+// Where an expert's rows begin is on the device only. The kernels are those of the linear operators (gemm.h, narrow.h):
+// the rows are cut into units of up to so many rows of one expert, and a workgroup finds its unit in the offsets by a scan
+// over the experts (1 to 2 us, under the launch of the others). A grid holds as many units as there can be, rows / size
+// and one more for each expert, and the workgroups behind the last one leave. Weights of experts without rows are not
+// read. Bound, as there: by HBM for narrow layers, by reading the weights for few rows, by the matrix cores for the rest.
+#include "linear_plan.h"
+
+namespace gsr {
+
+namespace {
+
+constexpr int kDzBlocks = 2048;          // workgroups of dz, about
+constexpr int64_t kNarrowRows = 128;     // of a unit of a narrow layer, at least
+
+int64_t units_most(int64_t rows, int64_t experts, int64_t size) { return rows / size + std::min(rows, experts); }
+
+// The tile, and for dW the rows of a unit, that the rates of plan_product make fastest for experts of about equal shares.
+Plan plan_mix(int type, bool tt, int64_t rows, int64_t cols, int64_t len, int64_t experts, int planes, bool fast_operand)
+{
+    Plan best = {kTile64, 1, std::min<int64_t>(std::max<int64_t>(len, 64), 1 << 30)};
+    double best_us = 1e300;
+    const TileRate* rates = type == GS_F32 ? kRates32 : kRates16;
+    const int count = type == GS_F32 ? 3 : 5;
+    const int64_t some = std::max<int64_t>(1, std::min(tt ? len : rows, experts));
+    for (int k = 0; k < count; ++k) {
+        const TileRate& r = rates[k];
+        if (!fast_operand && (r.tile == kTile256 || r.tile == kTile64By4)) continue;
+        if (tt && r.tile == kTile128x64) continue;
+        const double slow = fast_operand ? 1.0 : kSlowRate, area = 2.0 * r.rows * r.cols * kFillTiles;
+        const int threads = r.tile == kTile64By4 ? 1024 : r.tile == kTile256 ? 512 : 256;
+        if (!tt) {
+            if (len < r.least) continue;
+            if (units_most(rows, experts, r.rows) * div_up(cols, r.cols) * threads >> 32) continue;
+            const int64_t tiles = std::max(some, rows / r.rows + some / 2) * div_up(cols, r.cols);
+            const int64_t share = div_up(tiles, kFillTiles), rounds = div_up(share, r.held);
+            const bool alone = (share - 1) % r.held == 0;
+            const double us = area * (double)len * ((double)(share - alone) / r.flop_us + alone / r.flop_us_one) / slow +
+                              (double)rounds * r.round_us;
+            if (us < best_us) {
+                best_us = us;
+                best = {r.tile, 1, len};
+            }
+            continue;
+        }
+        const int64_t tiles = div_up(rows, r.rows) * div_up(cols, r.cols);
+        if (tiles * threads >> 32) continue;
+        for (int64_t want = 1; want == 1 || len / want >= kRowSplitLen; want *= 2) {
+            const int64_t size = std::min<int64_t>(std::max<int64_t>(64, div_up(div_up(len, want), 64) * 64), 1 << 30);
+            if (units_most(len, experts, size) + experts > 65535) break;
+            const double longest = (double)std::min<int64_t>(size, 2 * div_up(len, some));   // (a larger share than most)
+            const double units = (double)len / size + 0.5 * some, each = (double)len / units;
+            const int64_t share = div_up((int64_t)(units * tiles) + 1, kFillTiles), rounds = div_up(share, r.held);
+            double us = std::max(area * each * share / r.flop_us, area * longest / r.flop_us_one) * planes / slow +
+                        (double)rounds * r.round_us;
+            if ((double)size < longest * 1.01 && want > 1) us += kJoinUs + 8.0 * units * (double)rows * (double)cols / kBytesUs;
+            if (us < best_us) {
+                best_us = us;
+                best = {r.tile, (int)want, size};
+            }
+        }
+    }
+    return best;
+}
+
+// Parts of dW: the units of experts that have several.
+int64_t parts_most(const Plan& p, int64_t rows, int64_t experts)
+{
+    return p.split_len >= rows ? 0 : std::min(units_most(rows, experts, p.split_len), 2 * (rows / p.split_len));
+}
+
+int64_t dz_size(int type, int64_t rows, int64_t cols)
+{
+    const int64_t across = div_up(div_up(cols, vec(type)), 64);
+    return std::max<int64_t>(32, div_up(div_up(rows * across, kDzBlocks), 32) * 32);
+}
+
+int64_t narrow_size(int64_t rows, int64_t in, int64_t out)
+{
+    const int64_t most = in > 64 && out > 64 ? kNarrowBlocks : 2 * kNarrowBlocks;
+    return std::max(kNarrowRows, div_up(div_up(rows, most), 64) * 64);
+}
+
+bool narrow_taken(int type, int64_t rows, int64_t in, int64_t out) { return rows > kFewRows && narrow(type, in, out); }
+
+bool fast_w(const gs_experts& p)
+{
+    return fast(p.layer.w, p.layer.ldw, p.layer.n_in, p.layer.type) && p.w_stride % vec(p.layer.type) == 0;
+}
+
+// W with padded rows, where its own cannot be read in vectors
+size_t fwd_bytes(int type, int64_t rows, int64_t experts, int64_t in, int64_t out, bool copy_w)
+{
+    if (rows <= kFewRows || narrow_taken(type, rows, in, out) || !copy_w) return 0;
+    return align_up((size_t)(experts * out * padded(type, in) * elem(type)), 256);
+}
+
+struct BwdSpace {
+    void *x, *dz, *wt;   // x with padded rows, dz in planes, each W transposed
+    float *sums, *part;
+    size_t bytes;
+};
+
+// dw_type: -1 without dW
+BwdSpace bwd_space(void* base, int type, int act, int64_t rows, int64_t experts, int64_t in, int64_t out, int dw_type,
+                   bool need_dz)
+{
+    Regions r{(char*)base};
+    BwdSpace b = {};
+    if (narrow(type, in, out)) {
+        b.part = (float*)r.take(units_most(rows, experts, narrow_size(rows, in, out)) * narrow_part((int)out, (int)in) * 4);
+        b.bytes = r.at;
+        return b;
+    }
+    const bool want_dw = dw_type >= 0;
+    const int planes = planes_of(type, act, dw_type);
+    if (need_dz) b.dz = r.take(planes * rows * padded(type, out) * elem(type));
+    if (want_dw && in % vec(type)) b.x = r.take(rows * padded(type, in) * elem(type));
+    b.wt = r.take(experts * in * padded(type, out) * elem(type));
+    b.sums = (float*)r.take(units_most(rows, experts, dz_size(type, rows, out)) * out * 4);
+    int64_t parts = 0;
+    // (a workspace is sized for either operand's alignment)
+    for (int fast_x = 0; want_dw && fast_x < 2; ++fast_x)
+        parts = std::max(parts, parts_most(plan_mix(type, true, out, in, rows, experts, planes, fast_x != 0), rows, experts));
+    b.part = (float*)r.take(parts * out * in * 4);
+    b.bytes = r.at;
+    return b;
+}
+
+Mix mix_of(const gs_experts& p, int64_t size)
+{
+    Mix m = {};
+    m.offsets = p.offsets;
+    m.experts = (int32_t)p.experts;
+    m.rows = p.layer.rows;
+    m.w_stride = p.w_stride;
+    m.size = (int32_t)size;
+    return m;
+}
+
+template <typename T>
+hipError_t run_nt(int type, GemmArgs g, bool fast_a, hipStream_t s)
+{
+    g.splits = g.planes = 1;
+    g.split_len = g.len;
+    if (g.rows <= kFewRows) return MixtureOps<T>::skinny(g, s);
+    return MixtureOps<T>::gemm_nt(plan_mix(type, false, g.rows, g.cols, g.len, g.mix.experts, 1, fast_a).tile, fast_a, g, s);
+}
+
+template <typename T>
+hipError_t experts_fwd(const gs_experts& p, void* y, int64_t ldy, void* z, int64_t ldz, void* ws, hipStream_t s)
+{
+    const gs_linear& l = p.layer;
+    const bool fast_x = fast(l.x, l.ldx, l.n_in, l.type);
+    GemmArgs g = {};
+    g.a = l.x;
+    g.lda = l.ldx;
+    g.b = l.w;
+    g.ldb = l.ldw;
+    g.rows = l.rows;
+    g.cols = l.n_out;
+    g.len = l.n_in;
+    g.bias = l.bias;
+    g.act = l.act;
+    g.out = y;
+    g.ldo = ldy;
+    g.z = z;
+    g.ldz = ldz;
+    g.mix = mix_of(p, 0);
+    if (narrow_taken(l.type, l.rows, l.n_in, l.n_out)) {
+        g.mix.size = (int32_t)narrow_size(l.rows, l.n_in, l.n_out);
+        return MixtureOps<T>::narrow_fwd(g, fast_x, units_most(l.rows, p.experts, g.mix.size), s);
+    }
+    if (fwd_bytes(l.type, l.rows, p.experts, l.n_in, l.n_out, !fast_w(p))) {
+        SlopeArgs copy = copy_of(l.type, l.w, l.ldw, l.n_out, l.n_in, ws);
+        copy.row_blocks = (int)std::max<int64_t>(1, copy.row_blocks / p.experts);
+        const int64_t each = l.n_out * padded(l.type, l.n_in);
+        const hipError_t e = MixtureOps<T>::prepare(g.mix, 0, nullptr, nullptr, &copy, nullptr, each, s);
+        if (e != hipSuccess) return e;
+        g.b = ws;
+        g.ldb = padded(l.type, l.n_in);
+        g.mix.w_stride = each;
+    }
+    return run_nt<T>(l.type, g, fast_x, s);
+}
+
+template <typename T>
+hipError_t experts_bwd(const gs_experts& p, const void* dy, int64_t lddy, const void* z, int64_t ldz, void* dx,
+                       int64_t lddx, void* dw, int64_t lddw, int64_t dw_stride, int dw_type, float* db, void* ws,
+                       hipStream_t s)
+{
+    const gs_linear& l = p.layer;
+    const bool need_dz = l.act != GS_ACT_NONE || !fast(dy, lddy, l.n_out, l.type);
+    const int planes = planes_of(l.type, l.act, dw ? dw_type : -1);
+    const BwdSpace b = bwd_space(ws, l.type, l.act, l.rows, p.experts, l.n_in, l.n_out, dw ? dw_type : -1, need_dz);
+    if (narrow(l.type, l.n_in, l.n_out)) {
+        NarrowArgs a = {dy,        z,           l.x,  l.w, lddy,  ldz, l.ldx, l.ldw, lddx, lddw, l.rows, (int)l.n_out,
+                        (int)l.n_in, l.act, dw_type == GS_F32, dx, dw,    db,  b.part};
+        a.mix = mix_of(p, narrow_size(l.rows, l.n_in, l.n_out));
+        a.mix.dw_stride = dw_stride;
+        a.mix.limit = units_most(l.rows, p.experts, a.mix.size);
+        const bool whole = fast(dy, lddy, l.n_out, l.type) && fast(l.x, l.ldx, l.n_in, l.type) &&
+                           (l.act == GS_ACT_NONE || fast(z, ldz, l.n_out, l.type));
+        return MixtureOps<T>::narrow_bwd(a, whole, planes, a.mix.limit, s);
+    }
+    const int64_t ldo = need_dz ? padded(l.type, l.n_out) : lddy, ldt = padded(l.type, l.n_out);
+    const void* dz = need_dz ? b.dz : dy;
+    SlopeArgs slope = {}, copy = {};
+    Mix rows = mix_of(p, dz_size(l.type, l.rows, l.n_out));
+    rows.limit = units_most(l.rows, p.experts, rows.size);
+    const bool want_slope = l.rows > 0 && (need_dz || db), want_dx = dx && l.rows > 0, copy_x = b.x && l.rows > 0;
+    if (want_slope) {
+        slope.dy = dy;
+        slope.lddy = lddy;
+        slope.z = z;
+        slope.ldz = ldz;
+        slope.cols = l.n_out;
+        slope.act = l.act;
+        slope.planes = planes;
+        slope.out = need_dz ? b.dz : nullptr;
+        slope.ldo = need_dz ? ldo : 0;
+        slope.plane_stride = l.rows * ldo;
+        slope.sums = db ? b.sums : nullptr;
+    }
+    if (copy_x) copy = copy_of(l.type, l.x, l.ldx, l.rows, l.n_in, b.x);
+    const TransposeArgs transpose = {l.w, l.ldw, l.n_out, l.n_in, b.wt, ldt};
+    hipError_t e = MixtureOps<T>::prepare(rows, rows.limit, want_slope ? &slope : nullptr,
+                                          copy_x ? &copy : nullptr, nullptr, want_dx ? &transpose : nullptr, l.n_in * ldt, s);
+    if (e == hipSuccess && db) e = MixtureOps<T>::sums(rows, b.sums, l.n_out, db, s);
+    if (e != hipSuccess) return e;
+    if (want_dx) {
+        GemmArgs g = {};
+        g.a = dz;
+        g.lda = ldo;
+        g.b = b.wt;
+        g.ldb = ldt;
+        g.rows = l.rows;
+        g.cols = l.n_in;
+        g.len = l.n_out;
+        g.out = dx;
+        g.ldo = lddx;
+        g.mix = mix_of(p, 0);
+        g.mix.w_stride = l.n_in * ldt;
+        e = run_nt<T>(l.type, g, true, s);
+        if (e != hipSuccess) return e;
+    }
+    if (dw) {
+        GemmArgs g = {};
+        const void* x = copy_x ? b.x : l.x;
+        const int64_t ldx = copy_x ? padded(l.type, l.n_in) : l.ldx;
+        const bool fast_x = copy_x || fast(x, ldx, l.n_in, l.type);
+        const Plan plan = plan_mix(l.type, true, l.n_out, l.n_in, l.rows, p.experts, planes, fast_x);
+        g.a = dz;
+        g.lda = ldo;
+        g.b = x;
+        g.ldb = ldx;
+        g.rows = l.n_out;
+        g.cols = l.n_in;
+        g.len = l.rows;
+        g.splits = 1;
+        g.split_len = plan.split_len;
+        g.planes = planes;
+        g.plane_stride = l.rows * ldo;
+        g.plane_scale = plane_scale(l.type);
+        g.out = dw;
+        g.ldo = lddw;
+        g.out_f32 = dw_type == GS_F32;
+        g.mix = mix_of(p, 0);
+        g.mix.limit = parts_most(plan, l.rows, p.experts);
+        g.part = g.mix.limit > 0 ? b.part : nullptr;
+        g.mix.dw_stride = dw_stride;
+        e = MixtureOps<T>::gemm_tt(plan.tile, fast_x, g, s);
+    }
+    return e;
+}
+
+}  // namespace
+
+size_t experts_fwd_workspace(const gs_experts& p)
+{
+    return fwd_bytes(p.layer.type, p.layer.rows, p.experts, p.layer.n_in, p.layer.n_out, !fast_w(p));
+}
+
+size_t experts_bwd_workspace(const gs_experts& p, const void* dy, int64_t lddy, int dw_type)
+{
+    const gs_linear& l = p.layer;
+    return bwd_space(nullptr, l.type, l.act, l.rows, p.experts, l.n_in, l.n_out, dw_type,
+                     l.act != GS_ACT_NONE || !fast(dy, lddy, l.n_out, l.type)).bytes;
+}
+
+size_t experts_workspace(int type, int act, int64_t rows, int64_t experts, int64_t in, int64_t out, int dw_type)
+{
+    const size_t fwd = fwd_bytes(type, rows, experts, in, out, true);
+    if (dw_type < 0) return fwd;
+    // (fewer planes of dz can mean more parts of dW: the size for an fp32 dW does for one in the type as well)
+    return std::max({fwd, bwd_space(nullptr, type, act, rows, experts, in, out, dw_type, true).bytes,
+                     bwd_space(nullptr, type, act, rows, experts, in, out, type, true).bytes});
+}
+
+// Work items of a launch are counted in 32 bits, for the smallest tiles, W transposed or copied, and dz.
+bool experts_grid_fits(int64_t rows, int64_t experts, int64_t in, int64_t out)
+{
+    const int64_t most = std::max(in, out), limit = (int64_t)1 << 32;
+    return units_most(rows, experts, 64) * div_up(most, 64) * 256 < limit &&
+           (experts * (div_up(in, 64) + 1) * (div_up(out, 64) + 1) + 32768 + experts * div_up(most, 256)) * kBlock < limit;
+}
+
+hipError_t launch_experts_fwd(const gs_experts& p, void* y, int64_t ldy, void* z, int64_t ldz, void* ws, hipStream_t s)
+{
+    if (p.layer.type == GS_F16) return experts_fwd<f16>(p, y, ldy, z, ldz, ws, s);
+    if (p.layer.type == GS_BF16) return experts_fwd<bf16>(p, y, ldy, z, ldz, ws, s);
+    return experts_fwd<float>(p, y, ldy, z, ldz, ws, s);
+}
+
+hipError_t launch_experts_bwd(const gs_experts& p, const void* dy, int64_t lddy, const void* z, int64_t ldz, void* dx,
+                              int64_t lddx, void* dw, int64_t lddw, int64_t dw_stride, int dw_type, float* db, void* ws,
+                              hipStream_t s)
+{
+#define CALL(T) experts_bwd<T>(p, dy, lddy, z, ldz, dx, lddx, dw, lddw, dw_stride, dw_type, db, ws, s)
+    if (p.layer.type == GS_F16) return CALL(f16);
+    if (p.layer.type == GS_BF16) return CALL(bf16);
+    return CALL(float);
+#undef CALL
+}
+
+}  // namespace gsr

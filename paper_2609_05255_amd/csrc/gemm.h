@@ -255,16 +255,24 @@ struct Tile {
 
 // Tiles in an order in which neighbours in time on one XCD (workgroups b, b + 8, ...) share operand rows: each
 // XCD takes a contiguous range of tiles, columns fastest within panels of kPanel tile rows.
-__device__ __forceinline__ void tile_of(int64_t b, int64_t tiles_i, int64_t tiles_j, int64_t* ti, int64_t* tj)
+__device__ __forceinline__ int64_t xcd_order(int64_t b, int64_t total)
 {
-    const int64_t total = tiles_i * tiles_j;
     const int64_t per = total >> 3, rest = total & 7, xcd = b & 7, k = b >> 3;
-    int64_t t = xcd * per + (xcd < rest ? xcd : rest) + k;
+    return xcd * per + (xcd < rest ? xcd : rest) + k;
+}
+
+__device__ __forceinline__ void panel_of(int64_t t, int64_t tiles_i, int64_t tiles_j, int64_t* ti, int64_t* tj)
+{
     constexpr int64_t kPanel = 8;
     const int64_t panel = t / (kPanel * tiles_j), in = t - panel * kPanel * tiles_j;
     const int64_t left = tiles_i - panel * kPanel, h = left < kPanel ? left : kPanel;
     *ti = panel * kPanel + in % h;
     *tj = in / h;
+}
+
+__device__ __forceinline__ void tile_of(int64_t b, int64_t tiles_i, int64_t tiles_j, int64_t* ti, int64_t* tj)
+{
+    panel_of(xcd_order(b, tiles_i * tiles_j), tiles_i, tiles_j, ti, tj);
 }
 
 // BI, BJ: the workgroup's tile; WI, WJ: the waves that share it; AHEAD: fragments are read half a tile ahead of their
@@ -314,7 +322,10 @@ __device__ __forceinline__ void store_block(const char* lds, T* out, int64_t ld,
     }
 }
 
-template <typename T, class S>
+// MIX: the product of each expert's rows with its own B (NT: workgroups take tiles of units of BI rows, and those beyond
+// the last one leave), or the sum over each expert's rows (TT: blockIdx.y is a unit of rows, and the results of an expert
+// that has several go to their parts).
+template <typename T, class S, bool MIX = false>
 __global__ __launch_bounds__(S::THREADS * S::WAYS) void k_gemm(GemmArgs g)
 {
     constexpr bool TT = S::TT;
@@ -336,11 +347,45 @@ __global__ __launch_bounds__(S::THREADS * S::WAYS) void k_gemm(GemmArgs g)
     const int group = S::WAYS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / S::THREADS) : 0;
     char* lds = S::STATIC_LDS ? lds_own + group * 2 * kTileBytes : lds_given;
 
-    const int64_t tiles_i = (g.rows + BI - 1) / BI, tiles_j = (g.cols + BJ - 1) / BJ;
-    int64_t ti, tj;
-    tile_of(blockIdx.x, tiles_i, tiles_j, &ti, &tj);
+    const int64_t tiles_j = (g.cols + BJ - 1) / BJ;
+    int64_t tiles_i = (g.rows + BI - 1) / BI, ti, tj, split = blockIdx.y;
+    if constexpr (MIX && !TT) {
+        // the order of the tiles is tile_of's over all experts' units; a panel's tiles are of one expert
+        const int64_t total = uniform(mix_total(g.mix, BI, 0));
+        if (blockIdx.x >= total * tiles_j) return;
+        const int64_t t = xcd_order(blockIdx.x, total * tiles_j);
+        const MixUnit u = mix_unit(g.mix, BI, 0, t / tiles_j);
+        tiles_i = u.units;
+        panel_of(t - u.before * tiles_j, tiles_i, tiles_j, &ti, &tj);
+        g.rows = u.rows;
+        g.a = (const T*)g.a + u.first * g.lda;
+        g.b = (const T*)g.b + u.expert * g.mix.w_stride;
+        if (g.bias) g.bias += u.expert * g.cols;
+        if (g.z) g.z = (T*)g.z + u.first * g.ldz;
+        g.out = (T*)g.out + u.first * g.ldo;
+    } else {
+        tile_of(blockIdx.x, tiles_i, tiles_j, &ti, &tj);
+    }
+    if constexpr (MIX && TT) {
+        const MixUnit u = mix_unit(g.mix, (int)g.split_len, 1, blockIdx.y);
+        if (u.expert < 0) return;
+        split = u.unit;
+        if (u.units > 1) {
+            const int64_t at = mix_parts_before(g.mix, (int)g.split_len, u.expert) + u.unit;
+            if (at >= g.mix.limit) return;
+            g.part += at * g.rows * g.cols;
+        }
+        g.len = u.rows;
+        g.a = (const T*)g.a + u.first * g.lda;
+        g.b = (const T*)g.b + u.first * g.ldb;
+        if (u.units == 1) {
+            g.part = nullptr;
+            g.out = g.out_f32 ? (void*)((float*)g.out + u.expert * g.mix.dw_stride)
+                              : (void*)((T*)g.out + u.expert * g.mix.dw_stride);
+        }
+    }
     const int64_t i0 = ti * BI, j0 = tj * BJ;
-    int64_t c_begin = blockIdx.y * g.split_len;
+    int64_t c_begin = split * g.split_len;
     int64_t c_end = c_begin + g.split_len < g.len ? c_begin + g.split_len : g.len;
     int steps = c_end > c_begin ? (int)((c_end - c_begin + kBK - 1) / kBK) : 0;
     if constexpr (S::WAYS > 1) {
@@ -532,7 +577,7 @@ __global__ __launch_bounds__(S::THREADS * S::WAYS) void k_gemm(GemmArgs g)
     auto value = [&](int p, int k, int e) -> float { return acc[p][(k * kGroup + e) / 4][e & 3]; };
     const int64_t i1 = i0 + wi, j1 = j0 + wj;
     if (TT || g.part) {
-        float* out = g.part ? g.part + (int64_t)blockIdx.y * g.rows * g.cols : (float*)g.out;
+        float* out = !g.part ? (float*)g.out : MIX ? g.part : g.part + (int64_t)blockIdx.y * g.rows * g.cols;
         const int64_t ldo = g.part ? g.cols : g.ldo;
 #pragma unroll
         for (int p = 0; p < FI; ++p)
@@ -667,9 +712,21 @@ struct Flight<T, true> {
     }
 };
 
-template <typename T, int MF, bool ODD>
+// MIX: blockIdx.y is the expert.
+template <typename T, int MF, bool ODD, bool MIX = false>
 __global__ __launch_bounds__(kSkinnyWaves * 64) void k_skinny(GemmArgs g)
 {
+    if constexpr (MIX) {
+        const int e = blockIdx.y;
+        const int32_t first = mix_offset(g.mix, e), end = mix_offset(g.mix, e + 1);
+        if (end <= first) return;
+        g.rows = end - first;
+        g.a = (const T*)g.a + first * g.lda;
+        g.b = (const T*)g.b + e * g.mix.w_stride;
+        if (g.bias) g.bias += e * g.cols;
+        if (g.z) g.z = (T*)g.z + first * g.ldz;
+        g.out = (T*)g.out + first * g.ldo;
+    }
     constexpr int N = Vec<T>::N;
     constexpr int kStep = 4 * N;                     // values of the sum per MFMA step
     constexpr int kUnroll = MF == 1 ? 8 : 4;         // steps whose loads are under way together
@@ -903,20 +960,69 @@ __global__ __launch_bounds__(kBlock) void k_prepare(PrepareArgs a)
     slope_rows<T>(p, k / p.row_blocks, k % p.row_blocks, lds);
 }
 
-template <typename T, class S>
+// Units of up to `size` rows that `rows` rows of `experts` experts can have, at most (least: of each expert).
+inline int64_t mix_units(int64_t rows, int64_t experts, int64_t size, int least)
+{
+    const int64_t some = std::min(rows, experts);
+    return rows / size + (least ? experts : some);
+}
+
+template <typename T, class S, bool MIX = false>
 hipError_t run_gemm(const GemmArgs& g, hipStream_t s)
 {
-    const int64_t tiles = div_up(g.rows, S::BI) * div_up(g.cols, S::BJ);
+    int64_t tiles_i = div_up(g.rows, S::BI), splits = g.splits;
+    if (MIX && !S::TT) tiles_i = mix_units(g.rows, g.mix.experts, S::BI, 0);
+    if (MIX && S::TT) splits = mix_units(g.len, g.mix.experts, g.split_len, 1);
+    const int64_t tiles = tiles_i * div_up(g.cols, S::BJ);
     const int lds = S::STATIC_LDS ? 0 : S::lds_bytes(div_up(g.split_len, 128 / (int)sizeof(T)), sizeof(T));
-    hipLaunchKernelGGL((k_gemm<T, S>), dim3((unsigned)tiles, (unsigned)g.splits), dim3(S::THREADS * S::WAYS), lds, s, g);
+    hipLaunchKernelGGL((k_gemm<T, S, MIX>), dim3((unsigned)tiles, (unsigned)splits), dim3(S::THREADS * S::WAYS), lds, s,
+                       g);
     return hipGetLastError();
 }
 
-template <typename T, bool TT, int BI, int BJ, int WI, int WJ>
+template <typename T, bool TT, int BI, int BJ, int WI, int WJ, bool MIX = false>
 hipError_t run_any(bool fast, const GemmArgs& g, hipStream_t s)
 {
-    return fast ? run_gemm<T, Shape<TT, BI, BJ, WI, WJ, false, true>>(g, s)
-                : run_gemm<T, Shape<TT, BI, BJ, WI, WJ, false, false>>(g, s);
+    return fast ? run_gemm<T, Shape<TT, BI, BJ, WI, WJ, false, true>, MIX>(g, s)
+                : run_gemm<T, Shape<TT, BI, BJ, WI, WJ, false, false>, MIX>(g, s);
+}
+
+template <typename T, bool MIX>
+hipError_t run_nt(int tile, bool fast_a, const GemmArgs& g, hipStream_t s)
+{
+    if (tile == kTile256) {   // fast_a, 16-bit
+        if constexpr (sizeof(T) == 2) return run_gemm<T, Shape<false, 256, 256, 2, 4, true, true>, MIX>(g, s);
+    }
+    if (tile == kTile128) return run_any<T, false, 128, 128, 2, 2, MIX>(fast_a, g, s);
+    if (tile == kTile128x64) return run_any<T, false, 128, 64, 4, 1, MIX>(fast_a, g, s);
+    if (tile == kTile64By4) return run_gemm<T, Shape<false, 64, 64, 2, 2, false, true, 4>, MIX>(g, s);   // fast_a
+    return run_any<T, false, 64, 64, 2, 2, MIX>(fast_a, g, s);
+}
+
+template <typename T, bool MIX>
+hipError_t run_tt(int tile, bool fast_b, const GemmArgs& g, hipStream_t s)
+{
+    if (tile == kTile256) {   // fast_b, 16-bit
+        if constexpr (sizeof(T) == 2) return run_gemm<T, Shape<true, 256, 256, 2, 4, true, true>, MIX>(g, s);
+    }
+    if (tile == kTile128) return run_any<T, true, 128, 128, 2, 2, MIX>(fast_b, g, s);
+    if (tile == kTile64By4) return run_gemm<T, Shape<true, 64, 64, 2, 2, false, true, 4>, MIX>(g, s);   // fast_b
+    return run_any<T, true, 64, 64, 2, 2, MIX>(fast_b, g, s);
+}
+
+template <typename T, bool MIX>
+hipError_t run_skinny(const GemmArgs& g, hipStream_t s)
+{
+    const dim3 grid((unsigned)div_up(g.cols, 16), MIX ? (unsigned)g.mix.experts : 1);
+    auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kSkinnyWaves * 64), 0, s, g); };
+    if constexpr (sizeof(T) == 2) {
+        if ((((uintptr_t)g.a | (uintptr_t)g.b) & 2) || ((g.lda | g.ldb | (MIX ? g.mix.w_stride : 0)) & 1)) {
+            run(g.rows <= 16 ? k_skinny<T, 1, true, MIX> : k_skinny<T, 2, true, MIX>);
+            return hipGetLastError();
+        }
+    }
+    run(g.rows <= 16 ? k_skinny<T, 1, false, MIX> : k_skinny<T, 2, false, MIX>);   // (up to 32 rows)
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -924,39 +1030,19 @@ hipError_t run_any(bool fast, const GemmArgs& g, hipStream_t s)
 template <typename T>
 hipError_t LinearOps<T>::gemm_nt(int tile, bool fast_a, const GemmArgs& g, hipStream_t s)
 {
-    if (tile == kTile256) {   // fast_a, 16-bit
-        if constexpr (sizeof(T) == 2) return run_gemm<T, Shape<false, 256, 256, 2, 4, true, true>>(g, s);
-    }
-    if (tile == kTile128) return run_any<T, false, 128, 128, 2, 2>(fast_a, g, s);
-    if (tile == kTile128x64) return run_any<T, false, 128, 64, 4, 1>(fast_a, g, s);
-    if (tile == kTile64By4) return run_gemm<T, Shape<false, 64, 64, 2, 2, false, true, 4>>(g, s);   // fast_a
-    return run_any<T, false, 64, 64, 2, 2>(fast_a, g, s);
+    return run_nt<T, false>(tile, fast_a, g, s);
 }
 
 template <typename T>
 hipError_t LinearOps<T>::gemm_tt(int tile, bool fast_b, const GemmArgs& g, hipStream_t s)
 {
-    if (tile == kTile256) {   // fast_b, 16-bit
-        if constexpr (sizeof(T) == 2) return run_gemm<T, Shape<true, 256, 256, 2, 4, true, true>>(g, s);
-    }
-    if (tile == kTile128) return run_any<T, true, 128, 128, 2, 2>(fast_b, g, s);
-    if (tile == kTile64By4) return run_gemm<T, Shape<true, 64, 64, 2, 2, false, true, 4>>(g, s);   // fast_b
-    return run_any<T, true, 64, 64, 2, 2>(fast_b, g, s);
+    return run_tt<T, false>(tile, fast_b, g, s);
 }
 
 template <typename T>
 hipError_t LinearOps<T>::skinny(const GemmArgs& g, hipStream_t s)
 {
-    const dim3 grid((unsigned)div_up(g.cols, 16));
-    auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kSkinnyWaves * 64), 0, s, g); };
-    if constexpr (sizeof(T) == 2) {
-        if ((((uintptr_t)g.a | (uintptr_t)g.b) & 2) || ((g.lda | g.ldb) & 1)) {
-            run(g.rows <= 16 ? k_skinny<T, 1, true> : k_skinny<T, 2, true>);
-            return hipGetLastError();
-        }
-    }
-    run(g.rows <= 16 ? k_skinny<T, 1, false> : k_skinny<T, 2, false>);   // (up to 32 rows)
-    return hipGetLastError();
+    return run_skinny<T, false>(g, s);
 }
 
 template <typename T>

@@ -243,6 +243,14 @@ hipError_t launch_sum_choices(int type, const void* src, int64_t lds, const gs_r
 hipError_t launch_combine_bwd(int type, const void* dy, int64_t lddy, const void* ys, int64_t ldys, const gs_row_order& o,
                               const float* weight, int64_t rows, int64_t dim, void* dys, int64_t lddys, float* dweight,
                               hipStream_t s);
+size_t experts_workspace(int type, int act, int64_t rows, int64_t experts, int64_t in, int64_t out, int dw_type);
+size_t experts_fwd_workspace(const gs_experts& p);
+size_t experts_bwd_workspace(const gs_experts& p, const void* dy, int64_t lddy, int dw_type);   // -1: without dW
+bool experts_grid_fits(int64_t rows, int64_t experts, int64_t in, int64_t out);
+hipError_t launch_experts_fwd(const gs_experts& p, void* y, int64_t ldy, void* z, int64_t ldz, void* ws, hipStream_t s);
+hipError_t launch_experts_bwd(const gs_experts& p, const void* dy, int64_t lddy, const void* z, int64_t ldz, void* dx,
+                              int64_t lddx, void* dw, int64_t lddw, int64_t dw_stride, int dw_type, float* db, void* ws,
+                              hipStream_t s);
 hipError_t launch_mlp_eval(const uint16_t* x, int64_t rows, const uint16_t* w, float* out, hipStream_t s);
 hipError_t launch_neural_fold(const uint16_t* features, const uint16_t* w, int64_t n, uint16_t* preact,
                               hipStream_t s);

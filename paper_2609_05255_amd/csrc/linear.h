@@ -3,6 +3,7 @@
 #pragma once
 
 #include "gs_internal.h"
+#include "mix.h"
 #include "vec.h"
 
 namespace gsr {
@@ -30,6 +31,7 @@ struct GemmArgs {
     int32_t act;
     int32_t out_f32;               // out is fp32 whatever the type (residual, z: unused)
     float* part;                   // [splits][rows][cols] fp32 instead of the epilogue, or NULL
+    Mix mix;                       // a mixture's products: rows (NT) or len (TT) are those of all experts
 };
 
 // dz = dy act'(z) of [rows][cols], as `planes` planes of the element type whose sum it is (plane k scaled by
@@ -74,6 +76,7 @@ struct NarrowArgs {
     void* dw;
     float* db;
     float* part;                   // [workgroups][narrow_part] dW [out][in], then db
+    Mix mix;
 };
 __host__ __device__ inline int64_t narrow_part(int out, int in) { return (out * in + out + 3) / 4 * 4; }
 
@@ -96,6 +99,32 @@ struct LinearOps {
     static hipError_t prepare(const SlopeArgs* slope, const SlopeArgs* copy, const TransposeArgs* transpose,
                               hipStream_t s);
     static hipError_t join(const GemmArgs& g, hipStream_t s);   // adds the parts up, with the epilogue
+};
+
+// What the products of a mixture's backward need before them, in one launch: dz with its column sums over units of each
+// expert's rows, a copy of x with aligned rows, and each expert's W transposed, or copied with aligned rows.
+struct MixPrepareArgs {
+    Mix mix;                       // size: rows of dz's units
+    SlopeArgs slope, copy, weights;
+    TransposeArgs transpose;
+    int64_t w_out;                 // values of an expert's W in the copy or transposed
+    int64_t slope_x, slope_blocks, copy_blocks, weight_blocks;   // workgroups across dz, in all, of x, of one expert's W
+};
+
+// per type T (the files experts_*.hip)
+template <typename T>
+struct MixtureOps {
+    static hipError_t gemm_nt(int tile, bool fast_a, const GemmArgs& g, hipStream_t s);
+    static hipError_t gemm_tt(int tile, bool fast_b, const GemmArgs& g, hipStream_t s);   // with the join of its parts
+    static hipError_t skinny(const GemmArgs& g, hipStream_t s);
+    // slope, copy, weights, transpose: those that are wanted; units: of dz, at most
+    static hipError_t prepare(const Mix& mix, int64_t units, const SlopeArgs* slope, const SlopeArgs* copy,
+                              const SlopeArgs* weights, const TransposeArgs* transpose, int64_t w_out, hipStream_t s);
+    // db[e][c]: the sums of e's units (mix.size rows) over part [units][cols]
+    static hipError_t sums(const Mix& mix, const float* part, int64_t cols, float* db, hipStream_t s);
+    // 16-bit layers of up to 128 inputs and outputs, in units of mix.size rows
+    static hipError_t narrow_fwd(const GemmArgs& g, bool fast, int64_t units, hipStream_t s);
+    static hipError_t narrow_bwd(const NarrowArgs& a, bool fast, int planes, int64_t units, hipStream_t s);
 };
 
 }  // namespace gsr

@@ -94,9 +94,22 @@ __device__ __forceinline__ V finite_of(V v)
 
 // FAST: rows of dy, z and x are whole aligned vectors, and come through buffer loads whose range check turns what lies
 // beyond the matrix into zeros; otherwise they are loaded at any alignment.
-template <typename T, int OUT, int IN, int P, bool FAST>
+// MIX: a workgroup takes a unit of an expert's rows, with its part at the unit's place.
+template <typename T, int OUT, int IN, int P, bool FAST, bool MIX = false>
 __global__ __launch_bounds__(kNarrowThreads, 2) void k_narrow_bwd(NarrowArgs a)
 {
+    if constexpr (MIX) {
+        const MixUnit u = mix_unit(a.mix, a.mix.size, 0, blockIdx.x);
+        if (u.expert < 0) return;
+        const int64_t first = u.first + u.unit * a.mix.size, left = u.rows - u.unit * a.mix.size;
+        a.rows = left < a.mix.size ? left : a.mix.size;
+        a.dy = (const T*)a.dy + first * a.lddy;
+        if (a.act != GS_ACT_NONE) a.z = (const T*)a.z + first * a.ldz;
+        a.x = (const T*)a.x + first * a.ldx;
+        a.w = (const T*)a.w + u.expert * a.mix.w_stride;
+        if (a.dx) a.dx = (T*)a.dx + first * a.lddx;
+    }
+    const int64_t first_tile = MIX ? 0 : blockIdx.x, tile_step = MIX ? 1 : gridDim.x;
     constexpr int R = narrow_tile_rows(OUT, IN, P, FAST), VO = OUT / 8, VI = IN / 8;
     constexpr int NO = R * VO / kNarrowThreads, NI = R * VI / kNarrowThreads;   // vectors of a thread
     constexpr int FO = OUT / 32, FI = IN / 32;                                  // fragments of a wave's part of dW
@@ -166,8 +179,8 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void k_narrow_bwd(NarrowArgs a)
     float db[8] = {};
     const int wo = (wave >> 1) * (OUT / 32), wn = (wave & 1) * (IN / 32);   // first groups of 16 of the wave's part of dW
     const int64_t tiles = (a.rows + R - 1) / R;
-    if (blockIdx.x < tiles) fetch((int64_t)blockIdx.x * R);
-    for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
+    if (first_tile < tiles) fetch(first_tile * R);
+    for (int64_t t = first_tile; t < tiles; t += tile_step) {
 #pragma unroll
         for (int k = 0; k < NO; ++k) {
             const int r = ro + k * (kNarrowThreads / VO);
@@ -199,7 +212,7 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void k_narrow_bwd(NarrowArgs a)
             for (int k = 0; k < NI; ++k)
                 *reinterpret_cast<Packed*>(lds_x + narrow_at(R, ri + k * (kNarrowThreads / VI), vi)) = rx[k];
         __syncthreads();
-        if (t + gridDim.x < tiles) fetch((t + gridDim.x) * R);
+        if (t + tile_step < tiles) fetch((t + tile_step) * R);
         if (a.dx)
 #pragma unroll
             for (int k = 0; k < kBlocksX; ++k) {
@@ -288,9 +301,18 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void k_narrow_bwd(NarrowArgs a)
 }
 
 // dW and db: the sums of the workgroups' parts. A workgroup takes 16 places of 4 values, 16 threads share a place.
-template <typename T>
+// MIX: blockIdx.y is the expert, whose units' parts are added up.
+template <typename T, bool MIX = false>
 __global__ __launch_bounds__(kBlock) void k_narrow_join(NarrowArgs a, int parts)
 {
+    if constexpr (MIX) {
+        const MixUnit u = mix_expert(a.mix, a.mix.size, 0, blockIdx.y);
+        parts = (int)min(u.units, a.mix.limit - u.before);
+        a.part += u.before * narrow_part(a.out, a.in);
+        if (a.dw) a.dw = a.dw_f32 ? (void*)((float*)a.dw + u.expert * a.mix.dw_stride)
+                                  : (void*)((T*)a.dw + u.expert * a.mix.dw_stride);
+        if (a.db) a.db += u.expert * a.out;
+    }
     __shared__ f32x4 sums[kBlock];
     const int place = threadIdx.x & 15, slice = threadIdx.x >> 4;
     const int size = a.out * a.in + a.out, at = (blockIdx.x * 16 + place) * 4;
@@ -326,9 +348,21 @@ __global__ __launch_bounds__(kBlock) void k_narrow_join(NarrowArgs a, int parts)
 // from memory in the layout of the MFMAs' fragments, the next rows' while these are worked on, and the results leave
 // through the wave's part of LDS as whole rows. Bound by HBM: 1,000,000 x 128 x 128 in binary16 with gelu and a residual
 // 162 us, 4.7 TB/s (242 in tiles of the general product).
-template <typename T, int OUT, int IN, bool FAST>
+// MIX: a workgroup takes a unit of an expert's rows.
+template <typename T, int OUT, int IN, bool FAST, bool MIX = false>
 __global__ __launch_bounds__(kNarrowThreads) void k_narrow_fwd(GemmArgs g)
 {
+    if constexpr (MIX) {
+        const MixUnit u = mix_unit(g.mix, g.mix.size, 0, blockIdx.x);
+        if (u.expert < 0) return;
+        const int64_t first = u.first + u.unit * g.mix.size, left = u.rows - u.unit * g.mix.size;
+        g.rows = left < g.mix.size ? left : g.mix.size;
+        g.a = (const T*)g.a + first * g.lda;
+        g.b = (const T*)g.b + u.expert * g.mix.w_stride;
+        if (g.bias) g.bias += u.expert * g.cols;
+        if (g.z) g.z = (T*)g.z + first * g.ldz;
+        g.out = (T*)g.out + first * g.ldo;
+    }
     constexpr int FJ = OUT / 16, KS = IN / 32, kRow = (IN < 64 ? 64 : IN) * 2, kBlock16 = 16 * OUT * 2;
     typedef typename Mma<T>::Frag Frag;
     typedef typename Vec<T>::Packed Packed;
@@ -346,7 +380,7 @@ __global__ __launch_bounds__(kNarrowThreads) void k_narrow_fwd(GemmArgs g)
     for (int c = tid; c < OUT; c += kNarrowThreads) bias[c] = g.bias && c < out ? g.bias[c] : 0.f;
     __syncthreads();
 
-    const int64_t blocks = (g.rows + 15) / 16, step = (int64_t)gridDim.x * 4;
+    const int64_t blocks = (g.rows + 15) / 16, step = MIX ? 4 : (int64_t)gridDim.x * 4;
     Packed next[KS];
     auto fetch = [&](int64_t b) {
         const int64_t r = b * 16 + li < g.rows ? b * 16 + li : g.rows - 1;   // (rows beyond are not stored)
@@ -369,7 +403,7 @@ __global__ __launch_bounds__(kNarrowThreads) void k_narrow_fwd(GemmArgs g)
             for (int s = 0; s < KS; ++s) next[s] = load_any(src + 32 * s, in - 32 * s - lg * 8);
         }
     };
-    const int64_t first = (int64_t)blockIdx.x * 4 + wave;
+    const int64_t first = MIX ? wave : (int64_t)blockIdx.x * 4 + wave;
     if (first < blocks) fetch(first);
     for (int64_t b = first; b < blocks; b += step) {
         Frag x[KS];
@@ -436,24 +470,50 @@ void with_width(int n, F f)
         f(std::integral_constant<int, 128>());
 }
 
-template <typename T, int OUT, int IN, bool FAST>
+template <typename T, int OUT, int IN, bool FAST, bool MIX>
 void run_narrow(const NarrowArgs& a, int planes, int blocks, hipStream_t s)
 {
     constexpr int kMost = __is_same(T, f16) ? 2 : 3;
     if (planes == 1)
-        hipLaunchKernelGGL((k_narrow_bwd<T, OUT, IN, 1, FAST>), dim3(blocks), dim3(kNarrowThreads), 0, s, a);
+        hipLaunchKernelGGL((k_narrow_bwd<T, OUT, IN, 1, FAST, MIX>), dim3(blocks), dim3(kNarrowThreads), 0, s, a);
     else
-        hipLaunchKernelGGL((k_narrow_bwd<T, OUT, IN, kMost, FAST>), dim3(blocks), dim3(kNarrowThreads), 0, s, a);
+        hipLaunchKernelGGL((k_narrow_bwd<T, OUT, IN, kMost, FAST, MIX>), dim3(blocks), dim3(kNarrowThreads), 0, s, a);
 }
 
-template <typename T, bool FAST>
+template <typename T, bool FAST, bool MIX>
 void run_narrow(const NarrowArgs& a, int planes, int blocks, hipStream_t s)
 {
     with_width(a.out, [&](auto out) {
         with_width(a.in, [&](auto in) {
-            run_narrow<T, decltype(out)::value, decltype(in)::value, FAST>(a, planes, blocks, s);
+            run_narrow<T, decltype(out)::value, decltype(in)::value, FAST, MIX>(a, planes, blocks, s);
         });
     });
+}
+
+template <typename T, bool MIX>
+hipError_t run_narrow_bwd(const NarrowArgs& a, bool fast, int planes, int blocks, hipStream_t s)
+{
+    if (blocks > 0) fast ? run_narrow<T, true, MIX>(a, planes, blocks, s) : run_narrow<T, false, MIX>(a, planes, blocks, s);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !(a.dw || a.db)) return e;
+    hipLaunchKernelGGL((k_narrow_join<T, MIX>), dim3((unsigned)div_up(a.out * a.in + a.out, 64), MIX ? a.mix.experts : 1),
+                       dim3(kBlock), 0, s, a, blocks);
+    return hipGetLastError();
+}
+
+template <typename T, bool MIX>
+hipError_t run_narrow_fwd(const GemmArgs& g, bool fast, int blocks, hipStream_t s)
+{
+    with_width((int)g.cols, [&](auto out) {
+        with_width((int)g.len, [&](auto in) {
+            constexpr int OUT = decltype(out)::value, IN = decltype(in)::value;
+            if (fast)
+                hipLaunchKernelGGL((k_narrow_fwd<T, OUT, IN, true, MIX>), dim3(blocks), dim3(kNarrowThreads), 0, s, g);
+            else
+                hipLaunchKernelGGL((k_narrow_fwd<T, OUT, IN, false, MIX>), dim3(blocks), dim3(kNarrowThreads), 0, s, g);
+        });
+    });
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -461,27 +521,13 @@ void run_narrow(const NarrowArgs& a, int planes, int blocks, hipStream_t s)
 template <typename T>
 hipError_t NarrowOps<T>::backward(const NarrowArgs& a, bool fast, int planes, int blocks, hipStream_t s)
 {
-    fast ? run_narrow<T, true>(a, planes, blocks, s) : run_narrow<T, false>(a, planes, blocks, s);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || !(a.dw || a.db)) return e;
-    hipLaunchKernelGGL((k_narrow_join<T>), dim3((unsigned)div_up(a.out * a.in + a.out, 64)), dim3(kBlock), 0, s, a,
-                       blocks);
-    return hipGetLastError();
+    return run_narrow_bwd<T, false>(a, fast, planes, blocks, s);
 }
 
 template <typename T>
 hipError_t NarrowOps<T>::forward(const GemmArgs& g, bool fast, int blocks, hipStream_t s)
 {
-    with_width((int)g.cols, [&](auto out) {
-        with_width((int)g.len, [&](auto in) {
-            constexpr int OUT = decltype(out)::value, IN = decltype(in)::value;
-            if (fast)
-                hipLaunchKernelGGL((k_narrow_fwd<T, OUT, IN, true>), dim3(blocks), dim3(kNarrowThreads), 0, s, g);
-            else
-                hipLaunchKernelGGL((k_narrow_fwd<T, OUT, IN, false>), dim3(blocks), dim3(kNarrowThreads), 0, s, g);
-        });
-    });
-    return hipGetLastError();
+    return run_narrow_fwd<T, false>(g, fast, blocks, s);
 }
 
 }  // namespace gsr

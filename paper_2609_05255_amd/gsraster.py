@@ -102,6 +102,10 @@ class GradTensor(C.Structure):
     _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("type", C.c_int32)]
 
 
+class Experts(C.Structure):
+    _fields_ = [("layer", Linear), ("experts", C.c_int64), ("w_stride", C.c_int64), ("offsets", C.c_void_p)]
+
+
 class RowOrderArrays(C.Structure):
     _fields_ = [("count", C.c_int64), ("groups", C.c_int64), ("order", C.c_void_p), ("sorted", C.c_void_p),
                 ("place", C.c_void_p), ("offsets", C.c_void_p)]
@@ -152,6 +156,9 @@ def lib() -> C.CDLL:
         L.gs_dispatch_bwd.argtypes = [i32, i64, i64, vp, i64, O, vp, i64, vp, i64, vp]
         L.gs_combine_fwd.argtypes = [i32, i64, i64, vp, i64, O, vp, vp, i64, vp, i64, vp]
         L.gs_combine_bwd.argtypes = [i32, i64, i64, vp, i64, vp, i64, O, vp, vp, i64, vp, vp]
+        L.gs_experts_fwd.argtypes = [P(Experts), vp, i64, vp, i64, vp, sz, vp]
+        L.gs_experts_bwd.argtypes = [P(Experts), vp, i64, vp, i64, vp, i64, vp, i64, i64, i32, vp, vp, sz, vp]
+        L.gs_experts_workspace_size.argtypes = [i32, i32, i64, i64, i64, i64, i32, P(sz)]
         L.gs_render_bwd_adam.argtypes = [P(Camera), P(Gaussians), P(Appearance), P(Preprocessed), vp, vp, vp, vp,
                                          vp, P(Grads), P(AdamTensor), C.c_float, C.c_float, i64, vp, sz, vp]
         L.gs_timer_create.argtypes = [P(vp)]
@@ -165,7 +172,8 @@ def lib() -> C.CDLL:
                   "gs_layer_norm_workspace_size", "gs_linear_fwd", "gs_linear_bwd", "gs_linear_workspace_size",
                   "gs_grad_norm", "gs_grad_clip", "gs_grad_workspace_size", "gs_sort_rows", "gs_sort_rows_workspace_size",
                   "gs_embedding_fwd", "gs_embedding_bwd", "gs_embedding_workspace_size", "gs_route_fwd", "gs_route_bwd",
-                  "gs_dispatch_fwd", "gs_dispatch_bwd", "gs_combine_fwd", "gs_combine_bwd", "gs_timer_create", "gs_timer_destroy", "gs_timer_attach", "gs_timer_reset",
+                  "gs_dispatch_fwd", "gs_dispatch_bwd", "gs_combine_fwd", "gs_combine_bwd", "gs_experts_fwd",
+                  "gs_experts_bwd", "gs_experts_workspace_size", "gs_timer_create", "gs_timer_destroy", "gs_timer_attach", "gs_timer_reset",
                   "gs_timer_read"):
             getattr(L, f).restype = C.c_int
         L.gs_last_error.restype = C.c_char_p
@@ -715,6 +723,73 @@ def gs_combine_bwd(dy, ys, order: RowOrder, weight, dys, dweight, stream=None):
     _check(lib().gs_combine_bwd(_type_id(dy), rows, dim, pdy, lddy, ps, lds, C.byref(order.arrays()),
                                 _choices("weight", weight, rows, order), pd, ldd,
                                 _choices("dweight", dweight, rows, order), _stream(stream)))
+
+
+def _stack(name, t, shape, dtype):
+    """Address, row stride and stride between the matrices of an [experts][rows][cols] tensor on the GPU."""
+    if t.shape != shape or t.dtype != dtype or not t.is_cuda:
+        raise ValueError("%s: %s of %s, %s of %s on the GPU expected" % (name, tuple(t.shape), t.dtype, tuple(shape),
+                                                                        dtype))
+    _, rows, cols = shape
+    stride, ld, step = t.stride()
+    if cols > 1 and step != 1:
+        raise ValueError("%s: columns %d elements apart, neighbours expected" % (name, step))
+    return t.data_ptr(), (ld if rows > 1 else cols), stride
+
+
+def _experts(x, offsets, w, bias, act):
+    rows, n_in = _shape("x", x)
+    if w.dim() != 3:
+        raise ValueError("w: [experts][out][in] expected, not %s" % (tuple(w.shape),))
+    experts, n_out, _ = w.shape
+    px, ldx = _matrix("x", x, rows, n_in, x.dtype)
+    pw, ldw, stride = _stack("w", w, (experts, n_out, n_in), x.dtype)
+    pb = None if bias is None else _array("bias", bias, (experts, n_out), torch.float32)
+    po = _array("offsets", offsets, (experts + 1,), torch.int32)
+    return Experts(Linear(_type_id(x), _activation(act), rows, n_in, n_out, px, pw, pb, ldx, ldw), experts, stride, po)
+
+
+def gs_experts_workspace_size(x, w, act: str = "none", dw_type=torch.float32) -> int:
+    """Workspace bytes of gs_experts_fwd and gs_experts_bwd for these shapes; dw_type: the weight gradient's type
+    (float32: enough for one of x's type too; None: for the forward alone)."""
+    rows, n_in = _shape("x", x)
+    out = C.c_size_t(0)
+    _check(lib().gs_experts_workspace_size(_type_id(x), _activation(act), rows, w.shape[0], n_in, w.shape[1],
+                                           -1 if dw_type is None else TYPE_IDS[dw_type], C.byref(out)))
+    return out.value
+
+
+def gs_experts_fwd(x, offsets, w, bias, y, workspace=None, act: str = "none", z=None, stream=None):
+    """y = act(x w[e]^T + bias[e]) for the rows offsets[e] .. offsets[e + 1] - 1 of every expert e; x: [rows][in] sorted
+    by expert, offsets: int32 [experts + 1] (RowOrder.offsets), w: [experts][out][in] of x's type, bias: float32
+    [experts][out] or None; z, if given, receives what the activation takes, for the backward. Rows that are no expert's
+    stay as they are."""
+    _one_device(x, offsets, w, bias, y, workspace, z)
+    p = _experts(x, offsets, w, bias, act)
+    rows, n_out, t = p.layer.rows, p.layer.n_out, x.dtype
+    py, ldy = _matrix("y", y, rows, n_out, t)
+    pz, ldz = (None, 0) if z is None else _matrix("z", z, rows, n_out, t)
+    ws, ws_bytes = _space(workspace)
+    _check(lib().gs_experts_fwd(C.byref(p), py, ldy, pz, ldz, ws, ws_bytes, _stream(stream)))
+
+
+def gs_experts_bwd(dy, x, offsets, w, z, dx, dw, db, workspace, act: str = "none", stream=None):
+    """Backward of gs_experts_fwd: dx of x's type, dw [experts][out][in] float32 or of x's type, db float32
+    [experts][out] (each may be None); z as the forward wrote it (None without an activation)."""
+    _one_device(dy, x, offsets, w, z, dx, dw, db, workspace)
+    p = _experts(x, offsets, w, None, act)
+    rows, n_in, n_out, t = p.layer.rows, p.layer.n_in, p.layer.n_out, x.dtype
+    pdy, lddy = _matrix("dy", dy, rows, n_out, t)
+    pz, ldz = (None, 0) if z is None else _matrix("z", z, rows, n_out, t)
+    pdx, lddx = (None, 0) if dx is None else _matrix("dx", dx, rows, n_in, t)
+    pdw, lddw, stride, dw_type = None, 0, 0, 0
+    if dw is not None:
+        pdw, lddw, stride = _stack("dw", dw, w.shape, torch.float32 if dw.dtype == torch.float32 else t)
+        dw_type = TYPE_IDS[dw.dtype]
+    pdb = None if db is None else _array("db", db, (p.experts, n_out), torch.float32)
+    ws, ws_bytes = _space(workspace)
+    _check(lib().gs_experts_bwd(C.byref(p), pdy, lddy, pz, ldz, pdx, lddx, pdw, lddw, stride, dw_type, pdb, ws, ws_bytes,
+                                _stream(stream)))
 
 
 class Timer:
