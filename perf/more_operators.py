@@ -315,11 +315,12 @@ def _scratch(s, name, size):
     return s[name]
 
 
-def _order(s, count, groups):
-    """The arrays that sorting rows fills, which a program keeps; with the sort's result where that was prepared."""
+def _order(s, count, groups, lookup=False):
+    """The arrays that sorting rows fills, which a program keeps (a lookup's gradient takes the sorted keys, rows on their
+    way back their places); with the sort's result where that was prepared."""
     from paper_2609_05255_amd import gsraster as gs
     if "plan" not in s:
-        s["plan"] = gs.RowOrder(count, groups, device=DEVICE)
+        s["plan"] = gs.RowOrder(count, groups, device=DEVICE, sorted=lookup, place=not lookup)
         if "order" in s:
             s["plan"].order, s["plan"].place, s["plan"].offsets = s["order"], s["place"], s["offsets"]
     return s["plan"]
@@ -333,7 +334,7 @@ def _kernels(s):
         gs.gs_embedding_fwd(s["table"], s["index"], s["scale"], s["y"])
         return s["y"]
     if op == "lookup_bwd":
-        plan = _order(s, rows, case["entries"])
+        plan = _order(s, rows, case["entries"], lookup=True)
         gs.gs_sort_rows(s["index"], plan, _scratch(s, "sort", lambda: gs.gs_sort_rows_workspace_size(plan)))
         gs.gs_embedding_bwd(s["dy"], plan, s["scale"], s["dtable"],
                             _scratch(s, "sums", lambda: gs.gs_embedding_workspace_size(s["dy"])))
