@@ -18,12 +18,15 @@ namespace gsr {
 
 namespace {
 
-// Lanes that share a row of `vecs` vectors: a power of two up to a wave.
+// Lanes that share a row of `vecs` vectors: a power of two up to a wave, from 16 on the one whose last turn leaves the
+// fewest idle (84 vectors: three turns of 32 lanes rather than two of 64).
 int row_lanes(int64_t vecs)
 {
-    int g = 1;
-    while (g < 64 && g < vecs) g <<= 1;
-    return g;
+    if (vecs <= 16) return vecs > 8 ? 16 : vecs > 4 ? 8 : vecs > 2 ? 4 : (int)vecs;
+    int best = 64;
+    for (int g = 32; g >= 16; g >>= 1)
+        if (div_up(vecs, g) * g < div_up(vecs, best) * best) best = g;
+    return best;
 }
 
 template <typename F>
@@ -40,7 +43,7 @@ void with_lanes(int g, F f)
     }
 }
 
-constexpr int64_t kMoveBlocks = 256 * 8;   // workgroups that take rows in turn
+constexpr int64_t kMoveBlocks = 256 * 64;   // workgroups at most; they take rows in turn
 
 int64_t move_blocks(int64_t rows, int g, int fly)
 {
@@ -61,6 +64,13 @@ __device__ __forceinline__ void put_vec(T* p, int64_t left, typename Vec<T>::Pac
     }
 }
 
+// A vector of a row; WHOLE: the row ends with a whole one.
+template <typename T, bool WHOLE>
+__device__ __forceinline__ typename Vec<T>::Packed get_vec(const T* p, int64_t left)
+{
+    return WHOLE ? *reinterpret_cast<const typename Vec<T>::Any*>(p) : load_any(p, left);
+}
+
 // ---- one row to one row -----------------------------------------------------
 
 struct GatherArgs {
@@ -74,53 +84,96 @@ struct GatherArgs {
     float scale;
 };
 
-constexpr int kGatherRows = 4;   // of a group under way together
+constexpr int kGatherRows = 4;   // neighbours, of a group under way together
 
-// LOOKUP: an index outside [0, entries) gives a row of zeros. Otherwise index[p] / k is the row, below *used.
-template <typename T, int G, bool LOOKUP>
+// LOOKUP: an index outside [0, entries) gives a row of zeros. Otherwise index[p] / k is the row, below *used. Where there
+// is no row to read, the first one is, and left out.
+template <typename T, int G, bool LOOKUP, bool WHOLE>
 __global__ __launch_bounds__(kBlock) void k_gather(GatherArgs a)
 {
     constexpr int N = Vec<T>::N, U = kGatherRows, kGroups = kBlock / G;
+    constexpr int kIndexed = G < U ? G : U;   // rows that the lanes of a group look up together
     typedef typename Vec<T>::Packed Packed;
     const int lane = threadIdx.x & (G - 1);
     const int64_t rows = LOOKUP ? a.rows : min((int64_t)*a.used, a.rows);
-    const int64_t step = (int64_t)gridDim.x * kGroups;
-    for (int64_t r0 = (int64_t)blockIdx.x * kGroups + threadIdx.x / G; r0 < rows; r0 += U * step) {
+    const int64_t step = (int64_t)gridDim.x * kGroups * U;
+    for (int64_t r0 = ((int64_t)blockIdx.x * kGroups + threadIdx.x / G) * U; r0 < rows; r0 += step) {
         const T* from[U];
         bool in[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t r = r0 + u * step;
-            const int32_t i = r < rows ? a.index[r] : -1;
-            if (LOOKUP) {
-                in[u] = i >= 0 && i < a.entries;
-                from[u] = (const T*)a.src + (in[u] ? i : 0) * a.lds;
-            } else {
-                in[u] = i >= 0 && i < a.rows;
-                from[u] = (const T*)a.src + (in[u] ? (uint32_t)i / (uint32_t)a.k : 0) * a.lds;
+        for (int q = 0; q < U; q += kIndexed) {
+            const int64_t r = r0 + q + (lane & (kIndexed - 1));
+            int32_t i = r < rows ? a.index[r] : -1;
+            if (LOOKUP)
+                i = i >= 0 && i < a.entries ? i : -1;
+            else
+                i = i >= 0 && i < a.rows ? (int32_t)((uint32_t)i / (uint32_t)a.k) : -1;
+#pragma unroll
+            for (int u = 0; u < kIndexed; ++u) {
+                const int32_t iu = G == 1 ? i : __shfl(i, u, kIndexed);
+                in[q + u] = iu >= 0;
+                from[q + u] = (const T*)a.src + (int64_t)(iu >= 0 ? iu : 0) * a.lds;
             }
         }
         for (int64_t c = (int64_t)lane * N; c < a.dim; c += G * N) {
             const int64_t left = a.dim - c;
             Packed v[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) v[u] = load_any(from[u] + c, in[u] ? left : 0);
+            for (int u = 0; u < U; ++u) v[u] = get_vec<T, WHOLE>(from[u] + c, left);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int64_t r = r0 + u * step;
-                if (r >= rows) break;
-                T* to = (T*)a.dst + r * a.ldd + c;
+                if (r0 + u >= rows) break;
+                T* to = (T*)a.dst + (r0 + u) * a.ldd + c;
                 if (LOOKUP) {
                     float f[N];
 #pragma unroll
                     for (int e = 0; e < N; ++e) f[e] = in[u] ? (float)v[u][e] * a.scale : 0.f;
-                    store_vec(to, left, f);
-                } else {
-                    put_vec(to, left, v[u]);
+                    store_vec(to, WHOLE ? N : left, f);
+                } else if (in[u]) {
+                    put_vec(to, WHOLE ? N : left, v[u]);
                 }
             }
         }
     }
+}
+
+// ---- one row to several -----------------------------------------------------
+
+struct ScatterArgs {
+    const void* src;
+    void* dst;
+    int64_t lds, ldd, rows, dim;
+    const int32_t* place;
+    const int32_t* used;
+    int32_t k;
+};
+
+// Rows copied to the places of their choices: x is read once, in order, where the gather reads it once for each choice.
+// 1,000,000 x 128 in binary16, two choices, 16 experts: see the dispatch's figures above the launches.
+template <typename T, int G, bool WHOLE>
+__global__ __launch_bounds__(kBlock) void k_scatter(ScatterArgs a)
+{
+    constexpr int N = Vec<T>::N, U = kGatherRows, kGroups = kBlock / G;
+    typedef typename Vec<T>::Packed Packed;
+    const int lane = threadIdx.x & (G - 1);
+    const int64_t used = min((int64_t)*a.used, a.rows * a.k);
+    const int64_t step = (int64_t)gridDim.x * kGroups * U;
+    for (int64_t r0 = ((int64_t)blockIdx.x * kGroups + threadIdx.x / G) * U; r0 < a.rows; r0 += step)
+        for (int64_t c = (int64_t)lane * N; c < a.dim; c += G * N) {
+            const int64_t left = a.dim - c;
+            Packed v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t r = r0 + u < a.rows ? r0 + u : a.rows - 1;
+                v[u] = get_vec<T, WHOLE>((const T*)a.src + r * a.lds + c, left);
+            }
+            for (int j = 0; j < a.k; ++j)
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int32_t p = r0 + u < a.rows ? a.place[(r0 + u) * a.k + j] : -1;
+                    if (p >= 0 && p < used) put_vec((T*)a.dst + p * a.ldd + c, WHOLE ? N : left, v[u]);
+                }
+        }
 }
 
 // ---- the choices of a row added up ------------------------------------------
@@ -138,7 +191,8 @@ struct SumArgs {
 
 constexpr int kSumChoices = 4;   // under way together
 
-template <typename T, int G>
+// (a choice of no expert loads the first row, which is left out)
+template <typename T, int G, bool WHOLE>
 __global__ __launch_bounds__(kBlock) void k_sum_choices(SumArgs a)
 {
     constexpr int N = Vec<T>::N, U = kSumChoices, kGroups = kBlock / G;
@@ -147,30 +201,34 @@ __global__ __launch_bounds__(kBlock) void k_sum_choices(SumArgs a)
     const int64_t used = min((int64_t)*a.used, a.rows * a.k);
     const int64_t step = (int64_t)gridDim.x * kGroups;
     for (int64_t r = (int64_t)blockIdx.x * kGroups + threadIdx.x / G; r < a.rows; r += step) {
-        const int32_t* place = a.place + r * a.k;
-        const float* weight = a.weight ? a.weight + r * a.k : nullptr;
+        const int64_t at = r * a.k;
         for (int64_t c = (int64_t)lane * N; c < a.dim; c += G * N) {
             const int64_t left = a.dim - c;
             float sum[N] = {};
-            if (a.add) load_vec((const T*)a.add + r * a.ldadd + c, left, sum);
+            Packed add = {};
+            if (a.add) add = get_vec<T, WHOLE>((const T*)a.add + r * a.ldadd + c, left);
             for (int j0 = 0; j0 < a.k; j0 += U) {
                 Packed v[U];
+                float w[U];
                 bool in[U];
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int32_t p = j0 + u < a.k ? place[j0 + u] : -1;
-                    in[u] = p >= 0 && p < used;
-                    v[u] = load_any((const T*)a.src + (in[u] ? p : 0) * a.lds + c, in[u] ? left : 0);
-                }
+                for (int u = 0; u < U; ++u)
+                    if (j0 + u < a.k) {
+                        const int32_t p = a.place[at + j0 + u];
+                        w[u] = a.weight ? a.weight[at + j0 + u] : 1.f;
+                        in[u] = p >= 0 && p < used;
+                        v[u] = get_vec<T, WHOLE>((const T*)a.src + (in[u] ? p : 0) * a.lds + c, left);
+                    }
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    if (!in[u]) continue;
-                    const float w = weight ? weight[j0 + u] : 1.f;
+                for (int u = 0; u < U; ++u)
+                    if (j0 + u < a.k && in[u])
 #pragma unroll
-                    for (int e = 0; e < N; ++e) sum[e] = fmaf(w, (float)v[u][e], sum[e]);
-                }
+                        for (int e = 0; e < N; ++e) sum[e] = fmaf(w[u], (float)v[u][e], sum[e]);
             }
-            store_vec((T*)a.dst + r * a.ldd + c, left, sum);
+            if (a.add)
+#pragma unroll
+                for (int e = 0; e < N; ++e) sum[e] += (float)add[e];
+            store_vec((T*)a.dst + r * a.ldd + c, WHOLE ? N : left, sum);
         }
     }
 }
@@ -188,7 +246,7 @@ struct CombineBwdArgs {
     int32_t k;
 };
 
-template <typename T, int G>
+template <typename T, int G, bool WHOLE>
 __global__ __launch_bounds__(kBlock) void k_combine_bwd(CombineBwdArgs a)
 {
     constexpr int N = Vec<T>::N, U = kSumChoices, kGroups = kBlock / G;
@@ -199,39 +257,41 @@ __global__ __launch_bounds__(kBlock) void k_combine_bwd(CombineBwdArgs a)
     for (int64_t r = (int64_t)blockIdx.x * kGroups + threadIdx.x / G; r < a.rows; r += step) {
         const int64_t at = r * a.k;
         for (int j0 = 0; j0 < a.k; j0 += U) {
-            int32_t p[U];
+            int64_t p[U];
             float w[U], dot[U] = {};
             bool in[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                p[u] = j0 + u < a.k ? a.place[at + j0 + u] : -1;
-                in[u] = p[u] >= 0 && p[u] < used;
-                p[u] = in[u] ? p[u] : 0;
-                w[u] = in[u] ? a.weight[at + j0 + u] : 0.f;
-            }
+            for (int u = 0; u < U; ++u)
+                if (j0 + u < a.k) {
+                    const int32_t to = a.place[at + j0 + u];
+                    w[u] = a.weight[at + j0 + u];
+                    in[u] = to >= 0 && to < used;
+                    p[u] = in[u] ? to : 0;
+                }
             for (int64_t c = (int64_t)lane * N; c < a.dim; c += G * N) {
                 const int64_t left = a.dim - c;
-                float g[N];
-                load_vec((const T*)a.dy + r * a.lddy + c, left, g);
+                const Packed g = get_vec<T, WHOLE>((const T*)a.dy + r * a.lddy + c, left);
                 Packed v[U];
 #pragma unroll
-                for (int u = 0; u < U; ++u) v[u] = load_any((const T*)a.ys + p[u] * a.ldys + c, in[u] ? left : 0);
+                for (int u = 0; u < U; ++u)
+                    if (j0 + u < a.k) v[u] = get_vec<T, WHOLE>((const T*)a.ys + p[u] * a.ldys + c, left);
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    if (!in[u]) continue;
+                    if (j0 + u >= a.k || !in[u]) continue;
                     float o[N];
 #pragma unroll
                     for (int e = 0; e < N; ++e) {
-                        dot[u] = fmaf(g[e], (float)v[u][e], dot[u]);
-                        o[e] = g[e] * w[u];
+                        dot[u] = fmaf((float)g[e], (float)v[u][e], dot[u]);
+                        o[e] = (float)g[e] * w[u];
                     }
-                    store_vec((T*)a.dys + p[u] * a.lddys + c, left, o);
+                    store_vec((T*)a.dys + p[u] * a.lddys + c, WHOLE ? N : left, o);
                 }
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
+                if (j0 + u >= a.k) continue;
                 const float d = lane_sum<G>(dot[u]);
-                if (lane == 0 && j0 + u < a.k) a.dweight[at + j0 + u] = d;
+                if (lane == 0) a.dweight[at + j0 + u] = d;
             }
         }
     }
@@ -267,10 +327,28 @@ __device__ __forceinline__ void store_entry(const EntriesArgs& a, int64_t v, int
         ((T*)a.dtable)[v * a.lddt + c] = (T)(value * a.scale);
 }
 
-template <typename T, int G>
+// N values, of which the first `left` are the row's.
+template <typename T, int N>
+__device__ __forceinline__ void store_entries(const EntriesArgs& a, int64_t v, int64_t c, int64_t left, const float* values)
+{
+    float o[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) o[e] = values[e] * a.scale;
+    if (a.out_f32) {
+        float* to = (float*)a.dtable + v * a.lddt + c;
+#pragma unroll
+        for (int e = 0; e < N; e += 4) store_vec(to + e, left - e, o + e);
+    } else {
+        store_vec((T*)a.dtable + v * a.lddt + c, left, o);
+    }
+}
+
+// WHOLE: rows are whole vectors. Lanes behind a row's end load its first vector and store nothing.
+template <typename T, int G, bool WHOLE>
 __global__ __launch_bounds__(kBlock) void k_sum_entries(EntriesArgs a)
 {
     constexpr int N = Vec<T>::N, U = kEntryRows, kGroups = kBlock / G, kCols = G * N;
+    constexpr int kIndexed = G < U ? G : U;   // positions that the lanes of a group look up together
     typedef typename Vec<T>::Packed Packed;
     // a group's sums of its first entry, and of its last where that is another one
     __shared__ float sums[kGroups][2][kCols];
@@ -281,21 +359,34 @@ __global__ __launch_bounds__(kBlock) void k_sum_entries(EntriesArgs a)
     const int64_t w0 = (int64_t)blockIdx.x * kGroups * a.per;
     const int64_t w1 = w0 + kGroups * a.per < used ? w0 + kGroups * a.per : used;
     const int64_t p0 = w0 + (int64_t)group * a.per, p1 = p0 + a.per < w1 ? p0 + a.per : w1;
+    const T* dy = (const T*)a.dy + (left > 0 ? c : 0);
     int32_t first = -1, key = -1;
     float sum[N] = {};
     for (int64_t p = p0; p < p1; p += U) {
         Packed v[U];
         int32_t k[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const bool in = p + u < p1;
-            const uint32_t i = in ? (uint32_t)a.order[p + u] : 0;
-            k[u] = in && i < a.count ? a.sorted[p + u] : -1;
-            v[u] = load_any((const T*)a.dy + (int64_t)i * a.lddy + c, k[u] >= 0 ? left : 0);
+        for (int q = 0; q < U; q += kIndexed) {
+            // (positions behind the last one: its row again, and no entry)
+            const int64_t at = p + q + (lane & (kIndexed - 1)), in = at < p1 ? at : p1 - 1;
+            uint32_t i = (uint32_t)a.order[in];
+            int32_t e = a.sorted[in];
+            if (at >= p1 || i >= a.count || (uint32_t)e >= a.entries) e = -1;
+            i = i < a.count ? i : 0;
+#pragma unroll
+            for (int u = 0; u < kIndexed; ++u) {
+                const uint32_t iu = G == 1 ? i : (uint32_t)__shfl((int)i, u, kIndexed);
+                k[q + u] = G == 1 ? e : __shfl(e, u, kIndexed);
+                const T* row = dy + (int64_t)iu * a.lddy;
+                if (WHOLE)
+                    v[q + u] = *reinterpret_cast<const typename Vec<T>::Any*>(row);
+                else
+                    v[q + u] = load_any(row, left);
+            }
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (k[u] < 0 || k[u] >= a.entries) continue;
+            if (k[u] < 0) continue;
             if (k[u] != key) {
                 if (key == first) {   // (nothing yet, or the first entry)
                     if (key < 0)
@@ -303,10 +394,8 @@ __global__ __launch_bounds__(kBlock) void k_sum_entries(EntriesArgs a)
                     else
 #pragma unroll
                         for (int e = 0; e < N; ++e) sums[group][0][lane * N + e] = sum[e];
-                } else {
-#pragma unroll
-                    for (int e = 0; e < N; ++e)
-                        if (e < left) store_entry<T>(a, key, c + e, sum[e]);
+                } else if (left > 0) {
+                    store_entries<T, N>(a, key, c, left, sum);
                 }
                 key = k[u];
 #pragma unroll
@@ -366,20 +455,25 @@ constexpr int kJoinCols = 16, kJoinSlices = kBlock / kJoinCols;
 constexpr int64_t kZeroBlocks = 4096;
 
 template <typename T>
-__global__ __launch_bounds__(kBlock) void k_join_entries(EntriesArgs a, int64_t parts, int64_t span)
+__global__ __launch_bounds__(kBlock) void k_join_entries(EntriesArgs a, int64_t parts, int64_t span, int lanes)
 {
     const int64_t first_col = (int64_t)blockIdx.y * kJoinCols * 16;
     const int64_t end_col = min(a.dim, first_col + kJoinCols * 16);
     if (blockIdx.x >= parts) {
-        // a wave looks at 64 entries and clears the empty ones' columns
-        const int lane = threadIdx.x & 63;
+        // a wave looks at 64 entries, and each group of a row's lanes clears the empty ones among its share of them
+        if (blockIdx.y > 0) return;
+        a.scale = 1.f;
+        constexpr int N = Vec<T>::N;
+        const int lane = threadIdx.x & 63, groups = 64 / lanes, group = lane / lanes, part = lane % lanes;
+        const float zero[N] = {};
         const int64_t step = (gridDim.x - parts) * kBlock;
         for (int64_t v0 = (blockIdx.x - parts) * kBlock + (threadIdx.x & ~63); v0 < a.entries; v0 += step) {
             const int64_t v = v0 + lane;
-            uint64_t empty = __ballot(v < a.entries && a.offsets[v] == a.offsets[v + 1]);
-            for (; empty; empty &= empty - 1)
-                for (int64_t c = first_col + lane; c < end_col; c += 64)
-                    store_entry<T>(a, v0 + __builtin_ctzll(empty), c, 0.f);
+            const uint64_t empty = __ballot(v < a.entries && a.offsets[v] == a.offsets[v + 1]);
+            for (int k = group; k < 64; k += groups)
+                if (empty >> k & 1)
+                    for (int64_t c = (int64_t)part * N; c < a.dim; c += lanes * N)
+                        store_entries<T, N>(a, v0 + k, c, a.dim - c, zero);
         }
         return;
     }
@@ -412,6 +506,8 @@ __global__ __launch_bounds__(kBlock) void k_join_entries(EntriesArgs a, int64_t 
     }
 }
 
+constexpr int64_t kEntryBlocks = 256 * 8;   // workgroups of k_sum_entries, about
+
 struct EntriesPlan {
     int lanes;
     int64_t per, span, parts;   // positions of a group and of a workgroup, workgroups
@@ -421,48 +517,72 @@ EntriesPlan entries_plan(int type, int64_t count, int64_t dim)
 {
     EntriesPlan p;
     p.lanes = row_lanes(div_up(dim, type == GS_F32 ? 4 : 8));
-    const int64_t groups = kBlock / p.lanes, all = kMoveBlocks * groups;
+    const int64_t groups = kBlock / p.lanes, all = kEntryBlocks * groups;
     p.per = std::max<int64_t>(kEntryRows, div_up(div_up(count, all), kEntryRows) * kEntryRows);
     p.span = p.per * groups;
     p.parts = std::max<int64_t>(1, div_up(count, p.span));
     return p;
 }
 
-template <typename T>
-hipError_t gather(bool lookup, const GatherArgs& a, hipStream_t s)
+// Calls f with the lanes of a row and whether it ends with a whole vector.
+template <typename T, typename F>
+hipError_t with_row(int64_t dim, F f)
 {
-    const int g = row_lanes(div_up(a.dim, Vec<T>::N));
-    const dim3 grid((unsigned)move_blocks(a.rows, g, kGatherRows));
+    const int g = row_lanes(div_up(dim, Vec<T>::N));
     with_lanes(g, [&](auto lanes) {
-        constexpr int G = decltype(lanes)::value;
-        if (lookup)
-            hipLaunchKernelGGL((k_gather<T, G, true>), grid, dim3(kBlock), 0, s, a);
+        if (dim % Vec<T>::N == 0)
+            f(lanes, std::true_type());
         else
-            hipLaunchKernelGGL((k_gather<T, G, false>), grid, dim3(kBlock), 0, s, a);
+            f(lanes, std::false_type());
     });
     return hipGetLastError();
+}
+
+template <typename T>
+hipError_t lookup(const GatherArgs& a, hipStream_t s)
+{
+    return with_row<T>(a.dim, [&](auto lanes, auto whole) {
+        constexpr int G = decltype(lanes)::value;
+        hipLaunchKernelGGL((k_gather<T, G, true, decltype(whole)::value>),
+                           dim3((unsigned)move_blocks(a.rows, G, kGatherRows)), dim3(kBlock), 0, s, a);
+    });
+}
+
+template <typename T>
+hipError_t dispatch(const GatherArgs& a, const int32_t* place, hipStream_t s)
+{
+    return with_row<T>(a.dim, [&](auto lanes, auto whole) {
+        constexpr int G = decltype(lanes)::value;
+        constexpr bool WHOLE = decltype(whole)::value;
+        if (place) {
+            const ScatterArgs b = {a.src, a.dst, a.lds, a.ldd, a.rows / a.k, a.dim, place, a.used, a.k};
+            hipLaunchKernelGGL((k_scatter<T, G, WHOLE>), dim3((unsigned)move_blocks(b.rows, G, kGatherRows)), dim3(kBlock),
+                               0, s, b);
+        } else {
+            hipLaunchKernelGGL((k_gather<T, G, false, WHOLE>), dim3((unsigned)move_blocks(a.rows, G, kGatherRows)),
+                               dim3(kBlock), 0, s, a);
+        }
+    });
 }
 
 template <typename T>
 hipError_t sum_choices(const SumArgs& a, hipStream_t s)
 {
-    const int g = row_lanes(div_up(a.dim, Vec<T>::N));
-    with_lanes(g, [&](auto lanes) {
-        hipLaunchKernelGGL((k_sum_choices<T, decltype(lanes)::value>), dim3((unsigned)move_blocks(a.rows, g, 1)),
+    return with_row<T>(a.dim, [&](auto lanes, auto whole) {
+        constexpr int G = decltype(lanes)::value;
+        hipLaunchKernelGGL((k_sum_choices<T, G, decltype(whole)::value>), dim3((unsigned)move_blocks(a.rows, G, 1)),
                            dim3(kBlock), 0, s, a);
     });
-    return hipGetLastError();
 }
 
 template <typename T>
 hipError_t combine_bwd(const CombineBwdArgs& a, hipStream_t s)
 {
-    const int g = row_lanes(div_up(a.dim, Vec<T>::N));
-    with_lanes(g, [&](auto lanes) {
-        hipLaunchKernelGGL((k_combine_bwd<T, decltype(lanes)::value>), dim3((unsigned)move_blocks(a.rows, g, 1)),
+    return with_row<T>(a.dim, [&](auto lanes, auto whole) {
+        constexpr int G = decltype(lanes)::value;
+        hipLaunchKernelGGL((k_combine_bwd<T, G, decltype(whole)::value>), dim3((unsigned)move_blocks(a.rows, G, 1)),
                            dim3(kBlock), 0, s, a);
     });
-    return hipGetLastError();
 }
 
 template <typename T>
@@ -475,8 +595,11 @@ hipError_t embedding_bwd(int type, const EntriesArgs& args, hipStream_t s)
     if (a.count > 0) {
         with_lanes(p.lanes, [&](auto lanes) {
             constexpr int G = decltype(lanes)::value;
-            hipLaunchKernelGGL((k_sum_entries<T, G>), dim3((unsigned)p.parts, (unsigned)div_up(a.dim, G * Vec<T>::N)),
-                               dim3(kBlock), 0, s, a);
+            const dim3 grid((unsigned)p.parts, (unsigned)div_up(a.dim, G * Vec<T>::N));
+            if (a.dim % Vec<T>::N == 0)
+                hipLaunchKernelGGL((k_sum_entries<T, G, true>), grid, dim3(kBlock), 0, s, a);
+            else
+                hipLaunchKernelGGL((k_sum_entries<T, G, false>), grid, dim3(kBlock), 0, s, a);
         });
         e = hipGetLastError();
     }
@@ -484,7 +607,7 @@ hipError_t embedding_bwd(int type, const EntriesArgs& args, hipStream_t s)
     const int64_t parts = a.count > 0 ? p.parts : 0;
     hipLaunchKernelGGL((k_join_entries<T>), dim3((unsigned)(parts + std::min(div_up(a.entries, kBlock), kZeroBlocks)),
                                                  (unsigned)div_up(a.dim, kJoinCols * 16)),
-                       dim3(kBlock), 0, s, a, parts, p.span);
+                       dim3(kBlock), 0, s, a, parts, p.span, p.lanes);
     return hipGetLastError();
 }
 
@@ -494,18 +617,18 @@ hipError_t launch_embedding_fwd(int type, const void* table, int64_t ldt, int64_
                                 float scale, int64_t rows, int64_t dim, void* y, int64_t ldy, hipStream_t s)
 {
     const GatherArgs a = {table, y, ldt, ldy, rows, dim, index, nullptr, entries, 1, scale};
-    if (type == GS_F16) return gather<f16>(true, a, s);
-    if (type == GS_BF16) return gather<bf16>(true, a, s);
-    return gather<float>(true, a, s);
+    if (type == GS_F16) return lookup<f16>(a, s);
+    if (type == GS_BF16) return lookup<bf16>(a, s);
+    return lookup<float>(a, s);
 }
 
 hipError_t launch_dispatch_fwd(int type, const void* x, int64_t ldx, const gs_row_order& o, int k, int64_t dim, void* xs,
                                int64_t ldxs, hipStream_t s)
 {
     const GatherArgs a = {x, xs, ldx, ldxs, o.count, dim, o.order, o.offsets + o.groups, 0, k, 1.f};
-    if (type == GS_F16) return gather<f16>(false, a, s);
-    if (type == GS_BF16) return gather<bf16>(false, a, s);
-    return gather<float>(false, a, s);
+    if (type == GS_F16) return dispatch<f16>(a, o.place, s);
+    if (type == GS_BF16) return dispatch<bf16>(a, o.place, s);
+    return dispatch<float>(a, o.place, s);
 }
 
 hipError_t launch_sum_choices(int type, const void* src, int64_t lds, const gs_row_order& o, const float* weight,

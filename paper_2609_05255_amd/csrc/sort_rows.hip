@@ -5,11 +5,11 @@
 //   sorted[p] = the key of order[p], place[order[p]] = p (-1: no group),
 //   offsets[g] = number of positions with a key below g
 //
-// A least-significant-digit radix sort of up to 8 bits a pass over keys in [0, groups] (groups: none). One pass is
-// k_keys_count (digit counts of each workgroup's keys, and their sums over groups of workgroups) and k_keys_move (each
-// workgroup adds up the counts before its own, ranks its keys by ballots, reorders them by digit in LDS and writes each
-// digit's run). Where one pass is enough the offsets are its digits' totals; otherwise k_offsets searches the sorted
-// keys. Up to kSmallCount keys one workgroup sorts in LDS, in one launch.
+// A least-significant-digit radix sort of up to 9 bits a pass over keys in [0, groups] (groups: none). One pass is
+// k_keys_count (digit counts of each workgroup's keys, and with many workgroups their sums over groups of these) and
+// k_keys_move (each workgroup adds up the counts before its own, ranks its keys by ballots, reorders them by digit in LDS
+// and writes each digit's run). Where one pass is enough the offsets are its digits' totals; otherwise k_offsets searches
+// the sorted keys. Up to kSmallCount keys one workgroup sorts in LDS, in one launch.
 #include "gs_internal.h"
 #include "wave.h"
 
@@ -18,10 +18,13 @@ namespace gsr {
 namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
-constexpr int kDigits = 256;
-constexpr int kItems = 4, kKeysTile = kThreads * kItems;   // keys of a workgroup
+constexpr int kMostBits = 9;             // of a digit
+constexpr int kSmallBits = 9;            // of a digit in LDS
 constexpr int kSmallCount = 8192;
 constexpr int kSmallGroups = 16384;      // whose offsets the one workgroup writes as well
+constexpr int kFewBlocks = 64;           // workgroups whose counts the others add up one by one
+// Keys of a thread: 4, or 6 where that many workgroups are more than the compute units hold at once (two each).
+constexpr int64_t kFewItems = 512 * kThreads * 4;
 
 __device__ __forceinline__ uint32_t key_of(const int32_t* group_of, int64_t i, uint32_t groups)
 {
@@ -55,8 +58,8 @@ struct KeysPass {
     int64_t count;
     uint32_t groups;
     int32_t shift;
-    uint32_t* hist;              // [workgroups][kDigits]
-    uint32_t* sup;               // [workgroups / group][kDigits], cleared beforehand
+    uint32_t* hist;              // [workgroups][digits]
+    uint32_t* sup;               // [workgroups / group][digits], cleared beforehand; NULL: few workgroups
     int32_t group;
     uint32_t* keys_out;          // or NULL
     uint32_t* vals_out;
@@ -69,131 +72,181 @@ __device__ __forceinline__ uint32_t pass_key(const KeysPass& a, int64_t i)
     return a.group_of ? key_of(a.group_of, i, a.groups) : a.keys_in[i];
 }
 
+template <int BITS, int ITEMS>
 __global__ __launch_bounds__(kThreads) void k_keys_count(KeysPass a)
 {
+    constexpr int R = 1 << BITS;
     // 16 copies of the counts, so that few lanes of an instruction meet on the counter of a frequent digit
-    __shared__ uint32_t h[16][kDigits];
-    for (int k = threadIdx.x; k < 16 * kDigits; k += kThreads) (&h[0][0])[k] = 0;
-    __syncthreads();
+    __shared__ uint32_t h[16][R];
+    for (int k = threadIdx.x; k < 16 * R; k += kThreads) (&h[0][0])[k] = 0;
     const int copy = ((threadIdx.x >> 6) & 3) * 4 + (threadIdx.x & 3);
-    const int64_t base = (int64_t)blockIdx.x * kKeysTile;
-    uint32_t k[kItems];
+    const int64_t base = (int64_t)blockIdx.x * (kThreads * ITEMS);
+    uint32_t k[ITEMS];
 #pragma unroll
-    for (int r = 0; r < kItems; ++r) {
+    for (int r = 0; r < ITEMS; ++r) {
         const int64_t i = base + r * kThreads + threadIdx.x;
         k[r] = i < a.count ? pass_key(a, i) : 0;
     }
-#pragma unroll
-    for (int r = 0; r < kItems; ++r)
-        if (base + r * kThreads + threadIdx.x < a.count) atomicAdd(&h[copy][(k[r] >> a.shift) & (kDigits - 1)], 1u);
     __syncthreads();
-    if (threadIdx.x >= kDigits) return;
+#pragma unroll
+    for (int r = 0; r < ITEMS; ++r)
+        if (base + r * kThreads + threadIdx.x < a.count) atomicAdd(&h[copy][(k[r] >> a.shift) & (R - 1)], 1u);
+    __syncthreads();
+    if (threadIdx.x >= R) return;
     uint32_t c = 0;
 #pragma unroll
     for (int w = 0; w < 16; ++w) c += h[w][threadIdx.x];
-    a.hist[(int64_t)blockIdx.x * kDigits + threadIdx.x] = c;
-    if (c) atomicAdd(&a.sup[(int64_t)(blockIdx.x / a.group) * kDigits + threadIdx.x], c);
+    a.hist[(int64_t)blockIdx.x * R + threadIdx.x] = c;
+    if (a.sup && c) atomicAdd(&a.sup[(int64_t)(blockIdx.x / a.group) * R + threadIdx.x], c);
 }
 
 // Ranks a wave's slice of ITEMS * 64 keys by digit: rank[k] = keys of the same digit before the lane's k-th one in the
-// slice; counts[digit] of the wave (cleared beforehand) ends up as their number.
-template <int ITEMS>
-__device__ __forceinline__ void rank_slice(const uint32_t (&digit)[ITEMS], const bool (&valid)[ITEMS],
-                                           uint32_t* counts, uint32_t (&rank)[ITEMS])
+// slice, the lane's k-th being key 64 k of which `left` there are; counts[digit] of the wave (cleared beforehand) ends up
+// as their number.
+template <int BITS, int ITEMS>
+__device__ __forceinline__ void rank_slice(const uint32_t (&key)[ITEMS], int shift, int left, uint16_t* counts,
+                                           uint32_t (&rank)[ITEMS])
 {
 #pragma unroll
     for (int k = 0; k < ITEMS; ++k) {
-        const uint64_t same = match_digit<8>(digit[k], valid[k]);
+        const bool valid = k * 64 < left;
+        const uint32_t digit = (key[k] >> shift) & ((1 << BITS) - 1);
+        const uint64_t same = match_digit<BITS>(digit, valid);
         const uint32_t below = __popcll(same & lanemask_lt());
         uint32_t base = 0;
-        if (valid[k]) base = counts[digit[k]];
+        if (valid) base = counts[digit];
         rank[k] = base + below;
         // (LDS keeps a wave's order: all its lanes have read before the first lane of each digit writes)
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if (valid[k] && below == 0) counts[digit[k]] = base + (uint32_t)__popcll(same);
+        if (valid && below == 0) counts[digit] = (uint16_t)(base + (uint32_t)__popcll(same));
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 }
 
-__global__ __launch_bounds__(kThreads) void k_keys_move(KeysPass a)
+// Sums over rows [0, rows) of R digits, of all and of those before `mine`: four digits of a thread and every slice-th row,
+// added up within a wave. sums: [sum_slices(R)][R] each.
+constexpr int sum_slices(int digits) { return digits >= 256 ? kThreads * 4 / digits : kWaves; }
+
+template <int R>
+__device__ __forceinline__ void sum_rows(const uint32_t* table, int64_t rows, int64_t mine, uint32_t* total,
+                                         uint32_t* before)
 {
-    __shared__ uint32_t counts[kWaves][kDigits];   // of each wave, then the first place of its keys of each digit
-    __shared__ uint32_t start[kDigits];            // global place of a digit's first key, less its place in the workgroup
-    __shared__ uint32_t buf_k[kKeysTile], buf_v[kKeysTile];
-    __shared__ uint32_t sums[2][4][kDigits], lds[kWaves];
-    const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
-    const int64_t base = (int64_t)blockIdx.x * kKeysTile;
-    const int n = (int)(a.count - base < kKeysTile ? a.count - base : kKeysTile);
-    const int at0 = wave * kItems * 64 + lane;
-    uint32_t key[kItems], digit[kItems], val[kItems], rank[kItems];
-    bool valid[kItems];
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    constexpr int kQuads = R / 4, kSlices = kThreads / kQuads, kFly = 4;
+    const int quad = threadIdx.x % kQuads, slice = threadIdx.x / kQuads;
+    u32x4 t = {0, 0, 0, 0}, b = {0, 0, 0, 0};
+    for (int64_t r = slice; r < rows; r += kSlices * kFly) {
+        u32x4 v[kFly];
 #pragma unroll
-    for (int k = 0; k < kItems; ++k) {
-        const int i = at0 + k * 64;
-        valid[k] = i < n;
-        key[k] = valid[k] ? pass_key(a, base + i) : 0;
-        val[k] = a.vals_in && valid[k] ? a.vals_in[base + i] : (uint32_t)(base + i);
-        digit[k] = (key[k] >> a.shift) & (kDigits - 1);
-    }
-    for (int k = t; k < kWaves * kDigits; k += kThreads) (&counts[0][0])[k] = 0;
-    {   // the digits' totals, and those before this workgroup: four threads a digit
-        const int d = t & (kDigits - 1), q = t >> 8;
-        const int64_t mine = blockIdx.x / a.group, groups = (gridDim.x + a.group - 1) / a.group;
-        uint32_t total = 0, before = 0;
-        for (int64_t g = q; g < groups; g += 4) {
-            const uint32_t v = a.sup[g * kDigits + d];
-            total += v;
-            before += g < mine ? v : 0;
+        for (int u = 0; u < kFly; ++u) {
+            const int64_t at = r + u * kSlices;
+            v[u] = at < rows ? *reinterpret_cast<const u32x4*>(table + at * R + quad * 4) : u32x4{0, 0, 0, 0};
         }
-        for (int64_t b = mine * a.group + q; b < blockIdx.x; b += 4) before += a.hist[b * kDigits + d];
-        sums[0][q][d] = total;
-        sums[1][q][d] = before;
+#pragma unroll
+        for (int u = 0; u < kFly; ++u) {
+            t += v[u];
+            if (r + u * kSlices < mine) b += v[u];
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+#pragma unroll
+        for (int d = kQuads; d < 64; d <<= 1) {
+            if (total) t[e] += (uint32_t)__shfl_xor((int)t[e], d, 64);
+            b[e] += (uint32_t)__shfl_xor((int)b[e], d, 64);
+        }
+        const int at = kQuads < 64 ? (int)(threadIdx.x >> 6) : slice;
+        if (total) total[at * R + quad * 4 + e] = t[e];
+        before[at * R + quad * 4 + e] = b[e];
+    }
+}
+
+// (two workgroups on a compute unit: 64 registers)
+template <int BITS, int ITEMS>
+__global__ __launch_bounds__(kThreads, 8) void k_keys_move(KeysPass a)
+{
+    constexpr int R = 1 << BITS, kTile = kThreads * ITEMS, kSums = sum_slices(R) * R;
+    static_assert(ITEMS * 64 < 65536 && kTile < 65536, "counts of 16 bits");
+    __shared__ uint16_t counts[kWaves][R];         // of each wave, then the first place of its keys of each digit
+    __shared__ uint32_t start[R];                  // global place of a digit's first key, less its place in the workgroup
+    // the rows' sums (up to three tables), then the keys in their order, then the values
+    __shared__ __attribute__((aligned(16))) uint32_t buf[kTile > 3 * kSums ? kTile : 3 * kSums];
+    __shared__ uint32_t lds[kWaves];
+    const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
+    const int64_t base = (int64_t)blockIdx.x * kTile;
+    const int n = (int)(a.count - base < kTile ? a.count - base : kTile);
+    const int at0 = wave * ITEMS * 64 + lane;
+    uint32_t key[ITEMS], rank[ITEMS];
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) key[k] = at0 + k * 64 < n ? pass_key(a, base + at0 + k * 64) : 0;
+    for (int k = t; k < kWaves * R; k += kThreads) (&counts[0][0])[k] = 0;
+    uint32_t *totals = buf, *before0 = buf + kSums, *before1 = before0 + kSums;
+    if (a.sup) {
+        const int64_t mine = blockIdx.x / a.group;
+        sum_rows<R>(a.sup, (gridDim.x + a.group - 1) / a.group, mine, totals, before0);
+        const int64_t left = blockIdx.x - mine * a.group;
+        sum_rows<R>(a.hist + mine * a.group * R, left, left, nullptr, before1);
+    } else {
+        sum_rows<R>(a.hist, gridDim.x, blockIdx.x, totals, before0);
     }
     __syncthreads();
-    rank_slice<kItems>(digit, valid, counts[wave], rank);
+    rank_slice<BITS, ITEMS>(key, a.shift, n - at0, counts[wave], rank);
     uint32_t total = 0, before = 0, here = 0;
     __syncthreads();
-    if (t < kDigits) {
+    if (t < R) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            total += sums[0][q][t];
-            before += sums[1][q][t];
+        for (int q = 0; q < sum_slices(R); ++q) {
+            total += totals[q * R + t];
+            before += before0[q * R + t];
+            if (a.sup) before += before1[q * R + t];
         }
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) here += counts[w][t];
     }
     const uint32_t first = scan_before(total, lds);   // global place of the digit's first key
     const uint32_t local = scan_before(here, lds);    // place in the workgroup
-    if (t < kDigits) {
+    if (t < R) {
         start[t] = first + before - local;
         uint32_t c = local;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
             const uint32_t mine = counts[w][t];
-            counts[w][t] = c;
+            counts[w][t] = (uint16_t)c;
             c += mine;
         }
         if (a.offsets && blockIdx.x == 0 && t <= (int)a.groups) a.offsets[t] = (int32_t)first;
     }
-    // (groups = 256: the keys of no group would be a 257th digit, and the pass is not the only one)
-    __syncthreads();
+    __syncthreads();   // (and the sums in buf have been read)
+    uint32_t val[ITEMS];
 #pragma unroll
-    for (int k = 0; k < kItems; ++k) {
-        if (!valid[k]) continue;
-        const uint32_t at = counts[wave][digit[k]] + rank[k];
-        buf_k[at] = key[k];
-        buf_v[at] = val[k];
-        if (a.place) a.place[val[k]] = key[k] < a.groups ? (int32_t)(start[digit[k]] + at) : -1;
+    for (int k = 0; k < ITEMS; ++k) {
+        const int i = at0 + k * 64;
+        if (i >= n) continue;
+        const uint32_t digit = (key[k] >> a.shift) & (R - 1);
+        val[k] = a.vals_in ? a.vals_in[base + i] : (uint32_t)(base + i);
+        rank[k] += counts[wave][digit];
+        buf[rank[k]] = key[k];
+        if (a.place) a.place[val[k]] = key[k] < a.groups ? (int32_t)(start[digit] + rank[k]) : -1;
+    }
+    __syncthreads();
+    uint32_t to[ITEMS];   // where the workgroup's places t, t + kThreads, ... go
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
+        const int at = k * kThreads + t;
+        if (at >= n) continue;
+        const uint32_t q = buf[at];
+        to[k] = start[(q >> a.shift) & (R - 1)] + at;
+        if (a.keys_out) a.keys_out[to[k]] = q;
     }
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < kItems; ++k) {
+    for (int k = 0; k < ITEMS; ++k)
+        if (at0 + k * 64 < n) buf[rank[k]] = val[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
         const int at = k * kThreads + t;
-        if (at >= n) continue;
-        const uint32_t q = buf_k[at];
-        const int64_t to = (int64_t)start[(q >> a.shift) & (kDigits - 1)] + at;
-        if (a.keys_out) a.keys_out[to] = q;
-        a.vals_out[to] = buf_v[at];
+        if (at < n) a.vals_out[to[k]] = buf[at];
     }
 }
 
@@ -224,27 +277,23 @@ __global__ __launch_bounds__(kThreads) void k_keys_small(const int32_t* __restri
                                                          int32_t* __restrict__ sorted, int32_t* __restrict__ place,
                                                          int32_t* __restrict__ offsets)
 {
-    constexpr int kI = kSmallCount / kThreads;
-    __shared__ uint32_t counts[kWaves][kDigits];
+    constexpr int kI = kSmallCount / kThreads, kDigits = 1 << kSmallBits;
+    __shared__ uint16_t counts[kWaves][kDigits];
     __shared__ uint32_t buf_k[kSmallCount], lds[kWaves];
     __shared__ uint16_t buf_v[kSmallCount];
     const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
     const int at0 = wave * kI * 64 + lane;
-    uint32_t key[kI], val[kI], digit[kI], rank[kI];
-    bool valid[kI];
+    uint32_t key[kI], val[kI], rank[kI];
 #pragma unroll
     for (int k = 0; k < kI; ++k) {
         const int i = at0 + k * 64;
-        valid[k] = i < count;
-        key[k] = valid[k] ? key_of(group_of, i, groups) : 0;
+        key[k] = i < count ? key_of(group_of, i, groups) : 0;
         val[k] = i;
     }
-    for (int shift = 0;; shift += 8) {
-#pragma unroll
-        for (int k = 0; k < kI; ++k) digit[k] = (key[k] >> shift) & (kDigits - 1);
+    for (int shift = 0;; shift += kSmallBits) {
         for (int k = t; k < kWaves * kDigits; k += kThreads) (&counts[0][0])[k] = 0;
         __syncthreads();
-        rank_slice<kI>(digit, valid, counts[wave], rank);
+        rank_slice<kSmallBits, kI>(key, shift, count - at0, counts[wave], rank);
         __syncthreads();
         uint32_t here = 0;
         if (t < kDigits)
@@ -255,22 +304,22 @@ __global__ __launch_bounds__(kThreads) void k_keys_small(const int32_t* __restri
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) {
                 const uint32_t mine = counts[w][t];
-                counts[w][t] = c;
+                counts[w][t] = (uint16_t)c;
                 c += mine;
             }
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < kI; ++k) {
-            if (!valid[k]) continue;
-            const uint32_t at = counts[wave][digit[k]] + rank[k];
+            if (at0 + k * 64 >= count) continue;
+            const uint32_t at = counts[wave][(key[k] >> shift) & (kDigits - 1)] + rank[k];
             buf_k[at] = key[k];
             buf_v[at] = (uint16_t)val[k];
         }
         __syncthreads();
-        if (shift + 8 >= bits) break;
+        if (shift + kSmallBits >= bits) break;
 #pragma unroll
         for (int k = 0; k < kI; ++k)
-            if (valid[k]) {
+            if (at0 + k * 64 < count) {
                 key[k] = buf_k[at0 + k * 64];
                 val[k] = buf_v[at0 + k * 64];
             }
@@ -292,7 +341,14 @@ int bits_of(int64_t groups)   // of keys up to `groups`
     return b;
 }
 
-int passes_of(int64_t groups) { return (int)div_up(bits_of(groups), 8); }
+int passes_of(int64_t groups) { return (int)div_up(bits_of(groups), kMostBits); }
+
+// Bits of a pass's digits that the kernels are built for: 5, 7 or 9.
+int digit_bits(int64_t groups)
+{
+    const int64_t each = div_up(bits_of(groups), passes_of(groups));
+    return each <= 5 ? 5 : each <= 7 ? 7 : 9;
+}
 
 struct SortSpace {
     uint32_t *hist, *sup, *keys[2], *vals[2];
@@ -309,14 +365,16 @@ SortSpace sort_space(void* base, int64_t count, int64_t groups)
         at += align_up((size_t)values * 4, 256);
         return p;
     };
-    const int passes = passes_of(groups);
+    const int passes = passes_of(groups), digits = 1 << digit_bits(groups);
     if (count > kSmallCount) {
-        w.blocks = div_up(count, kKeysTile);
+        w.blocks = div_up(count, kThreads * (count <= kFewItems ? 4 : 6));
+        w.hist = take(w.blocks * digits);
         w.group = 1;
-        while (w.group * w.group < w.blocks) ++w.group;
-        w.groups = div_up(w.blocks, w.group);
-        w.hist = take(w.blocks * kDigits);
-        w.sup = take(passes * w.groups * kDigits);
+        if (w.blocks > kFewBlocks) {
+            while (w.group * w.group < w.blocks) ++w.group;
+            w.groups = div_up(w.blocks, w.group);
+            w.sup = take(passes * w.groups * digits);
+        }
         // the last pass writes the caller's arrays, or keys that only the offsets are read from
         for (int k = 0; k < 2; ++k) {
             if (passes > 1) w.keys[k] = take(count);
@@ -329,6 +387,14 @@ SortSpace sort_space(void* base, int64_t count, int64_t groups)
     return w;
 }
 
+template <int BITS, int ITEMS>
+hipError_t sort_pass(const KeysPass& a, int64_t blocks, hipStream_t s)
+{
+    hipLaunchKernelGGL((k_keys_count<BITS, ITEMS>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((k_keys_move<BITS, ITEMS>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
+    return hipGetLastError();
+}
+
 }  // namespace
 
 size_t sort_rows_workspace(int64_t count, int64_t groups) { return sort_space(nullptr, count, groups).bytes; }
@@ -336,7 +402,7 @@ size_t sort_rows_workspace(int64_t count, int64_t groups) { return sort_space(nu
 hipError_t launch_sort_rows(const int32_t* group_of, const gs_row_order& o, void* ws, hipStream_t s)
 {
     const SortSpace w = sort_space(ws, o.count, o.groups);
-    const int passes = passes_of(o.groups);
+    const int passes = passes_of(o.groups), bits = digit_bits(o.groups);
     auto find_offsets = [&](const uint32_t* sorted) {
         hipLaunchKernelGGL(k_offsets, dim3((unsigned)div_up(o.groups + 1, kBlock)), dim3(kBlock), 0, s, sorted,
                            (uint32_t)o.count, (uint32_t)o.groups, o.offsets);
@@ -350,7 +416,8 @@ hipError_t launch_sort_rows(const int32_t* group_of, const gs_row_order& o, void
         const hipError_t e = hipGetLastError();
         return e != hipSuccess || few ? e : find_offsets((const uint32_t*)sorted);
     }
-    hipError_t e = launch_fill_u32(w.sup, passes * w.groups * kDigits, 0u, s);
+    const int64_t sup = w.groups << bits;   // values of a pass
+    hipError_t e = w.sup ? launch_fill_u32(w.sup, passes * sup, 0u, s) : hipSuccess;
     KeysPass a = {};
     a.count = o.count;
     a.groups = (uint32_t)o.groups;
@@ -361,15 +428,19 @@ hipError_t launch_sort_rows(const int32_t* group_of, const gs_row_order& o, void
         a.group_of = p == 0 ? group_of : nullptr;
         a.keys_in = p == 0 ? nullptr : w.keys[(p - 1) & 1];
         a.vals_in = p == 0 ? nullptr : w.vals[(p - 1) & 1];
-        a.shift = 8 * p;
-        a.sup = w.sup + p * w.groups * kDigits;
+        a.shift = bits * p;
+        a.sup = w.sup ? w.sup + p * sup : nullptr;
         a.keys_out = last && (o.sorted || passes == 1) ? (uint32_t*)o.sorted : w.keys[p & 1];
         a.vals_out = last ? (uint32_t*)o.order : w.vals[p & 1];
         a.place = last ? o.place : nullptr;
         a.offsets = passes == 1 ? o.offsets : nullptr;
-        hipLaunchKernelGGL(k_keys_count, dim3((unsigned)w.blocks), dim3(kThreads), 0, s, a);
-        hipLaunchKernelGGL(k_keys_move, dim3((unsigned)w.blocks), dim3(kThreads), 0, s, a);
-        e = hipGetLastError();
+        const bool few = o.count <= kFewItems;
+        if (bits == 5)
+            e = few ? sort_pass<5, 4>(a, w.blocks, s) : sort_pass<5, 6>(a, w.blocks, s);
+        else if (bits == 7)
+            e = few ? sort_pass<7, 4>(a, w.blocks, s) : sort_pass<7, 6>(a, w.blocks, s);
+        else
+            e = few ? sort_pass<9, 4>(a, w.blocks, s) : sort_pass<9, 6>(a, w.blocks, s);
     }
     return e != hipSuccess || passes == 1 ? e : find_offsets(a.keys_out);
 }
