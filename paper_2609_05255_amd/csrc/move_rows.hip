@@ -12,7 +12,7 @@
 #include <type_traits>
 
 #include "gs_internal.h"
-#include "vec.h"
+#include "rows.h"
 
 namespace gsr {
 
@@ -50,25 +50,11 @@ int64_t move_blocks(int64_t rows, int g, int fly)
     return std::max<int64_t>(1, std::min<int64_t>(div_up(rows, (int64_t)kBlock / g * fly), kMoveBlocks));
 }
 
-// The stored vector as it is, or its first `left` elements.
+// Behind the last row's end.
 template <typename T>
-__device__ __forceinline__ void put_vec(T* p, int64_t left, typename Vec<T>::Packed v)
+__device__ __forceinline__ const T* end_of(const void* p, int64_t ld, int64_t rows, int64_t dim)
 {
-    constexpr int N = Vec<T>::N;
-    if (left >= N) {
-        *reinterpret_cast<typename Vec<T>::Any*>(p) = v;
-    } else {
-#pragma unroll
-        for (int j = 0; j < N; ++j)
-            if (j < left) p[j] = v[j];
-    }
-}
-
-// A vector of a row; WHOLE: the row ends with a whole one.
-template <typename T, bool WHOLE>
-__device__ __forceinline__ typename Vec<T>::Packed get_vec(const T* p, int64_t left)
-{
-    return WHOLE ? *reinterpret_cast<const typename Vec<T>::Any*>(p) : load_any(p, left);
+    return (const T*)p + (rows - 1) * ld + dim;
 }
 
 // ---- one row to one row -----------------------------------------------------
@@ -96,6 +82,7 @@ __global__ __launch_bounds__(kBlock) void k_gather(GatherArgs a)
     typedef typename Vec<T>::Packed Packed;
     const int lane = threadIdx.x & (G - 1);
     const int64_t rows = LOOKUP ? a.rows : min((int64_t)*a.used, a.rows);
+    const T* end = end_of<T>(a.src, a.lds, LOOKUP ? a.entries : a.rows / a.k, a.dim);
     const int64_t step = (int64_t)gridDim.x * kGroups * U;
     for (int64_t r0 = ((int64_t)blockIdx.x * kGroups + threadIdx.x / G) * U; r0 < rows; r0 += step) {
         const T* from[U];
@@ -119,7 +106,7 @@ __global__ __launch_bounds__(kBlock) void k_gather(GatherArgs a)
             const int64_t left = a.dim - c;
             Packed v[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) v[u] = get_vec<T, WHOLE>(from[u] + c, left);
+            for (int u = 0; u < U; ++u) v[u] = get_vec<T, WHOLE>(from[u] + c, left, end);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 if (r0 + u >= rows) break;
@@ -128,9 +115,9 @@ __global__ __launch_bounds__(kBlock) void k_gather(GatherArgs a)
                     float f[N];
 #pragma unroll
                     for (int e = 0; e < N; ++e) f[e] = in[u] ? (float)v[u][e] * a.scale : 0.f;
-                    store_vec(to, WHOLE ? N : left, f);
+                    put_floats<T, WHOLE>(to, left, f);
                 } else if (in[u]) {
-                    put_vec(to, WHOLE ? N : left, v[u]);
+                    put_vec<T, WHOLE>(to, left, v[u]);
                 }
             }
         }
@@ -157,6 +144,7 @@ __global__ __launch_bounds__(kBlock) void k_scatter(ScatterArgs a)
     typedef typename Vec<T>::Packed Packed;
     const int lane = threadIdx.x & (G - 1);
     const int64_t used = min((int64_t)*a.used, a.rows * a.k);
+    const T* end = end_of<T>(a.src, a.lds, a.rows, a.dim);
     const int64_t step = (int64_t)gridDim.x * kGroups * U;
     for (int64_t r0 = ((int64_t)blockIdx.x * kGroups + threadIdx.x / G) * U; r0 < a.rows; r0 += step)
         for (int64_t c = (int64_t)lane * N; c < a.dim; c += G * N) {
@@ -165,13 +153,13 @@ __global__ __launch_bounds__(kBlock) void k_scatter(ScatterArgs a)
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int64_t r = r0 + u < a.rows ? r0 + u : a.rows - 1;
-                v[u] = get_vec<T, WHOLE>((const T*)a.src + r * a.lds + c, left);
+                v[u] = get_vec<T, WHOLE>((const T*)a.src + r * a.lds + c, left, end);
             }
             for (int j = 0; j < a.k; ++j)
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     const int32_t p = r0 + u < a.rows ? a.place[(r0 + u) * a.k + j] : -1;
-                    if (p >= 0 && p < used) put_vec((T*)a.dst + p * a.ldd + c, WHOLE ? N : left, v[u]);
+                    if (p >= 0 && p < used) put_vec<T, WHOLE>((T*)a.dst + p * a.ldd + c, left, v[u]);
                 }
         }
 }
@@ -199,6 +187,7 @@ __global__ __launch_bounds__(kBlock) void k_sum_choices(SumArgs a)
     typedef typename Vec<T>::Packed Packed;
     const int lane = threadIdx.x & (G - 1);
     const int64_t used = min((int64_t)*a.used, a.rows * a.k);
+    const T *end = end_of<T>(a.src, a.lds, a.rows * a.k, a.dim), *add_end = end_of<T>(a.add, a.ldadd, a.rows, a.dim);
     const int64_t step = (int64_t)gridDim.x * kGroups;
     for (int64_t r = (int64_t)blockIdx.x * kGroups + threadIdx.x / G; r < a.rows; r += step) {
         const int64_t at = r * a.k;
@@ -206,7 +195,7 @@ __global__ __launch_bounds__(kBlock) void k_sum_choices(SumArgs a)
             const int64_t left = a.dim - c;
             float sum[N] = {};
             Packed add = {};
-            if (a.add) add = get_vec<T, WHOLE>((const T*)a.add + r * a.ldadd + c, left);
+            if (a.add) add = get_vec<T, WHOLE>((const T*)a.add + r * a.ldadd + c, left, add_end);
             for (int j0 = 0; j0 < a.k; j0 += U) {
                 Packed v[U];
                 float w[U];
@@ -217,7 +206,7 @@ __global__ __launch_bounds__(kBlock) void k_sum_choices(SumArgs a)
                         const int32_t p = a.place[at + j0 + u];
                         w[u] = a.weight ? a.weight[at + j0 + u] : 1.f;
                         in[u] = p >= 0 && p < used;
-                        v[u] = get_vec<T, WHOLE>((const T*)a.src + (in[u] ? p : 0) * a.lds + c, left);
+                        v[u] = get_vec<T, WHOLE>((const T*)a.src + (in[u] ? p : 0) * a.lds + c, left, end);
                     }
 #pragma unroll
                 for (int u = 0; u < U; ++u)
@@ -228,7 +217,7 @@ __global__ __launch_bounds__(kBlock) void k_sum_choices(SumArgs a)
             if (a.add)
 #pragma unroll
                 for (int e = 0; e < N; ++e) sum[e] += (float)add[e];
-            store_vec((T*)a.dst + r * a.ldd + c, WHOLE ? N : left, sum);
+            put_floats<T, WHOLE>((T*)a.dst + r * a.ldd + c, left, sum);
         }
     }
 }
@@ -253,6 +242,7 @@ __global__ __launch_bounds__(kBlock) void k_combine_bwd(CombineBwdArgs a)
     typedef typename Vec<T>::Packed Packed;
     const int lane = threadIdx.x & (G - 1);
     const int64_t used = min((int64_t)*a.used, a.rows * a.k);
+    const T *end = end_of<T>(a.ys, a.ldys, a.rows * a.k, a.dim), *dy_end = end_of<T>(a.dy, a.lddy, a.rows, a.dim);
     const int64_t step = (int64_t)gridDim.x * kGroups;
     for (int64_t r = (int64_t)blockIdx.x * kGroups + threadIdx.x / G; r < a.rows; r += step) {
         const int64_t at = r * a.k;
@@ -270,27 +260,27 @@ __global__ __launch_bounds__(kBlock) void k_combine_bwd(CombineBwdArgs a)
                 }
             for (int64_t c = (int64_t)lane * N; c < a.dim; c += G * N) {
                 const int64_t left = a.dim - c;
-                const Packed g = get_vec<T, WHOLE>((const T*)a.dy + r * a.lddy + c, left);
+                const Packed g = get_vec<T, WHOLE>((const T*)a.dy + r * a.lddy + c, left, dy_end);
                 Packed v[U];
 #pragma unroll
                 for (int u = 0; u < U; ++u)
-                    if (j0 + u < a.k) v[u] = get_vec<T, WHOLE>((const T*)a.ys + p[u] * a.ldys + c, left);
+                    if (j0 + u < a.k) v[u] = get_vec<T, WHOLE>((const T*)a.ys + p[u] * a.ldys + c, left, end);
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     if (j0 + u >= a.k || !in[u]) continue;
                     float o[N];
 #pragma unroll
                     for (int e = 0; e < N; ++e) {
-                        dot[u] = fmaf((float)g[e], (float)v[u][e], dot[u]);
+                        if (WHOLE || e < left) dot[u] = fmaf((float)g[e], (float)v[u][e], dot[u]);
                         o[e] = (float)g[e] * w[u];
                     }
-                    store_vec((T*)a.dys + p[u] * a.lddys + c, WHOLE ? N : left, o);
+                    put_floats<T, WHOLE>((T*)a.dys + p[u] * a.lddys + c, left, o);
                 }
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 if (j0 + u >= a.k) continue;
-                const float d = lane_sum<G>(dot[u]);
+                const float d = group_sum<G>(dot[u]);
                 if (lane == 0) a.dweight[at + j0 + u] = d;
             }
         }
@@ -337,9 +327,10 @@ __device__ __forceinline__ void store_entries(const EntriesArgs& a, int64_t v, i
     if (a.out_f32) {
         float* to = (float*)a.dtable + v * a.lddt + c;
 #pragma unroll
-        for (int e = 0; e < N; e += 4) store_vec(to + e, left - e, o + e);
+        for (int e = 0; e < N; e += 4)
+            if (left > e) put_floats<float, false>(to + e, left - e, o + e);
     } else {
-        store_vec((T*)a.dtable + v * a.lddt + c, left, o);
+        put_floats<T, false>((T*)a.dtable + v * a.lddt + c, left, o);
     }
 }
 
@@ -359,7 +350,7 @@ __global__ __launch_bounds__(kBlock) void k_sum_entries(EntriesArgs a)
     const int64_t w0 = (int64_t)blockIdx.x * kGroups * a.per;
     const int64_t w1 = w0 + kGroups * a.per < used ? w0 + kGroups * a.per : used;
     const int64_t p0 = w0 + (int64_t)group * a.per, p1 = p0 + a.per < w1 ? p0 + a.per : w1;
-    const T* dy = (const T*)a.dy + (left > 0 ? c : 0);
+    const T *dy = (const T*)a.dy + (left > 0 ? c : 0), *end = end_of<T>(a.dy, a.lddy, a.count, a.dim);
     int32_t first = -1, key = -1;
     float sum[N] = {};
     for (int64_t p = p0; p < p1; p += U) {
@@ -378,10 +369,7 @@ __global__ __launch_bounds__(kBlock) void k_sum_entries(EntriesArgs a)
                 const uint32_t iu = G == 1 ? i : (uint32_t)__shfl((int)i, u, kIndexed);
                 k[q + u] = G == 1 ? e : __shfl(e, u, kIndexed);
                 const T* row = dy + (int64_t)iu * a.lddy;
-                if (WHOLE)
-                    v[q + u] = *reinterpret_cast<const typename Vec<T>::Any*>(row);
-                else
-                    v[q + u] = load_any(row, left);
+                v[q + u] = get_vec<T, WHOLE>(row, left > 0 ? left : a.dim, end);
             }
         }
 #pragma unroll

@@ -122,17 +122,20 @@ def test_masks(dtype, normalise):
 
 @pytest.mark.parametrize("normalise", [True, False])
 @pytest.mark.parametrize("dtype", TYPES)
-def test_undefined_and_infinite(dtype, normalise):
-    """Experts are valid whatever the logits; other rows keep their weights."""
-    l = make(40, 24, dtype, 2)
+@pytest.mark.parametrize("experts", [24, 27, 64, 300])
+def test_undefined_and_infinite(dtype, normalise, experts):
+    """Experts are valid whatever the logits, undefined ones first whatever their sign; other rows keep their weights."""
+    l = make(40, experts, dtype, 2)
     clean = l.clone()
     l[3, 5], l[17, 20], l[17, 2] = float("nan"), INF, INF
+    l[30, experts - 1] = -torch.tensor(float("nan"), dtype=dtype, device="cuda")
     expert, weight = forward(l, 3, normalise)
     e0, w0 = forward(clean, 3, normalise)
-    others = [r for r in range(40) if r not in (3, 17)]
+    others = [r for r in range(40) if r not in (3, 17, 30)]
+    assert expert[30, 0] == experts - 1 and torch.isnan(weight[30]).all()
     assert torch.equal(expert[others], e0[others]) and torch.equal(weight[others], w0[others])
     assert expert[3, 0] == 5 and expert[17, :2].tolist() == [2, 20]
-    assert ((expert >= 0) & (expert < 24)).all()
+    assert ((expert >= 0) & (expert < experts)).all()
     assert torch.isnan(weight[3]).all()
     assert all(len(set(r)) == 3 for r in expert.tolist())
 
