@@ -17,7 +17,7 @@ __global__ __launch_bounds__(kBlock) void k_mix_prepare(MixPrepareArgs a)
         const int64_t unit = b / a.slope_x;
         const MixUnit u = mix_unit(a.mix, a.mix.size, 0, unit);
         if (u.expert < 0) return;
-        const int64_t first = u.first + u.unit * a.mix.size, left = u.rows - u.unit * a.mix.size;
+        const int64_t first = u.first + (int64_t)u.unit * a.mix.size, left = u.rows - (int64_t)u.unit * a.mix.size;
         SlopeArgs p = a.slope;
         p.rows = left < a.mix.size ? left : a.mix.size;
         p.row_blocks = 1;
@@ -51,26 +51,44 @@ __global__ __launch_bounds__(kBlock) void k_mix_prepare(MixPrepareArgs a)
     }
 }
 
-// Adds up the parts of an expert's dW where it has several; blockIdx.y is the expert.
+// Adds up the parts of an expert's dW where it has several, and of its db; blockIdx.y is the expert, and workgroups from
+// `join` on take 16 columns of db each, 16 threads one's units.
 template <typename T>
-__global__ __launch_bounds__(kBlock) void k_mix_join(GemmArgs g)
+__global__ __launch_bounds__(kBlock) void k_mix_join(GemmArgs g, int join, MixSums b)
 {
+    __shared__ float s[16][16];
+    if ((int)blockIdx.x >= join) {
+        const MixUnit u = mix_expert(b.mix, b.mix.size, 0, blockIdx.y);
+        const int col = threadIdx.x & 15, slice = threadIdx.x >> 4;
+        const int64_t c = (int64_t)(blockIdx.x - join) * 16 + col, units = min((int64_t)u.units, b.mix.limit - u.before);
+        float t = 0.f;
+        if (c < b.cols)
+#pragma unroll 8
+            for (int64_t k = slice; k < units; k += 16) t += b.part[(u.before + k) * b.cols + c];
+        s[slice][col] = t;
+        __syncthreads();
+        if (slice != 0 || c >= b.cols) return;
+#pragma unroll
+        for (int k = 1; k < 16; ++k) t += s[k][col];
+        b.db[u.expert * b.cols + c] = t;
+        return;
+    }
     const MixUnit u = mix_expert(g.mix, (int)g.split_len, 1, blockIdx.y);
     if (u.units < 2) return;
     const int64_t quads = (g.cols + 3) / 4, size = g.rows * g.cols;
     const int64_t before = mix_parts_before(g.mix, (int)g.split_len, u.expert);
-    const int64_t units = min(u.units, g.mix.limit - before);
+    const int64_t units = min((int64_t)u.units, g.mix.limit - before);
     const float* parts = g.part + before * size;
-    for (int64_t k = (int64_t)blockIdx.x * kBlock + threadIdx.x; k < g.rows * quads; k += (int64_t)gridDim.x * kBlock) {
+    for (int64_t k = (int64_t)blockIdx.x * kBlock + threadIdx.x; k < g.rows * quads; k += (int64_t)join * kBlock) {
         const int64_t i = k / quads, j = (k - i * quads) * 4, left = g.cols - j;
         const float* part = parts + i * g.cols + j;
         float v[4] = {};
 #pragma unroll 8
-        for (int64_t s = 0; s < units; ++s) {
-            float p[4];
-            load_vec(part + s * size, left, p);
+        for (int64_t p = 0; p < units; ++p) {
+            float t[4];
+            load_vec(part + p * size, left, t);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] += p[e];
+            for (int e = 0; e < 4; ++e) v[e] += t[e];
         }
         const int64_t o = u.expert * g.mix.dw_stride + i * g.ldo + j;
         if (g.out_f32) {
@@ -81,26 +99,6 @@ __global__ __launch_bounds__(kBlock) void k_mix_join(GemmArgs g)
                 if (e < left) ((T*)g.out)[o + e] = (T)v[e];
         }
     }
-}
-
-// blockIdx.y is the expert; 16 columns, 16 threads share one's units
-__global__ __launch_bounds__(kBlock) void k_mix_sums(Mix mix, const float* __restrict__ part, int64_t cols,
-                                                     float* __restrict__ db)
-{
-    __shared__ float s[16][16];
-    const MixUnit u = mix_expert(mix, mix.size, 0, blockIdx.y);
-    const int col = threadIdx.x & 15, slice = threadIdx.x >> 4;
-    const int64_t c = (int64_t)blockIdx.x * 16 + col;
-    float t = 0.f;
-    if (c < cols)
-#pragma unroll 8
-        for (int64_t k = slice; k < min(u.units, mix.limit - u.before); k += 16) t += part[(u.before + k) * cols + c];
-    s[slice][col] = t;
-    __syncthreads();
-    if (slice != 0 || c >= cols) return;
-#pragma unroll
-    for (int k = 1; k < 16; ++k) t += s[k][col];
-    db[u.expert * cols + c] = t;
 }
 
 }  // namespace
@@ -114,10 +112,17 @@ hipError_t MixtureOps<T>::gemm_nt(int tile, bool fast_a, const GemmArgs& g, hipS
 template <typename T>
 hipError_t MixtureOps<T>::gemm_tt(int tile, bool fast_b, const GemmArgs& g, hipStream_t s)
 {
-    const hipError_t e = run_tt<T, true>(tile, fast_b, g, s);
-    if (e != hipSuccess || !g.part) return e;
-    const int64_t blocks = std::min<int64_t>(div_up(g.rows * div_up(g.cols, 4), kBlock), 4096);
-    hipLaunchKernelGGL((k_mix_join<T>), dim3((unsigned)blocks, (unsigned)g.mix.experts), dim3(kBlock), 0, s, g);
+    return run_tt<T, true>(tile, fast_b, g, s);
+}
+
+template <typename T>
+hipError_t MixtureOps<T>::join(const GemmArgs& g, const MixSums& b, hipStream_t s)
+{
+    const int join = g.part ? (int)std::min<int64_t>(div_up(g.rows * div_up(g.cols, 4), kBlock), 4096) : 0;
+    const int64_t sums = b.db ? div_up(b.cols, 16) : 0;
+    if (join + sums == 0) return hipSuccess;
+    const int experts = g.part ? g.mix.experts : b.mix.experts;
+    hipLaunchKernelGGL((k_mix_join<T>), dim3((unsigned)(join + sums), (unsigned)experts), dim3(kBlock), 0, s, g, join, b);
     return hipGetLastError();
 }
 
@@ -158,14 +163,6 @@ hipError_t MixtureOps<T>::prepare(const Mix& mix, int64_t units, const SlopeArgs
     }
     if (all == 0) return hipSuccess;
     hipLaunchKernelGGL((k_mix_prepare<T>), dim3((unsigned)all), dim3(kBlock), 0, s, a);
-    return hipGetLastError();
-}
-
-template <typename T>
-hipError_t MixtureOps<T>::sums(const Mix& mix, const float* part, int64_t cols, float* db, hipStream_t s)
-{
-    hipLaunchKernelGGL(k_mix_sums, dim3((unsigned)div_up(cols, 16), (unsigned)mix.experts), dim3(kBlock), 0, s, mix, part,
-                       cols, db);
     return hipGetLastError();
 }
 

@@ -16,6 +16,9 @@ namespace {
 
 constexpr int kDzBlocks = 2048;          // workgroups of dz, about
 constexpr int64_t kNarrowRows = 128;     // of a unit of a narrow layer, at least
+constexpr int64_t kPlaces = 5 * kFillTiles;   // workgroups that the compute units hold at once, of any tile at most
+constexpr int64_t kMostSplits = 8;
+constexpr double kSplitGain = 2.0;       // us that a split of the last tiles has to gain by the plan
 
 int64_t units_most(int64_t rows, int64_t experts, int64_t size) { return rows / size + std::min(rows, experts); }
 
@@ -35,15 +38,27 @@ Plan plan_mix(int type, bool tt, int64_t rows, int64_t cols, int64_t len, int64_
         const int threads = r.tile == kTile64By4 ? 1024 : r.tile == kTile256 ? 512 : 256;
         if (!tt) {
             if (len < r.least) continue;
-            if (units_most(rows, experts, r.rows) * div_up(cols, r.cols) * threads >> 32) continue;
-            const int64_t tiles = std::max(some, rows / r.rows + some / 2) * div_up(cols, r.cols);
-            const int64_t share = div_up(tiles, kFillTiles), rounds = div_up(share, r.held);
-            const bool alone = (share - 1) % r.held == 0;
-            const double us = area * (double)len * ((double)(share - alone) / r.flop_us + alone / r.flop_us_one) / slow +
-                              (double)rounds * r.round_us;
-            if (us < best_us) {
-                best_us = us;
+            if ((units_most(rows, experts, r.rows) * div_up(cols, r.cols) + kPlaces) * threads >> 32) continue;
+            // rounds of tiles that fill the compute units, and the rest, whole or split along the sum
+            const int64_t places = r.held * kFillTiles;
+            const int64_t tiles = std::max(some, rows / r.rows + some / 2) * div_up(cols, r.cols), rest = tiles % places;
+            const auto round = [&](int64_t count, int64_t sum) {   // of so many tiles, places at most
+                const int64_t share = div_up(count, kFillTiles);
+                return area * (double)sum * (share > 1 ? share / r.flop_us : 1 / r.flop_us_one) / slow + r.round_us;
+            };
+            const double whole = (double)(tiles / places) * round(places, len) + (rest ? round(rest, len) : 0.0);
+            if (whole < best_us) {
+                best_us = whole;
                 best = {r.tile, 1, len};
+            }
+            const int64_t least = 4 * 128 / elem(type);   // values of a part
+            const int64_t splits = rest ? std::min({places / 2 / rest, len / least, kMostSplits}) : 1;
+            if (splits < 2 || r.tile == kTile64By4 || !fast_operand) continue;
+            const double us = (double)(tiles / places) * round(places, len) + round(rest * splits, div_up(len, splits)) +
+                              kJoinUs + 8.0 * rest * splits * r.rows * r.cols / kBytesUs;
+            if (us + kSplitGain < best_us) {
+                best_us = us;
+                best = {r.tile, (int)splits, len};
             }
             continue;
         }
@@ -73,10 +88,14 @@ int64_t parts_most(const Plan& p, int64_t rows, int64_t experts)
     return p.split_len >= rows ? 0 : std::min(units_most(rows, experts, p.split_len), 2 * (rows / p.split_len));
 }
 
+// Rows of a unit of dz: two of each thread, more where that would be more workgroups than it takes.
 int64_t dz_size(int type, int64_t rows, int64_t cols)
 {
-    const int64_t across = div_up(div_up(cols, vec(type)), 64);
-    return std::max<int64_t>(32, div_up(div_up(rows * across, kDzBlocks), 32) * 32);
+    const int64_t vecs = div_up(cols, vec(type)), across = div_up(vecs, 64);
+    int64_t lanes = 1;
+    while (lanes < 64 && lanes < vecs) lanes <<= 1;
+    const int64_t least = 2 * kBlock / lanes;
+    return div_up(std::max(least, div_up(rows * across, kDzBlocks)), least) * least;
 }
 
 int64_t narrow_size(int64_t rows, int64_t in, int64_t out)
@@ -92,11 +111,38 @@ bool fast_w(const gs_experts& p)
     return fast(p.layer.w, p.layer.ldw, p.layer.n_in, p.layer.type) && p.w_stride % vec(p.layer.type) == 0;
 }
 
-// W with padded rows, where its own cannot be read in vectors
-size_t fwd_bytes(int type, int64_t rows, int64_t experts, int64_t in, int64_t out, bool copy_w)
+// Bytes of the parts that the last tiles of a product along rows are split into.
+int64_t tail_bytes(int type, const Plan& p)
 {
-    if (rows <= kFewRows || narrow_taken(type, rows, in, out) || !copy_w) return 0;
-    return align_up((size_t)(experts * out * padded(type, in) * elem(type)), 256);
+    if (p.splits < 2) return 0;
+    for (const TileRate* r = type == GS_F32 ? kRates32 : kRates16;; ++r)
+        if (r->tile == p.tile) return (int64_t)r->held * kFillTiles / 2 * r->rows * r->cols * 4;
+}
+
+Plan plan_rows(int type, int64_t rows, int64_t experts, int64_t cols, int64_t len, bool fast_a)
+{
+    if (rows <= kFewRows) return {kTile64, 1, len};
+    return plan_mix(type, false, rows, cols, len, experts, 1, fast_a);
+}
+
+struct FwdSpace {
+    void* w;       // W with padded rows, where its own cannot be read in vectors
+    float* part;
+    size_t bytes;
+};
+
+FwdSpace fwd_space(void* base, int type, int64_t rows, int64_t experts, int64_t in, int64_t out, bool copy_w)
+{
+    Regions r{(char*)base};
+    FwdSpace f = {};
+    if (rows > kFewRows && !narrow(type, in, out)) {
+        if (copy_w) f.w = r.take(experts * out * padded(type, in) * elem(type));
+        // (a workspace is sized for either alignment of x)
+        f.part = (float*)r.take(std::max(tail_bytes(type, plan_rows(type, rows, experts, out, in, false)),
+                                         tail_bytes(type, plan_rows(type, rows, experts, out, in, true))));
+    }
+    f.bytes = r.at;
+    return f;
 }
 
 struct BwdSpace {
@@ -126,7 +172,7 @@ BwdSpace bwd_space(void* base, int type, int act, int64_t rows, int64_t experts,
     // (a workspace is sized for either operand's alignment)
     for (int fast_x = 0; want_dw && fast_x < 2; ++fast_x)
         parts = std::max(parts, parts_most(plan_mix(type, true, out, in, rows, experts, planes, fast_x != 0), rows, experts));
-    b.part = (float*)r.take(parts * out * in * 4);
+    b.part = (float*)r.take(std::max(parts * out * in * 4, tail_bytes(type, plan_rows(type, rows, experts, in, out, true))));
     b.bytes = r.at;
     return b;
 }
@@ -143,12 +189,22 @@ Mix mix_of(const gs_experts& p, int64_t size)
 }
 
 template <typename T>
-hipError_t run_nt(int type, GemmArgs g, bool fast_a, hipStream_t s)
+hipError_t run_nt(int type, GemmArgs g, bool fast_a, float* part, hipStream_t s)
 {
     g.splits = g.planes = 1;
     g.split_len = g.len;
     if (g.rows <= kFewRows) return MixtureOps<T>::skinny(g, s);
-    return MixtureOps<T>::gemm_nt(plan_mix(type, false, g.rows, g.cols, g.len, g.mix.experts, 1, fast_a).tile, fast_a, g, s);
+    const Plan p = plan_rows(type, g.rows, g.mix.experts, g.cols, g.len, fast_a);
+    if (p.splits > 1) {
+        g.splits = p.splits;
+        g.part = part;
+        for (const TileRate* r = type == GS_F32 ? kRates32 : kRates16;; ++r)
+            if (r->tile == p.tile) {
+                g.mix.size = r->held * kFillTiles;
+                break;
+            }
+    }
+    return MixtureOps<T>::gemm_nt(p.tile, fast_a, g, s);
 }
 
 template <typename T>
@@ -175,17 +231,18 @@ hipError_t experts_fwd(const gs_experts& p, void* y, int64_t ldy, void* z, int64
         g.mix.size = (int32_t)narrow_size(l.rows, l.n_in, l.n_out);
         return MixtureOps<T>::narrow_fwd(g, fast_x, units_most(l.rows, p.experts, g.mix.size), s);
     }
-    if (fwd_bytes(l.type, l.rows, p.experts, l.n_in, l.n_out, !fast_w(p))) {
-        SlopeArgs copy = copy_of(l.type, l.w, l.ldw, l.n_out, l.n_in, ws);
+    const FwdSpace f = fwd_space(ws, l.type, l.rows, p.experts, l.n_in, l.n_out, !fast_w(p));
+    if (f.w) {
+        SlopeArgs copy = copy_of(l.type, l.w, l.ldw, l.n_out, l.n_in, f.w);
         copy.row_blocks = (int)std::max<int64_t>(1, copy.row_blocks / p.experts);
         const int64_t each = l.n_out * padded(l.type, l.n_in);
         const hipError_t e = MixtureOps<T>::prepare(g.mix, 0, nullptr, nullptr, &copy, nullptr, each, s);
         if (e != hipSuccess) return e;
-        g.b = ws;
+        g.b = f.w;
         g.ldb = padded(l.type, l.n_in);
         g.mix.w_stride = each;
     }
-    return run_nt<T>(l.type, g, fast_x, s);
+    return run_nt<T>(l.type, g, fast_x, f.part, s);
 }
 
 template <typename T>
@@ -230,7 +287,7 @@ hipError_t experts_bwd(const gs_experts& p, const void* dy, int64_t lddy, const 
     const TransposeArgs transpose = {l.w, l.ldw, l.n_out, l.n_in, b.wt, ldt};
     hipError_t e = MixtureOps<T>::prepare(rows, rows.limit, want_slope ? &slope : nullptr,
                                           copy_x ? &copy : nullptr, nullptr, want_dx ? &transpose : nullptr, l.n_in * ldt, s);
-    if (e == hipSuccess && db) e = MixtureOps<T>::sums(rows, b.sums, l.n_out, db, s);
+    GemmArgs weights = {};   // dW's product, if its parts have to be added up
     if (e != hipSuccess) return e;
     if (want_dx) {
         GemmArgs g = {};
@@ -245,7 +302,7 @@ hipError_t experts_bwd(const gs_experts& p, const void* dy, int64_t lddy, const 
         g.ldo = lddx;
         g.mix = mix_of(p, 0);
         g.mix.w_stride = l.n_in * ldt;
-        e = run_nt<T>(l.type, g, true, s);
+        e = run_nt<T>(l.type, g, true, b.part, s);
         if (e != hipSuccess) return e;
     }
     if (dw) {
@@ -274,15 +331,17 @@ hipError_t experts_bwd(const gs_experts& p, const void* dy, int64_t lddy, const 
         g.part = g.mix.limit > 0 ? b.part : nullptr;
         g.mix.dw_stride = dw_stride;
         e = MixtureOps<T>::gemm_tt(plan.tile, fast_x, g, s);
+        if (e != hipSuccess) return e;
+        weights = g;
     }
-    return e;
+    return MixtureOps<T>::join(weights, {rows, b.sums, l.n_out, db}, s);
 }
 
 }  // namespace
 
 size_t experts_fwd_workspace(const gs_experts& p)
 {
-    return fwd_bytes(p.layer.type, p.layer.rows, p.experts, p.layer.n_in, p.layer.n_out, !fast_w(p));
+    return fwd_space(nullptr, p.layer.type, p.layer.rows, p.experts, p.layer.n_in, p.layer.n_out, !fast_w(p)).bytes;
 }
 
 size_t experts_bwd_workspace(const gs_experts& p, const void* dy, int64_t lddy, int dw_type)
@@ -294,7 +353,7 @@ size_t experts_bwd_workspace(const gs_experts& p, const void* dy, int64_t lddy, 
 
 size_t experts_workspace(int type, int act, int64_t rows, int64_t experts, int64_t in, int64_t out, int dw_type)
 {
-    const size_t fwd = fwd_bytes(type, rows, experts, in, out, true);
+    const size_t fwd = fwd_space(nullptr, type, rows, experts, in, out, true).bytes;
     if (dw_type < 0) return fwd;
     // (fewer planes of dz can mean more parts of dW: the size for an fp32 dW does for one in the type as well)
     return std::max({fwd, bwd_space(nullptr, type, act, rows, experts, in, out, dw_type, true).bytes,

@@ -322,18 +322,45 @@ __device__ __forceinline__ void store_block(const char* lds, T* out, int64_t ld,
     }
 }
 
-// MIX: the product of each expert's rows with its own B (NT: workgroups take tiles of units of BI rows, and those beyond
-// the last one leave), or the sum over each expert's rows (TT: blockIdx.y is a unit of rows, and the results of an expert
-// that has several go to their parts).
-template <typename T, class S, bool MIX = false>
-__global__ __launch_bounds__(S::THREADS * S::WAYS) void k_gemm(GemmArgs g)
+// A mixture's product. NT: of each expert's rows with its own B; workgroups take tiles of units of BI rows, and those
+// beyond the last one leave. With parts (g.part), tiles that do not fill the compute units another time are split along
+// the sum into as many as do, up to half of the places that a round has: their sums go to the parts as the lanes have
+// them, and a second launch (kMixTail) adds them up and takes them through the epilogue. 16,384 x 2,048 -> 2,048 in
+// bfloat16, 8 experts of uneven shares, 528 tiles of 256 x 256: see the figures beside the plan.
+// TT: the sum over each expert's rows; blockIdx.y is a unit of rows, and the results of an expert that has several go to
+// their parts.
+enum { kNoMix = 0, kMix, kMixTail };
+
+// The tiles at the end that are split, and into how many.
+struct MixTail {
+    int64_t full, rest, splits;
+    __device__ __forceinline__ MixTail(const GemmArgs& g, int64_t tiles)
+    {
+        full = tiles;
+        rest = 0;
+        splits = 1;
+        if (!g.part) return;
+        const int64_t left = tiles % g.mix.size, most = left ? g.mix.size / 2 / left : 0;
+        if (most < 2) return;
+        splits = most < g.splits ? most : g.splits;
+        full = tiles - left;
+        rest = left;
+    }
+};
+
+// (kMixTail: a workgroup is one wave, for 16 rows of the block that a wave of WI x WJ has summed, S's waves being those
+// of 16 rows each.)
+template <typename T, class S, int MODE = kNoMix, int SUM_WI = 1>
+__global__ __launch_bounds__(MODE == kMixTail ? 64 : S::THREADS * S::WAYS) void k_gemm(GemmArgs g)
 {
+    constexpr bool MIX = MODE != kNoMix;
     constexpr bool TT = S::TT;
     constexpr int BI = S::BI, BJ = S::BJ, WI = S::WI, WJ = S::WJ;
     constexpr int WR = BI / WI, WC = BJ / WJ, FI = WR / 16, FJ = WC / 16;
     using Mm = Mma<T>;
-    using TA = Tile<T, BI, TT, false, S::THREADS>;
-    using TB = Tile<T, BJ, TT, true, S::THREADS>;
+    constexpr int kLoadThreads = MODE == kMixTail ? 64 : S::THREADS;
+    using TA = Tile<T, BI, TT, false, kLoadThreads>;
+    using TB = Tile<T, BJ, TT, true, kLoadThreads>;
     constexpr int kBK = TA::kBK, kSteps = kBK / Mm::kStep;   // of the sum, and of MFMAs, per tile
     constexpr int kTileBytes = TA::kBytes + TB::kBytes;
     [[maybe_unused]] constexpr bool kAsyncA = S::FAST || TT, kAsyncB = S::FAST || !TT;
@@ -341,20 +368,40 @@ __global__ __launch_bounds__(S::THREADS * S::WAYS) void k_gemm(GemmArgs g)
     static_assert(TT || BI * BJ * (int)sizeof(T) <= S::lds_bytes(1, sizeof(T)), "the results pass through LDS");
     // (as much as the launch gives: two tiles, or one if the sum has no more, so that more workgroups fit)
     extern __shared__ __attribute__((aligned(1024))) char lds_given[];
-    __shared__ __attribute__((aligned(1024))) char lds_own[S::AHEAD  ? 2 * kTileBytes + TA::kBytes
+    __shared__ __attribute__((aligned(1024))) char lds_own[MODE == kMixTail ? WR * WC * (int)sizeof(T)
+                                                           : S::AHEAD       ? 2 * kTileBytes + TA::kBytes
                                                            : S::WAYS > 1 ? S::WAYS * 2 * kTileBytes
                                                                          : 16];
     const int group = S::WAYS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / S::THREADS) : 0;
-    char* lds = S::STATIC_LDS ? lds_own + group * 2 * kTileBytes : lds_given;
+    char* lds = S::STATIC_LDS || MODE == kMixTail ? lds_own + group * 2 * kTileBytes : lds_given;
 
     const int64_t tiles_j = (g.cols + BJ - 1) / BJ;
-    int64_t tiles_i = (g.rows + BI - 1) / BI, ti, tj, split = blockIdx.y;
+    int64_t tiles_i = (g.rows + BI - 1) / BI, ti, tj;
+    [[maybe_unused]] int64_t split = MIX && !TT ? 0 : blockIdx.y;
     if constexpr (MIX && !TT) {
         // the order of the tiles is tile_of's over all experts' units; a panel's tiles are of one expert
-        const int64_t total = uniform(mix_total(g.mix, BI, 0));
-        if (blockIdx.x >= total * tiles_j) return;
-        const int64_t t = xcd_order(blockIdx.x, total * tiles_j);
-        const MixUnit u = mix_unit(g.mix, BI, 0, t / tiles_j);
+        const int64_t total = mix_total(g.mix, BI, 0) * tiles_j;
+        const MixTail tail(g, total);
+        int64_t t = blockIdx.x;
+        if constexpr (MODE == kMixTail) {
+            t /= WI * WJ;
+            if (t >= tail.rest) return;
+            g.part += t * tail.splits * (BI * BJ);
+            g.splits = (int32_t)tail.splits;
+            t += tail.full;
+        } else if (t < tail.full) {
+            t = xcd_order(t, tail.full);
+            g.part = nullptr;
+        } else {
+            const int64_t at = t - tail.full;
+            if (at >= tail.rest * tail.splits) return;
+            t = tail.full + at / tail.splits;
+            split = at % tail.splits;
+            const int64_t tiles = (g.len + kBK - 1) / kBK;
+            g.split_len = (tiles + tail.splits - 1) / tail.splits * kBK;
+            g.part += at * (BI * BJ);
+        }
+        const MixUnit u = mix_unit(g.mix, BI, 0, (int32_t)(t / tiles_j));
         tiles_i = u.units;
         panel_of(t - u.before * tiles_j, tiles_i, tiles_j, &ti, &tj);
         g.rows = u.rows;
@@ -395,7 +442,8 @@ __global__ __launch_bounds__(S::THREADS * S::WAYS) void k_gemm(GemmArgs g)
         c_end = c_begin + (int64_t)steps * kBK < c_end ? c_begin + (int64_t)steps * kBK : c_end;
     }
     const T* b = (const T*)g.b;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x % S::THREADS >> 6);
+    const int wave = MODE == kMixTail ? blockIdx.x % (WI * WJ)
+                                      : __builtin_amdgcn_readfirstlane(threadIdx.x % S::THREADS >> 6);
     const int wi = (wave / WJ) * WR, wj = (wave % WJ) * WC;
     const int lane = threadIdx.x & 63;
 
@@ -419,7 +467,18 @@ __global__ __launch_bounds__(S::THREADS * S::WAYS) void k_gemm(GemmArgs g)
                 for (int q = 0; q < FJ; ++q) acc[p][q] = Mm::mma(fb[s][q], fa[s][p], acc[p][q]);
     };
     // A's planes, the least significant one first, whose sums are scaled into the next one's
-    for (int plane = (TT ? g.planes : 1) - 1; plane >= 0; --plane) {
+    if constexpr (MODE == kMixTail) {
+        static_assert(FI == 1 || MODE != kMixTail, "16 rows");
+        constexpr int kRows = BI / 16 / SUM_WI, kThreads = SUM_WI * WJ * 64;
+        const int row = wave / WJ, sum_wave = row / kRows * WJ + wave % WJ;
+        const float* from = g.part + ((row % kRows) * FJ * kThreads + sum_wave * 64 + lane) * 4;
+#pragma unroll 8
+        for (int s = 0; s < g.splits; ++s)
+#pragma unroll
+            for (int q = 0; q < FJ; ++q)
+                acc[0][q] += *reinterpret_cast<const f32x4*>(from + s * (BI * BJ) + q * (kThreads * 4));
+        g.part = nullptr;
+    } else for (int plane = (TT ? g.planes : 1) - 1; plane >= 0; --plane) {
         const T* a = (const T*)g.a + (TT ? plane * g.plane_stride : 0);
         if constexpr (S::FAST) {
             constexpr int kLoads = TA::kPasses + TB::kPasses;   // of a thread per tile
@@ -569,6 +628,17 @@ __global__ __launch_bounds__(S::THREADS * S::WAYS) void k_gemm(GemmArgs g)
         }
     }
 
+    if constexpr (MODE == kMix && !TT) {
+        if (g.part) {
+            float* to = g.part + threadIdx.x * 4;
+#pragma unroll
+            for (int p = 0; p < FI; ++p)
+#pragma unroll
+                for (int q = 0; q < FJ; ++q) *reinterpret_cast<f32x4*>(to + (p * FJ + q) * (S::THREADS * 4)) = acc[p][q];
+            return;
+        }
+    }
+
     // A lane's values of row i0 + wi + 16 p + li, in groups of 4 (TT) or 8 (NT) neighbouring columns: group k is
     // acc[p][k], or acc[p][2 k] and acc[p][2 k + 1].
     const int li = lane & 15, lg = lane >> 4;
@@ -612,7 +682,7 @@ __global__ __launch_bounds__(S::THREADS * S::WAYS) void k_gemm(GemmArgs g)
     // A wave's results go through its own part of LDS, so that they are stored as whole rows of its block: z, then y.
     if constexpr (!TT) {
         constexpr int N = Vec<T>::N, kVecs = WC / N;
-        char* block = lds + wave * (WR * WC * (int)sizeof(T));
+        char* block = lds + (MODE == kMixTail ? 0 : wave) * (WR * WC * (int)sizeof(T));
         auto put = [&](int p, int k, const float* v) {
             const int r = 16 * p + li;
 #pragma unroll
@@ -712,20 +782,19 @@ struct Flight<T, true> {
     }
 };
 
-// MIX: blockIdx.y is the expert.
+// MIX: blockIdx.y counts the experts that have rows.
 template <typename T, int MF, bool ODD, bool MIX = false>
 __global__ __launch_bounds__(kSkinnyWaves * 64) void k_skinny(GemmArgs g)
 {
     if constexpr (MIX) {
-        const int e = blockIdx.y;
-        const int32_t first = mix_offset(g.mix, e), end = mix_offset(g.mix, e + 1);
-        if (end <= first) return;
-        g.rows = end - first;
-        g.a = (const T*)g.a + first * g.lda;
-        g.b = (const T*)g.b + e * g.mix.w_stride;
-        if (g.bias) g.bias += e * g.cols;
-        if (g.z) g.z = (T*)g.z + first * g.ldz;
-        g.out = (T*)g.out + first * g.ldo;
+        const MixUnit u = mix_unit(g.mix, 16 * MF, 0, blockIdx.y);   // (a unit is all of an expert's rows)
+        if (u.expert < 0) return;
+        g.rows = u.rows;
+        g.a = (const T*)g.a + u.first * g.lda;
+        g.b = (const T*)g.b + u.expert * g.mix.w_stride;
+        if (g.bias) g.bias += u.expert * g.cols;
+        if (g.z) g.z = (T*)g.z + u.first * g.ldz;
+        g.out = (T*)g.out + u.first * g.ldo;
     }
     constexpr int N = Vec<T>::N;
     constexpr int kStep = 4 * N;                     // values of the sum per MFMA step
@@ -971,12 +1040,21 @@ template <typename T, class S, bool MIX = false>
 hipError_t run_gemm(const GemmArgs& g, hipStream_t s)
 {
     int64_t tiles_i = div_up(g.rows, S::BI), splits = g.splits;
-    if (MIX && !S::TT) tiles_i = mix_units(g.rows, g.mix.experts, S::BI, 0);
+    if (MIX && !S::TT) {
+        tiles_i = mix_units(g.rows, g.mix.experts, S::BI, 0);
+        splits = 1;
+    }
     if (MIX && S::TT) splits = mix_units(g.len, g.mix.experts, g.split_len, 1);
-    const int64_t tiles = tiles_i * div_up(g.cols, S::BJ);
+    const int64_t tiles = tiles_i * div_up(g.cols, S::BJ) + (MIX && !S::TT && g.part ? g.mix.size / 2 : 0);
     const int lds = S::STATIC_LDS ? 0 : S::lds_bytes(div_up(g.split_len, 128 / (int)sizeof(T)), sizeof(T));
-    hipLaunchKernelGGL((k_gemm<T, S, MIX>), dim3((unsigned)tiles, (unsigned)splits), dim3(S::THREADS * S::WAYS), lds, s,
-                       g);
+    hipLaunchKernelGGL((k_gemm<T, S, MIX ? kMix : kNoMix>), dim3((unsigned)tiles, (unsigned)splits),
+                       dim3(S::THREADS * S::WAYS), lds, s, g);
+    if constexpr (MIX && !S::TT && S::WAYS == 1 && S::FAST) {
+        using Tail = Shape<false, S::BI, S::BJ, S::BI / 16, S::WJ, false, true>;
+        if (g.part)
+            hipLaunchKernelGGL((k_gemm<T, Tail, kMixTail, S::WI>), dim3((unsigned)(g.mix.size / 4 * Tail::WI * Tail::WJ)),
+                               dim3(64), 0, s, g);
+    }
     return hipGetLastError();
 }
 
@@ -1013,7 +1091,7 @@ hipError_t run_tt(int tile, bool fast_b, const GemmArgs& g, hipStream_t s)
 template <typename T, bool MIX>
 hipError_t run_skinny(const GemmArgs& g, hipStream_t s)
 {
-    const dim3 grid((unsigned)div_up(g.cols, 16), MIX ? (unsigned)g.mix.experts : 1);
+    const dim3 grid((unsigned)div_up(g.cols, 16), MIX ? (unsigned)std::min<int64_t>(g.rows, g.mix.experts) : 1);
     auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kSkinnyWaves * 64), 0, s, g); };
     if constexpr (sizeof(T) == 2) {
         if ((((uintptr_t)g.a | (uintptr_t)g.b) & 2) || ((g.lda | g.ldb | (MIX ? g.mix.w_stride : 0)) & 1)) {

@@ -111,17 +111,25 @@ struct MixPrepareArgs {
     int64_t slope_x, slope_blocks, copy_blocks, weight_blocks;   // workgroups across dz, in all, of x, of one expert's W
 };
 
+// db[e][c]: the sums over expert e's units (mix.size rows) of part [units][cols].
+struct MixSums {
+    Mix mix;
+    const float* part;
+    int64_t cols;
+    float* db;
+};
+
 // per type T (the files experts_*.hip)
 template <typename T>
 struct MixtureOps {
     static hipError_t gemm_nt(int tile, bool fast_a, const GemmArgs& g, hipStream_t s);
-    static hipError_t gemm_tt(int tile, bool fast_b, const GemmArgs& g, hipStream_t s);   // with the join of its parts
+    static hipError_t gemm_tt(int tile, bool fast_b, const GemmArgs& g, hipStream_t s);
+    // the parts of dW (g.part NULL: none) and of db (b.db NULL: none) added up
+    static hipError_t join(const GemmArgs& g, const MixSums& b, hipStream_t s);
     static hipError_t skinny(const GemmArgs& g, hipStream_t s);
     // slope, copy, weights, transpose: those that are wanted; units: of dz, at most
     static hipError_t prepare(const Mix& mix, int64_t units, const SlopeArgs* slope, const SlopeArgs* copy,
                               const SlopeArgs* weights, const TransposeArgs* transpose, int64_t w_out, hipStream_t s);
-    // db[e][c]: the sums of e's units (mix.size rows) over part [units][cols]
-    static hipError_t sums(const Mix& mix, const float* part, int64_t cols, float* db, hipStream_t s);
     // 16-bit layers of up to 128 inputs and outputs, in units of mix.size rows
     static hipError_t narrow_fwd(const GemmArgs& g, bool fast, int64_t units, hipStream_t s);
     static hipError_t narrow_bwd(const NarrowArgs& a, bool fast, int planes, int64_t units, hipStream_t s);

@@ -101,7 +101,7 @@ __global__ __launch_bounds__(kNarrowThreads, 2) void k_narrow_bwd(NarrowArgs a)
     if constexpr (MIX) {
         const MixUnit u = mix_unit(a.mix, a.mix.size, 0, blockIdx.x);
         if (u.expert < 0) return;
-        const int64_t first = u.first + u.unit * a.mix.size, left = u.rows - u.unit * a.mix.size;
+        const int64_t first = u.first + (int64_t)u.unit * a.mix.size, left = u.rows - (int64_t)u.unit * a.mix.size;
         a.rows = left < a.mix.size ? left : a.mix.size;
         a.dy = (const T*)a.dy + first * a.lddy;
         if (a.act != GS_ACT_NONE) a.z = (const T*)a.z + first * a.ldz;
@@ -307,11 +307,11 @@ __global__ __launch_bounds__(kBlock) void k_narrow_join(NarrowArgs a, int parts)
 {
     if constexpr (MIX) {
         const MixUnit u = mix_expert(a.mix, a.mix.size, 0, blockIdx.y);
-        parts = (int)min(u.units, a.mix.limit - u.before);
-        a.part += u.before * narrow_part(a.out, a.in);
+        parts = (int)min((int64_t)u.units, a.mix.limit - u.before);
+        a.part += (int64_t)u.before * narrow_part(a.out, a.in);
         if (a.dw) a.dw = a.dw_f32 ? (void*)((float*)a.dw + u.expert * a.mix.dw_stride)
                                   : (void*)((T*)a.dw + u.expert * a.mix.dw_stride);
-        if (a.db) a.db += u.expert * a.out;
+        if (a.db) a.db += (int64_t)u.expert * a.out;
     }
     __shared__ f32x4 sums[kBlock];
     const int place = threadIdx.x & 15, slice = threadIdx.x >> 4;
@@ -355,7 +355,7 @@ __global__ __launch_bounds__(kNarrowThreads) void k_narrow_fwd(GemmArgs g)
     if constexpr (MIX) {
         const MixUnit u = mix_unit(g.mix, g.mix.size, 0, blockIdx.x);
         if (u.expert < 0) return;
-        const int64_t first = u.first + u.unit * g.mix.size, left = u.rows - u.unit * g.mix.size;
+        const int64_t first = u.first + (int64_t)u.unit * g.mix.size, left = u.rows - (int64_t)u.unit * g.mix.size;
         g.rows = left < g.mix.size ? left : g.mix.size;
         g.a = (const T*)g.a + first * g.lda;
         g.b = (const T*)g.b + u.expert * g.mix.w_stride;
