@@ -17,6 +17,7 @@ namespace {
 constexpr int kDzBlocks = 2048;          // workgroups of dz, about
 constexpr int64_t kNarrowRows = 128;     // of a unit of a narrow layer, at least
 constexpr int64_t kPlaces = 5 * kFillTiles;   // workgroups that the compute units hold at once, of any tile at most
+constexpr int64_t kNarrowForward = 2048; // workgroups of a narrow layer's forward, about
 constexpr int64_t kMostSplits = 8;
 constexpr double kSplitGain = 2.0;       // us that a split of the last tiles has to gain by the plan
 
@@ -98,10 +99,11 @@ int64_t dz_size(int type, int64_t rows, int64_t cols)
     return div_up(std::max(least, div_up(rows * across, kDzBlocks)), least) * least;
 }
 
-int64_t narrow_size(int64_t rows, int64_t in, int64_t out)
+// Rows of a unit of a narrow layer: as many units as there are places for workgroups, those of the experts' ends with them.
+int64_t narrow_size(int64_t rows, int64_t experts, int64_t in, int64_t out, bool backward)
 {
-    const int64_t most = in > 64 && out > 64 ? kNarrowBlocks : 2 * kNarrowBlocks;
-    return std::max(kNarrowRows, div_up(div_up(rows, most), 64) * 64);
+    const int64_t most = backward ? kNarrowBlocks : kNarrowForward;
+    return std::max(kNarrowRows, div_up(div_up(rows, std::max(most / 2, most - experts)), 64) * 64);
 }
 
 bool narrow_taken(int type, int64_t rows, int64_t in, int64_t out) { return rows > kFewRows && narrow(type, in, out); }
@@ -158,7 +160,7 @@ BwdSpace bwd_space(void* base, int type, int act, int64_t rows, int64_t experts,
     Regions r{(char*)base};
     BwdSpace b = {};
     if (narrow(type, in, out)) {
-        b.part = (float*)r.take(units_most(rows, experts, narrow_size(rows, in, out)) * narrow_part((int)out, (int)in) * 4);
+        b.part = (float*)r.take(units_most(rows, experts, narrow_size(rows, experts, in, out, true)) * narrow_part((int)out, (int)in) * 4);
         b.bytes = r.at;
         return b;
     }
@@ -228,7 +230,7 @@ hipError_t experts_fwd(const gs_experts& p, void* y, int64_t ldy, void* z, int64
     g.ldz = ldz;
     g.mix = mix_of(p, 0);
     if (narrow_taken(l.type, l.rows, l.n_in, l.n_out)) {
-        g.mix.size = (int32_t)narrow_size(l.rows, l.n_in, l.n_out);
+        g.mix.size = (int32_t)narrow_size(l.rows, p.experts, l.n_in, l.n_out, false);
         return MixtureOps<T>::narrow_fwd(g, fast_x, units_most(l.rows, p.experts, g.mix.size), s);
     }
     const FwdSpace f = fwd_space(ws, l.type, l.rows, p.experts, l.n_in, l.n_out, !fast_w(p));
@@ -257,7 +259,7 @@ hipError_t experts_bwd(const gs_experts& p, const void* dy, int64_t lddy, const 
     if (narrow(l.type, l.n_in, l.n_out)) {
         NarrowArgs a = {dy,        z,           l.x,  l.w, lddy,  ldz, l.ldx, l.ldw, lddx, lddw, l.rows, (int)l.n_out,
                         (int)l.n_in, l.act, dw_type == GS_F32, dx, dw,    db,  b.part};
-        a.mix = mix_of(p, narrow_size(l.rows, l.n_in, l.n_out));
+        a.mix = mix_of(p, narrow_size(l.rows, p.experts, l.n_in, l.n_out, true));
         a.mix.dw_stride = dw_stride;
         a.mix.limit = units_most(l.rows, p.experts, a.mix.size);
         const bool whole = fast(dy, lddy, l.n_out, l.type) && fast(l.x, l.ldx, l.n_in, l.type) &&

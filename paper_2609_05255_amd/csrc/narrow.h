@@ -94,22 +94,23 @@ __device__ __forceinline__ V finite_of(V v)
 
 // FAST: rows of dy, z and x are whole aligned vectors, and come through buffer loads whose range check turns what lies
 // beyond the matrix into zeros; otherwise they are loaded at any alignment.
-// MIX: a workgroup takes a unit of an expert's rows, with its part at the unit's place.
+// MIX: as many workgroups as an expert has units of rows take its tiles in turn, each with its part at the unit's place.
 template <typename T, int OUT, int IN, int P, bool FAST, bool MIX = false>
 __global__ __launch_bounds__(kNarrowThreads, 2) void k_narrow_bwd(NarrowArgs a)
 {
+    int64_t first_tile = blockIdx.x, tile_step = gridDim.x;
     if constexpr (MIX) {
         const MixUnit u = mix_unit(a.mix, a.mix.size, 0, blockIdx.x);
         if (u.expert < 0) return;
-        const int64_t first = u.first + (int64_t)u.unit * a.mix.size, left = u.rows - (int64_t)u.unit * a.mix.size;
-        a.rows = left < a.mix.size ? left : a.mix.size;
-        a.dy = (const T*)a.dy + first * a.lddy;
-        if (a.act != GS_ACT_NONE) a.z = (const T*)a.z + first * a.ldz;
-        a.x = (const T*)a.x + first * a.ldx;
+        a.rows = u.rows;
+        a.dy = (const T*)a.dy + u.first * a.lddy;
+        if (a.act != GS_ACT_NONE) a.z = (const T*)a.z + u.first * a.ldz;
+        a.x = (const T*)a.x + u.first * a.ldx;
         a.w = (const T*)a.w + u.expert * a.mix.w_stride;
-        if (a.dx) a.dx = (T*)a.dx + first * a.lddx;
+        if (a.dx) a.dx = (T*)a.dx + u.first * a.lddx;
+        first_tile = u.unit;
+        tile_step = u.units;
     }
-    const int64_t first_tile = MIX ? 0 : blockIdx.x, tile_step = MIX ? 1 : gridDim.x;
     constexpr int R = narrow_tile_rows(OUT, IN, P, FAST), VO = OUT / 8, VI = IN / 8;
     constexpr int NO = R * VO / kNarrowThreads, NI = R * VI / kNarrowThreads;   // vectors of a thread
     constexpr int FO = OUT / 32, FI = IN / 32;                                  // fragments of a wave's part of dW
@@ -348,20 +349,22 @@ __global__ __launch_bounds__(kBlock) void k_narrow_join(NarrowArgs a, int parts)
 // from memory in the layout of the MFMAs' fragments, the next rows' while these are worked on, and the results leave
 // through the wave's part of LDS as whole rows. Bound by HBM: 1,000,000 x 128 x 128 in binary16 with gelu and a residual
 // 162 us, 4.7 TB/s (242 in tiles of the general product).
-// MIX: a workgroup takes a unit of an expert's rows.
+// MIX: as many workgroups as an expert has units of rows take its rows in turn.
 template <typename T, int OUT, int IN, bool FAST, bool MIX = false>
 __global__ __launch_bounds__(kNarrowThreads) void k_narrow_fwd(GemmArgs g)
 {
+    int64_t first_block = blockIdx.x, group_step = gridDim.x;
     if constexpr (MIX) {
         const MixUnit u = mix_unit(g.mix, g.mix.size, 0, blockIdx.x);
         if (u.expert < 0) return;
-        const int64_t first = u.first + (int64_t)u.unit * g.mix.size, left = u.rows - (int64_t)u.unit * g.mix.size;
-        g.rows = left < g.mix.size ? left : g.mix.size;
-        g.a = (const T*)g.a + first * g.lda;
+        g.rows = u.rows;
+        g.a = (const T*)g.a + u.first * g.lda;
         g.b = (const T*)g.b + u.expert * g.mix.w_stride;
         if (g.bias) g.bias += u.expert * g.cols;
-        if (g.z) g.z = (T*)g.z + first * g.ldz;
-        g.out = (T*)g.out + first * g.ldo;
+        if (g.z) g.z = (T*)g.z + u.first * g.ldz;
+        g.out = (T*)g.out + u.first * g.ldo;
+        first_block = u.unit;
+        group_step = u.units;
     }
     constexpr int FJ = OUT / 16, KS = IN / 32, kRow = (IN < 64 ? 64 : IN) * 2, kBlock16 = 16 * OUT * 2;
     typedef typename Mma<T>::Frag Frag;
@@ -380,7 +383,7 @@ __global__ __launch_bounds__(kNarrowThreads) void k_narrow_fwd(GemmArgs g)
     for (int c = tid; c < OUT; c += kNarrowThreads) bias[c] = g.bias && c < out ? g.bias[c] : 0.f;
     __syncthreads();
 
-    const int64_t blocks = (g.rows + 15) / 16, step = MIX ? 4 : (int64_t)gridDim.x * 4;
+    const int64_t blocks = (g.rows + 15) / 16, step = group_step * 4;
     Packed next[KS];
     auto fetch = [&](int64_t b) {
         const int64_t r = b * 16 + li < g.rows ? b * 16 + li : g.rows - 1;   // (rows beyond are not stored)
@@ -403,7 +406,7 @@ __global__ __launch_bounds__(kNarrowThreads) void k_narrow_fwd(GemmArgs g)
             for (int s = 0; s < KS; ++s) next[s] = load_any(src + 32 * s, in - 32 * s - lg * 8);
         }
     };
-    const int64_t first = MIX ? wave : (int64_t)blockIdx.x * 4 + wave;
+    const int64_t first = first_block * 4 + wave;
     if (first < blocks) fetch(first);
     for (int64_t b = first; b < blocks; b += step) {
         Frag x[KS];
