@@ -346,32 +346,39 @@ __global__ __launch_bounds__(kBlock) void k_sum_entries(EntriesArgs a)
     __shared__ int32_t keys[kGroups][2];
     const int lane = threadIdx.x & (G - 1), group = threadIdx.x / G;
     const int64_t c = (int64_t)blockIdx.y * kCols + lane * N, left = a.dim - c;
-    const int64_t used = min((int64_t)a.offsets[a.entries], a.count);
     const int64_t w0 = (int64_t)blockIdx.x * kGroups * a.per;
-    const int64_t w1 = w0 + kGroups * a.per < used ? w0 + kGroups * a.per : used;
+    const int64_t w1 = w0 + kGroups * a.per < a.count ? w0 + kGroups * a.per : a.count;
+    const int32_t key_before = w0 > 0 ? a.sorted[w0 - 1] : -1, key_behind = w1 < a.count ? a.sorted[w1] : -1;
     const int64_t p0 = w0 + (int64_t)group * a.per, p1 = p0 + a.per < w1 ? p0 + a.per : w1;
     const T *dy = (const T*)a.dy + (left > 0 ? c : 0), *end = end_of<T>(a.dy, a.lddy, a.count, a.dim);
     int32_t first = -1, key = -1;
     float sum[N] = {};
+    constexpr int kLooks = U / kIndexed;
+    uint32_t row_next[kLooks];
+    int32_t key_next[kLooks];
+    // (positions behind the last one: its row again, and no entry)
+    auto look = [&](int64_t p) {
+#pragma unroll
+        for (int q = 0; q < kLooks; ++q) {
+            const int64_t at = p + q * kIndexed + (lane & (kIndexed - 1)), in = at < p1 ? at : p1 - 1;
+            const uint32_t i = (uint32_t)a.order[in];
+            const int32_t e = a.sorted[in];
+            key_next[q] = at >= p1 || i >= a.count || (uint32_t)e >= a.entries ? -1 : e;
+            row_next[q] = i < a.count ? i : 0;
+        }
+    };
+    if (p0 < p1) look(p0);
     for (int64_t p = p0; p < p1; p += U) {
         Packed v[U];
         int32_t k[U];
 #pragma unroll
-        for (int q = 0; q < U; q += kIndexed) {
-            // (positions behind the last one: its row again, and no entry)
-            const int64_t at = p + q + (lane & (kIndexed - 1)), in = at < p1 ? at : p1 - 1;
-            uint32_t i = (uint32_t)a.order[in];
-            int32_t e = a.sorted[in];
-            if (at >= p1 || i >= a.count || (uint32_t)e >= a.entries) e = -1;
-            i = i < a.count ? i : 0;
-#pragma unroll
-            for (int u = 0; u < kIndexed; ++u) {
-                const uint32_t iu = G == 1 ? i : (uint32_t)__shfl((int)i, u, kIndexed);
-                k[q + u] = G == 1 ? e : __shfl(e, u, kIndexed);
-                const T* row = dy + (int64_t)iu * a.lddy;
-                v[q + u] = get_vec<T, WHOLE>(row, left > 0 ? left : a.dim, end);
-            }
+        for (int u = 0; u < U; ++u) {
+            const int q = u / kIndexed;
+            const uint32_t i = G == 1 ? row_next[q] : (uint32_t)__shfl((int)row_next[q], u % kIndexed, kIndexed);
+            k[u] = G == 1 ? key_next[q] : __shfl(key_next[q], u % kIndexed, kIndexed);
+            v[u] = get_vec<T, WHOLE>(dy + (int64_t)i * a.lddy, left > 0 ? left : a.dim, end);
         }
+        if (p + U < p1) look(p + U);   // under the rows' loads
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (k[u] < 0) continue;
@@ -400,10 +407,8 @@ __global__ __launch_bounds__(kBlock) void k_sum_entries(EntriesArgs a)
         keys[group][1] = key;
     }
     __syncthreads();
-    if (w0 >= w1) return;
-    const bool before = w0 > 0 && a.sorted[w0 - 1] == a.sorted[w0];
-    const bool behind = w1 < used && a.sorted[w1] == a.sorted[w1 - 1];
     const int32_t w_first = keys[0][0];
+    if (w_first < 0) return;   // (rows without an entry are the last ones)
     float* part = a.part + (int64_t)blockIdx.x * 2 * a.dim;
     for (int col = threadIdx.x; col < kCols; col += kBlock) {
         const int64_t cc = (int64_t)blockIdx.y * kCols + col;
@@ -411,26 +416,39 @@ __global__ __launch_bounds__(kBlock) void k_sum_entries(EntriesArgs a)
         int32_t at = w_first;
         float t = 0.f;
         auto finish = [&](bool last) {
-            if (at == w_first && before)
+            if (at == w_first && at == key_before)
                 part[cc] = t;
-            else if (last && behind)
+            else if (last && at == key_behind)
                 part[a.dim + cc] = t;
             else
                 store_entry<T>(a, at, cc, t);
         };
-        for (int g = 0; g < kGroups; ++g) {
-            const int32_t k0 = keys[g][0], k1 = keys[g][1];
-            if (k0 < 0) break;
-            if (k0 != at) {
-                finish(false);
-                at = k0;
-                t = 0.f;
+        constexpr int kFly = kGroups < 8 ? kGroups : 8;   // groups whose sums are read together
+        for (int g0 = 0; g0 < kGroups; g0 += kFly) {
+            int32_t k0[kFly], k1[kFly];
+            float head[kFly], tail[kFly];
+#pragma unroll
+            for (int u = 0; u < kFly; ++u) {
+                k0[u] = keys[g0 + u][0];
+                k1[u] = keys[g0 + u][1];
+                head[u] = sums[g0 + u][0][col];
+                tail[u] = sums[g0 + u][1][col];
             }
-            t += sums[g][0][col];
-            if (k1 != k0) {
-                finish(false);
-                at = k1;
-                t = sums[g][1][col];
+            if (k0[0] < 0) break;
+#pragma unroll
+            for (int u = 0; u < kFly; ++u) {
+                if (k0[u] < 0) continue;
+                if (k0[u] != at) {
+                    finish(false);
+                    at = k0[u];
+                    t = 0.f;
+                }
+                t += head[u];
+                if (k1[u] != k0[u]) {
+                    finish(false);
+                    at = k1[u];
+                    t = tail[u];
+                }
             }
         }
         finish(true);
@@ -466,14 +484,13 @@ __global__ __launch_bounds__(kBlock) void k_join_entries(EntriesArgs a, int64_t 
         return;
     }
     __shared__ float s[kJoinSlices][kJoinCols];
-    const int64_t used = min((int64_t)a.offsets[a.entries], a.count);
     const int64_t w0 = (int64_t)blockIdx.x * span, w1 = w0 + span;
-    if (w1 >= used) return;
-    const int32_t key = a.sorted[w1 - 1];
-    if (key != a.sorted[w1]) return;                                       // it ends here
-    if (a.sorted[w0] == key && w0 > 0 && a.sorted[w0 - 1] == key) return;   // it began before
-    if (key < 0 || key >= a.entries) return;
-    const int64_t last = min((int64_t)a.offsets[key + 1] - 1, used - 1) / span;
+    if (w1 >= a.count) return;
+    const int32_t key = a.sorted[w1 - 1], behind = a.sorted[w1], first = a.sorted[w0];
+    const int32_t before = w0 > 0 ? a.sorted[w0 - 1] : -1;
+    if (key != behind || key < 0 || key >= a.entries) return;   // it ends here, or is none
+    if (first == key && before == key) return;                  // it began before
+    const int64_t last = min((int64_t)a.offsets[key + 1] - 1, a.count - 1) / span;
     const int col = threadIdx.x % kJoinCols, slice = threadIdx.x / kJoinCols;
     for (int64_t c0 = first_col; c0 < end_col; c0 += kJoinCols) {
         const int64_t c = c0 + col;
@@ -494,7 +511,10 @@ __global__ __launch_bounds__(kBlock) void k_join_entries(EntriesArgs a, int64_t 
     }
 }
 
-constexpr int64_t kEntryBlocks = 256 * 8;   // workgroups of k_sum_entries, about
+// Workgroups of k_sum_entries, about; four times as many of rows of up to 4 vectors, whose lanes then look up positions
+// that lie closer together (us with 2,048 and 8,192: 10,000,000 x 8 in binary16 424 and 253, 3,000,000 x 16 119 and 113,
+// but 3,000,000 x 64 103 and 105, 1,000,000 x 128 in fp32 112 and 132).
+constexpr int64_t kEntryBlocks = 256 * 8;
 
 struct EntriesPlan {
     int lanes;
@@ -505,7 +525,7 @@ EntriesPlan entries_plan(int type, int64_t count, int64_t dim)
 {
     EntriesPlan p;
     p.lanes = row_lanes(div_up(dim, type == GS_F32 ? 4 : 8));
-    const int64_t groups = kBlock / p.lanes, all = kEntryBlocks * groups;
+    const int64_t groups = kBlock / p.lanes, all = kEntryBlocks * (p.lanes < 8 ? 4 : 1) * groups;
     p.per = std::max<int64_t>(kEntryRows, div_up(div_up(count, all), kEntryRows) * kEntryRows);
     p.span = p.per * groups;
     p.parts = std::max<int64_t>(1, div_up(count, p.span));
