@@ -657,13 +657,13 @@ typedef struct gs_experts {
     int64_t experts;
     int64_t w_stride;         /* elements from an expert's w to the next one's */
     const int32_t* offsets;   /* [experts + 1] device array: expert e's rows are offsets[e] .. offsets[e + 1] - 1,
-                               * as gs_sort_rows writes it (never falling, offsets[experts] <= rows) */
+                               * as gs_sort_rows writes it, or a part of that (never falling, within the rows) */
 } gs_experts;
 
 /*
  * gs_experts_fwd -- z = x w_e^T + bias_e, y = act(z) for the rows of every expert e, as
- * gs_linear_fwd does for one layer. Rows from offsets[experts] on are neither read nor
- * written, and the weights of an expert without rows are not read.
+ * gs_linear_fwd does for one layer. Rows before offsets[0] and from offsets[experts] on are
+ * neither read nor written, and the weights of an expert without rows are not read.
  * Limits: those of gs_linear_fwd, 1 <= experts <= GS_MAX_EXPERTS (GS_ERR_UNSUPPORTED if
  * rows times n_out or n_in exceed the grid: about 2^36 values).
  * workspace: gs_experts_workspace_size bytes, 256-byte aligned; NULL where that is 0.

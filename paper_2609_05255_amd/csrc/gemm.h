@@ -402,6 +402,7 @@ __global__ __launch_bounds__(MODE == kMixTail ? 64 : S::THREADS * S::WAYS) void 
             g.part += at * (BI * BJ);
         }
         const MixUnit u = mix_unit(g.mix, BI, 0, (int32_t)(t / tiles_j));
+        if (u.expert < 0) return;
         tiles_i = u.units;
         panel_of(t - u.before * tiles_j, tiles_i, tiles_j, &ti, &tj);
         g.rows = u.rows;

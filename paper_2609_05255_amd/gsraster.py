@@ -566,29 +566,44 @@ def _one_device(*tensors):
     """The launches go to the current device: all tensors (None: left out) have to be there."""
     device = torch.cuda.current_device()
     for t in tensors:
-        if t is not None and t.is_cuda and t.get_device() != device:
+        if t is not None and t.get_device() != device and t.is_cuda:
             raise ValueError("a tensor on %s while the current device is %d" % (t.device, device))
+
+
+def _order_array(name):
+    def get(self):
+        return self._tensors[name]
+
+    def put(self, t):
+        n = self.groups + 1 if name == "offsets" else self.count
+        address = None if t is None else _array(name, t, (n,), torch.int32)
+        devices = {o.device for o in (*self._tensors.values(), t) if o is not None}
+        if len(devices) > 1:
+            raise ValueError("%s: the arrays of an order are on one device" % name)
+        self._tensors[name] = t
+        setattr(self._arrays, name, address)
+
+    return property(get, put)
 
 
 class RowOrder:
     """The order of `count` positions by their group (gs_row_order): int32 tensors order, sorted, place and offsets,
     which gs_sort_rows fills. sorted is what gs_embedding_bwd needs, place what rows on their way back from experts do;
-    either may be left out."""
+    either may be left out. A tensor may be put in the place of one of them; its storage may not change after that."""
+
+    order, sorted = _order_array("order"), _order_array("sorted")
+    place, offsets = _order_array("place"), _order_array("offsets")
 
     def __init__(self, count: int, groups: int, device="cuda", sorted: bool = True, place: bool = True):
-        ints = lambda n: torch.empty(n, dtype=torch.int32, device=device)  # noqa: E731
         self.count, self.groups = int(count), int(groups)
+        self._tensors, self._arrays = dict.fromkeys(("order", "sorted", "place", "offsets")), RowOrderArrays()
+        self._arrays.count, self._arrays.groups = self.count, self.groups
+        ints = lambda n: torch.empty(n, dtype=torch.int32, device=device)  # noqa: E731
         self.order, self.offsets = ints(self.count), ints(self.groups + 1)
-        self.sorted = ints(self.count) if sorted else None
-        self.place = ints(self.count) if place else None
-
-    def arrays(self) -> RowOrderArrays:
-        n, i32 = self.count, torch.int32
-        _one_device(self.order, self.sorted, self.place, self.offsets)
-        return RowOrderArrays(n, self.groups, _array("order", self.order, (n,), i32),
-                              None if self.sorted is None else _array("sorted", self.sorted, (n,), i32),
-                              None if self.place is None else _array("place", self.place, (n,), i32),
-                              _array("offsets", self.offsets, (self.groups + 1,), i32))
+        if sorted:
+            self.sorted = ints(self.count)
+        if place:
+            self.place = ints(self.count)
 
 
 def gs_sort_rows_workspace_size(order: RowOrder) -> int:
@@ -602,9 +617,9 @@ def gs_sort_rows(group_of, order: RowOrder, workspace=None, stream=None):
     values outside [0, order.groups) are no group."""
     if group_of.numel() != order.count:
         raise ValueError("group_of: %d values, %d expected" % (group_of.numel(), order.count))
-    _one_device(group_of, workspace)
+    _one_device(group_of, order.offsets, workspace)
     ws, ws_bytes = _space(workspace)
-    _check(lib().gs_sort_rows(_array("group_of", group_of, group_of.shape, torch.int32), C.byref(order.arrays()), ws,
+    _check(lib().gs_sort_rows(_array("group_of", group_of, group_of.shape, torch.int32), C.byref(order._arrays), ws,
                               ws_bytes, _stream(stream)))
 
 
@@ -634,12 +649,12 @@ def gs_embedding_bwd(dy, order: RowOrder, scale: float, dtable, workspace, strea
     rows, dim = _shape("dy", dy)
     if rows != order.count:
         raise ValueError("dy: %d rows, %d sorted" % (rows, order.count))
-    _one_device(dy, dtable, workspace)
+    _one_device(dy, order.offsets, dtable, workspace)
     pdy, lddy = _matrix("dy", dy, rows, dim, dy.dtype)
     out_type = torch.float32 if dtable.dtype == torch.float32 else dy.dtype
     pdt, lddt = _matrix("dtable", dtable, order.groups, dim, out_type)
     ws, ws_bytes = _space(workspace)
-    _check(lib().gs_embedding_bwd(_type_id(dy), dim, pdy, lddy, C.byref(order.arrays()), scale, pdt, lddt,
+    _check(lib().gs_embedding_bwd(_type_id(dy), dim, pdy, lddy, C.byref(order._arrays), scale, pdt, lddt,
                                   TYPE_IDS[out_type], ws, ws_bytes, _stream(stream)))
 
 
@@ -681,21 +696,21 @@ def gs_dispatch_fwd(x, order: RowOrder, xs, stream=None):
     """xs[p] = x[order[p] // k]: x [rows][dim] copied to where its k choices are sorted; xs [order.count][dim], rows
     behind the last place in use stay as they are."""
     rows, dim = _shape("x", x)
-    _one_device(x, xs)
+    _one_device(x, order.offsets, xs)
     px, ldx = _matrix("x", x, rows, dim, x.dtype)
     pxs, ldxs = _matrix("xs", xs, order.count, dim, x.dtype)
-    _check(lib().gs_dispatch_fwd(_type_id(x), rows, dim, px, ldx, C.byref(order.arrays()), pxs, ldxs, _stream(stream)))
+    _check(lib().gs_dispatch_fwd(_type_id(x), rows, dim, px, ldx, C.byref(order._arrays), pxs, ldxs, _stream(stream)))
 
 
 def gs_dispatch_bwd(dxs, order: RowOrder, dx, add=None, stream=None):
     """dx[i] = the sum of dxs over the places of row i's choices, plus `add`, a gradient of dx's shape."""
     rows, dim = _shape("dx", dx)
     t = dx.dtype
-    _one_device(dxs, dx, add)
+    _one_device(dxs, order.offsets, dx, add)
     ps, lds = _matrix("dxs", dxs, order.count, dim, t)
     pa, lda = (None, 0) if add is None else _matrix("add", add, rows, dim, t)
     pd, ldd = _matrix("dx", dx, rows, dim, t)
-    _check(lib().gs_dispatch_bwd(_type_id(dx), rows, dim, ps, lds, C.byref(order.arrays()), pa, lda, pd, ldd,
+    _check(lib().gs_dispatch_bwd(_type_id(dx), rows, dim, ps, lds, C.byref(order._arrays), pa, lda, pd, ldd,
                                  _stream(stream)))
 
 
@@ -703,11 +718,11 @@ def gs_combine_fwd(ys, order: RowOrder, weight, y, residual=None, stream=None):
     """y[i] = the sum over row i's choices of weight (float32 [rows][k]) times their rows of ys, plus the residual."""
     rows, dim = _shape("y", y)
     t = y.dtype
-    _one_device(ys, weight, y, residual)
+    _one_device(ys, order.offsets, weight, y, residual)
     ps, lds = _matrix("ys", ys, order.count, dim, t)
     pr, ldr = (None, 0) if residual is None else _matrix("residual", residual, rows, dim, t)
     py, ldy = _matrix("y", y, rows, dim, t)
-    _check(lib().gs_combine_fwd(_type_id(y), rows, dim, ps, lds, C.byref(order.arrays()),
+    _check(lib().gs_combine_fwd(_type_id(y), rows, dim, ps, lds, C.byref(order._arrays),
                                 _choices("weight", weight, rows, order), pr, ldr, py, ldy, _stream(stream)))
 
 
@@ -716,11 +731,11 @@ def gs_combine_bwd(dy, ys, order: RowOrder, weight, dys, dweight, stream=None):
     (float32 [rows][k])."""
     rows, dim = _shape("dy", dy)
     t = dy.dtype
-    _one_device(dy, ys, weight, dys, dweight)
+    _one_device(dy, ys, order.offsets, weight, dys, dweight)
     pdy, lddy = _matrix("dy", dy, rows, dim, t)
     ps, lds = _matrix("ys", ys, order.count, dim, t)
     pd, ldd = _matrix("dys", dys, order.count, dim, t)
-    _check(lib().gs_combine_bwd(_type_id(dy), rows, dim, pdy, lddy, ps, lds, C.byref(order.arrays()),
+    _check(lib().gs_combine_bwd(_type_id(dy), rows, dim, pdy, lddy, ps, lds, C.byref(order._arrays),
                                 _choices("weight", weight, rows, order), pd, ldd,
                                 _choices("dweight", dweight, rows, order), _stream(stream)))
 

@@ -212,6 +212,27 @@ def test_parts_of_the_gradients(rows, n_in, n_out, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,n_in,n_out", [(30, 64, 64), (900, 64, 96), (900, 264, 144)])
+def test_some_of_the_experts(rows, n_in, n_out, dtype):
+    """Offsets that begin behind the first row: the experts of a part of the order."""
+    d = make(rows, 6, n_in, n_out, dtype, 13, "even")
+    a, b = 2, 5
+    first, last = d["ends"][a], d["ends"][b]
+    y, z = forward(d, "silu")
+    dx, dw, db = backward(d, "silu", torch.float32)
+    part = dict(d, w=d["w"][a:b], b=d["b"][a:b], offsets=d["offsets"][a:b + 1], ends=d["ends"][a:b + 1])
+    y2, z2 = forward(part, "silu")
+    dx2, dw2, db2 = backward(part, "silu", torch.float32)
+    for whole, some in ((y, y2), (z, z2), (dx, dx2)):
+        assert torch.isnan(some[:first]).all() and torch.isnan(some[last:]).all()
+        # (another number of tiles may be summed in another order)
+        near = (whole[first:last].double() - some[first:last].double()).abs()
+        assert (near <= 4 * UNIT[dtype] * whole[first:last].double().abs() + 64 * U32).all()
+    check_forward(part, "silu", y2, z2)
+    check_backward(part, "silu", dx2, dw2, db2)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("n_in,n_out", [(64, 64), (264, 144)])
 @pytest.mark.parametrize("rows", [0, 50])
 def test_no_rows(rows, n_in, n_out, dtype):
