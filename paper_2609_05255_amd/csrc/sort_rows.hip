@@ -83,8 +83,8 @@ __global__ __launch_bounds__(THREADS) void k_keys_count(KeysPass a)
 {
     constexpr int R = 1 << BITS;
     // 16 copies of the counts, so that few lanes of an instruction meet on the counter of a frequent digit
-    __shared__ uint32_t h[16][R];
-    for (int k = threadIdx.x; k < 16 * R; k += THREADS) (&h[0][0])[k] = 0;
+    __shared__ uint32_t h[16][R + 1];   // (the copies of a digit in different banks)
+    for (int k = threadIdx.x; k < 16 * (R + 1); k += THREADS) (&h[0][0])[k] = 0;
     const int copy = ((threadIdx.x >> 6) & 3) * 4 + (threadIdx.x & 3);
     const int64_t base = (int64_t)blockIdx.x * (THREADS * ITEMS);
     uint32_t k[ITEMS];
@@ -169,17 +169,67 @@ __device__ __forceinline__ void sum_rows(const uint32_t* table, int64_t rows, in
     }
 }
 
+// A digit's keys in all workgroups, and in those before `block`, added to total[R] and before[R] (cleared beforehand): the
+// counts of groups of workgroups and then those of the workgroup's own group, or with few workgroups all of them. Four
+// digits of a thread and every slice-th row; the rows of both kinds are under way together.
+template <int R, int THREADS>
+__device__ __forceinline__ void add_rows(const KeysPass& a, uint32_t* total, uint32_t* before)
+{
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    constexpr int kQuads = R / 4, kSlices = THREADS / kQuads, kFly = 4;
+    const int quad = threadIdx.x % kQuads, slice = threadIdx.x / kQuads;
+    const int64_t mine = a.sup ? blockIdx.x / a.group : blockIdx.x, first = a.sup ? mine * a.group : 0;
+    const uint32_t* sums = (a.sup ? a.sup : a.hist) + quad * 4;
+    const uint32_t* own = a.hist + first * R + quad * 4;
+    const int64_t rows = a.sup ? (gridDim.x + a.group - 1) / a.group : gridDim.x, left = a.sup ? blockIdx.x - first : 0;
+    u32x4 t = {0, 0, 0, 0}, b = {0, 0, 0, 0};
+    for (int64_t r0 = slice; r0 < rows || r0 < left; r0 += kSlices * kFly) {
+        u32x4 v[kFly], w[kFly];
+#pragma unroll
+        for (int u = 0; u < kFly; ++u) {
+            const int64_t r = r0 + u * kSlices;
+            v[u] = r < rows ? *reinterpret_cast<const u32x4*>(sums + r * R) : u32x4{0, 0, 0, 0};
+            w[u] = r < left ? *reinterpret_cast<const u32x4*>(own + r * R) : u32x4{0, 0, 0, 0};
+        }
+#pragma unroll
+        for (int u = 0; u < kFly; ++u) {
+            t += v[u];
+            b += w[u];
+            if (r0 + u * kSlices < mine) b += v[u];
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+#pragma unroll
+        for (int d = kQuads; d < 64; d <<= 1) {
+            t[e] += (uint32_t)__shfl_xor((int)t[e], d, 64);
+            b[e] += (uint32_t)__shfl_xor((int)b[e], d, 64);
+        }
+        if (kQuads >= 64 || (threadIdx.x & 63) < kQuads) {
+            atomicAdd(&total[quad * 4 + e], t[e]);
+            atomicAdd(&before[quad * 4 + e], b[e]);
+        }
+    }
+}
+
 // (two workgroups on a compute unit: 64 registers)
 template <int BITS, int ITEMS, int THREADS>
 __global__ __launch_bounds__(THREADS, THREADS == kThreads ? 8 : 4) void k_keys_move(KeysPass a)
 {
-    constexpr int R = 1 << BITS, kTile = THREADS * ITEMS, kSlices = sum_slices(R, THREADS), kSums = kSlices * R;
+    constexpr int R = 1 << BITS, kTile = THREADS * ITEMS;
+    // Many digits: the rows' sums are tables of each slice of threads, up to three (meeting on counters in LDS, and with the
+    // registers for all rows at once, a sort of 3,000,000 keys takes 74 us instead of 61). Few: they meet in LDS.
+    constexpr bool kTables = R >= 256;
+    constexpr int kSlices = sum_slices(R, THREADS), kSums = kTables ? kSlices * R : R;
     constexpr int kWaves = THREADS / 64, kEach = R > THREADS ? R / THREADS : 1;   // digits of a thread, neighbours
     static_assert(ITEMS * 64 < 65536 && kTile < 65536, "counts of 16 bits");
     __shared__ uint16_t counts[kWaves][R];         // of each wave, then the first place of its keys of each digit
     __shared__ uint32_t start[R];                  // global place of a digit's first key, less its place in the workgroup
-    // the rows' sums (up to three tables), then the keys in their order, then the values
-    __shared__ __attribute__((aligned(16))) uint32_t buf[kTile > 3 * kSums ? kTile : 3 * kSums];
+    // keys of a digit: all, and those of the workgroups before; then the workgroup's keys in their order, then the values
+    constexpr int kLds = kTables ? 3 * kSums : 2 * kSums + kTile;
+    __shared__ __attribute__((aligned(16))) uint32_t buf_sums[kLds > kTile ? kLds : kTile];
+    uint32_t *totals = buf_sums, *before0 = buf_sums + kSums, *before1 = before0 + kSums;
+    uint32_t* buf = kTables ? buf_sums : buf_sums + 2 * kSums;
     __shared__ uint32_t lds[kWaves];
     const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
     const int64_t base = (int64_t)blockIdx.x * kTile;
@@ -189,36 +239,40 @@ __global__ __launch_bounds__(THREADS, THREADS == kThreads ? 8 : 4) void k_keys_m
 #pragma unroll
     for (int k = 0; k < ITEMS; ++k) key[k] = at0 + k * 64 < n ? pass_key(a, base + at0 + k * 64) : 0;
     for (int k = t; k < kWaves * R; k += THREADS) (&counts[0][0])[k] = 0;
-    uint32_t *totals = buf, *before0 = buf + kSums, *before1 = before0 + kSums;
-    if (a.sup) {
-        const int64_t mine = blockIdx.x / a.group;
-        sum_rows<R, THREADS>(a.sup, (gridDim.x + a.group - 1) / a.group, mine, totals, before0);
-        const int64_t left = blockIdx.x - mine * a.group;
-        sum_rows<R, THREADS>(a.hist + mine * a.group * R, left, left, nullptr, before1);
+    if constexpr (kTables) {
+        if (a.sup) {
+            const int64_t mine = blockIdx.x / a.group, left = blockIdx.x - mine * a.group;
+            sum_rows<R, THREADS>(a.sup, (gridDim.x + a.group - 1) / a.group, mine, totals, before0);
+            sum_rows<R, THREADS>(a.hist + mine * a.group * R, left, left, nullptr, before1);
+        } else {
+            sum_rows<R, THREADS>(a.hist, gridDim.x, blockIdx.x, totals, before0);
+        }
+        __syncthreads();
     } else {
-        sum_rows<R, THREADS>(a.hist, gridDim.x, blockIdx.x, totals, before0);
+        for (int k = t; k < 2 * R; k += THREADS) totals[k] = 0;
+        __syncthreads();
+        add_rows<R, THREADS>(a, totals, before0);
     }
-    __syncthreads();
     rank_slice<BITS, ITEMS>(key, a.shift, n - at0, counts[wave], rank);
-    uint32_t total[kEach] = {}, before[kEach] = {}, here[kEach] = {}, totals_here = 0, heres_here = 0;
+    uint32_t here[kEach] = {}, total[kEach] = {}, before[kEach] = {}, all = 0, all_here = 0;
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < kEach; ++k) {
         const int d = t * kEach + k;
         if (d >= R) break;
 #pragma unroll
-        for (int q = 0; q < kSlices; ++q) {
+        for (int q = 0; q < (kTables ? kSlices : 1); ++q) {
             total[k] += totals[q * R + d];
             before[k] += before0[q * R + d];
-            if (a.sup) before[k] += before1[q * R + d];
+            if (kTables && a.sup) before[k] += before1[q * R + d];
         }
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) here[k] += counts[w][d];
-        totals_here += total[k];
-        heres_here += here[k];
+        all += total[k];
+        all_here += here[k];
     }
-    uint32_t first = scan_before<THREADS>(totals_here, lds);   // global place of the digit's first key
-    uint32_t local = scan_before<THREADS>(heres_here, lds);    // place in the workgroup
+    uint32_t first = scan_before<THREADS>(all, lds);      // global place of the digit's first key
+    uint32_t local = scan_before<THREADS>(all_here, lds);   // place in the workgroup
 #pragma unroll
     for (int k = 0; k < kEach; ++k) {
         const int d = t * kEach + k;
@@ -235,7 +289,7 @@ __global__ __launch_bounds__(THREADS, THREADS == kThreads ? 8 : 4) void k_keys_m
         first += total[k];
         local += here[k];
     }
-    __syncthreads();   // (and the sums in buf have been read)
+    __syncthreads();
     uint32_t val[ITEMS];
 #pragma unroll
     for (int k = 0; k < ITEMS; ++k) {
