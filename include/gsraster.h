@@ -621,7 +621,8 @@ gs_status gs_route_fwd(int32_t type, int64_t rows, int64_t experts, int32_t k, c
  * (not read for choices that are -1); logits, expert and weight as gs_route_fwd took and wrote them.
  * With inner = sum of dweight weight: normalised, weight (dweight - inner) at the chosen
  * experts and 0 elsewhere (logits: not read, may be NULL); otherwise p (dweight - inner)
- * at these and -p inner elsewhere, p the softmax of the row. dlogits: [rows][experts].
+ * at these and -p inner elsewhere, p the softmax of the row. dlogits: [rows][experts], or
+ * the logits themselves, which it then replaces.
  */
 gs_status gs_route_bwd(int32_t type, int64_t rows, int64_t experts, int32_t k, const float* dweight, const void* logits,
                        int64_t ldl, const int32_t* expert, const float* weight, int32_t normalise, void* dlogits,
@@ -637,6 +638,7 @@ gs_status gs_route_bwd(int32_t type, int64_t rows, int64_t experts, int32_t k, c
  * gs_combine_fwd: y[i] = sum over j of weight[i][j] ys[place[i k + j]] [+ residual[i]].
  * gs_combine_bwd: dys[p] = weight[order[p]] dy[order[p] / k], dweight[i][j] = dy[i] . ys[place[i k + j]], 0 for no
  * expert (the residual's gradient is dy itself).
+ * dx may be add itself, y the residual, dys ys (whose rows in use it then replaces).
  * weight, dweight: [rows][k] fp32. Limits: 0 <= rows, count < 2^31, 1 <= dim <= GS_MAX_DIM.
  */
 gs_status gs_dispatch_fwd(int32_t type, int64_t rows, int64_t dim, const void* x, int64_t ldx, const gs_row_order* order,
@@ -655,7 +657,7 @@ gs_status gs_combine_bwd(int32_t type, int64_t rows, int64_t dim, const void* dy
 typedef struct gs_experts {
     gs_linear layer;          /* rows: those of x, y, ...; w: the first expert's; bias: [experts][n_out], or NULL */
     int64_t experts;
-    int64_t w_stride;         /* elements from an expert's w to the next one's */
+    int64_t w_stride;         /* elements from an expert's w to the next one's (0: all have the same) */
     const int32_t* offsets;   /* [experts + 1] device array: expert e's rows are offsets[e] .. offsets[e + 1] - 1,
                                * as gs_sort_rows writes it, or a part of that (never falling, within the rows) */
 } gs_experts;

@@ -593,11 +593,11 @@ class RowOrder:
 
     order, sorted = _order_array("order"), _order_array("sorted")
     place, offsets = _order_array("place"), _order_array("offsets")
+    count, groups = property(lambda self: self._arrays.count), property(lambda self: self._arrays.groups)
 
     def __init__(self, count: int, groups: int, device="cuda", sorted: bool = True, place: bool = True):
-        self.count, self.groups = int(count), int(groups)
         self._tensors, self._arrays = dict.fromkeys(("order", "sorted", "place", "offsets")), RowOrderArrays()
-        self._arrays.count, self._arrays.groups = self.count, self.groups
+        self._arrays.count, self._arrays.groups = int(count), int(groups)
         ints = lambda n: torch.empty(n, dtype=torch.int32, device=device)  # noqa: E731
         self.order, self.offsets = ints(self.count), ints(self.groups + 1)
         if sorted:

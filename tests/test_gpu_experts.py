@@ -317,3 +317,15 @@ def test_long_rows_of_weights():
     y = torch.full((2, n_out), NAN, dtype=torch.bfloat16, device="cuda")
     gs.gs_experts_fwd(x, offsets, w, None, y)
     assert (y[0] == 1).all() and (y[1] == 3).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,n_in,n_out", [(20, 96, 40), (700, 64, 96), (900, 264, 144), (900, 133, 61)])
+def test_experts_with_the_same_weights(rows, n_in, n_out, dtype):
+    """Weights a stride of 0 apart."""
+    d = make(rows, 5, n_in, n_out, dtype, 21, "even")
+    same = dict(d, w=d["w"][:1].expand(5, n_out, n_in))
+    whole = dict(d, w=same["w"].contiguous())
+    for a, b in zip((*forward(same, "silu"), *backward(same, "silu", torch.float32)),
+                    (*forward(whole, "silu"), *backward(whole, "silu", torch.float32))):
+        assert torch.equal(a.nan_to_num(nan=7), b.nan_to_num(nan=7))

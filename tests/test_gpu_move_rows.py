@@ -194,3 +194,20 @@ def test_a_long_sorted_matrix():
     y, w = torch.empty_like(x), torch.full((rows, k), 0.5, device="cuda")
     gs.gs_combine_fwd(xs, o, w, y)
     assert torch.equal(y, x)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,k,dim", [(1, 1, 1), (33, 2, 37), (500, 3, 64), (40, 5, 1001), (20_011, 2, 24)])
+def test_results_in_the_place_of_an_operand(rows, k, dim, dtype):
+    """A sum's addend and a combination's rows may be replaced by the result."""
+    o, used = make_order(rows, k, 7, 11)
+    ys, x, w = normal(1, rows * k, dim, dtype=dtype), normal(2, rows, dim, dtype=dtype), normal(3, rows, k)
+    y, dx, dys, dw = torch.empty_like(x), torch.empty_like(x), ys.clone(), torch.empty_like(w)
+    gs.gs_combine_fwd(ys, o, w, y, residual=x)
+    gs.gs_dispatch_bwd(ys, o, dx, add=x)
+    gs.gs_combine_bwd(x, ys, o, w, dys, dw)
+    a, b, c, dw2 = x.clone(), x.clone(), ys.clone(), torch.empty_like(w)
+    gs.gs_combine_fwd(ys, o, w, a, residual=a)
+    gs.gs_dispatch_bwd(ys, o, b, add=b)
+    gs.gs_combine_bwd(x, c, o, w, c, dw2)
+    assert torch.equal(a, y) and torch.equal(b, dx) and torch.equal(c, dys) and torch.equal(dw2, dw)

@@ -182,3 +182,32 @@ def test_no_rows():
     forward(torch.empty(0, 8, device="cuda"), 2, True)
     gs.gs_route_bwd(torch.empty(0, 2, device="cuda"), None, torch.empty(0, 2, dtype=torch.int32, device="cuda"),
                     torch.empty(0, 2, device="cuda"), torch.empty(0, 8, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("experts", [1, 5, 37, 64, 600])
+def test_gradient_in_the_place_of_the_logits(experts, dtype):
+    l = make(203, experts, dtype, 8)
+    k = min(experts, 6)
+    expert, weight = forward(l, k, False)
+    dw, dl = torch.randn(203, k, device="cuda"), torch.empty_like(l)
+    gs.gs_route_bwd(dw, l, expert, weight, dl, normalise=False)
+    gs.gs_route_bwd(dw, l, expert, weight, l, normalise=False)
+    assert torch.equal(l, dl)
+
+
+def test_a_long_matrix_of_logits():
+    """Rows that begin more than 2^31 values behind the first."""
+    rows, experts = 2 ** 25 + 3, 72
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("4.8 GB of logits")
+    l = torch.zeros(rows, experts, dtype=torch.float16, device="cuda")
+    l[-1, 70], l[-1, 3] = 2.0, 1.0
+    expert, weight = forward(l, 2, True)
+    assert expert[-1].tolist() == [70, 3] and expert[0].tolist() == [0, 1] and expert[-2].tolist() == [0, 1]
+    last = forward(l[-1:], 2, True)[1]
+    dw = torch.zeros(rows, 2, device="cuda")
+    dw[-1, 0] = 1.0
+    gs.gs_route_bwd(dw, None, expert, weight, l)
+    assert torch.equal(weight[-1:], last) and int(torch.count_nonzero(l)) == 2
+    assert float(l[-1, 70]) > 0 > float(l[-1, 3])

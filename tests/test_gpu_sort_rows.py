@@ -105,3 +105,19 @@ def test_other_stream():
     gs.gs_sort_rows(v, o, ws, stream=s)
     s.synchronize()
     assert torch.equal(o.order.cpu().long(), sort_rows(v, 1000)[0])
+
+
+@pytest.mark.parametrize("groups", [16, 1_000_000])
+def test_many_positions(groups):
+    """300 million positions: more than the rest of the tests has in all, checked on the GPU."""
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("15 GB")
+    count = 300_000_007
+    v = torch.randint(-1, groups, (count,), dtype=torch.int32, device="cuda")
+    o = run(v, groups, place=False)
+    key = torch.where(v < 0, groups, v)
+    assert torch.equal(key[o.order.long()], o.sorted)
+    rising = o.sorted[1:] > o.sorted[:-1]
+    assert ((o.order[1:] > o.order[:-1]) & (o.sorted[1:] == o.sorted[:-1]) | rising).all()
+    counts = torch.bincount(key, minlength=groups + 1)
+    assert torch.equal(o.offsets[1:].long(), counts[:-1].cumsum(0)) and int(o.offsets[0]) == 0
