@@ -13,7 +13,7 @@
 // shares, silu, backward 179 and 179, forward with z 131 and 134; 16,384 x 2,048 -> 2,048 in bfloat16, 8 experts, gelu,
 // forward with z 171 (of even shares 151, one expert 136) and 154, backward with fp32 dW 647 and 547; 50,000 x 256 -> 512 in
 // binary16, 16 experts, backward 153 and 154; 5,003 x 333 -> 215 in fp32, 7 experts, backward 45 and 45; 8 rows of
-// 2,048 -> 2,048 in bfloat16 by five of 16 experts 15.3 (42 MB of weights at 2.7 TB/s).
+// 2,048 -> 2,048 in bfloat16 by five of 16 experts 11.3 (42 MB of weights at 3.7 TB/s).
 #include "linear_plan.h"
 
 namespace gsr {

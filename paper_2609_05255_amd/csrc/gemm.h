@@ -751,6 +751,12 @@ __global__ __launch_bounds__(MODE == kMixTail ? 64 : S::THREADS * S::WAYS) void 
 // further than these, so never beyond a word that holds a value) and shifted: one row of 4,095 x 4,096 in bfloat16 takes
 // 12.6 us, 16 rows 16.3; loaded as they are 17.3 and 28.8.
 constexpr int kSkinnyWaves = 8;
+// A mixture's with more workgroups than the compute units hold at once of eight waves each (two, by their registers): four,
+// so that one round holds them all (us with eight and four: 8 rows of 2,048 -> 2,048 in bfloat16 by five of 16 experts,
+// 640 workgroups, 15.4 and 11.3; 32 rows of 1,024 -> 4,096 by eight 17.7 and 14.5; but two rows of 2,048 -> 2,048 by two, 256
+// workgroups, 8.7 and 9.0).
+constexpr int kSkinnyFew = 4;
+constexpr int64_t kSkinnyPlaces = 2 * 256;
 
 // A whole vector on its way.
 template <typename T, bool ODD>
@@ -783,9 +789,9 @@ struct Flight<T, true> {
     }
 };
 
-// MIX: blockIdx.y counts the experts that have rows.
-template <typename T, int MF, bool ODD, bool MIX = false>
-__global__ __launch_bounds__(kSkinnyWaves * 64) void k_skinny(GemmArgs g)
+// MIX: blockIdx.y counts the experts that have rows. WAVES: of a workgroup.
+template <typename T, int MF, bool ODD, bool MIX = false, int WAVES = kSkinnyWaves>
+__global__ __launch_bounds__(WAVES * 64) void k_skinny(GemmArgs g)
 {
     if constexpr (MIX) {
         const MixUnit u = mix_unit(g.mix, 16 * MF, 0, blockIdx.y);   // (a unit is all of an expert's rows)
@@ -800,7 +806,7 @@ __global__ __launch_bounds__(kSkinnyWaves * 64) void k_skinny(GemmArgs g)
     constexpr int N = Vec<T>::N;
     constexpr int kStep = 4 * N;                     // values of the sum per MFMA step
     constexpr int kUnroll = MF == 1 ? 8 : 4;         // steps whose loads are under way together
-    __shared__ float sums[kSkinnyWaves][MF][16][17];
+    __shared__ float sums[WAVES][MF][16][17];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, lg = lane >> 4, li = lane & 15;
     const int64_t j0 = (int64_t)blockIdx.x * 16;
     const T* w = (const T*)g.b + (j0 + li < g.cols ? j0 + li : g.cols - 1) * g.ldb + lg * N;
@@ -814,7 +820,7 @@ __global__ __launch_bounds__(kSkinnyWaves * 64) void k_skinny(GemmArgs g)
     }
     f32x4 acc[MF] = {};
     const int64_t steps = (g.len + kStep - 1) / kStep;
-    const int64_t per = (steps + kSkinnyWaves - 1) / kSkinnyWaves;
+    const int64_t per = (steps + WAVES - 1) / WAVES;
     const int64_t s0 = wave * per, s1 = s0 + per < steps ? s0 + per : steps;
     typedef typename Vec<T>::Packed Packed;
     const int64_t left = g.len - lg * N;
@@ -850,14 +856,14 @@ __global__ __launch_bounds__(kSkinnyWaves * 64) void k_skinny(GemmArgs g)
 #pragma unroll
         for (int r = 0; r < 4; ++r) sums[wave][m][li][4 * lg + r] = acc[m][r];
     __syncthreads();
-    for (int k = threadIdx.x; k < MF * 256; k += kSkinnyWaves * 64) {
+    for (int k = threadIdx.x; k < MF * 256; k += WAVES * 64) {
         const int m = k >> 8, ii = (k >> 4) & 15, jj = k & 15;
         const int64_t i = 16 * m + ii, j = j0 + jj;
         if (i >= g.rows || j >= g.cols) continue;
         float v = g.bias ? g.bias[j] : 0.f;
         float t = 0.f;
 #pragma unroll
-        for (int q = 0; q < kSkinnyWaves; ++q) t += sums[q][m][ii][jj];
+        for (int q = 0; q < WAVES; ++q) t += sums[q][m][ii][jj];
         v += t;
         if (g.z) ((T*)g.z)[i * g.ldz + j] = (T)v;
         activate<1>(g.act, &v);
@@ -1093,10 +1099,16 @@ template <typename T, bool MIX>
 hipError_t run_skinny(const GemmArgs& g, hipStream_t s)
 {
     const dim3 grid((unsigned)div_up(g.cols, 16), MIX ? (unsigned)std::min<int64_t>(g.rows, g.mix.experts) : 1);
-    auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kSkinnyWaves * 64), 0, s, g); };
+    auto run = [&](auto kernel, int waves = kSkinnyWaves) { hipLaunchKernelGGL(kernel, grid, dim3(waves * 64), 0, s, g); };
     if constexpr (sizeof(T) == 2) {
         if ((((uintptr_t)g.a | (uintptr_t)g.b) & 2) || ((g.lda | g.ldb | (MIX ? g.mix.w_stride : 0)) & 1)) {
             run(g.rows <= 16 ? k_skinny<T, 1, true, MIX> : k_skinny<T, 2, true, MIX>);
+            return hipGetLastError();
+        }
+    }
+    if constexpr (MIX) {
+        if ((int64_t)grid.x * grid.y > kSkinnyPlaces) {
+            run(g.rows <= 16 ? k_skinny<T, 1, false, true, kSkinnyFew> : k_skinny<T, 2, false, true, kSkinnyFew>, kSkinnyFew);
             return hipGetLastError();
         }
     }

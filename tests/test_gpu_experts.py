@@ -329,3 +329,11 @@ def test_experts_with_the_same_weights(rows, n_in, n_out, dtype):
     for a, b in zip((*forward(same, "silu"), *backward(same, "silu", torch.float32)),
                     (*forward(whole, "silu"), *backward(whole, "silu", torch.float32))):
         assert torch.equal(a.nan_to_num(nan=7), b.nan_to_num(nan=7))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,experts,n_in,n_out", [(16, 16, 100, 530), (32, 20, 96, 520), (9, 70, 1000, 1100), (20, 40, 133, 400)])
+def test_few_rows_and_many_columns(rows, experts, n_in, n_out, dtype):
+    """More groups of columns than the compute units take at once."""
+    d = make(rows, experts, n_in, n_out, dtype, 17)
+    check_forward(d, "silu", *forward(d, "silu"))
