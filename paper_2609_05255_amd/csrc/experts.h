@@ -116,6 +116,19 @@ hipError_t MixtureOps<T>::gemm_tt(int tile, bool fast_b, const GemmArgs& g, hipS
 }
 
 template <typename T>
+hipError_t MixtureOps<T>::gemm_pair(const GemmArgs& w, const GemmArgs& x, hipStream_t s)
+{
+    using TT = Shape<true, 64, 64, 2, 2, false, true>;
+    using NT = Shape<false, 64, 64, 2, 2, false, true>;
+    const int64_t tiles = div_up(w.rows, 64) * div_up(w.cols, 64), units = mix_units(w.len, w.mix.experts, w.split_len, 1);
+    const int64_t others = mix_units(x.rows, x.mix.experts, 64, 0) * div_up(x.cols, 64), bk = 128 / (int)sizeof(T);
+    const int lds = std::max(TT::lds_bytes(div_up(w.split_len, bk), sizeof(T)), NT::lds_bytes(div_up(x.split_len, bk), sizeof(T)));
+    hipLaunchKernelGGL((k_gemm_pair<T, TT, NT>), dim3((unsigned)(tiles * units + others)), dim3(TT::THREADS), lds, s, w, x,
+                       (uint32_t)tiles, (uint32_t)units);
+    return hipGetLastError();
+}
+
+template <typename T>
 hipError_t MixtureOps<T>::join(const GemmArgs& g, const MixSums& b, hipStream_t s)
 {
     const int join = g.part ? (int)std::min<int64_t>(div_up(g.rows * div_up(g.cols, 4), kBlock), 4096) : 0;

@@ -12,7 +12,7 @@
 // Measured (us; one linear layer over all the rows beside it): 1,000,000 x 64 -> 128 in binary16, 16 experts of uneven
 // shares, silu, backward 179 and 179, forward with z 131 and 134; 16,384 x 2,048 -> 2,048 in bfloat16, 8 experts, gelu,
 // forward with z 171 (of even shares 151, one expert 136) and 154, backward with fp32 dW 647 and 547; 50,000 x 256 -> 512 in
-// binary16, 16 experts, backward 153 and 154; 5,003 x 333 -> 215 in fp32, 7 experts, backward 45 and 45; 8 rows of
+// binary16, 16 experts, backward 153 and 154; 5,003 x 333 -> 215 in fp32, 7 experts, backward 40 and 45; 8 rows of
 // 2,048 -> 2,048 in bfloat16 by five of 16 experts 11.3 (42 MB of weights at 3.7 TB/s).
 #include "linear_plan.h"
 
@@ -302,54 +302,62 @@ hipError_t experts_bwd(const gs_experts& p, const void* dy, int64_t lddy, const 
     const TransposeArgs transpose = {l.w, l.ldw, l.n_out, l.n_in, b.wt, ldt};
     hipError_t e = MixtureOps<T>::prepare(rows, rows.limit, want_slope ? &slope : nullptr,
                                           copy_x ? &copy : nullptr, nullptr, want_dx ? &transpose : nullptr, l.n_in * ldt, s);
-    GemmArgs weights = {};   // dW's product, if its parts have to be added up
     if (e != hipSuccess) return e;
+    GemmArgs gx = {}, gw = {};   // dx's product and dW's
     if (want_dx) {
-        GemmArgs g = {};
-        g.a = dz;
-        g.lda = ldo;
-        g.b = b.wt;
-        g.ldb = ldt;
-        g.rows = l.rows;
-        g.cols = l.n_in;
-        g.len = l.n_out;
-        g.out = dx;
-        g.ldo = lddx;
-        g.mix = mix_of(p, 0);
-        g.mix.w_stride = l.n_in * ldt;
-        e = run_nt<T>(l.type, g, true, b.part, s);
-        if (e != hipSuccess) return e;
+        gx.a = dz;
+        gx.lda = ldo;
+        gx.b = b.wt;
+        gx.ldb = ldt;
+        gx.rows = l.rows;
+        gx.cols = l.n_in;
+        gx.len = l.n_out;
+        gx.out = dx;
+        gx.ldo = lddx;
+        gx.mix = mix_of(p, 0);
+        gx.mix.w_stride = l.n_in * ldt;
     }
+    Plan plan = {};
+    bool fast_x = true;
     if (dw) {
-        GemmArgs g = {};
         const void* x = copy_x ? b.x : l.x;
         const int64_t ldx = copy_x ? padded(l.type, l.n_in) : l.ldx;
-        const bool fast_x = copy_x || fast(x, ldx, l.n_in, l.type);
-        const Plan plan = plan_mix(l.type, true, l.n_out, l.n_in, l.rows, p.experts, planes, fast_x);
-        g.a = dz;
-        g.lda = ldo;
-        g.b = x;
-        g.ldb = ldx;
-        g.rows = l.n_out;
-        g.cols = l.n_in;
-        g.len = l.rows;
-        g.splits = 1;
-        g.split_len = plan.split_len;
-        g.planes = planes;
-        g.plane_stride = l.rows * ldo;
-        g.plane_scale = plane_scale(l.type);
-        g.out = dw;
-        g.ldo = lddw;
-        g.out_f32 = dw_type == GS_F32;
-        g.mix = mix_of(p, 0);
-        g.mix.limit = parts_most(plan, l.rows, p.experts);
-        g.part = g.mix.limit > 0 ? b.part : nullptr;
-        g.mix.dw_stride = dw_stride;
-        e = MixtureOps<T>::gemm_tt(plan.tile, fast_x, g, s);
-        if (e != hipSuccess) return e;
-        weights = g;
+        fast_x = copy_x || fast(x, ldx, l.n_in, l.type);
+        plan = plan_mix(l.type, true, l.n_out, l.n_in, l.rows, p.experts, planes, fast_x);
+        gw.a = dz;
+        gw.lda = ldo;
+        gw.b = x;
+        gw.ldb = ldx;
+        gw.rows = l.n_out;
+        gw.cols = l.n_in;
+        gw.len = l.rows;
+        gw.splits = 1;
+        gw.split_len = plan.split_len;
+        gw.planes = planes;
+        gw.plane_stride = l.rows * ldo;
+        gw.plane_scale = plane_scale(l.type);
+        gw.out = dw;
+        gw.ldo = lddw;
+        gw.out_f32 = dw_type == GS_F32;
+        gw.mix = mix_of(p, 0);
+        gw.mix.limit = parts_most(plan, l.rows, p.experts);
+        gw.part = gw.mix.limit > 0 ? b.part : nullptr;
+        gw.mix.dw_stride = dw_stride;
     }
-    return MixtureOps<T>::join(weights, {rows, b.sums, l.n_out, db}, s);
+    if (want_dx && dw && l.rows > kFewRows && fast_x && plan.tile == kTile64) {
+        const Plan px = plan_rows(l.type, l.rows, p.experts, l.n_in, l.n_out, true);
+        const int64_t blocks = (div_up(l.n_out, 64) * (l.rows / plan.split_len + p.experts) + units_most(l.rows, p.experts, 64)) *
+                               div_up(l.n_in, 64);
+        if (px.tile == kTile64 && px.splits == 1 && blocks * 256 >> 32 == 0) {
+            gx.splits = gx.planes = 1;
+            gx.split_len = gx.len;
+            e = MixtureOps<T>::gemm_pair(gw, gx, s);
+            return e != hipSuccess ? e : MixtureOps<T>::join(gw, {rows, b.sums, l.n_out, db}, s);
+        }
+    }
+    if (want_dx && (e = run_nt<T>(l.type, gx, true, b.part, s)) != hipSuccess) return e;
+    if (dw && (e = MixtureOps<T>::gemm_tt(plan.tile, fast_x, gw, s)) != hipSuccess) return e;
+    return MixtureOps<T>::join(gw, {rows, b.sums, l.n_out, db}, s);
 }
 
 }  // namespace

@@ -350,8 +350,8 @@ struct MixTail {
 
 // (kMixTail: a workgroup is one wave, for 16 rows of the block that a wave of WI x WJ has summed, S's waves being those
 // of 16 rows each.)
-template <typename T, class S, int MODE = kNoMix, int SUM_WI = 1>
-__global__ __launch_bounds__(MODE == kMixTail ? 64 : S::THREADS * S::WAYS) void k_gemm(GemmArgs g)
+template <typename T, class S, int MODE, int SUM_WI>
+__device__ __forceinline__ void gemm_tile(GemmArgs g, uint32_t block_x, uint32_t block_y)
 {
     constexpr bool MIX = MODE != kNoMix;
     constexpr bool TT = S::TT;
@@ -377,12 +377,12 @@ __global__ __launch_bounds__(MODE == kMixTail ? 64 : S::THREADS * S::WAYS) void 
 
     const int64_t tiles_j = (g.cols + BJ - 1) / BJ;
     int64_t tiles_i = (g.rows + BI - 1) / BI, ti, tj;
-    [[maybe_unused]] int64_t split = MIX && !TT ? 0 : blockIdx.y;
+    [[maybe_unused]] int64_t split = MIX && !TT ? 0 : block_y;
     if constexpr (MIX && !TT) {
         // the order of the tiles is tile_of's over all experts' units; a panel's tiles are of one expert
         const int64_t total = mix_total(g.mix, BI, 0) * tiles_j;
         const MixTail tail(g, total);
-        int64_t t = blockIdx.x;
+        int64_t t = block_x;
         if constexpr (MODE == kMixTail) {
             t /= WI * WJ;
             if (t >= tail.rest) return;
@@ -412,10 +412,10 @@ __global__ __launch_bounds__(MODE == kMixTail ? 64 : S::THREADS * S::WAYS) void 
         if (g.z) g.z = (T*)g.z + u.first * g.ldz;
         g.out = (T*)g.out + u.first * g.ldo;
     } else {
-        tile_of(blockIdx.x, tiles_i, tiles_j, &ti, &tj);
+        tile_of(block_x, tiles_i, tiles_j, &ti, &tj);
     }
     if constexpr (MIX && TT) {
-        const MixUnit u = mix_unit(g.mix, (int)g.split_len, 1, blockIdx.y);
+        const MixUnit u = mix_unit(g.mix, (int)g.split_len, 1, block_y);
         if (u.expert < 0) return;
         split = u.unit;
         if (u.units > 1) {
@@ -443,7 +443,7 @@ __global__ __launch_bounds__(MODE == kMixTail ? 64 : S::THREADS * S::WAYS) void 
         c_end = c_begin + (int64_t)steps * kBK < c_end ? c_begin + (int64_t)steps * kBK : c_end;
     }
     const T* b = (const T*)g.b;
-    const int wave = MODE == kMixTail ? blockIdx.x % (WI * WJ)
+    const int wave = MODE == kMixTail ? block_x % (WI * WJ)
                                       : __builtin_amdgcn_readfirstlane(threadIdx.x % S::THREADS >> 6);
     const int wi = (wave / WJ) * WR, wj = (wave % WJ) * WC;
     const int lane = threadIdx.x & 63;
@@ -648,7 +648,7 @@ __global__ __launch_bounds__(MODE == kMixTail ? 64 : S::THREADS * S::WAYS) void 
     auto value = [&](int p, int k, int e) -> float { return acc[p][(k * kGroup + e) / 4][e & 3]; };
     const int64_t i1 = i0 + wi, j1 = j0 + wj;
     if (TT || g.part) {
-        float* out = !g.part ? (float*)g.out : MIX ? g.part : g.part + (int64_t)blockIdx.y * g.rows * g.cols;
+        float* out = !g.part ? (float*)g.out : MIX ? g.part : g.part + (int64_t)block_y * g.rows * g.cols;
         const int64_t ldo = g.part ? g.cols : g.ldo;
 #pragma unroll
         for (int p = 0; p < FI; ++p)
@@ -741,6 +741,26 @@ __global__ __launch_bounds__(MODE == kMixTail ? 64 : S::THREADS * S::WAYS) void 
             }
         store_block<T, WR, WC>(block, (T*)g.out, g.ldo, i1, g.rows, j1, g.cols);
     }
+}
+
+template <typename T, class S, int MODE = kNoMix, int SUM_WI = 1>
+__global__ __launch_bounds__(MODE == kMixTail ? 64 : S::THREADS * S::WAYS) void k_gemm(GemmArgs g)
+{
+    gemm_tile<T, S, MODE, SUM_WI>(g, blockIdx.x, blockIdx.y);
+}
+
+// Two products of a mixture in one launch, where the tiles of one do not keep the compute units busy: dW's, `tiles` of each
+// of `units` units of rows, and behind them dx's (a backward with two launches and with one: 5,003 x 333 -> 215 in fp32 of
+// 7 experts 45.6 and 40.2 us, 2,000 x 256 -> 512 in binary16 of 16 34.9 and 27.0, 20,000 x 256 -> 256 of 8 55.7 and 46.2).
+template <typename T, class TT, class NT>
+__global__ __launch_bounds__(TT::THREADS) void k_gemm_pair(GemmArgs w, GemmArgs x, uint32_t tiles, uint32_t units)
+{
+    static_assert(TT::THREADS == NT::THREADS && !TT::STATIC_LDS && !NT::STATIC_LDS, "the same workgroups");
+    const uint32_t first = tiles * units;
+    if (blockIdx.x < first)
+        gemm_tile<T, TT, kMix, 1>(w, blockIdx.x % tiles, blockIdx.x / tiles);
+    else
+        gemm_tile<T, NT, kMix, 1>(x, blockIdx.x - first, 0);
 }
 
 // Few rows (NT, rows <= 16 MF): a workgroup takes 16 columns j and its waves share the sum; the weights go from

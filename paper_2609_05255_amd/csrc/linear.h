@@ -124,6 +124,8 @@ template <typename T>
 struct MixtureOps {
     static hipError_t gemm_nt(int tile, bool fast_a, const GemmArgs& g, hipStream_t s);
     static hipError_t gemm_tt(int tile, bool fast_b, const GemmArgs& g, hipStream_t s);
+    // dW's product and dx's together, in tiles of 64 x 64 (w's B, like x's operands, with whole aligned rows)
+    static hipError_t gemm_pair(const GemmArgs& w, const GemmArgs& x, hipStream_t s);
     // the parts of dW (g.part NULL: none) and of db (b.db NULL: none) added up
     static hipError_t join(const GemmArgs& g, const MixSums& b, hipStream_t s);
     static hipError_t skinny(const GemmArgs& g, hipStream_t s);
