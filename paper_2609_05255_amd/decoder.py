@@ -142,8 +142,8 @@ class Codebook:
         self.set_codes(codes)
 
     def set_codes(self, codes, stream=None):
-        self.codes = codes
         gs.gs_sort_rows(codes, self.order, self.workspace, stream)
+        self.codes = codes
 
     def forward(self, stream=None):
         """The embeddings [n][dim] (binary16)."""
