@@ -123,8 +123,11 @@ hipError_t MixtureOps<T>::gemm_pair(const GemmArgs& w, const GemmArgs& x, hipStr
     const int64_t tiles = div_up(w.rows, 64) * div_up(w.cols, 64), units = mix_units(w.len, w.mix.experts, w.split_len, 1);
     const int64_t others = mix_units(x.rows, x.mix.experts, 64, 0) * div_up(x.cols, 64), bk = 128 / (int)sizeof(T);
     const int lds = std::max(TT::lds_bytes(div_up(w.split_len, bk), sizeof(T)), NT::lds_bytes(div_up(x.split_len, bk), sizeof(T)));
+    // the longer workgroups first (the other way round 600 x 1,024 -> 1,024 in fp32 of 4 experts takes 72 us for 52, 20,000 x
+    // 256 -> 256 in binary16 of 8 50 for 46)
+    const bool x_first = x.len >= w.planes * std::min(w.split_len, div_up(w.len, w.mix.experts));
     hipLaunchKernelGGL((k_gemm_pair<T, TT, NT>), dim3((unsigned)(tiles * units + others)), dim3(TT::THREADS), lds, s, w, x,
-                       (uint32_t)tiles, (uint32_t)units);
+                       (uint32_t)tiles, x_first ? (uint32_t)others : 0, x_first ? 0 : (uint32_t)(tiles * units));
     return hipGetLastError();
 }
 

@@ -206,12 +206,11 @@ Mix mix_of(const gs_experts& p, int64_t size)
 }
 
 template <typename T>
-hipError_t run_nt(int type, GemmArgs g, bool fast_a, float* part, hipStream_t s)
+hipError_t run_nt(int type, GemmArgs g, const Plan& p, bool fast_a, float* part, hipStream_t s)
 {
     g.splits = g.planes = 1;
     g.split_len = g.len;
     if (g.rows <= kFewRows) return MixtureOps<T>::skinny(g, s);
-    const Plan p = plan_rows(type, g.rows, g.mix.experts, g.cols, g.len, fast_a);
     if (p.splits > 1) {
         g.splits = p.splits;
         g.part = part;
@@ -259,7 +258,7 @@ hipError_t experts_fwd(const gs_experts& p, void* y, int64_t ldy, void* z, int64
         g.ldb = padded(l.type, l.n_in);
         g.mix.w_stride = each;
     }
-    return run_nt<T>(l.type, g, fast_x, f.part, s);
+    return run_nt<T>(l.type, g, plan_rows(l.type, l.rows, p.experts, l.n_out, l.n_in, fast_x), fast_x, f.part, s);
 }
 
 template <typename T>
@@ -346,18 +345,26 @@ hipError_t experts_bwd(const gs_experts& p, const void* dy, int64_t lddy, const 
         gw.part = gw.mix.limit > 0 ? b.part : nullptr;
         gw.mix.dw_stride = dw_stride;
     }
-    if (want_dx && dw && l.rows > kFewRows && fast_x && plan.tile == kTile64) {
-        const Plan px = plan_rows(l.type, l.rows, p.experts, l.n_in, l.n_out, true);
-        const int64_t blocks = (div_up(l.n_out, 64) * (l.rows / plan.split_len + p.experts) + units_most(l.rows, p.experts, 64)) *
-                               div_up(l.n_in, 64);
-        if (px.tile == kTile64 && px.splits == 1 && blocks * 256 >> 32 == 0) {
-            gx.splits = gx.planes = 1;
-            gx.split_len = gx.len;
-            e = MixtureOps<T>::gemm_pair(gw, gx, s);
-            return e != hipSuccess ? e : MixtureOps<T>::join(gw, {rows, b.sums, l.n_out, db}, s);
+    // Small tiles of both products: plain ones of 64 x 64, in one launch. (Which they are is a matter of the sizes, so that a
+    // gradient has the same bits alone.)
+    Plan px = plan_rows(l.type, l.rows, p.experts, l.n_in, l.n_out, true);
+    const auto small = [](int tile) { return tile == kTile64 || tile == kTile64By4; };
+    if (l.rows > kFewRows && small(px.tile) && px.splits == 1) {
+        const bool dw_small = dw && small(plan.tile);
+        if (dw_small) plan.tile = kTile64;
+        if (small(plan_mix(l.type, true, l.n_out, l.n_in, l.rows, p.experts, 1, true).tile)) {
+            px.tile = kTile64;
+            const int64_t blocks = (dw_small ? div_up(l.n_out, 64) * (l.rows / plan.split_len + p.experts) : 0) +
+                                   units_most(l.rows, p.experts, 64);
+            if (want_dx && dw_small && fast_x && blocks * div_up(l.n_in, 64) * 256 >> 32 == 0) {
+                gx.splits = gx.planes = 1;
+                gx.split_len = gx.len;
+                e = MixtureOps<T>::gemm_pair(gw, gx, s);
+                return e != hipSuccess ? e : MixtureOps<T>::join(gw, {rows, b.sums, l.n_out, db}, s);
+            }
         }
     }
-    if (want_dx && (e = run_nt<T>(l.type, gx, true, b.part, s)) != hipSuccess) return e;
+    if (want_dx && (e = run_nt<T>(l.type, gx, px, true, b.part, s)) != hipSuccess) return e;
     if (dw && (e = MixtureOps<T>::gemm_tt(plan.tile, fast_x, gw, s)) != hipSuccess) return e;
     return MixtureOps<T>::join(gw, {rows, b.sums, l.n_out, db}, s);
 }

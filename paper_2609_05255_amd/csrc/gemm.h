@@ -749,18 +749,21 @@ __global__ __launch_bounds__(MODE == kMixTail ? 64 : S::THREADS * S::WAYS) void 
     gemm_tile<T, S, MODE, SUM_WI>(g, blockIdx.x, blockIdx.y);
 }
 
-// Two products of a mixture in one launch, where the tiles of one do not keep the compute units busy: dW's, `tiles` of each
-// of `units` units of rows, and behind them dx's (a backward with two launches and with one: 5,003 x 333 -> 215 in fp32 of
-// 7 experts 45.6 and 40.2 us, 2,000 x 256 -> 512 in binary16 of 16 34.9 and 27.0, 20,000 x 256 -> 256 of 8 55.7 and 46.2).
+// Two products of a mixture in one launch, where the tiles of one do not keep the compute units busy: dx's from x_begin on,
+// and from w_begin on dW's, `tiles` of each unit of rows; one of the two begins at 0. (A backward with two launches, of
+// tiles of 64 x 64 or of four groups of waves, and with one: 5,003 x 333 -> 215 in fp32 of 7 experts 45.6 and 40 us, 2,000 x
+// 256 -> 512 in binary16 of 16 34.9 and 27, 20,000 x 256 -> 256 of 8 55.7 and 46, 1,000 x 512 -> 512 in bfloat16 of 8 38
+// and 26, 600 x 1,024 -> 1,024 in fp32 of 4 59 and 52.)
 template <typename T, class TT, class NT>
-__global__ __launch_bounds__(TT::THREADS) void k_gemm_pair(GemmArgs w, GemmArgs x, uint32_t tiles, uint32_t units)
+__global__ __launch_bounds__(TT::THREADS) void k_gemm_pair(GemmArgs w, GemmArgs x, uint32_t tiles, uint32_t w_begin,
+                                                           uint32_t x_begin)
 {
     static_assert(TT::THREADS == NT::THREADS && !TT::STATIC_LDS && !NT::STATIC_LDS, "the same workgroups");
-    const uint32_t first = tiles * units;
-    if (blockIdx.x < first)
-        gemm_tile<T, TT, kMix, 1>(w, blockIdx.x % tiles, blockIdx.x / tiles);
+    const uint32_t b = blockIdx.x;
+    if (w_begin ? b < w_begin : b >= x_begin)
+        gemm_tile<T, NT, kMix, 1>(x, b - x_begin, 0);
     else
-        gemm_tile<T, NT, kMix, 1>(x, blockIdx.x - first, 0);
+        gemm_tile<T, TT, kMix, 1>(w, (b - w_begin) % tiles, (b - w_begin) / tiles);
 }
 
 // Few rows (NT, rows <= 16 MF): a workgroup takes 16 columns j and its waves share the sum; the weights go from
