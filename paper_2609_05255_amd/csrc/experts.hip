@@ -175,7 +175,8 @@ BwdSpace bwd_space(void* base, int type, int act, int64_t rows, int64_t experts,
     Regions r{(char*)base};
     BwdSpace b = {};
     if (narrow(type, in, out)) {
-        b.part = (float*)r.take(units_most(rows, experts, narrow_size(rows, experts, in, out, true)) * narrow_part((int)out, (int)in) * 4);
+        b.part = (float*)r.take(units_most(rows, experts, narrow_size(rows, experts, in, out, true)) *
+                                narrow_part((int)out, (int)in) * 4);
         b.bytes = r.at;
         return b;
     }

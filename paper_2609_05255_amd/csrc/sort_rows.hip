@@ -12,9 +12,10 @@
 // the sorted keys. Up to kSmallCount keys one workgroup sorts in LDS, in one launch.
 //
 // Bound by the chain of steps in a workgroup: of the 10 us that one of 4,096 keys took (2,000,000 keys, all workgroups at
-// the same time) 3 were reading the counts, 2 adding them up in LDS, where a few digits' now meet, and 0.7 ranking; keys and
-// results are 24 MB, 5 us at the rate of a copy. Measured (us a call): 8 keys 5.4, 8,192 keys 10.7, 100,000 by 256 groups 12.8, 2,000,000
-// by 16 20, 3,000,000 by 65,536 60 (in two passes; with places, which are written one by one, 91), by 1,000,000 82.
+// the same time) 3 were reading the counts, 2 adding them up in LDS, where a few digits' now meet, and 0.7 ranking; keys
+// and results are 24 MB, 5 us at the rate of a copy. Measured (us a call): 8 keys 5.4, 8,192 keys 10.7, 100,000 by 256
+// groups 12.3, 2,000,000 by 16 20, 3,000,000 by 65,536 60 (in two passes; with places, which are written one by one, 91),
+// by 1,000,000 82.
 #include <type_traits>
 
 #include "gs_internal.h"
