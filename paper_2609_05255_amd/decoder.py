@@ -125,9 +125,11 @@ class ResidualDecoder(_FlatWeights):
 
 
 class Codebook:
-    """Embeddings that Gaussians share: row i of the decoder's input is scale * table[codes[i]] (codes int32 [n]; a
-    Gaussian whose code is none of the table's has an embedding of zeros). The table is kept in fp32 with a binary16 copy
-    that the lookups read; the codes are sorted once, for the table's gradient, and again when set_codes changes them."""
+    """Embeddings that Gaussians share: row i of the decoder's input is scale * table[codes[i]] (codes int32, n values of
+    any shape; a Gaussian whose code is none of the table's has an embedding of zeros). The table is kept in fp32 with a
+    binary16 copy that the lookups read. The book keeps a copy of the codes, sorted once for the table's gradient, and
+    again when set_codes changes them or a forward finds them written in place; what becomes of the caller's tensor does
+    not matter. (A forward that was captured in a graph does not look again: there, set_codes is captured with it.)"""
 
     def __init__(self, codes, entries: int, dim: int, scale: float = 1.0, seed: int = 0):
         device = codes.device
@@ -139,15 +141,38 @@ class Codebook:
         self.order = gs.RowOrder(codes.numel(), entries, device=device, place=False)
         size = max(gs.gs_sort_rows_workspace_size(self.order), gs.gs_embedding_workspace_size(self.x), 1)
         self.workspace = torch.empty(size, dtype=torch.uint8, device=device)
+        with torch.inference_mode(False):   # (a tensor whose version tells of writes)
+            self._codes = torch.empty(codes.numel(), dtype=torch.int32, device=device)
         self.set_codes(codes)
 
+    @property
+    def codes(self):
+        """The book's own codes, int32 [n]."""
+        return self._codes
+
     def set_codes(self, codes, stream=None):
-        gs.gs_sort_rows(codes, self.order, self.workspace, stream)
-        self.codes = codes
+        """Other codes, as many: copied and sorted. Codes that are refused change nothing."""
+        n = self._codes.numel()
+        if (codes.numel() != n or codes.dtype != torch.int32 or codes.device != self._codes.device
+                or not codes.is_contiguous()):
+            raise ValueError("codes: %s of %s on %s, a contiguous int32 tensor of %d values on %s expected" % (
+                tuple(codes.shape), codes.dtype, codes.device, n, self._codes.device))
+        gs._one_device(codes)
+        if codes is not self._codes:
+            if isinstance(stream, int):
+                stream = torch.cuda.ExternalStream(stream, device=codes.device)
+            with torch.cuda.stream(stream):   # (None: the current one)
+                self._codes.copy_(codes.view(-1))
+            if stream is not None:
+                codes.record_stream(stream)   # (the caller may let go of them before they are read)
+        gs.gs_sort_rows(self._codes, self.order, self.workspace, stream)
+        self._sorted = self._codes._version
 
     def forward(self, stream=None):
         """The embeddings [n][dim] (binary16)."""
-        gs.gs_embedding_fwd(self.half, self.codes, self.scale, self.x, stream)
+        if self._codes._version != self._sorted:
+            self.set_codes(self._codes, stream)
+        gs.gs_embedding_fwd(self.half, self._codes, self.scale, self.x, stream)
         return self.x
 
     def backward(self, dx, stream=None):
