@@ -9,7 +9,8 @@
 // k_keys_count (digit counts of each workgroup's keys, and with many workgroups their sums over groups of these) and
 // k_keys_move (each workgroup adds up the counts before its own, ranks its keys by ballots, reorders them by digit in LDS
 // and writes each digit's run). Where one pass is enough the offsets are its digits' totals; otherwise k_offsets searches
-// the sorted keys. Up to kSmallCount keys one workgroup sorts in LDS, in one launch.
+// the sorted keys. Up to kSmallCount keys one workgroup sorts in LDS, in one launch; with more than kSmallGroups groups
+// k_offsets is a second one, which reads the keys back.
 //
 // Bound by the chain of steps in a workgroup: of the 10 us that one of 4,096 keys took (2,000,000 keys, all workgroups at
 // the same time) 3 were reading the counts, 2 adding them up in LDS, where a few digits' now meet, and 0.7 ranking; keys
@@ -136,16 +137,15 @@ __device__ __forceinline__ void rank_slice(const uint32_t (&key)[ITEMS], int shi
     }
 }
 
-// Sums over rows [0, rows) of R digits, of all and of those before `mine`: four digits of a thread and every slice-th row,
-// added up within a wave. sums: [sum_slices][R] each.
-constexpr int sum_slices(int digits, int threads) { return digits >= 256 ? threads * 4 / digits : threads / 64; }
-
+// Sums over rows [0, rows) of R digits, of all and of those before `mine`: four digits of a thread and every slice-th row.
+// total (or NULL), before: [THREADS * 4 / R slices][R] each.
 template <int R, int THREADS>
 __device__ __forceinline__ void sum_rows(const uint32_t* table, int64_t rows, int64_t mine, uint32_t* total,
                                          uint32_t* before)
 {
     typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
     constexpr int kQuads = R / 4, kSlices = THREADS / kQuads;
+    static_assert(kQuads >= 64, "a wave's digits are of one slice");
     constexpr int kFly = THREADS == kThreads ? 4 : 16;   // (fewer threads have more rows each, and more registers)
     const int quad = threadIdx.x % kQuads, slice = threadIdx.x / kQuads;
     u32x4 t = {0, 0, 0, 0}, b = {0, 0, 0, 0};
@@ -164,14 +164,8 @@ __device__ __forceinline__ void sum_rows(const uint32_t* table, int64_t rows, in
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-#pragma unroll
-        for (int d = kQuads; d < 64; d <<= 1) {
-            if (total) t[e] += (uint32_t)__shfl_xor((int)t[e], d, 64);
-            b[e] += (uint32_t)__shfl_xor((int)b[e], d, 64);
-        }
-        const int at = kQuads < 64 ? (int)(threadIdx.x >> 6) : slice;
-        if (total) total[at * R + quad * 4 + e] = t[e];
-        before[at * R + quad * 4 + e] = b[e];
+        if (total) total[slice * R + quad * 4 + e] = t[e];
+        before[slice * R + quad * 4 + e] = b[e];
     }
 }
 
@@ -183,6 +177,7 @@ __device__ __forceinline__ void add_rows(const KeysPass& a, uint32_t* total, uin
 {
     typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
     constexpr int kQuads = R / 4, kSlices = THREADS / kQuads, kFly = 4;
+    static_assert(kQuads < 64, "a wave has several slices");
     const int quad = threadIdx.x % kQuads, slice = threadIdx.x / kQuads;
     const int64_t mine = a.sup ? blockIdx.x / a.group : blockIdx.x, first = a.sup ? mine * a.group : 0;
     const uint32_t* sums = (a.sup ? a.sup : a.hist) + quad * 4;
@@ -211,7 +206,7 @@ __device__ __forceinline__ void add_rows(const KeysPass& a, uint32_t* total, uin
             t[e] += (uint32_t)__shfl_xor((int)t[e], d, 64);
             b[e] += (uint32_t)__shfl_xor((int)b[e], d, 64);
         }
-        if (kQuads >= 64 || (threadIdx.x & 63) < kQuads) {
+        if ((threadIdx.x & 63) < kQuads) {
             atomicAdd(&total[quad * 4 + e], t[e]);
             atomicAdd(&before[quad * 4 + e], b[e]);
         }
@@ -226,7 +221,7 @@ __global__ __launch_bounds__(THREADS, THREADS == kThreads ? 8 : 4) void k_keys_m
     // Many digits: the rows' sums are tables of each slice of threads, up to three (meeting on counters in LDS, and with the
     // registers for all rows at once, a sort of 3,000,000 keys takes 74 us instead of 61). Few: they meet in LDS.
     constexpr bool kTables = R >= 256;
-    constexpr int kSlices = sum_slices(R, THREADS), kSums = kTables ? kSlices * R : R;
+    constexpr int kSlices = kTables ? THREADS * 4 / R : 1, kSums = kSlices * R;
     constexpr int kWaves = THREADS / 64, kEach = R > THREADS ? R / THREADS : 1;   // digits of a thread, neighbours
     static_assert(ITEMS * 64 < 65536 && kTile < 65536, "counts of 16 bits");
     __shared__ uint16_t counts[kWaves][R];         // of each wave, then the first place of its keys of each digit
@@ -267,7 +262,7 @@ __global__ __launch_bounds__(THREADS, THREADS == kThreads ? 8 : 4) void k_keys_m
         const int d = t * kEach + k;
         if (d >= R) break;
 #pragma unroll
-        for (int q = 0; q < (kTables ? kSlices : 1); ++q) {
+        for (int q = 0; q < kSlices; ++q) {
             total[k] += totals[q * R + d];
             before[k] += before0[q * R + d];
             if (kTables && a.sup) before[k] += before1[q * R + d];
