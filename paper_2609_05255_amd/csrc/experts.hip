@@ -23,10 +23,11 @@ namespace {
 constexpr int kDzBlocks = 2048;          // workgroups of dz, about
 constexpr int64_t kNarrowRows = 128;     // of a unit of a narrow layer, at least
 constexpr int64_t kPlaces = 5 * kFillTiles;   // workgroups that the compute units hold at once, of any tile at most
-// Workgroups of a narrow layer's forward, about, and of its backward kNarrowBlocks: with 512, 1,024, 2,048 and 4,096 the
-// forward of 1,000,000 rows and 16 experts takes 133, 140, 132 and 126 us (64 -> 128 in binary16), 171, 172, 180 and 191
-// (128 -> 128) and 51, 44, 46 and 42 (32 -> 32); the backward with 512 and 1,024 200 and 205 (64 -> 128), 59 and 60
-// (32 -> 32), of 200,000 x 64 -> 64 and 64 experts in bfloat16 41 and 45.
+// Workgroups of a narrow layer's forward, about, and of its backward kNarrowBlocks. The forward's number matters little: with
+// 512, 1,024, 2,048 and 4,096 1,000,000 rows of 16 experts take 133, 140, 132 and 126 us (64 -> 128 in binary16), 171, 172,
+// 180 and 191 (128 -> 128) and 51, 44, 46 and 42 (32 -> 32), so that none is the best for all three, and 355, 356, 358 and
+// 359 together. The backward takes with 512 and 1,024 200 and 205 (64 -> 128), 59 and 60 (32 -> 32), of 200,000 x 64 -> 64
+// and 64 experts in bfloat16 41 and 45.
 constexpr int64_t kNarrowForward = 2048;
 constexpr int64_t kMostSplits = 8;       // parts of one of the last tiles
 constexpr double kSplitGain = 2.0;       // us that a split of the last tiles has to gain by the plan
@@ -115,7 +116,7 @@ int64_t dz_size(int type, int64_t rows, int64_t cols)
 }
 
 // Rows of a unit of a narrow layer: as many units as there are places for workgroups, those of the experts' ends with them.
-int64_t narrow_size(int64_t rows, int64_t experts, int64_t in, int64_t out, bool backward)
+int64_t narrow_size(int64_t rows, int64_t experts, bool backward)
 {
     const int64_t most = backward ? kNarrowBlocks : kNarrowForward;
     return std::max(kNarrowRows, div_up(div_up(rows, std::max(most / 2, most - experts)), 64) * 64);
@@ -175,7 +176,7 @@ BwdSpace bwd_space(void* base, int type, int act, int64_t rows, int64_t experts,
     Regions r{(char*)base};
     BwdSpace b = {};
     if (narrow(type, in, out)) {
-        b.part = (float*)r.take(units_most(rows, experts, narrow_size(rows, experts, in, out, true)) *
+        b.part = (float*)r.take(units_most(rows, experts, narrow_size(rows, experts, true)) *
                                 narrow_part((int)out, (int)in) * 4);
         b.bytes = r.at;
         return b;
@@ -245,7 +246,7 @@ hipError_t experts_fwd(const gs_experts& p, void* y, int64_t ldy, void* z, int64
     g.ldz = ldz;
     g.mix = mix_of(p, 0);
     if (narrow_taken(l.type, l.rows, l.n_in, l.n_out)) {
-        g.mix.size = (int32_t)narrow_size(l.rows, p.experts, l.n_in, l.n_out, false);
+        g.mix.size = (int32_t)narrow_size(l.rows, p.experts, false);
         return MixtureOps<T>::narrow_fwd(g, fast_x, units_most(l.rows, p.experts, g.mix.size), s);
     }
     const FwdSpace f = fwd_space(ws, l.type, l.rows, p.experts, l.n_in, l.n_out, !fast_w(p));
@@ -274,7 +275,7 @@ hipError_t experts_bwd(const gs_experts& p, const void* dy, int64_t lddy, const 
     if (narrow(l.type, l.n_in, l.n_out)) {
         NarrowArgs a = {dy,        z,           l.x,  l.w, lddy,  ldz, l.ldx, l.ldw, lddx, lddw, l.rows, (int)l.n_out,
                         (int)l.n_in, l.act, dw_type == GS_F32, dx, dw,    db,  b.part};
-        a.mix = mix_of(p, narrow_size(l.rows, p.experts, l.n_in, l.n_out, true));
+        a.mix = mix_of(p, narrow_size(l.rows, p.experts, true));
         a.mix.dw_stride = dw_stride;
         a.mix.limit = units_most(l.rows, p.experts, a.mix.size);
         const bool whole = fast(dy, lddy, l.n_out, l.type) && fast(l.x, l.ldx, l.n_in, l.type) &&
