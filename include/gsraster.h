@@ -675,7 +675,8 @@ gs_status gs_experts_fwd(const gs_experts* p, void* y, int64_t ldy, void* z, int
 /*
  * gs_experts_bwd -- dz = dy act'(z), dx = dz w_e for the rows of every expert e, dw_e = dz^T x
  * and db_e = sum of dz over its rows, zero for an expert without rows: as gs_linear_bwd for
- * one layer, with its types and precisions (in binary16 an x or w below 2^-14 counts as
+ * one layer, with its types and precisions: for dx, and for dw in a 16-bit type, dz is rounded
+ * to the type, whose rounding adds to that of the result (in binary16 an x or w below 2^-14 counts as
  * 2^-14 in how finely its products' sums are kept, as the matrix cores take it). dw: [experts][n_out][n_in] with row stride lddw
  * and dw_stride from an expert to the next, db: [experts][n_out]; dx, dw and db are
  * overwritten (dx: the experts' rows) and may each be NULL. The same call gives the same bits.

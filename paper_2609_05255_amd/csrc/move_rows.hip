@@ -13,7 +13,9 @@
 // Measured (us, and TB/s of what has to be moved): dispatch of 1,000,000 x 128 in binary16 to two of 16 experts 146 (5.3),
 // with the sort 169; combination of 20,003 x 333 in fp32, three choices and a residual 29 (4.2, rows at odd multiples of 4
 // bytes); its backward for 8,192 x 4,096 in bfloat16, two choices 75 (4.5); the gradient of 3,000,000 x 64 in binary16 into
-// 65,536 entries 98 and 8 for the entries that workgroups share (3.9), with the sort 168; of 50,001 x 333 in bfloat16 into
+// 65,536 entries 98 and 8 for the entries that workgroups share (3.9), with the sort 168 (without it 92 for even shares, 110
+// where one entry has all the rows; of 190,000 x 1,024 in bfloat16 133 and 203, as the workgroups that add up an entry's parts
+// are as few as its columns in 256s); of 50,001 x 333 in bfloat16 into
 // 150,007 entries 20, and 21 for the empty ones' zeros, with the sort 78. A row alone takes 6.6 a call.
 #include <type_traits>
 
