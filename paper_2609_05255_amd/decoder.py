@@ -128,8 +128,9 @@ class Codebook:
     """Embeddings that Gaussians share: row i of the decoder's input is scale * table[codes[i]] (codes int32, n values of
     any shape; a Gaussian whose code is none of the table's has an embedding of zeros). The table is kept in fp32 with a
     binary16 copy that the lookups read. The book keeps a copy of the codes, sorted once for the table's gradient, and
-    again when set_codes changes them or a forward finds them written in place; what becomes of the caller's tensor does
-    not matter. (A forward that was captured in a graph does not look again: there, set_codes is captured with it.)"""
+    again when set_codes changes them or a forward finds that torch has written them; what becomes of the caller's tensor
+    does not matter. (Neither a captured forward's replay nor a write by address is found: where codes change like that,
+    set_codes is captured with the forward, or called with the book's own codes.)"""
 
     def __init__(self, codes, entries: int, dim: int, scale: float = 1.0, seed: int = 0):
         device = codes.device
@@ -143,6 +144,7 @@ class Codebook:
         self.workspace = torch.empty(size, dtype=torch.uint8, device=device)
         with torch.inference_mode(False):   # (a tensor whose version tells of writes)
             self._codes = torch.empty(codes.numel(), dtype=torch.int32, device=device)
+        self._sorted = None   # the version of the codes that the order is of
         self.set_codes(codes)
 
     @property
@@ -166,7 +168,8 @@ class Codebook:
             if stream is not None:
                 codes.record_stream(stream)   # (the caller may let go of them before they are read)
         gs.gs_sort_rows(self._codes, self.order, self.workspace, stream)
-        self._sorted = self._codes._version
+        if not torch.cuda.is_current_stream_capturing():   # (else nothing is sorted before the graph runs)
+            self._sorted = self._codes._version
 
     def forward(self, stream=None):
         """The embeddings [n][dim] (binary16)."""

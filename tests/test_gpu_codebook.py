@@ -141,3 +141,24 @@ def test_captured():
         s.synchronize()
         check(book, make_codes(seed), x, grad, dx)
         torch.randn(1000, device="cuda").sum().item()
+
+
+def test_captured_and_not_yet_run():
+    """A capture sorts nothing: forwards beside it are of the codes as they are."""
+    book, dx, s = Codebook(make_codes(1), ENTRIES, DIM, SCALE), gradient_of(2), torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        step(book, dx)
+        given, other = make_codes(31), make_codes(32)
+        book.codes.copy_(given)   # not sorted yet
+    s.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        x, grad = step(book, dx)
+    check(book, given, *step(book, dx), dx)
+    with torch.cuda.graph(torch.cuda.CUDAGraph(), stream=s):
+        book.set_codes(other)
+    check(book, given, *step(book, dx), dx)
+    with torch.cuda.stream(s):
+        graph.replay()
+    s.synchronize()
+    check(book, given, x, grad, dx)
